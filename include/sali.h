@@ -409,6 +409,120 @@ int sali_set_profile_events(sali_ctx* ctx, int which, void* start_event, void* s
 /* Read and keep the sticky device status word.  Waits for `stream`. */
 int sali_get_status(sali_ctx* ctx, uint32_t* h_flags, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------
+ * Text tokens next to the video: a paged K/V cache and its causal attention.
+ *
+ * The calls above keep the frames' K/V; the tokens of the prompts and answers around them are kept here, in pages of a
+ * fixed number of tokens that any number of sequences take from one pool.  Which page holds which tokens of a
+ * sequence is the caller's (a page table per sequence); the library writes new rows into the pages (quantising them,
+ * if the pool is), reads rows back, and computes attention of new tokens over the pages, with the same
+ * "codes now, values when read" idea as the frame cache (Just-In-Time Dequantization) and the same quantiser (groups of
+ * 32 along head_dim, fp32 scales; symmetric INT8, asymmetric INT4 with the group's smallest value).  sali_attend_decode* give the
+ * attention over the frames as (out, lse); sali_pages_attend takes that pair as `prior` and joins the two.
+ *
+ * A call works on a batch of sequences (sali_page_batch), whose numbers lie in DEVICE memory, so that a captured graph
+ * can be replayed with other lengths:
+ *   d_start  int32[n_seqs + 1]  new tokens of sequence s are the rows d_start[s] .. d_start[s + 1] - 1 of every
+ *                               per-token array of the call (queries, keys, values, outputs); d_start[0] = 0
+ *   d_length int32[n_seqs]      tokens of the sequence, the new ones (its last) included
+ *   d_table  int32[n_seqs][table_width]  page of tokens p * page_tokens .. of the sequence; not read past its length
+ *   n_tokens                    rows that the per-token arrays have, d_start[n_seqs] <= n_tokens (rows past it are untouched)
+ *   max_q, max_kv               no sequence has more new tokens / more tokens than this
+ * A sequence whose numbers contradict each other or these bounds (more new tokens than tokens, rows outside
+ * 0 .. n_tokens, more tokens than its table row holds) is left out: nothing is read or written for it and
+ * SALI_FAULT_BATCH is set.  An entry of the table that is not a page of the pool sets SALI_FAULT_PAGE: its tokens are not
+ * written, read back as zeros and are invisible to attention.
+ *
+ * Layout.  The pool is [n_layers][n_pages][n_kv_heads][page_tokens / 16][block]; a block holds 16 tokens of one K/V head
+ * in the order in which the matrix-core kernels take them, K, V, then (quantised) the scales of K and of V as
+ * fp32, then (INT4) the smallest values of K and of V in the 16-bit type.  Token t = 8 a + 4 b + i of the block (i < 4) has
+ * place 8 b + 4 a + i in K's arrays; V's arrays have tokens in order:
+ *   SALI_STORE_16    K [D / 8][place][8 values]         V [2][D][8 tokens]
+ *   SALI_STORE_INT8  K [D / 16][place][16 codes]        V [2][D][8 tokens]               scales K [D / 32][place], V [D / 32][16]
+ *   SALI_STORE_INT4  K [D / 32][place][16 bytes]        V [2][D / 32][16][8 tokens]      the same, smallest values alike; byte e of 16
+ *                                                       holds value e of a group in its low half, value e + 16 in its high half
+ * Quantised values are those of sali_kv_compress / sali_kv_decompress, in the pool's 16-bit type (a group of bfloat16 values
+ * that are all below 2^-121 is stored as zeros: 127 and 15 divided by it are no fp32 numbers); a group that holds an inf or NaN
+ * sets SALI_FAULT_NONFINITE (for SALI_STORE_16 too, which stores it as it is) and is otherwise unspecified.
+ * ------------------------------------------------------------------------------------------------- */
+#define SALI_DTYPE_FP16  0
+#define SALI_DTYPE_BF16  1
+#define SALI_STORE_16    0      /* rows in the 16-bit type, bit for bit        */
+#define SALI_STORE_INT8  1
+#define SALI_STORE_INT4  2
+
+/* sticky device status bits of the pages (sali_pages_get_status), besides SALI_FAULT_NONFINITE */
+#define SALI_FAULT_PAGE   0x10u   /* a page table entry outside the pool       */
+#define SALI_FAULT_BATCH  0x20u   /* a sequence left out (see above)           */
+
+typedef struct sali_pages sali_pages;   /* opaque host object; owns no device memory */
+
+typedef struct sali_pages_config {
+    int32_t n_layers;
+    int32_t n_kv_heads;
+    int32_t n_heads;                 /* query heads, a multiple of n_kv_heads; head j reads K/V head j / (n_heads / n_kv_heads) */
+    int32_t head_dim;                /* 64 or 128                                                      */
+    int32_t page_tokens;             /* 16, 32, 64, 128 or 256                                         */
+    int32_t n_pages;                 /* pages of a layer                                               */
+    int32_t dtype;                   /* SALI_DTYPE_*: queries, keys, values and attention outputs      */
+    int32_t store;                   /* SALI_STORE_*                                                   */
+} sali_pages_config;
+
+typedef struct sali_page_batch {
+    const int32_t* d_start;
+    const int32_t* d_length;
+    const int32_t* d_table;
+    int32_t n_seqs, table_width, n_tokens, max_q, max_kv, reserved;
+} sali_page_batch;
+
+/* Rows of a per-token array: value e of head h of row t is element t * token_stride + h * head_stride + e.  Strides in
+ * elements.  16-bit arrays: 16-byte aligned, strides multiples of 8 (SALI_ERR_ALIGN). */
+typedef struct sali_rows {
+    void* d;
+    int64_t token_stride, head_stride;
+} sali_rows;
+
+/* Sizes of the two device buffers sali_pages_create needs.  Host only. */
+int sali_pages_bytes(const sali_pages_config* cfg, size_t* pool_bytes, size_t* scratch_bytes);
+
+/* Build the object over two caller-owned device buffers (256-byte aligned, at least the sizes sali_pages_bytes
+ * reports).  Synchronous: clears the status word.  The pool is not touched: it may hold pages that an earlier
+ * object of the same configuration wrote.  On error *out is NULL. */
+int sali_pages_create(const sali_pages_config* cfg, void* d_pool, void* d_scratch, sali_pages** out);
+void sali_pages_destroy(sali_pages* p);
+
+/* Store the K/V rows of the batch's new tokens (n_kv_heads heads) into their pages.  Other tokens of the pages keep
+ * their bytes.  No two sequences of a batch may write the same page.  Asynchronous on `stream`. */
+int sali_pages_append(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* k, const sali_rows* v,
+                      void* stream);
+
+/* Dequantise-on-read: the rows of the batch's new tokens as the pages hold them.  (For other tokens than the last ones pass
+ * a batch with smaller d_length.)  Asynchronous on `stream`. */
+int sali_pages_read(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* k_out, const sali_rows* v_out,
+                    void* stream);
+
+/* Causal attention of the batch's new tokens over the pages, which hold them already (sali_pages_append): for query head h
+ * of the token at position p of its sequence, over the positions j <= p with  window == 0,  or  j > p - window,  or  j < sinks:
+ *     s_j = softmax_scale * <q_h, K_j>,   out_h = sum_j softmax(s)_j V_j,   lse_h = log sum_j exp(s_j).
+ * K, V are the rows as sali_pages_read returns them; scores, softmax and sums in fp32, its weights rounded to the 16-bit type for
+ * the product with V.  Keys that a token does not see do not reach it, whatever they hold.
+ *   q             n_heads heads
+ *   out           n_heads heads, 16-bit; zeros where nothing is seen
+ *   d_lse_or_null fp32 [n_tokens][n_heads]; -inf where nothing is seen
+ *   window, sinks window = 0: all earlier positions (sinks then has no meaning)
+ *   d_prior_or_null, d_prior_lse_or_null   both or neither: fp32 [n_tokens][n_heads][head_dim] and [n_tokens][n_heads], the
+ *                 attention of the same queries over other keys (sali_attend_decode*; -inf: none).  out and lse are then those of all
+ *                 keys together.  16-byte aligned.
+ * Asynchronous on `stream`.  Calls on one object must not overlap each other (one area of partial results); calls on
+ * different objects may share a pool.
+ * SALI_ERR_CONFIG for a softmax_scale that is not finite, SALI_ERR_SHAPE for a layer, batch size, window or sinks out of range. */
+int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, float softmax_scale,
+                      int32_t window, int32_t sinks, const float* d_prior_or_null, const float* d_prior_lse_or_null,
+                      const sali_rows* out, float* d_lse_or_null, void* stream);
+
+/* Copies the status bits to host memory and waits for `stream`. */
+int sali_pages_get_status(sali_pages* p, uint32_t* h_status, void* stream);
+
 /* Static text for a return code. */
 const char* sali_error_string(int code);
 

@@ -20,7 +20,8 @@ _lib = None
 TOKENS = 576
 MAX_BATCH = 16          # SALI_MAX_BATCH
 TIER_FP16, TIER_INT8, TIER_INT4, TIER_PRUNE = 0, 1, 2, 3
-FAULT_OVERFLOW, FAULT_NONFINITE, FAULT_NAN_SCORE, FAULT_NO_DATA = 1, 2, 4, 8
+FAULT_OVERFLOW, FAULT_NONFINITE, FAULT_NAN_SCORE, FAULT_NO_DATA, FAULT_PAGE, FAULT_BATCH = 1, 2, 4, 8, 16, 32
+STORE_16, STORE_INT8, STORE_INT4 = 0, 1, 2
 
 
 class SaliError(RuntimeError):
@@ -65,6 +66,20 @@ class sali_pool_layout(C.Structure):
                 ("total_bytes", C.c_uint64)]
 
 
+class sali_pages_config(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_kv_heads", C.c_int32), ("n_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_tokens", C.c_int32), ("n_pages", C.c_int32), ("dtype", C.c_int32), ("store", C.c_int32)]
+
+
+class sali_page_batch(C.Structure):
+    _fields_ = [("d_start", C.c_void_p), ("d_length", C.c_void_p), ("d_table", C.c_void_p), ("n_seqs", C.c_int32), ("table_width", C.c_int32),
+                ("n_tokens", C.c_int32), ("max_q", C.c_int32), ("max_kv", C.c_int32), ("reserved", C.c_int32)]
+
+
+class sali_rows(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
 EXPORTS = {
     "sali_workspace_bytes": (C.c_int, [C.POINTER(sali_config), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t),
                                        C.POINTER(C.c_size_t)]),
@@ -104,6 +119,14 @@ EXPORTS = {
     "sali_set_profile_events": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
     "sali_get_status": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint32), C.c_void_p]),
     "sali_error_string": (C.c_char_p, [C.c_int]),
+    "sali_pages_bytes": (C.c_int, [C.POINTER(sali_pages_config), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "sali_pages_create": (C.c_int, [C.POINTER(sali_pages_config), C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p)]),
+    "sali_pages_destroy": (None, [C.c_void_p]),
+    "sali_pages_append": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(sali_page_batch), C.POINTER(sali_rows), C.POINTER(sali_rows), C.c_void_p]),
+    "sali_pages_read": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(sali_page_batch), C.POINTER(sali_rows), C.POINTER(sali_rows), C.c_void_p]),
+    "sali_pages_attend": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(sali_page_batch), C.POINTER(sali_rows), C.c_float, C.c_int32, C.c_int32,
+                                    C.c_void_p, C.c_void_p, C.POINTER(sali_rows), C.c_void_p, C.c_void_p]),
+    "sali_pages_get_status": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint32), C.c_void_p]),
 }
 
 
@@ -379,3 +402,124 @@ class SaliContext:
                     t[:, b:b + n] = a[b * P:(b + n) * P].view(P, n, a.shape[1])[sel]
             out[k] = t
         return out
+
+
+# ---- paged cache of text tokens ------------------------------------------------------------------
+_PAGE_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
+_PAGE_STORES = {"16": STORE_16, "int8": STORE_INT8, "int4": STORE_INT4}
+
+
+def make_pages_config(*, n_layers=1, n_kv_heads, n_heads, head_dim=128, page_tokens=64, n_pages, dtype=torch.float16, store="16") -> sali_pages_config:
+    """dtype: torch.float16 or torch.bfloat16; store: "16", "int8" or "int4" (what the pages hold)."""
+    if dtype not in _PAGE_DTYPES:
+        raise ValueError(f"pages hold float16 or bfloat16 tokens, not {dtype}")
+    if store not in _PAGE_STORES:
+        raise ValueError(f"store is one of {sorted(_PAGE_STORES)}, not {store!r}")
+    return sali_pages_config(n_layers, n_kv_heads, n_heads, head_dim, page_tokens, n_pages, _PAGE_DTYPES[dtype], _PAGE_STORES[store])
+
+
+def pages_bytes(cfg: sali_pages_config):
+    """(bytes of the pool, bytes of the scratch)"""
+    a, b = C.c_size_t(), C.c_size_t()
+    _check(load_library().sali_pages_bytes(C.byref(cfg), C.byref(a), C.byref(b)), "sali_pages_bytes")
+    return a.value, b.value
+
+
+class PageBatch:
+    """The sequences of a step, for all layers: int32 tensors start [n + 1], length [n] and table [n, width] on one GPU, as sali_page_batch has
+    them.  `tokens` is the number of rows of the per-token arrays; max_q (if not given, tokens) and max_kv bound the new tokens and the tokens of a
+    sequence.  The tensors are read when a call's kernels run: a captured call takes what they hold at its replay."""
+
+    def __init__(self, start: torch.Tensor, length: torch.Tensor, table: torch.Tensor, tokens: int, *, max_q: Optional[int] = None, max_kv: int):
+        for name, t, dims in (("start", start, 1), ("length", length, 1), ("table", table, 2)):
+            if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous():
+                raise ValueError(f"{name}: contiguous int32 tensor of {dims} dimension(s) expected, got {t.dtype} {tuple(t.shape)}")
+            if t.device != length.device:
+                raise ValueError("start, length and table lie on different devices")
+        n = length.shape[0]
+        if start.shape[0] != n + 1 or table.shape[0] != n:
+            raise ValueError(f"{n} lengths need {n + 1} starts and {n} rows of the table, got {start.shape[0]} and {table.shape[0]}")
+        self.tensors = (start, length, table)
+        self.tokens = tokens
+        self.device = length.device
+        self.c = sali_page_batch(start.data_ptr(), length.data_ptr(), table.data_ptr(), n, table.shape[1], tokens, tokens if max_q is None else max_q,
+                                 max_kv, 0)
+
+
+class SaliPages:
+    """Owns the pool (or works in the caller's) and the scratch of a paged cache and forwards the C calls.  Per-token tensors are [tokens, heads,
+    head_dim] with values side by side; tokens and heads may be strided (slices of one projection's output)."""
+
+    def __init__(self, cfg: sali_pages_config, device="cuda:0", pool: Optional[torch.Tensor] = None):
+        self.lib = load_library()
+        self.cfg = cfg
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("libsali runs on the GPU only")
+        pool_bytes, scratch_bytes = pages_bytes(cfg)
+        if pool is not None and (not pool.is_contiguous() or pool.numel() * pool.element_size() < pool_bytes or pool.device.type != "cuda"):
+            raise ValueError(f"pool: {pool_bytes} contiguous bytes on the GPU expected")
+        self.dtype = torch.bfloat16 if cfg.dtype else torch.float16
+        self.handle = None
+        with torch.cuda.device(self.device):
+            self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=self.device) if pool is None else pool
+            self.scratch = torch.empty(scratch_bytes, dtype=torch.uint8, device=self.device)
+            self.device = self.scratch.device
+            h = C.c_void_p()
+            _check(self.lib.sali_pages_create(C.byref(cfg), _ptr(self.pool), _ptr(self.scratch), C.byref(h)), "sali_pages_create")
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None):
+            torch.cuda.synchronize(self.device)
+            self.lib.sali_pages_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _rows(self, t: torch.Tensor, batch: PageBatch, heads: int, name: str) -> sali_rows:
+        if t.dtype != self.dtype or t.shape != (batch.tokens, heads, self.cfg.head_dim) or t.stride(2) != 1 or t.device != self.device:
+            raise ValueError(f"{name}: {self.dtype} [{batch.tokens}, {heads}, {self.cfg.head_dim}] on {self.device} with its last dimension side by "
+                             f"side expected, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
+        if batch.device != self.device:
+            raise ValueError(f"the batch lies on {batch.device}, the pages on {self.device}")
+        return sali_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+    def _dense(self, t: Optional[torch.Tensor], shape, name: str):
+        if t is None:
+            return None
+        if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: contiguous float32 {list(shape)} on {self.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def append(self, layer: int, batch: PageBatch, k: torch.Tensor, v: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
+        """Store the K/V rows of the batch's new tokens, [tokens, n_kv_heads, head_dim]."""
+        n = self.cfg.n_kv_heads
+        _check(self.lib.sali_pages_append(self.handle, layer, batch.c, self._rows(k, batch, n, "k"), self._rows(v, batch, n, "v"),
+                                          _stream() if stream is None else stream.cuda_stream), "sali_pages_append")
+
+    def read(self, layer: int, batch: PageBatch, k_out: torch.Tensor, v_out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
+        """The rows of the batch's new tokens as the pages hold them."""
+        n = self.cfg.n_kv_heads
+        _check(self.lib.sali_pages_read(self.handle, layer, batch.c, self._rows(k_out, batch, n, "k_out"), self._rows(v_out, batch, n, "v_out"),
+                                        _stream() if stream is None else stream.cuda_stream), "sali_pages_read")
+
+    def attend(self, layer: int, batch: PageBatch, q: torch.Tensor, softmax_scale: float, out: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
+               window: int = 0, sinks: int = 0, prior: Optional[torch.Tensor] = None, prior_lse: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None):
+        """Causal attention of the batch's new tokens over the pages: q, out [tokens, n_heads, head_dim], lse [tokens, n_heads] in fp32.  prior and
+        prior_lse (fp32): attention of the same queries over other keys, joined with this one."""
+        c, n = self.cfg, self.cfg.n_heads
+        _check(self.lib.sali_pages_attend(self.handle, layer, batch.c, self._rows(q, batch, n, "q"), softmax_scale, window, sinks,
+                                          self._dense(prior, (batch.tokens, n, c.head_dim), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
+                                          self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"),
+                                          _stream() if stream is None else stream.cuda_stream), "sali_pages_attend")
+
+    def get_status(self) -> int:
+        f = C.c_uint32()
+        _check(self.lib.sali_pages_get_status(self.handle, C.byref(f), _stream()), "sali_pages_get_status")
+        return f.value

@@ -30,6 +30,10 @@ SOURCES = {
     "attn_kernels.hip": ["-ffp-contract=fast"],
     "saliency_kernels.hip": [],
     "flow_kernels.hip": ["-ffp-contract=fast"],
+    "pages_api.hip": [],
+    "pages_kernels.hip": ["-ffp-contract=off"],
+    "pages_attn_fp16.hip": ["-ffp-contract=fast"],
+    "pages_attn_bf16.hip": ["-ffp-contract=fast"],
 }
 
 

@@ -1,0 +1,91 @@
+// Arithmetic of the paged cache that the host can run too (tests/test_pages_arithmetic.py does): layout, which blocks, tiles and units a batch has.
+#pragma once
+
+#include "arith.h"
+#include "sali.h"
+
+namespace sali {
+
+constexpr int kBlockTokens = 16;            // tokens of a block, the unit of the layout
+constexpr int kTileTokens = 32;             // tokens of a step of the attention: two blocks
+
+// bytes of a block's parts, in their order
+struct BlockLayout {
+    uint32_t v, ks, vs, kz, vz, bytes;      // K is at 0
+};
+constexpr BlockLayout block_layout(int store, int dim) {
+    const uint32_t d = (uint32_t)dim;
+    const uint32_t codes = store == SALI_STORE_16 ? 32 * d : (store == SALI_STORE_INT8 ? 16 * d : 8 * d);
+    const uint32_t scale = store == SALI_STORE_16 ? 0 : 2 * d, zero = store == SALI_STORE_INT4 ? d : 0;
+    return {codes, 2 * codes, 2 * codes + scale, 2 * codes + 2 * scale, 2 * codes + 2 * scale + zero, 2 * codes + 2 * scale + 2 * zero};
+}
+SALI_BOTH int place_of_token(int t) { return 8 * (t >> 2 & 1) + 4 * (t >> 3) + (t & 3); }      // t = 8 a + 4 b + i
+SALI_BOTH int token_of_place(int p) { return 8 * (p >> 2 & 1) + 4 * (p >> 3) + (p & 3); }      // the same exchange
+
+template <typename T>
+SALI_BOTH T least(T a, T b) { return a < b ? a : b; }
+template <typename T>
+SALI_BOTH T most(T a, T b) { return a < b ? b : a; }
+
+// One sequence of a batch: rows first .. first + n - 1 are its tokens len - n .. len - 1.  n = 0 where its numbers contradict each other, the
+// rows or its table.
+struct PageSeq {
+    int32_t first, n, len;
+};
+SALI_BOTH bool page_seq_holds(int64_t a, int64_t b, int64_t len, int64_t n_tokens, int64_t max_q, int64_t room) {
+    return a >= 0 && b >= a && b <= n_tokens && b - a <= max_q && len >= b - a && len <= room;
+}
+
+// Append and read take the batch by slots of one 16-token block each: sequence s owns the slots from first / 16 + 2 s on.  n tokens touch at
+// most n / 16 + 2 blocks, and up to the next sequence's first slot there are that many, so a slot's sequence is found without a sum over
+// those before it.
+SALI_BOTH int64_t first_slot(int32_t first, int s) { return (int64_t)(first < 0 ? 0 : first) / kBlockTokens + 2ll * s; }
+
+// The keys a set of rows sees: positions first .. last of the sequence (of the set's first and last token), window and sinks.  Tiles of kTokens
+// tokens that some row sees: the first `head` from the sequence's beginning, then from tile `from` on.
+struct View {
+    int32_t first, last;
+    int32_t head, from, tiles;
+};
+template <int kTokens>
+SALI_BOTH View view_of(int first, int last, int window, int sinks) {
+    View v = {first, last, 0, 0, 0};
+    const int lo = window > 0 ? most(0, first - window + 1) : 0;
+    v.from = lo / kTokens;
+    v.head = window > 0 ? least((sinks + kTokens - 1) / kTokens, v.from) : 0;
+    v.tiles = v.head + last / kTokens + 1 - v.from;
+    return v;
+}
+SALI_BOTH int tile_at(const View& v, int i) { return i < v.head ? i : v.from + (i - v.head); }
+// has some row of the view some key of the tile's n tokens (from j0) out of sight?
+SALI_BOTH bool partly_hidden(const View& v, int window, int sinks, int j0, int n) {
+    if (j0 + n - 1 > v.first) return true;
+    return window > 0 && j0 <= v.last - window && j0 + n > sinks;
+}
+SALI_BOTH bool sees(int p, int j, int window, int sinks) {
+    return j <= p && (window == 0 || j > p - window || j < sinks);
+}
+
+// the last block of a pair's stretch: blocks of `blocks` equal stretches of `total` tiles; block b starts at tile b * total / blocks
+SALI_BOTH int64_t stretch_start(int64_t b, int64_t total, int64_t blocks) { return b * total / blocks; }
+SALI_BOTH int64_t stretch_of(int64_t tile, int64_t total, int64_t blocks) { return ((tile + 1) * blocks + total - 1) / total - 1; }
+
+constexpr int kTileRows = 256;              // rows of a block of the tile kernel
+constexpr int kTileKeys = 64;               // keys of its steps
+constexpr int kTileShares = 256;            // fair shares that the whole work is cut into: one a compute unit
+
+// row tiles of a batch by slots, as those of blocks in append: sequence s owns the slots from first * group / kTileRows + s on
+SALI_BOTH int64_t tile_slots(int64_t n_tokens, int group, int64_t n_seqs) { return n_tokens * group / kTileRows + n_seqs; }
+// Tiles of a fair share of `sum` tiles a head.  Units longer than one are cut, into at most twice as many parts as they have shares, so there are
+// at most tile_parts of them a head.
+SALI_BOTH int tile_shares(int n_kv) { return (kTileShares + n_kv - 1) / n_kv; }
+SALI_BOTH int fair_share(int64_t sum, int n_kv) { return (int)((most(sum, (int64_t)1) + tile_shares(n_kv) - 1) / tile_shares(n_kv)); }
+SALI_BOTH int parts_of(int tiles, int share) { return tiles > share ? (tiles + share - 1) / share : 1; }
+SALI_BOTH int tile_parts(int n_kv) { return 2 * tile_shares(n_kv); }
+
+SALI_BOTH View view_of_rows(const PageSeq& q, int row_tile, int group, int window, int sinks) {
+    const int first = q.len - q.n, last_row = (int)least((int64_t)q.n * group, (int64_t)(row_tile + 1) * kTileRows) - 1;
+    return view_of<kTileKeys>(first + (int)((int64_t)row_tile * kTileRows / group), first + last_row / group, window, sinks);
+}
+
+}  // namespace sali

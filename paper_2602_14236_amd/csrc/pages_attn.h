@@ -1,0 +1,219 @@
+// Causal attention of new tokens over paged K/V (gfx950): what the kernels share.  The layout of a block of 16 tokens stands in sali.h.
+//
+// Rows.  For one sequence and K/V head the queries are rows r = token * group + head in group, so the heads of a group share every key that is
+// read, and a call of one token a sequence has group rows.  Keys are taken 32 at a time (two blocks).  The scores are computed transposed,
+// S^T = K Q^T: the matrix cores then leave a query's scores of 4 or 8 consecutive tokens in one lane, which is the operand that the second product,
+// out^T = V^T P^T, wants, so weights never leave their lane's registers.  K's places and V's pairs of 8 tokens are laid
+// out in memory as those operands: every load is 16 bytes a lane of contiguous memory, ready for use.
+//
+// Softmax.  Scores are kept in units of log 2 (scale2 = scale * log2 e).  Each row has a reference m and a sum of
+// exp2(s - m); the reference follows the row's maximum only when that is more than 2^kLag above it: until then weights of up
+// to 2^kLag are as good as weights up to 1 (fp32 sums, 16-bit weights of the same relative precision), and nothing has to be rescaled.
+// Nothing seen: m = -inf, sum 0.
+//
+// Masked keys.  Scores outside a row's view become -inf, whatever they were, and their weights 0.  A weight of 0 does not take
+// out an infinity or NaN in V, so tiles that are not wholly in view of all rows look at their values: if any is not finite, the product
+// runs over the finite ones and what the others add is found by two more products that count, for every output, the
+// infinities of each sign in its view (a NaN counts for both).
+#pragma once
+
+#include <type_traits>
+
+#include "pages.h"
+
+namespace sali {
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLag = 8.0f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// the 16-bit types and their matrix products
+template <bool kBf16>
+struct Num;
+template <>
+struct Num<false> {
+    typedef _Float16 T;
+    typedef half8 V8;
+    static constexpr uint32_t kExp = 0x7C007C00u, kExpOne = 0x04000400u;
+    static constexpr uint16_t kOne = 0x3C00u;
+    static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct Num<true> {
+    typedef __bf16 T;
+    typedef bhalf8 V8;
+    static constexpr uint32_t kExp = 0x7F807F80u, kExpOne = 0x00800080u;
+    static constexpr uint16_t kOne = 0x3F80u;
+    static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
+    }
+};
+
+// two fp32 numbers as a pair of 16-bit ones, rounded to nearest
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef typename Num<kBf16>::T T;
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    const T2 v = {(T)a, (T)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+// the same where a and b are products or sums: those are rounded to fp32 first
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack2_after_f32(float a, float b) {
+    asm("" : "+v"(a), "+v"(b));
+    return pack2<kBf16>(a, b);
+}
+template <bool kBf16>
+__device__ __forceinline__ float low_half(uint32_t w) {
+    return (float)__builtin_bit_cast(typename Num<kBf16>::T, (uint16_t)w);
+}
+template <bool kBf16>
+__device__ __forceinline__ float high_half(uint32_t w) {
+    return (float)__builtin_bit_cast(typename Num<kBf16>::T, (uint16_t)(w >> 16));
+}
+
+// eight 8-bit codes, signed, times one scale or each times its own
+__device__ __forceinline__ float code8(uint32_t w, int i) { return (float)(int)(int8_t)(w >> (8 * i) & 0xFFu); }
+// eight 4-bit codes, in the low halves of the bytes of two words (already masked)
+__device__ __forceinline__ float code4(uint32_t w, int i) { return (float)(w >> (8 * i) & 0xFFu); }
+
+// 8 codes of one token (K)
+template <bool kBf16>
+__device__ __forceinline__ u32x4 values8(uint32_t a, uint32_t b, float scale) {
+    u32x4 r;
+    r.x = pack2_after_f32<kBf16>(code8(a, 0) * scale, code8(a, 1) * scale);
+    r.y = pack2_after_f32<kBf16>(code8(a, 2) * scale, code8(a, 3) * scale);
+    r.z = pack2_after_f32<kBf16>(code8(b, 0) * scale, code8(b, 1) * scale);
+    r.w = pack2_after_f32<kBf16>(code8(b, 2) * scale, code8(b, 3) * scale);
+    return r;
+}
+template <bool kBf16>
+__device__ __forceinline__ u32x4 values4(uint32_t a, uint32_t b, float scale, float low) {
+    u32x4 r;
+    r.x = pack2_after_f32<kBf16>(__builtin_fmaf(code4(a, 0), scale, low), __builtin_fmaf(code4(a, 1), scale, low));
+    r.y = pack2_after_f32<kBf16>(__builtin_fmaf(code4(a, 2), scale, low), __builtin_fmaf(code4(a, 3), scale, low));
+    r.z = pack2_after_f32<kBf16>(__builtin_fmaf(code4(b, 0), scale, low), __builtin_fmaf(code4(b, 1), scale, low));
+    r.w = pack2_after_f32<kBf16>(__builtin_fmaf(code4(b, 2), scale, low), __builtin_fmaf(code4(b, 3), scale, low));
+    return r;
+}
+// 8 tokens' codes of one value (V)
+struct Scales8 {
+    f32x4 a, b;
+};
+template <bool kBf16>
+__device__ __forceinline__ u32x4 values8(uint32_t a, uint32_t b, const Scales8& s) {
+    u32x4 r;
+    r.x = pack2_after_f32<kBf16>(code8(a, 0) * s.a[0], code8(a, 1) * s.a[1]);
+    r.y = pack2_after_f32<kBf16>(code8(a, 2) * s.a[2], code8(a, 3) * s.a[3]);
+    r.z = pack2_after_f32<kBf16>(code8(b, 0) * s.b[0], code8(b, 1) * s.b[1]);
+    r.w = pack2_after_f32<kBf16>(code8(b, 2) * s.b[2], code8(b, 3) * s.b[3]);
+    return r;
+}
+template <bool kBf16>
+__device__ __forceinline__ u32x4 values4(uint32_t a, uint32_t b, const Scales8& s, const u32x4& z) {
+    u32x4 r;
+    const uint32_t z0 = z.x, z1 = z.y, z2 = z.z, z3 = z.w;
+    r.x = pack2_after_f32<kBf16>(__builtin_fmaf(code4(a, 0), s.a[0], low_half<kBf16>(z0)), __builtin_fmaf(code4(a, 1), s.a[1], high_half<kBf16>(z0)));
+    r.y = pack2_after_f32<kBf16>(__builtin_fmaf(code4(a, 2), s.a[2], low_half<kBf16>(z1)), __builtin_fmaf(code4(a, 3), s.a[3], high_half<kBf16>(z1)));
+    r.z = pack2_after_f32<kBf16>(__builtin_fmaf(code4(b, 0), s.b[0], low_half<kBf16>(z2)), __builtin_fmaf(code4(b, 1), s.b[1], high_half<kBf16>(z2)));
+    r.w = pack2_after_f32<kBf16>(__builtin_fmaf(code4(b, 2), s.b[2], low_half<kBf16>(z3)), __builtin_fmaf(code4(b, 3), s.b[3], high_half<kBf16>(z3)));
+    return r;
+}
+
+__device__ __forceinline__ u32x4 load16(const void* p) { return *static_cast<const u32x4*>(p); }
+
+// lanes 32 and 16 apart
+__device__ __forceinline__ float max_over_halves(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float sum_over_halves(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float max_over_quarters(float v) {
+    v = max_over_halves(v);
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float sum_over_quarters(float v) {
+    v = sum_over_halves(v);
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// V's values of 8 tokens: those that are finite, and 1 where an infinity of either sign (or a NaN) stands
+template <bool kBf16>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {        // bits 15 and 31
+    return ((w & 0x7FFF7FFFu) + Num<kBf16>::kExpOne) & 0x80008000u;
+}
+template <bool kBf16>
+__device__ __forceinline__ bool any_not_finite(const u32x4& v) {
+    return (not_finite<kBf16>(v.x) | not_finite<kBf16>(v.y) | not_finite<kBf16>(v.z) | not_finite<kBf16>(v.w)) != 0;
+}
+template <bool kBf16>
+__device__ __forceinline__ void take_apart(const u32x4& v, u32x4& finite, u32x4& plus, u32x4& minus) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = v[i], bad = not_finite<kBf16>(w), mask = (bad >> 15) * 0xFFFFu;
+        // a NaN has bits below the exponent
+        const uint32_t below = w & ~(Num<kBf16>::kExp | 0x80008000u);
+        const uint32_t nan = ((below & 0xFFFFu) != 0 ? 0xFFFFu : 0u) | (below >> 16 != 0 ? 0xFFFF0000u : 0u);
+        const uint32_t neg = (w >> 15 & 0x00010001u) * 0xFFFFu, one = Num<kBf16>::kOne | (uint32_t)Num<kBf16>::kOne << 16;
+        finite[i] = w & ~mask;
+        plus[i] = mask & (nan | ~neg) & one;
+        minus[i] = mask & (nan | neg) & one;
+    }
+}
+
+// A row's result from its sum (out and lse still apart): joined with the prior and rounded.  `out` is one value of the unnormalised sum.
+struct RowEnd {
+    float lse, by_own, by_prior;            // out = out * by_own + prior * by_prior
+};
+__device__ __forceinline__ RowEnd row_end(float m, float l, const PagesAttend& a, int64_t row) {
+    RowEnd r = {-INFINITY, 0.0f, 0.0f};
+    const bool some = l > 0.0f || l != l;   // a NaN stays one
+    float lse = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;      // log2
+    float own = some ? 1.0f / l : 0.0f;
+    if (a.prior == nullptr) {
+        r.lse = lse;
+        r.by_own = own;
+        return r;
+    }
+    const float lp = a.prior_lse[row], top = fmaxf(lse, lp);
+    if (top == -INFINITY && lse == lse && lp == lp) return r;
+    const float w1 = expf(lse - top), w2 = expf(lp - top), sum = w1 + w2;
+    r.lse = top + logf(sum);
+    r.by_own = own * (w1 / sum);
+    r.by_prior = w2 / sum;
+    return r;
+}
+// a weight of zero takes out whatever the other factor is
+__device__ __forceinline__ float joined(const RowEnd& e, float own, float prior) {
+    const float a = e.by_own == 0.0f ? 0.0f : own * e.by_own;
+    return e.by_prior == 0.0f ? a : __builtin_fmaf(prior, e.by_prior, a);
+}
+
+}  // namespace
+
+}  // namespace sali

@@ -1,0 +1,54 @@
+// Which kernels a call of paged attention takes, and its launches, for one 16-bit type.
+#pragma once
+
+#include "pages_stream.h"
+#include "pages_tile.h"
+
+namespace sali {
+
+namespace {
+
+template <int kStore, int kDim, bool kBf16>
+void launch_attend(const PagesAttend& a, hipStream_t s) {
+    const int n_kv = a.geom.n_kv, group = a.group;
+    const int64_t most_rows = (int64_t)a.seqs.max_q * group;
+    // Rows of a sequence that the stream takes at most.  In a batch that has longer sequences: those of single tokens.
+    int stream_rows = most_rows <= 16 ? 16 : (most_rows <= 32 ? 32 : 64);
+    if (most_rows > 64) stream_rows = a.seqs.n_seqs == 1 || group > 64 ? 0 : (group <= 16 ? 16 : (group <= 32 ? 32 : 64));
+    if (stream_rows > 0) {
+        const int64_t reach = a.window > 0 ? (int64_t)a.window + a.seqs.max_q + a.sinks + 3 * kTileTokens : (int64_t)a.seqs.max_kv + kTileTokens;
+        const int64_t tiles = min((int64_t)a.seqs.max_kv + kTileTokens, reach) / kTileTokens * a.seqs.n_seqs * n_kv;
+        auto go = [&](auto sets, int most) {
+            constexpr int kSets = decltype(sets)::value;
+            const int blocks = (int)max((int64_t)1, min((int64_t)most, (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
+            hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets>), dim3(blocks), dim3(64 * kStreamWaves), 0, s, a, stream_rows, kStreamMinTiles);
+            hipLaunchKernelGGL((k_pages_stream_merge<kDim, kBf16>), dim3(blocks, (unsigned)min((int64_t)stream_rows, most_rows)), dim3(256), 0, s, a, 16 * kSets);
+        };
+        if (stream_rows == 16) go(std::integral_constant<int, 1>{}, stream_blocks(1));
+        else if (stream_rows == 32) go(std::integral_constant<int, 2>{}, stream_blocks(2));
+        else go(std::integral_constant<int, 4>{}, stream_blocks(4));
+    }
+    if (most_rows > 64) {
+        constexpr int kWaves = 8;
+        const int64_t units = tile_slots(a.seqs.n_tokens, group, a.seqs.n_seqs) + tile_parts(n_kv);
+        hipLaunchKernelGGL(k_pages_plan, dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1);
+        hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16, kWaves>), dim3((unsigned)(units * n_kv)), dim3(64 * kWaves), 0, s, a);
+        hipLaunchKernelGGL((k_pages_tile_merge<kDim, kBf16>), dim3(tile_parts(n_kv) / 2 * n_kv, kTileRows / 8), dim3(256), 0, s, a);
+    }
+}
+
+template <bool kBf16>
+hipError_t launch_pages_attend(int store, int dim, const PagesAttend& a, hipStream_t s) {
+    auto with_dim = [&](auto st) {
+        if (dim == 64) launch_attend<decltype(st)::value, 64, kBf16>(a, s);
+        else launch_attend<decltype(st)::value, 128, kBf16>(a, s);
+    };
+    if (store == SALI_STORE_16) with_dim(std::integral_constant<int, SALI_STORE_16>{});
+    else if (store == SALI_STORE_INT8) with_dim(std::integral_constant<int, SALI_STORE_INT8>{});
+    else with_dim(std::integral_constant<int, SALI_STORE_INT4>{});
+    return hipGetLastError();
+}
+
+}  // namespace
+
+}  // namespace sali

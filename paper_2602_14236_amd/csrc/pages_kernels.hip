@@ -1,0 +1,378 @@
+// Writing K/V rows of text tokens into pages, quantised on the way, and reading them back (gfx950).  Layout of a block: sali.h.
+//
+// Per group of 32 values, every step one IEEE fp32 operation (this file is compiled with -ffp-contract=off), as in the frame cache:
+//   INT8  m = max |x|           scale = m / 127        code = rne(x * (127 / m))              value = code * scale
+//   INT4  low = min x           m = max (x - low)      scale = m / 15     code = rne((x - low) * (15 / m))    value = code * scale + low, rounded once
+// and the value is then rounded to the pool's 16-bit type.
+//
+// Both kernels move every byte once and are bound by memory; a block of 256 threads has one 16-token block of one K/V head.  Rows are
+// contiguous along the head's values, the layout has eight tokens of one value side by side (V) or a token's pieces 16 tokens apart
+// (K), so the block is turned over in LDS between 16-byte accesses on both sides: its rows (or their codes), padded so that a column's
+// reads fall on different banks.  Codes are made and expanded on the side of the rows, where a group lies in four adjacent lanes.
+// Blocks that the new tokens do not fill are written value by value, so that no byte of another token is touched.
+
+#include <type_traits>
+
+#include "pages.h"
+
+namespace sali {
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+template <bool kBf16>
+struct Half;
+template <>
+struct Half<false> {
+    typedef _Float16 type;
+    static constexpr uint32_t kExponent = 0x7C00u;
+};
+template <>
+struct Half<true> {
+    typedef __bf16 type;
+    static constexpr uint32_t kExponent = 0x7F80u;
+};
+
+template <bool kBf16>
+union Piece {                               // 16 bytes
+    u32x4 u;
+    typename Half<kBf16>::type h[8];
+    uint16_t b16[8];
+    uint8_t b8[16];
+};
+
+// rounded to fp32 first, then to 16 bits (a fused instruction would round once)
+template <typename T>
+__device__ __forceinline__ T rounded_after_f32(float v) {
+    asm volatile("" : "+v"(v));
+    return (T)v;
+}
+
+template <int kCtrl>
+__device__ __forceinline__ uint32_t quad_move(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, kCtrl, 0xF, 0xF, true); }
+template <int kCtrl>
+__device__ __forceinline__ float quad_move(float v) { return __builtin_bit_cast(float, quad_move<kCtrl>(__builtin_bit_cast(uint32_t, v))); }
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E;                 // quad_perm [1,0,3,2], [2,3,0,1]
+
+// the last sequence whose first slot is not past `slot`; all 64 lanes of a wave, 64 candidates a look
+__device__ __forceinline__ int seq_of_slot(const PageSeqs& q, int64_t slot) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = q.n_seqs;
+    while (n > 1) {
+        const int step = (n + 63) / 64, i = lane * step;
+        const bool before = i < n && first_slot(q.start[lo + i], lo + i) <= slot;
+        const int c = max(1, (int)__popcll(__ballot(before)));
+        lo += (c - 1) * step;
+        n = min(step, n - (c - 1) * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// the 16-token block a thread block has: which tokens of it are the batch's, where their rows and the block itself lie
+struct BlockWork {
+    char* block;                            // NULL: no such page
+    int32_t row0;                           // row of the block's token 0 (it may lie before the new tokens)
+    int32_t t0, t1;                         // the new tokens of the block
+    int32_t head;
+};
+__device__ __forceinline__ bool find_work(const PageGeom& g, const PageSeqs& q, BlockWork& w) {
+    const uint32_t id = blockIdx.x;
+    const uint32_t slot = id / (uint32_t)g.n_kv;
+    w.head = (int)(id - slot * (uint32_t)g.n_kv);
+    const int s = seq_of_slot(q, slot);
+    const PageSeq seq = load_seq(q, g, s, threadIdx.x == 0);
+    if (seq.n == 0) return false;
+    const int pos0 = seq.len - seq.n;                       // position of the first new token
+    const int64_t at = (int64_t)(pos0 / kBlockTokens) + (slot - first_slot(seq.first, s));
+    if (at * kBlockTokens >= seq.len) return false;         // one of the slots that the sequence has no use for
+    const int block = (int)at;
+    w.t0 = max(0, pos0 - block * kBlockTokens);
+    w.t1 = min(kBlockTokens, seq.len - block * kBlockTokens);
+    w.row0 = seq.first + (block * kBlockTokens - pos0);
+    const int page = q.table[(int64_t)s * q.width + (block >> g.blocks_log2)];
+    w.block = nullptr;
+    if (page >= 0 && page < g.n_pages) {
+        const int in_page = block & ((1 << g.blocks_log2) - 1);
+        const uint32_t block_bytes = g.head_bytes >> g.blocks_log2;
+        w.block = g.pool + (uint64_t)page * g.page_bytes + (uint64_t)w.head * g.head_bytes + (uint32_t)in_page * block_bytes;
+    } else if (threadIdx.x == 0) {
+        atomicOr(q.status, SALI_FAULT_PAGE);
+    }
+    return true;
+}
+
+// LDS: the 16 rows of K, then those of V, as values or as codes; a row's length in bytes with what keeps columns on different banks
+template <int kStore, int kDim>
+struct Rows {
+    static constexpr int kBytes = kStore == SALI_STORE_16 ? 2 * kDim : (kStore == SALI_STORE_INT8 ? kDim : kDim / 2);
+    static constexpr int kPitch = kBytes + 16;
+    static constexpr int kGroups = kDim / kGroup;
+};
+
+template <int kStore, int kDim, bool kBf16>
+__global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs, RowsIn k, RowsIn v) {
+    typedef Rows<kStore, kDim> R;
+    constexpr int kPieces = kDim / 8, kItems = 32 * kPieces;            // 16-byte pieces of a row, of all rows
+    constexpr BlockLayout kAt = block_layout(kStore, kDim);
+    __shared__ __align__(16) uint8_t s_rows[32 * R::kPitch];
+    __shared__ float s_scale[kStore == SALI_STORE_16 ? 1 : 32 * R::kGroups];
+    __shared__ uint16_t s_low[kStore == SALI_STORE_INT4 ? 32 * R::kGroups : 1];
+    BlockWork w;
+    if (!find_work(g, seqs, w) || w.block == nullptr) return;
+
+    Piece<kBf16> x[kItems / 256];
+#pragma unroll
+    for (int i = 0; i < kItems / 256; ++i) {
+        const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces, t = row & 15;
+        const RowsIn& in = row < 16 ? k : v;
+        x[i].u = (u32x4){0u, 0u, 0u, 0u};
+        if (t >= w.t0 && t < w.t1)
+            x[i].u = *reinterpret_cast<const u32x4*>(in.d + (int64_t)(w.row0 + t) * in.token_bytes + (int64_t)w.head * in.head_bytes + c * 16);
+    }
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kItems / 256; ++i) {
+        const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bad |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent;
+        if constexpr (kStore == SALI_STORE_16) {
+            *reinterpret_cast<u32x4*>(s_rows + row * R::kPitch + c * 16) = x[i].u;
+        } else {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = (float)x[i].h[e];
+            float m, low = 0.0f;
+            constexpr float kSteps = kStore == SALI_STORE_INT8 ? 127.0f : 15.0f;
+            if constexpr (kStore == SALI_STORE_INT8) {
+                m = fabsf(f[0]);
+#pragma unroll
+                for (int e = 1; e < 8; ++e) m = fmaxf(m, fabsf(f[e]));
+                m = fmaxf(m, quad_move<kSwap1>(m));
+                m = fmaxf(m, quad_move<kSwap2>(m));
+            } else {
+                float high = f[0];
+                low = f[0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) {
+                    low = fminf(low, f[e]);
+                    high = fmaxf(high, f[e]);
+                }
+                low = fminf(low, quad_move<kSwap1>(low));
+                low = fminf(low, quad_move<kSwap2>(low));
+                high = fmaxf(high, quad_move<kSwap1>(high));
+                high = fmaxf(high, quad_move<kSwap2>(high));
+                // rounding keeps the order of numbers, so the largest of the rounded differences is this one
+                m = high - low;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = f[e] - low;
+            }
+            float inv = kSteps / m;
+            const bool some = m > 0.0f && inv <= 3.402823466e38f;
+            const float scale = some ? m / kSteps : 0.0f;
+            inv = some ? inv : 0.0f;
+            if ((c & 3) == 0) {
+                s_scale[row * R::kGroups + c / 4] = scale;
+                if constexpr (kStore == SALI_STORE_INT4) {
+                    Piece<kBf16> z;
+                    z.h[0] = (typename Half<kBf16>::type)low;           // exact: one of the values
+                    s_low[row * R::kGroups + c / 4] = z.b16[0];
+                }
+            }
+            Piece<kBf16> code;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float q = fminf(fmaxf(rintf(f[e] * inv), kStore == SALI_STORE_INT8 ? -kSteps : 0.0f), kSteps);
+                code.b8[e] = (uint8_t)(int)q;
+            }
+            if constexpr (kStore == SALI_STORE_INT8) {
+                *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + c * 8) = (u32x2){code.u.x, code.u.y};
+            } else {
+                // lanes 0, 1 of a quad hold values 0 .. 15 of the group, lanes 2, 3 the others, which go to the high halves of the same bytes
+                const uint32_t a = quad_move<kSwap2>(code.u.x) << 4 | code.u.x, b = quad_move<kSwap2>(code.u.y) << 4 | code.u.y;
+                if ((c & 2) == 0) *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + (c / 4) * 16 + (c & 1) * 8) = (u32x2){a, b};
+            }
+        }
+    }
+    if (bad) atomicOr(seqs.status, SALI_FAULT_NONFINITE);
+    __syncthreads();
+
+    // K: pieces of 16 bytes, [piece of the row][place]
+#pragma unroll
+    for (int i = 0; i < (R::kBytes + 255) / 256; ++i) {
+        const int p = (int)threadIdx.x + 256 * i, t = token_of_place(p & 15);
+        if (p < R::kBytes && t >= w.t0 && t < w.t1)
+            *reinterpret_cast<u32x4*>(w.block + p * 16) = *reinterpret_cast<const u32x4*>(s_rows + t * R::kPitch + (p >> 4) * 16);
+    }
+    // V: for each half of the block and each element of a row (a value, a code, a byte of two codes) those of eight tokens
+    constexpr int kElem = kStore == SALI_STORE_16 ? 2 : 1, kElems = R::kBytes / kElem;
+#pragma unroll
+    for (int i = 0; i < (2 * kElems + 255) / 256; ++i) {
+        const int p = (int)threadIdx.x + 256 * i, a = p / kElems, e = p % kElems;
+        if (p >= 2 * kElems) continue;
+        Piece<kBf16> o;
+        o.u = (u32x4){0u, 0u, 0u, 0u};
+        const uint8_t* column = s_rows + (16 + 8 * a) * R::kPitch + e * kElem;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            if constexpr (kElem == 2) o.b16[t] = *reinterpret_cast<const uint16_t*>(column + t * R::kPitch);
+            else o.b8[t] = column[t * R::kPitch];
+        }
+        char* dst = w.block + kAt.v + (uint32_t)p * (8 * kElem);
+        if (w.t0 <= 8 * a && w.t1 >= 8 * a + 8) {
+            if constexpr (kElem == 2) *reinterpret_cast<u32x4*>(dst) = o.u;
+            else *reinterpret_cast<u32x2*>(dst) = (u32x2){o.u.x, o.u.y};
+        } else {
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                if (8 * a + t < w.t0 || 8 * a + t >= w.t1) continue;
+                if constexpr (kElem == 2) reinterpret_cast<uint16_t*>(dst)[t] = o.b16[t];
+                else reinterpret_cast<uint8_t*>(dst)[t] = o.b8[t];
+            }
+        }
+    }
+    if constexpr (kStore != SALI_STORE_16) {
+        const int p = (int)threadIdx.x;                     // [K, V][group][16]
+        if (p < 32 * R::kGroups) {
+            const int side = p / (16 * R::kGroups), group = p / 16 % R::kGroups, t = side == 0 ? token_of_place(p & 15) : p & 15;
+            if (t >= w.t0 && t < w.t1) {
+                const int from = (16 * side + t) * R::kGroups + group;
+                reinterpret_cast<float*>(w.block + kAt.ks)[p] = s_scale[from];
+                if constexpr (kStore == SALI_STORE_INT4) reinterpret_cast<uint16_t*>(w.block + kAt.kz)[p] = s_low[from];
+            }
+        }
+    }
+}
+
+template <int kStore, int kDim, bool kBf16>
+__global__ __launch_bounds__(256) void k_pages_read(PageGeom g, PageSeqs seqs, RowsOut k, RowsOut v) {
+    typedef Rows<kStore, kDim> R;
+    typedef typename Half<kBf16>::type T;
+    constexpr int kPieces = kDim / 8, kItems = 32 * kPieces;
+    constexpr BlockLayout kAt = block_layout(kStore, kDim);
+    constexpr int kElem = kStore == SALI_STORE_16 ? 2 : 1, kElems = R::kBytes / kElem;
+    constexpr int kKLoads = (R::kBytes + 255) / 256, kVLoads = (2 * kElems + 255) / 256;
+    __shared__ __align__(16) uint8_t s_rows[32 * R::kPitch];
+    __shared__ float s_scale[kStore == SALI_STORE_16 ? 1 : 32 * R::kGroups];
+    __shared__ uint16_t s_low[kStore == SALI_STORE_INT4 ? 32 * R::kGroups : 1];
+    BlockWork w;
+    if (!find_work(g, seqs, w)) return;
+    if (w.block != nullptr) {
+        u32x4 kp[kKLoads];
+        Piece<kBf16> vp[kVLoads];
+#pragma unroll
+        for (int i = 0; i < kKLoads; ++i) {
+            const int p = (int)threadIdx.x + 256 * i;
+            if (p < R::kBytes) kp[i] = *reinterpret_cast<const u32x4*>(w.block + p * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < kVLoads; ++i) {
+            const int p = (int)threadIdx.x + 256 * i;
+            if (p >= 2 * kElems) continue;
+            const char* src = w.block + kAt.v + (uint32_t)p * (8 * kElem);
+            if constexpr (kElem == 2) {
+                vp[i].u = *reinterpret_cast<const u32x4*>(src);
+            } else {
+                const u32x2 c = *reinterpret_cast<const u32x2*>(src);
+                vp[i].u = (u32x4){c.x, c.y, 0u, 0u};
+            }
+        }
+        if constexpr (kStore != SALI_STORE_16) {
+            const int p = (int)threadIdx.x;
+            if (p < 32 * R::kGroups) {
+                const int side = p / (16 * R::kGroups), group = p / 16 % R::kGroups, t = side == 0 ? token_of_place(p & 15) : p & 15;
+                const int to = (16 * side + t) * R::kGroups + group;
+                s_scale[to] = reinterpret_cast<const float*>(w.block + kAt.ks)[p];
+                if constexpr (kStore == SALI_STORE_INT4) s_low[to] = reinterpret_cast<const uint16_t*>(w.block + kAt.kz)[p];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kKLoads; ++i) {
+            const int p = (int)threadIdx.x + 256 * i;
+            if (p < R::kBytes) *reinterpret_cast<u32x4*>(s_rows + token_of_place(p & 15) * R::kPitch + (p >> 4) * 16) = kp[i];
+        }
+#pragma unroll
+        for (int i = 0; i < kVLoads; ++i) {
+            const int p = (int)threadIdx.x + 256 * i, a = p / kElems, e = p % kElems;
+            if (p >= 2 * kElems) continue;
+            uint8_t* column = s_rows + (16 + 8 * a) * R::kPitch + e * kElem;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                if constexpr (kElem == 2) *reinterpret_cast<uint16_t*>(column + t * R::kPitch) = vp[i].b16[t];
+                else column[t * R::kPitch] = vp[i].b8[t];
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems / 256; ++i) {
+        const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces, t = row & 15;
+        if (t < w.t0 || t >= w.t1) continue;
+        Piece<kBf16> o;
+        o.u = (u32x4){0u, 0u, 0u, 0u};
+        if (w.block != nullptr) {
+            if constexpr (kStore == SALI_STORE_16) {
+                o.u = *reinterpret_cast<const u32x4*>(s_rows + row * R::kPitch + c * 16);
+            } else {
+                const float scale = s_scale[row * R::kGroups + c / 4];
+                Piece<kBf16> code;
+                if constexpr (kStore == SALI_STORE_INT8) {
+                    const u32x2 q = *reinterpret_cast<const u32x2*>(s_rows + row * R::kPitch + c * 8);
+                    code.u = (u32x4){q.x, q.y, 0u, 0u};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o.h[e] = rounded_after_f32<T>((float)(int)(int8_t)code.b8[e] * scale);
+                } else {
+                    Piece<kBf16> z;
+                    z.b16[0] = s_low[row * R::kGroups + c / 4];
+                    const float low = (float)z.h[0];
+                    const u32x2 q = *reinterpret_cast<const u32x2*>(s_rows + row * R::kPitch + (c / 4) * 16 + (c & 1) * 8);
+                    const int shift = (c & 2) * 2;          // values 16 .. 31 of a group lie in the high halves
+                    code.u = (u32x4){q.x >> shift & 0x0F0F0F0Fu, q.y >> shift & 0x0F0F0F0Fu, 0u, 0u};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o.h[e] = rounded_after_f32<T>(__builtin_fmaf((float)code.b8[e], scale, low));
+                }
+            }
+        }
+        const RowsOut& out = row < 16 ? k : v;
+        *reinterpret_cast<u32x4*>(out.d + (int64_t)(w.row0 + t) * out.token_bytes + (int64_t)w.head * out.head_bytes + c * 16) = o.u;
+    }
+}
+
+template <typename F>
+hipError_t by_type(int dtype, int store, int dim, const F& go) {
+    auto with_dim = [&](auto bf16, auto st) {
+        if (dim == 64) go(bf16, st, std::integral_constant<int, 64>{});
+        else go(bf16, st, std::integral_constant<int, 128>{});
+    };
+    auto with_store = [&](auto bf16) {
+        if (store == SALI_STORE_16) with_dim(bf16, std::integral_constant<int, SALI_STORE_16>{});
+        else if (store == SALI_STORE_INT8) with_dim(bf16, std::integral_constant<int, SALI_STORE_INT8>{});
+        else with_dim(bf16, std::integral_constant<int, SALI_STORE_INT4>{});
+    };
+    if (dtype == SALI_DTYPE_BF16) with_store(std::true_type{});
+    else with_store(std::false_type{});
+    return hipGetLastError();
+}
+
+uint32_t slot_blocks(const PageGeom& g, const PageSeqs& q) {
+    return (uint32_t)((q.n_tokens / kBlockTokens + 2ll * q.n_seqs) * g.n_kv);
+}
+
+}  // namespace
+
+hipError_t launch_pages_append(int dtype, int store, int dim, const PageGeom& g, const PageSeqs& seqs, const RowsIn& k, const RowsIn& v, hipStream_t s) {
+    return by_type(dtype, store, dim, [&](auto bf16, auto st, auto d) {
+        hipLaunchKernelGGL((k_pages_append<decltype(st)::value, decltype(d)::value, decltype(bf16)::value>), dim3(slot_blocks(g, seqs)), dim3(256), 0, s,
+                           g, seqs, k, v);
+    });
+}
+
+hipError_t launch_pages_read(int dtype, int store, int dim, const PageGeom& g, const PageSeqs& seqs, const RowsOut& k, const RowsOut& v, hipStream_t s) {
+    return by_type(dtype, store, dim, [&](auto bf16, auto st, auto d) {
+        hipLaunchKernelGGL((k_pages_read<decltype(st)::value, decltype(d)::value, decltype(bf16)::value>), dim3(slot_blocks(g, seqs)), dim3(256), 0, s,
+                           g, seqs, k, v);
+    });
+}
+
+}  // namespace sali

@@ -1,0 +1,471 @@
+"""Paged cache of text tokens on the GPU: writing, reading back and attention against oracle/pages.py (float64, the layout value by
+value).  Bytes and read-back rows are compared for equality; attention within the bounds that oracle.pages.bounds derives."""
+import itertools
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as op
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+TORCH = {"fp16": torch.float16, "bf16": torch.bfloat16}
+FORMATS = [(st, dt, d) for st, dt, d in itertools.product(("16", "int8", "int4"), ("fp16", "bf16"), (64, 128))]
+
+
+def bits_of(t):
+    return t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def rows(rng, n, heads, d, dtype, scale=1.0):
+    """[n, heads, d] of the 16-bit type; channels differ in size."""
+    x = rng.standard_normal((n, heads, d)).astype(np.float32) * np.exp(0.5 * rng.standard_normal((heads, d))).astype(np.float32) * scale
+    return torch.from_numpy(op.to_bits(x, dtype).view(np.int16)).view(TORCH[dtype])
+
+
+class Cache:
+    """Pages with a history: every sequence's rows so far written in one call; pages shuffled, the pool full of NaN patterns before."""
+
+    def __init__(self, spec, lengths, seed, layers=1, layer=0, extra_pages=2, history=True):
+        from paper_2602_14236_amd import binding
+        self.b, self.spec, self.lengths, self.layer = binding, spec, list(lengths), layer
+        self.rng = np.random.default_rng(seed)
+        held = [-(-n // spec.page_tokens) for n in lengths]
+        n_pages = sum(held) + extra_pages
+        cfg = binding.make_pages_config(n_layers=layers, n_kv_heads=spec.n_kv_heads, n_heads=spec.n_heads, head_dim=spec.head_dim,
+                                        page_tokens=spec.page_tokens, n_pages=n_pages, dtype=TORCH[spec.dtype], store=spec.store)
+        self.pages = binding.SaliPages(cfg, DEV)
+        self.pages.pool.fill_(0xFF)
+        order = self.rng.permutation(n_pages).astype(np.int32)
+        self.table = np.full((len(lengths), max(held + [1])), -7, np.int32)
+        at = 0
+        for s, h in enumerate(held):
+            self.table[s, :h] = order[at:at + h]
+            at += h
+        self.k = [rows(self.rng, n, spec.n_kv_heads, spec.head_dim, spec.dtype) for n in lengths]
+        self.v = [rows(self.rng, n, spec.n_kv_heads, spec.head_dim, spec.dtype) for n in lengths]
+        if history and sum(lengths):
+            self.write([(n, n) for n in lengths])
+
+    def batch(self, new_and_len, room=0, table=None):
+        start = np.cumsum([0] + [n for n, _ in new_and_len]).astype(np.int32)
+        length = np.array([t for _, t in new_and_len], np.int32)
+        return self.b.PageBatch(torch.from_numpy(start).to(DEV), torch.from_numpy(length).to(DEV),
+                                torch.from_numpy(self.table if table is None else table).to(DEV), int(start[-1]) + room,
+                                max_q=max([n for n, _ in new_and_len] + [0]), max_kv=max([t for _, t in new_and_len] + [0]))
+
+    def new_rows(self, rows_of_seq, new_and_len):
+        parts = [r[t - n:t] for r, (n, t) in zip(rows_of_seq, new_and_len)]
+        return torch.cat(parts).to(DEV)
+
+    def write(self, new_and_len):
+        self.pages.append(self.layer, self.batch(new_and_len), self.new_rows(self.k, new_and_len), self.new_rows(self.v, new_and_len))
+
+    def stored(self, x):
+        """float64 of what rows read back as"""
+        return op.to_f32(op.read_back(bits_of(x), self.spec), self.spec.dtype).astype(np.float64)
+
+    def check(self, new_and_len, q, out, lse, scale, window=0, sinks=0, prior=None, prior_lse=None, hidden=None):
+        out, lse = op.to_f32(bits_of(out), self.spec.dtype).astype(np.float64), lse.cpu().numpy().astype(np.float64)
+        at = 0
+        for s, (n, t) in enumerate(new_and_len):
+            if n == 0:
+                continue
+            k, v = self.stored(self.k[s][:t]), self.stored(self.v[s][:t])
+            qs = op.to_f32(bits_of(q[at:at + n]), self.spec.dtype).astype(np.float64)
+            pr = None if prior is None else prior[at:at + n].cpu().numpy().astype(np.float64)
+            pl = None if prior_lse is None else prior_lse[at:at + n].cpu().numpy().astype(np.float64)
+            e_out, e_lse, mass, reach = op.attend(qs, k, v, t, scale, window, sinks, pr, pl, None if hidden is None else hidden.get(s))
+            d_out, d_lse = op.bounds(self.spec, e_out, e_lse, mass, reach, t, np.abs(v[np.isfinite(v)]).max(initial=0.0))
+            g_out, g_lse = out[at:at + n], lse[at:at + n]
+            for got, exp, far, what in ((g_out, e_out, d_out, "out"), (g_lse, e_lse, d_lse, "lse")):
+                same = (got == exp) | (np.isnan(got) & np.isnan(exp))
+                with np.errstate(invalid="ignore"):
+                    bad = ~(same | (np.abs(got - exp) <= far))
+                assert not bad.any(), f"{what} of sequence {s} ({n} of {t}): {bad.sum()} of {bad.size} off, first {np.argwhere(bad)[0]}: " \
+                                      f"{got[bad][0]} against {exp[bad][0]}, bound {np.broadcast_to(far, got.shape)[bad][0]}"
+            at += n
+
+    def attend(self, new_and_len, scale=None, window=0, sinks=0, prior=False, check=True, room=0, **kw):
+        spec = self.spec
+        t = sum(n for n, _ in new_and_len)
+        q = rows(self.rng, t + room, spec.n_heads, spec.head_dim, spec.dtype).to(DEV)
+        out = torch.full((t + room, spec.n_heads, spec.head_dim), 7.0, dtype=TORCH[spec.dtype], device=DEV)
+        lse = torch.full((t + room, spec.n_heads), 7.0, device=DEV)
+        scale = spec.head_dim ** -0.5 if scale is None else scale
+        pr = pl = None
+        if prior:
+            pr = torch.from_numpy(self.rng.standard_normal((t + room, spec.n_heads, spec.head_dim)).astype(np.float32)).to(DEV)
+            pl = torch.from_numpy(self.rng.standard_normal((t + room, spec.n_heads)).astype(np.float32) + 3).to(DEV)
+        self.pages.attend(self.layer, self.batch(new_and_len, room), q, scale, out, lse, window=window, sinks=sinks, prior=pr, prior_lse=pl)
+        torch.cuda.synchronize()
+        if check:
+            self.check(new_and_len, q, out, lse, scale, window, sinks, pr, pl, **kw)
+        return q, out, lse
+
+
+# ---- writing and reading back ----------------------------------------------------------------------
+@pytest.mark.parametrize("store,dtype,dim", FORMATS)
+def test_bytes_of_the_pages(store, dtype, dim):
+    """Every byte of the pool against the layout's description, written in several calls that end inside blocks and pages."""
+    spec = op.PagesSpec(2, 2, dim, 32, dtype, store)
+    c = Cache(spec, [70, 1, 33, 16, 0], 1, layers=2, layer=1, history=False)
+    for step in ([(5, 5), (1, 1), (16, 16), (3, 3), (0, 0)], [(1, 6), (0, 1), (17, 33), (13, 16), (0, 0)], [(64, 70), (0, 1), (0, 33), (0, 16), (0, 0)]):
+        c.write(step)
+    assert c.pages.get_status() == 0
+    pool = c.pages.pool.cpu().numpy()
+    n_pages = c.pages.cfg.n_pages
+    expected = np.full((2, n_pages, 2, 2, spec.block_bytes), 0xFF, np.uint8)
+    for s, n in enumerate(c.lengths):
+        kb, vb = bits_of(c.k[s]), bits_of(c.v[s])
+        for block in range(-(-n // 16)):
+            own = range(min(16, n - 16 * block))
+            pad = lambda x: np.concatenate([x, np.zeros((16, dim), np.uint16)])[:16]
+            page = c.table[s, block // 2]
+            for h in range(2):
+                e = expected[1, page, h, block % 2]
+                e[:] = op.block_bytes_of(spec, pad(kb[16 * block:, h]), pad(vb[16 * block:, h]), e, own)
+    got = pool[:expected.size].reshape(expected.shape)
+    bad = np.argwhere(got != expected)
+    assert bad.size == 0, f"{len(bad)} bytes differ, first {bad[0]}: {got[tuple(bad[0])]} against {expected[tuple(bad[0])]}"
+
+
+@pytest.mark.parametrize("store,dtype,dim", FORMATS)
+@pytest.mark.parametrize("page,heads", [(16, 1), (128, 3), (256, 8)])
+def test_rows_read_back(store, dtype, dim, page, heads):
+    lengths = [1, 17, 300, 16, 40, 129]
+    c = Cache(op.PagesSpec(heads, heads, dim, page, dtype, store), lengths, 2, history=False)
+    # values that tie, vanish, and groups of one value
+    for x in c.k + c.v:
+        if len(x) > 2:
+            x[0, :, :32] = 0
+            x[1, :, 32:64] = 1.25
+            x[2, :, :32] = torch.arange(32) * 0.5 - 3
+            x[2, :, 32:64] = torch.arange(32) * 1e-6
+    new = [(n, n) for n in lengths]
+    t = sum(lengths)
+    # slices of one projection's output, as a model has them
+    both = torch.zeros((t, 4 * heads, dim), dtype=TORCH[dtype], device=DEV)
+    both[:, heads:2 * heads], both[:, 3 * heads:] = c.new_rows(c.k, new), c.new_rows(c.v, new)
+    c.pages.append(0, c.batch(new), both[:, heads:2 * heads], both[:, 3 * heads:])
+    back = torch.full((t, 2, heads, dim), 9.0, dtype=TORCH[dtype], device=DEV)
+    c.pages.read(0, c.batch(new), back[:, 0], back[:, 1])
+    for i, x in ((0, c.k), (1, c.v)):
+        got, exp = bits_of(back[:, i]), op.read_back(bits_of(c.new_rows(x, new)), c.spec)
+        same = (got == exp) | (((got | exp) & 0x7FFF) == 0)                  # a zero's sign is not kept by codes
+        assert same.all(), f"{'KV'[i]}: {np.argwhere(~same)[0]}"
+    # some of them, and others than the last
+    some = [(0, 0), (3, 10), (100, 216), (1, 16), (8, 16), (0, 5)]
+    part = torch.full((sum(n for n, _ in some) + 4, 2, heads, dim), 9.0, dtype=TORCH[dtype], device=DEV)
+    c.pages.read(0, c.batch(some, room=4), part[:, 0], part[:, 1])
+    exp = torch.cat([back[sum(lengths[:s]) + t - n:sum(lengths[:s]) + t] for s, (n, t) in enumerate(some)])
+    assert np.array_equal(bits_of(part[:-4]), bits_of(exp))
+    assert bool((part[-4:] == 9).all())                                      # rows past the batch
+    assert c.pages.get_status() == 0
+
+
+@pytest.mark.parametrize("store", ["int8", "int4"])
+def test_tiny_and_infinite_groups(store):
+    from paper_2602_14236_amd import binding
+    c = Cache(op.PagesSpec(1, 1, 64, 16, "bf16", store), [4], 3, history=False)
+    c.k[0][0, 0, :32] = 1e-38                              # 127 / 1e-38 is no fp32 number
+    c.k[0][1, 0, :32] = torch.arange(32) * 2e-39
+    c.write([(4, 4)])
+    back = torch.empty((4, 2, 1, 64), dtype=torch.bfloat16, device=DEV)
+    c.pages.read(0, c.batch([(4, 4)]), back[:, 0], back[:, 1])
+    assert np.array_equal(bits_of(back[:, 0]) & 0x7FFF, op.read_back(bits_of(c.k[0]), c.spec) & 0x7FFF)
+    assert c.pages.get_status() == 0
+    c.k[0][2, 0, 40] = math.inf
+    c.write([(4, 4)])
+    assert c.pages.get_status() == binding.FAULT_NONFINITE
+
+
+# ---- attention -------------------------------------------------------------------------------------
+BATCHES = {
+    "one token of one": [(1, 1)],
+    "single tokens": [(1, 1), (1, 2), (1, 16), (1, 17), (1, 31), (1, 32), (1, 33), (1, 64), (1, 65), (1, 400)],
+    "drafts": [(3, 3), (5, 40), (1, 200), (4, 4), (0, 7), (2, 130)],
+    "short texts": [(16, 16), (7, 90), (16, 300)],
+    "chunks": [(70, 70), (33, 310), (128, 200)],
+    "mixed": [(1, 77), (100, 250), (1, 1), (0, 0), (1, 500), (90, 90), (2, 64)],
+    "long": [(1, 3000)],
+}
+
+
+@pytest.mark.parametrize("store,dtype,dim", FORMATS)
+@pytest.mark.parametrize("name", BATCHES)
+def test_attention(store, dtype, dim, name):
+    heads = {"one token of one": (2, 2), "single tokens": (8, 2), "drafts": (6, 2), "short texts": (8, 2), "chunks": (4, 1), "mixed": (8, 2),
+             "long": (4, 4)}[name]
+    new = BATCHES[name]
+    c = Cache(op.PagesSpec(heads[1], heads[0], dim, 32, dtype, store), [t for _, t in new], 4)
+    c.attend(new)
+    c.attend(new, prior=True)
+    assert c.pages.get_status() == 0
+
+
+@pytest.mark.parametrize("store,dtype,dim", FORMATS)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (5, 3), (40, 0), (40, 70), (100, 33), (1000, 20)])
+def test_window_and_sinks(store, dtype, dim, window, sinks):
+    new = [(1, 1), (1, 45), (6, 300), (1, 333), (2, 100)]
+    c = Cache(op.PagesSpec(2, 4, dim, 16, dtype, store), [t for _, t in new], 5)
+    c.attend(new, window=window, sinks=sinks)
+    new = [(80, 80), (100, 400), (1, 200)]
+    c = Cache(op.PagesSpec(1, 4, dim, 64, dtype, store), [t for _, t in new], 6)
+    c.attend(new, window=window, sinks=sinks, prior=True)
+    assert c.pages.get_status() == 0
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (3, 1), (24, 8), (40, 40), (16, 1), (17, 1), (48, 1), (64, 1), (80, 1), (300, 1)])
+def test_head_layouts(heads, kv):
+    for new in ([(1, 100), (1, 33)], [(3, 50), (1, 20)], [(20, 150), (1, 9)]):
+        c = Cache(op.PagesSpec(kv, heads, 64, 16, "bf16", "16"), [t for _, t in new], 7)
+        c.attend(new)
+
+
+@pytest.mark.parametrize("new", [[(1, 300)] * 300, [(70, 70)] + [(1, 40)] * 270], ids=["single", "mixed"])
+def test_many_sequences(new):
+    c = Cache(op.PagesSpec(1, 2, 64, 64, "fp16", "int8"), [t for _, t in new], 8)
+    c.attend(new)
+
+
+@pytest.mark.parametrize("scale", [0.3, -0.2, 0.0, 2.0])
+def test_scales(scale):
+    for new in ([(1, 90), (4, 40)], [(90, 200)]):
+        c = Cache(op.PagesSpec(2, 4, 128, 32, "fp16", "16"), [t for _, t in new], 9)
+        c.attend(new, scale=scale)
+
+
+@pytest.mark.parametrize("new", [[(1, 70), (5, 70)], [(70, 70)]], ids=["stream", "tile"])
+def test_strides_stream_and_rows_past_the_batch(new):
+    spec = op.PagesSpec(2, 6, 64, 16, "bf16", "16")
+    c = Cache(spec, [t for _, t in new], 10)
+    t = sum(n for n, _ in new)
+    qkv = torch.zeros((t + 3, 10, 64), dtype=torch.bfloat16, device=DEV)
+    qkv[:, 2:8] = rows(c.rng, t + 3, 6, 64, "bf16").to(DEV)
+    out = torch.full((6, t + 3, 72), 7.0, dtype=torch.bfloat16, device=DEV)
+    o = out.permute(1, 0, 2)[..., :64]
+    lse = torch.full((t + 3, 6), 7.0, device=DEV)
+    side = torch.cuda.Stream()
+    batch = c.batch(new, room=3)
+    side.wait_stream(torch.cuda.current_stream())
+    c.pages.attend(0, batch, qkv[:, 2:8], 0.125, o, lse, stream=side)
+    side.synchronize()
+    c.check(new, qkv[:t, 2:8], o[:t], lse[:t], 0.125)
+    assert bool((out[:, t:] == 7).all()) and bool((out[..., 64:] == 7).all()) and bool((lse[t:] == 7).all())
+    # without the log-sum
+    again = torch.empty((t + 3, 6, 64), dtype=torch.bfloat16, device=DEV)
+    c.pages.attend(0, batch, qkv[:, 2:8], 0.125, again)
+    assert torch.equal(again[:t], o[:t])
+
+
+@pytest.mark.parametrize("new", [[(1, 70), (5, 60)], [(80, 130)]], ids=["stream", "tile"])
+def test_priors_without_weight(new):
+    c = Cache(op.PagesSpec(1, 2, 64, 16, "fp16", "16"), [t for _, t in new], 11)
+    t = sum(n for n, _ in new)
+    q = rows(c.rng, t, 2, 64, "fp16").to(DEV)
+    out, lse = torch.empty((t, 2, 64), dtype=torch.float16, device=DEV), torch.empty((t, 2), device=DEV)
+    prior = torch.full((t, 2, 64), math.nan, device=DEV)                    # never looked at where its log-sum is -inf
+    prior_lse = torch.full((t, 2), -math.inf, device=DEV)
+    prior[::2], prior_lse[::2] = 0.25, 200.0                                 # and one that leaves nothing of the keys
+    c.pages.attend(0, c.batch(new), q, 0.125, out, lse, prior=prior, prior_lse=prior_lse)
+    torch.cuda.synchronize()
+    c.check(new, q, out, lse, 0.125, prior=prior, prior_lse=prior_lse)
+    assert bool((out[::2] == 0.25).all()) and bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("store", ["16", "int8", "int4"])
+@pytest.mark.parametrize("many", [False, True], ids=["stream", "tile"])
+def test_keys_out_of_sight_do_not_reach_a_token(store, many):
+    """Later tokens, and tokens behind the window, that hold infinities and NaN (and the NaN patterns past the end of a sequence, which every test
+    has): the rows that do not see them are those of finite keys, the rows that do are not finite where the values are not."""
+    n, t = (100, 150) if many else (6, 150)
+    spec = op.PagesSpec(1, 2, 64, 16, "bf16", store)
+    c = Cache(spec, [t], 12, history=False)
+    p = t - n // 2                                                          # a token in the middle of the new ones
+    if store == "16":
+        c.v[0][p, 0, 3], c.v[0][p, 0, 7], c.v[0][p, 0, 9] = math.inf, -math.inf, math.nan
+        c.v[0][p + 1, 0, 7] = math.inf
+        c.v[0][5, 0, 20] = math.nan                                         # behind the window below
+    else:
+        c.v[0][p, 0, :] = math.inf
+    c.write([(t, t)])
+    for window, sinks in ((0, 0), (40, 3)) if store == "16" else ((0, 0),):
+        q, out, lse = c.attend([(n, t)], window=window, sinks=sinks, check=store == "16")
+        before = out[:p - (t - n)].float()
+        if store == "16" and window == 0:
+            before = torch.cat([before[..., :20], before[..., 21:]], -1)
+        assert bool(torch.isfinite(before).all()), "a key out of sight reaches a row"
+        assert bool(torch.isfinite(lse).all())
+
+
+@pytest.mark.parametrize("many", [False, True], ids=["stream", "tile"])
+def test_a_key_that_is_not_a_number(many):
+    n, t = (100, 150) if many else (6, 150)
+    c = Cache(op.PagesSpec(1, 2, 64, 16, "fp16", "16"), [t], 13, history=False)
+    p = t - n // 2
+    c.k[0][p, 0, 3] = math.nan
+    c.write([(t, t)])
+    q, out, lse = c.attend([(n, t)], check=False)
+    assert bool(torch.isfinite(out[:n - n // 2]).all()) and bool(torch.isfinite(lse[:n - n // 2]).all())
+    assert bool(torch.isnan(out[n - n // 2:]).all()) and bool(torch.isnan(lse[n - n // 2:]).all())
+
+
+@pytest.mark.parametrize("many", [False, True], ids=["stream", "tile"])
+def test_pages_that_are_none(many):
+    """A table entry outside the pool hides its tokens from attention, is not written, reads back as zeros, and is noted; rows that see nothing
+    are zeros with a log-sum of -inf."""
+    from paper_2602_14236_amd import binding
+    n, t = (70, 200) if many else (1, 200)
+    spec = op.PagesSpec(1, 2, 64, 32, "fp16", "16")
+    new = [(n, t), (1, 20), (2, 40)]
+    c = Cache(spec, [x for _, x in new], 14)
+    c.table[0, 2], c.table[1, 0] = c.pages.cfg.n_pages, -1
+    hidden = {0: np.arange(t) // 32 == 2, 1: np.ones(20, bool)}
+    assert c.pages.get_status() == 0
+    q, out, lse = c.attend(new, hidden=hidden)
+    assert c.pages.get_status() == binding.FAULT_PAGE
+    assert bool((out[n] == 0).all()) and bool(torch.isneginf(lse[n]).all())
+    pool = c.pages.pool.clone()
+    c.write([(0, t), (20, 20), (0, 40)])
+    assert torch.equal(pool, c.pages.pool)
+    back = torch.full((20, 2, 1, 64), 9.0, dtype=torch.float16, device=DEV)
+    c.pages.read(0, c.batch([(0, t), (20, 20), (0, 40)]), back[:, 0], back[:, 1])
+    assert bool((back == 0).all())
+
+
+@pytest.mark.parametrize("many", [False, True], ids=["stream", "tile"])
+def test_sequences_that_contradict_the_batch(many):
+    """They are left out and noted; the others are as ever."""
+    from paper_2602_14236_amd import binding
+    n = 70 if many else 2
+    new = [(n, 90), (n, 100), (n, 80)]
+    c = Cache(op.PagesSpec(1, 2, 64, 32, "fp16", "16"), [t for _, t in new], 15)
+    for length in (n - 1, 101, 2 ** 31 - 1, -5):
+        batch = c.batch(new)
+        batch.tensors[1][1] = length
+        q = rows(c.rng, 3 * n, 2, 64, "fp16").to(DEV)
+        out, lse = torch.full((3 * n, 2, 64), 7.0, dtype=torch.float16, device=DEV), torch.full((3 * n, 2), 7.0, device=DEV)
+        c.pages.attend(0, batch, q, 0.125, out, lse)
+        torch.cuda.synchronize()
+        keep = torch.cat([torch.arange(n), torch.arange(2 * n, 3 * n)]).to(DEV)
+        assert bool((out[n:2 * n] == 7).all()) and bool((lse[n:2 * n] == 7).all())
+        table, k, v = c.table, c.k, c.v
+        c.k, c.v = [k[0], k[2]], [v[0], v[2]]
+        c.check([new[0], new[2]], q[keep], out[keep], lse[keep], 0.125)
+        c.k, c.v = k, v
+        pool = c.pages.pool.clone()
+        c.pages.append(0, batch, rows(c.rng, 3 * n, 1, 64, "fp16").to(DEV)[:, :1], rows(c.rng, 3 * n, 1, 64, "fp16").to(DEV))
+        changed = (c.pages.pool != pool).view(c.pages.cfg.n_pages, -1).any(1).cpu().numpy()
+        assert not changed[table[1, :4]].any()
+        c.write([(90, 90), (100, 100), (80, 80)])
+    assert c.pages.get_status() & binding.FAULT_BATCH
+    batch = c.batch(new)
+    batch.tensors[0][1] = 4 * n                              # rows past the arrays, and starts that fall
+    c.pages.attend(0, batch, q, 0.125, out, lse)
+    c.pages.read(0, batch, torch.empty((3 * n, 1, 64), dtype=torch.float16, device=DEV), torch.empty((3 * n, 1, 64), dtype=torch.float16, device=DEV))
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("many", [False, True], ids=["stream", "tile"])
+def test_captured_calls_follow_the_lengths(many):
+    """Append and attention captured once and replayed with other lengths and values, eager calls of another size between."""
+    n = 70 if many else 1
+    spec = op.PagesSpec(2, 4, 64, 32, "bf16", "int8")
+    lengths = [200, 300]
+    c = Cache(spec, lengths, 16)
+    batch = c.batch([(n, 100), (n, 300)])
+    k, v, q = (torch.zeros((2 * n, h, 64), dtype=torch.bfloat16, device=DEV) for h in (2, 2, 4))
+    out, lse = torch.empty_like(q), torch.empty((2 * n, 4), device=DEV)
+
+    def step():
+        c.pages.append(0, batch, k, v)
+        c.pages.attend(0, batch, q, 0.125, out, lse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for lens in ([100, 300], [130, 150], [200, 71]):
+        new = list(zip([n, n], lens))
+        batch.tensors[1].copy_(torch.tensor(lens, dtype=torch.int32))
+        k.copy_(c.new_rows(c.k, new))
+        v.copy_(c.new_rows(c.v, new))
+        q.copy_(rows(c.rng, 2 * n, 4, 64, "bf16"))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(new, q, out, lse, 0.125)
+        c.attend([(1, 50), (80, 100)])                       # another call's partial results and plans in the same scratch
+    assert c.pages.get_status() == 0
+
+
+def test_layers_and_objects_share_nothing():
+    spec = op.PagesSpec(1, 1, 64, 16, "fp16", "16")
+    a, b = Cache(spec, [50], 17, layers=3, layer=0), None
+    first = a.pages.pool.clone()
+    a.layer = 2
+    a.k = [rows(a.rng, 50, 1, 64, "fp16")]
+    a.write([(50, 50)])
+    per = a.pages.pool.numel() // 3
+    assert torch.equal(first[:2 * per], a.pages.pool[:2 * per]) and not torch.equal(first[2 * per:], a.pages.pool[2 * per:])
+    a.attend([(3, 50)])
+    # another object over the same pool
+    other = a.b.SaliPages(a.pages.cfg, DEV, pool=a.pages.pool)
+    a.pages, b = other, a.pages
+    a.attend([(3, 50)])
+    b.close()
+
+
+def test_refusals():
+    from paper_2602_14236_amd import binding
+    c = Cache(op.PagesSpec(2, 4, 64, 16, "fp16", "16"), [20, 20], 18)
+    good = c.batch([(1, 20), (1, 20)])
+    f16 = lambda *s: torch.zeros(s, dtype=torch.float16, device=DEV)
+    q, out, k = f16(2, 4, 64), f16(2, 4, 64), f16(2, 2, 64)
+    c.pages.attend(0, good, q, 1.0, out)
+
+    def code(f):
+        with pytest.raises(binding.SaliError) as e:
+            f()
+        return e.value.code
+
+    attend = c.pages.attend
+    for layer in (-1, 1):
+        assert code(lambda: attend(layer, good, q, 1.0, out)) == -2
+        assert code(lambda: c.pages.append(layer, good, k, k)) == -2
+        assert code(lambda: c.pages.read(layer, good, k, k)) == -2
+    assert code(lambda: attend(0, good, q, math.nan, out)) == -4
+    assert code(lambda: attend(0, good, q, math.inf, out)) == -4
+    assert code(lambda: attend(0, good, q, 3e38, out)) == -4
+    assert code(lambda: attend(0, good, q, 1.0, out, window=-1)) == -2
+    assert code(lambda: attend(0, good, q, 1.0, out, window=4, sinks=-1)) == -2
+    odd = f16(2 * 4 * 64 + 8)[1:2 * 4 * 64 + 1].view(2, 4, 64)
+    assert code(lambda: attend(0, good, odd, 1.0, out)) == -3
+    assert code(lambda: attend(0, good, q, 1.0, f16(2, 4, 65)[..., :64])) == -3
+    assert code(lambda: attend(0, good, q, 1.0, out, prior=torch.zeros((2, 4, 64), device=DEV))) == -1
+    for field, value, exp in (("n_seqs", -1, -2), ("n_seqs", 1 << 20, -2), ("max_q", -1, -2), ("table_width", -1, -2), ("d_start", None, -1), ("d_table", None, -1)):
+        bad = c.batch([(1, 20), (1, 20)])
+        setattr(bad.c, field, value)
+        assert code(lambda: attend(0, bad, q, 1.0, out)) == exp, field
+    for bad_q in (q.float(), f16(3, 4, 64), f16(2, 4, 128)[..., ::2], q.bfloat16(), q.cpu()):
+        with pytest.raises(ValueError):
+            attend(0, good, bad_q, 1.0, out)
+    with pytest.raises(ValueError):
+        attend(0, good, q, 1.0, out, torch.zeros((2, 4), dtype=torch.float16, device=DEV))
+    with pytest.raises(ValueError):
+        attend(0, good, q, 1.0, out, prior=torch.zeros((2, 4, 32), device=DEV), prior_lse=torch.zeros((2, 4), device=DEV))
+    # nothing to do
+    none = binding.PageBatch(torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV),
+                             torch.zeros((0, 1), dtype=torch.int32, device=DEV), 0, max_kv=0)
+    attend(0, none, q[:0], 1.0, out[:0])
+    c.pages.append(0, none, k[:0], k[:0])
+    torch.cuda.synchronize()
+    assert c.pages.get_status() == 0
