@@ -442,8 +442,8 @@ int sali_get_status(sali_ctx* ctx, uint32_t* h_flags, void* stream);
  *   SALI_STORE_INT4  K [D / 32][place][16 bytes]        V [2][D / 32][16][8 tokens]      the same, smallest values alike; byte e of 16
  *                                                       holds value e of a group in its low half, value e + 16 in its high half
  * Quantised values are those of sali_kv_compress / sali_kv_decompress, in the pool's 16-bit type (a group of bfloat16 values
- * that are all below 2^-121 is stored as zeros: 127 and 15 divided by it are no fp32 numbers); a group that holds an inf or NaN
- * sets SALI_FAULT_NONFINITE (for SALI_STORE_16 too, which stores it as it is) and is otherwise unspecified.
+ * that are all below 2^-121 is stored as zeros: 127 and 15 divided by it are no fp32 numbers).  A group that holds an inf or NaN
+ * sets SALI_FAULT_NONFINITE; SALI_STORE_16 keeps it as it is, the others store zeros for it.
  * ------------------------------------------------------------------------------------------------- */
 #define SALI_DTYPE_FP16  0
 #define SALI_DTYPE_BF16  1

@@ -61,21 +61,24 @@ def to_bits(x, dtype):
 
 # ---- the quantiser ---------------------------------------------------------------------------------
 def quantise(x, store):
-    """fp32 rows [..., D] -> (codes [..., D/32, 32], scale, smallest or None), every step one fp32 operation."""
+    """fp32 rows [..., D] -> (codes [..., D/32, 32], scale, smallest or None), every step one fp32 operation.  Groups with a value that is not
+    finite, or too wide or too small for steps in fp32, become zeros (codes, scale and, where a value is not finite or the group too wide, smallest)."""
     g = x.astype(np.float32).reshape(x.shape[:-1] + (-1, GROUP))
     steps = np.float32(127 if store == "int8" else 15)
-    if store == "int8":
-        low, m = None, np.abs(g).max(-1)
-    else:
-        low = g.min(-1)
-        m = (g.max(-1) - low).astype(np.float32)
-        g = (g - low[..., None]).astype(np.float32)
     with np.errstate(all="ignore"):
+        if store == "int8":
+            low, m = None, np.abs(g).max(-1)
+        else:
+            low = g.min(-1)
+            m = (g.max(-1) - low).astype(np.float32)
+            g = (g - low[..., None]).astype(np.float32)
+        sound = np.isfinite(x.reshape(g.shape)).all(-1) & np.isfinite(m)
         inv = (steps / m).astype(np.float32)
-        some = (m > 0) & np.isfinite(inv)
+        some = sound & (m > 0) & np.isfinite(inv)
         scale = np.where(some, m / steps, 0).astype(np.float32)
-        inv = np.where(some, inv, 0).astype(np.float32)
-    q = np.clip(np.rint((g * inv[..., None]).astype(np.float32)), -127 if store == "int8" else 0, steps)
+        q = np.where(some[..., None], np.clip(np.rint((g * inv[..., None]).astype(np.float32)), -127 if store == "int8" else 0, steps), 0)
+        if low is not None:
+            low = np.where(sound, low, 0).astype(np.float32)
     return q.astype(np.int32), scale, low
 
 

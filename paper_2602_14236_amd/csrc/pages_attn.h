@@ -12,9 +12,10 @@
 // Nothing seen: m = -inf, sum 0.
 //
 // Masked keys.  Scores outside a row's view become -inf, whatever they were, and their weights 0.  A weight of 0 does not take
-// out an infinity or NaN in V, so tiles that are not wholly in view of all rows look at their values: if any is not finite, the product
-// runs over the finite ones and what the others add is found by two more products that count, for every output, the
-// infinities of each sign in its view (a NaN counts for both).
+// out an infinity or NaN in V.  What no token has written (past a sequence's end, pages that are none) is set to zero before the product, by
+// position; quantised values are finite wherever they were written.  16-bit rows are looked at in tiles that are not wholly in view
+// of all rows: values that are not finite are set to zero for the product, two more products count, for every output, the
+// infinities of each sign in its view (a NaN counts for both), and what was found is added to the result at the end.
 #pragma once
 
 #include <type_traits>
@@ -171,8 +172,24 @@ template <bool kBf16>
 __device__ __forceinline__ bool any_not_finite(const u32x4& v) {
     return (not_finite<kBf16>(v.x) | not_finite<kBf16>(v.y) | not_finite<kBf16>(v.z) | not_finite<kBf16>(v.w)) != 0;
 }
+// the words of a piece of 8 tokens with those from `live` on set to zero
+__device__ __forceinline__ u32x4 live_tokens(const u32x4& v, int live) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (2 * i < live ? v[i] & 0xFFFFu : 0u) | (2 * i + 1 < live ? v[i] & 0xFFFF0000u : 0u);
+    return r;
+}
+__device__ __forceinline__ Scales8 live_tokens(const Scales8& s, int live) {
+    Scales8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.a[i] = i < live ? s.a[i] : 0.0f;
+        r.b[i] = i + 4 < live ? s.b[i] : 0.0f;
+    }
+    return r;
+}
 template <bool kBf16>
-__device__ __forceinline__ void take_apart(const u32x4& v, u32x4& finite, u32x4& plus, u32x4& minus) {
+__device__ __forceinline__ void take_apart(const u32x4 v, u32x4& finite, u32x4& plus, u32x4& minus) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t w = v[i], bad = not_finite<kBf16>(w), mask = (bad >> 15) * 0xFFFFu;
@@ -208,6 +225,8 @@ __device__ __forceinline__ RowEnd row_end(float m, float l, const PagesAttend& a
     r.by_prior = w2 / sum;
     return r;
 }
+// what values that are not finite add to a result
+__device__ __forceinline__ float found(bool up, bool down) { return (up ? INFINITY : 0.0f) + (down ? -INFINITY : 0.0f); }
 // a weight of zero takes out whatever the other factor is
 __device__ __forceinline__ float joined(const RowEnd& e, float own, float prior) {
     const float a = e.by_own == 0.0f ? 0.0f : own * e.by_own;

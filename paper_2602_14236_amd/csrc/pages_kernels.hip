@@ -135,9 +135,9 @@ __global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs,
 #pragma unroll
     for (int i = 0; i < kItems / 256; ++i) {
         const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) bad |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent;
         if constexpr (kStore == SALI_STORE_16) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) bad |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent;
             *reinterpret_cast<u32x4*>(s_rows + row * R::kPitch + c * 16) = x[i].u;
         } else {
             float f[8];
@@ -169,21 +169,29 @@ __global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs,
                 for (int e = 0; e < 8; ++e) f[e] = f[e] - low;
             }
             float inv = kSteps / m;
-            const bool some = m > 0.0f && inv <= 3.402823466e38f;
+            // a group with an infinity or NaN, or one too wide or too small for fp32 steps, is stored as zeros: every value of the pages is finite
+            uint32_t odd = 0u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) odd |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent ? 1u : 0u;
+            odd |= m <= 3.402823466e38f ? 0u : 1u;
+            odd |= quad_move<kSwap1>(odd);
+            odd |= quad_move<kSwap2>(odd);
+            bad |= odd != 0u;
+            const bool some = odd == 0u && m > 0.0f && inv <= 3.402823466e38f;
             const float scale = some ? m / kSteps : 0.0f;
             inv = some ? inv : 0.0f;
             if ((c & 3) == 0) {
                 s_scale[row * R::kGroups + c / 4] = scale;
                 if constexpr (kStore == SALI_STORE_INT4) {
                     Piece<kBf16> z;
-                    z.h[0] = (typename Half<kBf16>::type)low;           // exact: one of the values
+                    z.h[0] = (typename Half<kBf16>::type)(odd == 0u ? low : 0.0f);       // exact: one of the values
                     s_low[row * R::kGroups + c / 4] = z.b16[0];
                 }
             }
             Piece<kBf16> code;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float q = fminf(fmaxf(rintf(f[e] * inv), kStore == SALI_STORE_INT8 ? -kSteps : 0.0f), kSteps);
+                const float q = some ? fminf(fmaxf(rintf(f[e] * inv), kStore == SALI_STORE_INT8 ? -kSteps : 0.0f), kSteps) : 0.0f;
                 code.b8[e] = (uint8_t)(int)q;
             }
             if constexpr (kStore == SALI_STORE_INT8) {

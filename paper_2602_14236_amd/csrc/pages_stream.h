@@ -231,7 +231,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
         int page0 = -64, page_of_lane = -1;
         struct Tile {
             const char* b[2];
-            bool hidden[2];
+            int live[2];                     // tokens of the block that a row may see: none of a page that is none
         };
         auto locate = [&](int i) -> Tile {
             Tile t;
@@ -244,9 +244,10 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
                     page_of_lane = index + lane < pages ? table[index + lane] : -1;
                 }
                 int page = __builtin_amdgcn_readlane(page_of_lane, index - page0);
-                t.hidden[j] = (unsigned)page >= (unsigned)a.geom.n_pages;
-                if (t.hidden[j]) {
-                    if (block * kBlockTokens < seq.len && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
+                t.live[j] = min(kBlockTokens, seq.len - block * kBlockTokens);
+                if ((unsigned)page >= (unsigned)a.geom.n_pages) {
+                    if (t.live[j] > 0 && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
+                    t.live[j] = 0;
                     page = 0;
                 }
                 t.b[j] = heads + (uint64_t)page * a.geom.page_bytes + (uint32_t)(block & ((1 << a.geom.blocks_log2) - 1)) * block_bytes;
@@ -281,10 +282,12 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
         }
         float m[kSets], l[kSets];
         f32x4 acc[kSets][kFs];
+        uint32_t up[kSets], down[kSets];     // a bit for every value of acc: values that are not finite
 #pragma unroll
         for (int c = 0; c < kSets; ++c) {
             m[c] = -INFINITY;
             l[c] = 0.0f;
+            up[c] = down[c] = 0u;
 #pragma unroll
             for (int f = 0; f < kFs; ++f) acc[c][f] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
         }
@@ -308,7 +311,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
             if (more) stream_load_k<kStore, kDim>(next.b[0], next.b[1], lane, raw);
             // lane (row col, hh): tokens 8 (hh % 2) + 4 (hh / 2) .. + 3 of each block
             const int t0 = j0 + 8 * (hh & 1) + 4 * (hh >> 1);
-            const bool masked = now.hidden[0] || now.hidden[1] || partly_hidden(view, a.window, a.sinks, j0, kTileTokens);
+            const bool masked = now.live[0] < kBlockTokens || now.live[1] < kBlockTokens || partly_hidden(view, a.window, a.sinks, j0, kTileTokens);
             if (masked) {
 #pragma unroll
                 for (int c = 0; c < kSets; ++c)
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (now.hidden[j] || !sees(pos[c], t0 + 16 * j + r, a.window, a.sinks)) s2[c][j][r] = -INFINITY;
+                            if (now.live[j] <= 0 || !sees(pos[c], t0 + 16 * j + r, a.window, a.sinks)) s2[c][j][r] = -INFINITY;
             }
             u32x4 p[kSets];
 #pragma unroll
@@ -350,43 +353,62 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
                 const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
                 p[c] = (u32x4){(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]};
             }
-            bool odd = false;
             if (masked) {
+                const int live = (hh < 2 ? now.live[0] : now.live[1]) - 8 * (hh & 1);
+                if constexpr (kStore != SALI_STORE_16) {
 #pragma unroll
-                for (int f = 0; f < kFs; ++f) odd |= any_not_finite<kBf16>(stream_v<kStore, kDim, kBf16>(raw, f));
-                odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+                    for (int g = 0; g < kDim / 32; ++g) {
+                        raw.vs[g] = live_tokens(raw.vs[g], live);
+                        if constexpr (kStore == SALI_STORE_INT4) raw.vz[g] = live_tokens(raw.vz[g], live);
+                    }
+                } else {
+                    bool odd = false;
+#pragma unroll
+                    for (int f = 0; f < kFs; ++f) {
+                        raw.v[f] = live_tokens(raw.v[f], live);
+                        odd |= any_not_finite<kBf16>(raw.v[f]);
+                    }
+                    if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+                        u32x4 seen[kSets];
+#pragma unroll
+                        for (int c = 0; c < kSets; ++c)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int j = j0 + 16 * (hh >> 1) + 8 * (hh & 1) + 2 * e;
+                                seen[c][e] = (2 * e < live && sees(pos[c], j, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne : 0u) |
+                                             (2 * e + 1 < live && sees(pos[c], j + 1, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
+                            }
+                        // through the wave's part of LDS, one product at a time: this path is not to cost registers
+                        u32x4* const mine = reinterpret_cast<u32x4*>(&s_acc[wave][0][0]) + lane;
+                        static_assert(kFs * 1024 <= sizeof(s_acc[0]), "the operands of a tile's V");
+#pragma unroll
+                        for (int f = 0; f < kFs; ++f) mine[64 * f] = raw.v[f];
+#pragma unroll 1
+                        for (int f = 0; f < kFs; ++f) {
+                            u32x4 finite, plus, minus;
+                            take_apart<kBf16>(mine[64 * f], finite, plus, minus);
+                            mine[64 * f] = finite;
+#pragma unroll
+                            for (int c = 0; c < kSets; ++c) {
+                                const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                                const f32x4 ups = Num<kBf16>::mma16(plus, seen[c], zero), downs = Num<kBf16>::mma16(minus, seen[c], zero);
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    up[c] |= (ups[r] > 0.0f ? 1u << r : 0u) << (4 * f);
+                                    down[c] |= (downs[r] > 0.0f ? 1u << r : 0u) << (4 * f);
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int f = 0; f < kFs; ++f) raw.v[f] = mine[64 * f];
+                    }
+                }
             }
-            if (!odd) {
 #pragma unroll
-                for (int f = 0; f < kFs; ++f) {
-                    const u32x4 vf = stream_v<kStore, kDim, kBf16>(raw, f);
+            for (int f = 0; f < kFs; ++f) {
+                const u32x4 vf = stream_v<kStore, kDim, kBf16>(raw, f);
 #pragma unroll
-                    for (int c = 0; c < kSets; ++c) acc[c][f] = Num<kBf16>::mma16(vf, p[c], acc[c][f]);
-                }
-            } else {
-                u32x4 seen[kSets];
-#pragma unroll
-                for (int c = 0; c < kSets; ++c)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = j0 + 16 * (hh >> 1) + 8 * (hh & 1) + 2 * e;
-                        const bool hidden = hh < 2 ? now.hidden[0] : now.hidden[1];
-                        seen[c][e] = (!hidden && sees(pos[c], j, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne : 0u) |
-                                     (!hidden && sees(pos[c], j + 1, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
-                    }
-#pragma unroll
-                for (int f = 0; f < kFs; ++f) {
-                    u32x4 finite, plus, minus;
-                    take_apart<kBf16>(stream_v<kStore, kDim, kBf16>(raw, f), finite, plus, minus);
-#pragma unroll
-                    for (int c = 0; c < kSets; ++c) {
-                        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-                        acc[c][f] = Num<kBf16>::mma16(finite, p[c], acc[c][f]);
-                        const f32x4 up = Num<kBf16>::mma16(plus, seen[c], zero), down = Num<kBf16>::mma16(minus, seen[c], zero);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[c][f][r] += (up[r] > 0.0f ? INFINITY : 0.0f) + (down[r] > 0.0f ? -INFINITY : 0.0f);
-                    }
-                }
+                for (int c = 0; c < kSets; ++c) acc[c][f] = Num<kBf16>::mma16(vf, p[c], acc[c][f]);
             }
             if (more) stream_load_v<kStore, kDim>(next.b[0], next.b[1], lane, raw);
             now = next;
@@ -398,6 +420,12 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
             const int r = 16 * c + col;
             const float sum = sum_over_quarters(l[c]);
             if (r >= rows) continue;
+            if constexpr (kStore == SALI_STORE_16)
+                if ((up[c] | down[c]) != 0)
+#pragma unroll
+                    for (int f = 0; f < kFs; ++f)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[c][f][e] += found((up[c] >> (4 * f + e) & 1) != 0, (down[c] >> (4 * f + e) & 1) != 0);
             if (hh == 0) {
                 s_m[wave][r] = m[c];
                 s_l[wave][r] = sum;

@@ -177,16 +177,25 @@ __device__ __forceinline__ void tile_load(const char* block, int wave, int lane,
         }
     }
 }
+// ... with those of its tokens that are alive (the first `live`); V's others become zeros.  Are some of V's 16-bit values not finite?
 template <int kStore, int kDim, bool kBf16, int kWaves>
-__device__ __forceinline__ void tile_store(const TileRaw<kStore, kDim, kWaves>& r, int wave, int lane, uint8_t* k, uint8_t* v) {
+__device__ __forceinline__ bool tile_store(TileRaw<kStore, kDim, kWaves>& r, int live, int wave, int lane, bool look, uint8_t* k, uint8_t* v) {
     typedef TileRaw<kStore, kDim, kWaves> R;
     const int p0 = wave % (kWaves / 4) * R::kShare, at = wave / (kWaves / 4) * (32 * kDim);
+    bool odd = false;
     auto put = [](uint8_t* to, const u32x4& x) { *reinterpret_cast<u32x4*>(to) = x; };
 #pragma unroll
     for (int i = 0; i < R::kLoads; ++i) {
         if (R::kShare % 64 != 0 && lane + 64 * i >= R::kShare) continue;
         const int p = p0 + 64 * i + lane;
+        if (live < kBlockTokens) {
+            const int mine = live - 8 * (p / (R::kPieces / 2));
+            if constexpr (kStore == SALI_STORE_16) r.v[i] = live_tokens(r.v[i], mine);
+            else r.vs[i] = live_tokens(r.vs[i], mine);
+            if constexpr (kStore == SALI_STORE_INT4) r.vz[i] = live_tokens(r.vz[i], mine);
+        }
         if constexpr (kStore == SALI_STORE_16) {
+            if (look) odd |= any_not_finite<kBf16>(r.v[i]);
             put(k + at + p * 16, r.k[i]);
             put(v + at + p * 16, r.v[i]);
         } else if constexpr (kStore == SALI_STORE_INT8) {
@@ -211,6 +220,7 @@ __device__ __forceinline__ void tile_store(const TileRaw<kStore, kDim, kWaves>& 
             put(vd + 272, values4<kBf16>(r.v[i].z >> 4 & kLow, r.v[i].w >> 4 & kLow, r.vs[i], r.vz[i]));
         }
     }
+    return odd;
 }
 
 template <int kStore, int kDim, bool kBf16, int kWaves>
@@ -219,7 +229,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_pages_tile(PagesAttend a) {
     constexpr int kSteps = kDim / 16, kDt = kDim / 32, kPitch = kDim + 4;
     constexpr int kHalf = kTileKeys * kDim * 2;             // bytes of the tile's K or V
     __shared__ __align__(16) uint8_t s_k[2][kHalf], s_v[2][kHalf];
-    __shared__ int s_hidden[2][4];
+    __shared__ int s_live[2][4];            // of each block of 16 tokens: those that a row may see
+    __shared__ int s_odd[2][kWaves];        // V holds values that are not finite, and some row does not see some key
     const TileScratch t = tile_scratch(a.records, a.geom.n_kv);
     const int n_kv = a.geom.n_kv;
     const int nth = (int)(blockIdx.x / (uint32_t)n_kv), head = (int)blockIdx.x - nth * n_kv;
@@ -234,22 +245,35 @@ __global__ __launch_bounds__(64 * kWaves) void k_pages_tile(PagesAttend a) {
     const uint32_t block_bytes = a.geom.head_bytes >> a.geom.blocks_log2;
 
     // the wave's block of a tile
+    constexpr int kPer = kWaves / 4;                        // waves that share a block
     auto page_at = [&](int i) -> int {
-        const int block = 4 * tile_at(view, i) + wave / (kWaves / 4);
-        return block * kBlockTokens < seq.len ? table[block >> a.geom.blocks_log2] : -2;
+        const int block = 4 * tile_at(view, i) + wave / kPer;
+        return block * kBlockTokens < seq.len ? table[block >> a.geom.blocks_log2] : -1;
     };
-    auto block_at = [&](int i, int page, int buf) -> const char* {
-        const int block = 4 * tile_at(view, i) + wave / (kWaves / 4);
-        const bool hidden = (unsigned)page >= (unsigned)a.geom.n_pages;
-        if (hidden && page != -2 && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
-        if (lane == 0) s_hidden[buf][wave / (kWaves / 4)] = hidden ? 1 : 0;
-        return heads + (uint64_t)(hidden ? 0 : page) * a.geom.page_bytes + (uint32_t)(block & ((1 << a.geom.blocks_log2) - 1)) * block_bytes;
+    int live;
+    auto block_at = [&](int i, int page) -> const char* {
+        const int block = 4 * tile_at(view, i) + wave / kPer;
+        live = max(0, min(kBlockTokens, seq.len - block * kBlockTokens));
+        if ((unsigned)page >= (unsigned)a.geom.n_pages) {
+            if (live > 0 && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
+            live = page = 0;
+        }
+        return heads + (uint64_t)page * a.geom.page_bytes + (uint32_t)(block & ((1 << a.geom.blocks_log2) - 1)) * block_bytes;
+    };
+    auto put_tile = [&](auto& raw, int i, int buf) {
+        const bool look = kStore == SALI_STORE_16 && partly_hidden(view, a.window, a.sinks, tile_at(view, i) * kTileKeys, kTileKeys);
+        const bool odd = tile_store<kStore, kDim, kBf16, kWaves>(raw, live, wave, lane, look, s_k[buf], s_v[buf]);
+        if constexpr (kStore == SALI_STORE_16) {
+            const bool any = __builtin_amdgcn_ballot_w64(odd) != 0;
+            if (lane == 0) s_odd[buf][wave] = any ? 1 : 0;
+        }
+        if (lane == 0) s_live[buf][wave / kPer] = live;
     };
     typedef TileRaw<kStore, kDim, kWaves> Raw;
     Raw raw;
     int page = __builtin_amdgcn_readfirstlane(page_at(unit.lo));
-    tile_load<kStore, kDim, kWaves>(block_at(unit.lo, page, 0), wave, lane, raw);
-    int page_next = unit.lo + 1 < unit.hi ? page_at(unit.lo + 1) : -2;
+    tile_load<kStore, kDim, kWaves>(block_at(unit.lo, page), wave, lane, raw);
+    int page_next = unit.lo + 1 < unit.hi ? page_at(unit.lo + 1) : -1;
 
     const int64_t row0 = (int64_t)unit.row_tile * kTileRows + wave * 32 * kSets, rows = (int64_t)seq.n * group;
     const bool some = row0 < rows;                          // uniform over the wave
@@ -279,27 +303,71 @@ __global__ __launch_bounds__(64 * kWaves) void k_pages_tile(PagesAttend a) {
     }
     float m[kSets], l[kSets];
     f32x16 acc[kSets][kDt];
+    uint64_t up[kSets], down[kSets];                        // a bit for every value of acc: values that are not finite
 #pragma unroll
     for (int c = 0; c < kSets; ++c) {
         m[c] = -INFINITY;
         l[c] = 0.0f;
+        up[c] = down[c] = 0u;
 #pragma unroll
         for (int d = 0; d < kDt; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[c][d][r] = 0.0f;
     }
 
-    tile_store<kStore, kDim, kBf16, kWaves>(raw, wave, lane, s_k[0], s_v[0]);
+    put_tile(raw, unit.lo, 0);
     for (int i = unit.lo; i < unit.hi; ++i) {
         const int buf = (i - unit.lo) & 1;
         __syncthreads();                                    // this tile is there, and every wave is through with the other buffer
         const bool more = i + 1 < unit.hi;
         if (more) {
             page = __builtin_amdgcn_readfirstlane(page_next);
-            tile_load<kStore, kDim, kWaves>(block_at(i + 1, page, buf ^ 1), wave, lane, raw);
+            tile_load<kStore, kDim, kWaves>(block_at(i + 1, page), wave, lane, raw);
             if (i + 2 < unit.hi) page_next = page_at(i + 2);
         }
         const int tile0 = tile_at(view, i) * kTileKeys;
+        if constexpr (kStore == SALI_STORE_16) {
+            if (__builtin_amdgcn_ballot_w64(s_odd[buf][lane % kWaves] != 0) != 0) {          // the same for all waves
+                if (some) {
+#pragma unroll
+                    for (int c = 0; c < kSets; ++c)
+#pragma unroll 1
+                        for (int b = 0; b < 4; ++b) {
+                            u32x4 seen;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int j = tile0 + 16 * b + 8 * hh + 2 * e, there = s_live[buf][b] - 8 * hh;
+                                seen[e] = (2 * e < there && sees(pos[c], j, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne : 0u) |
+                                          (2 * e + 1 < there && sees(pos[c], j + 1, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
+                            }
+#pragma unroll 1                                            // not to cost registers
+                            for (int d = 0; d < kDt; ++d) {
+                                u32x4 finite, plus, minus;
+                                take_apart<kBf16>(load16(s_v[buf] + b * (32 * kDim) + (hh * kDim + col + 32 * d) * 16), finite, plus, minus);
+                                f32x16 zero;
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
+                                const f32x16 ups = Num<kBf16>::mma32(plus, seen, zero), downs = Num<kBf16>::mma32(minus, seen, zero);
+                                uint32_t u = 0, w = 0;
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) {
+                                    u |= ups[r] > 0.0f ? 1u << r : 0u;
+                                    w |= downs[r] > 0.0f ? 1u << r : 0u;
+                                }
+                                up[c] |= (uint64_t)u << (16 * d);
+                                down[c] |= (uint64_t)w << (16 * d);
+                            }
+                        }
+                }
+                __syncthreads();                            // every wave has looked
+                for (int p = (int)threadIdx.x; p < kHalf / 16; p += 64 * kWaves) {
+                    u32x4 finite, plus, minus;
+                    take_apart<kBf16>(load16(s_v[buf] + p * 16), finite, plus, minus);
+                    *reinterpret_cast<u32x4*>(s_v[buf] + p * 16) = finite;
+                }
+                __syncthreads();
+            }
+        }
 #pragma unroll 1
         for (int sub = 0; sub < 2; ++sub) {
             const int j0 = tile0 + 32 * sub;
@@ -317,14 +385,14 @@ __global__ __launch_bounds__(64 * kWaves) void k_pages_tile(PagesAttend a) {
                 for (int c = 0; c < kSets; ++c) s2[c] = Num<kBf16>::mma32(kf, q[c][s], s2[c]);
             }
             // lane (row col, hh): register r has token 8 hh + r % 8 of block r / 8
-            const int h0 = __builtin_amdgcn_readfirstlane(s_hidden[buf][2 * sub]), h1 = __builtin_amdgcn_readfirstlane(s_hidden[buf][2 * sub + 1]);
-            const bool masked = (h0 | h1) != 0 || partly_hidden(mine, a.window, a.sinks, j0, 32);
+            const int live0 = __builtin_amdgcn_readfirstlane(s_live[buf][2 * sub]), live1 = __builtin_amdgcn_readfirstlane(s_live[buf][2 * sub + 1]);
+            const bool masked = live0 < kBlockTokens || live1 < kBlockTokens || partly_hidden(mine, a.window, a.sinks, j0, 32);
             if (masked) {
 #pragma unroll
                 for (int c = 0; c < kSets; ++c)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if ((r < 8 ? h0 : h1) != 0 || !sees(pos[c], j0 + 16 * (r / 8) + 8 * hh + r % 8, a.window, a.sinks)) s2[c][r] = -INFINITY;
+                        if ((r < 8 ? live0 : live1) <= 0 || !sees(pos[c], j0 + 16 * (r / 8) + 8 * hh + r % 8, a.window, a.sinks)) s2[c][r] = -INFINITY;
             }
             u32x4 p[kSets][2];
 #pragma unroll
@@ -353,54 +421,17 @@ __global__ __launch_bounds__(64 * kWaves) void k_pages_tile(PagesAttend a) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r) p[c][r / 4][r % 4] = pack2<kBf16>(e[2 * r], e[2 * r + 1]);
             }
-            bool odd = false;
             const uint8_t* const vl = vb + (hh * kDim + col) * 16;
-            if (masked) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int d = 0; d < kDt; ++d) odd |= any_not_finite<kBf16>(load16(vl + b * (32 * kDim) + d * 512));
-                odd = __builtin_amdgcn_ballot_w64(odd) != 0;
-            }
-            if (!odd) {
+                for (int d = 0; d < kDt; ++d) {
+                    const u32x4 vf = load16(vl + b * (32 * kDim) + d * 512);
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int d = 0; d < kDt; ++d) {
-                        const u32x4 vf = load16(vl + b * (32 * kDim) + d * 512);
-#pragma unroll
-                        for (int c = 0; c < kSets; ++c) acc[c][d] = Num<kBf16>::mma32(vf, p[c][b], acc[c][d]);
-                    }
-            } else {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int c = 0; c < kSets; ++c) {
-                        u32x4 seen;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int j = j0 + 16 * b + 8 * hh + 2 * e;
-                            const bool there = (b == 0 ? h0 : h1) == 0;
-                            seen[e] = (there && sees(pos[c], j, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne : 0u) |
-                                      (there && sees(pos[c], j + 1, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
-                        }
-#pragma unroll
-                        for (int d = 0; d < kDt; ++d) {
-                            u32x4 finite, plus, minus;
-                            take_apart<kBf16>(load16(vl + b * (32 * kDim) + d * 512), finite, plus, minus);
-                            f32x16 zero, up, down;
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
-                            acc[c][d] = Num<kBf16>::mma32(finite, p[c][b], acc[c][d]);
-                            up = Num<kBf16>::mma32(plus, seen, zero);
-                            down = Num<kBf16>::mma32(minus, seen, zero);
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) acc[c][d][r] += (up[r] > 0.0f ? INFINITY : 0.0f) + (down[r] > 0.0f ? -INFINITY : 0.0f);
-                        }
-                    }
-            }
+                    for (int c = 0; c < kSets; ++c) acc[c][d] = Num<kBf16>::mma32(vf, p[c][b], acc[c][d]);
+                }
         }
-        if (more) tile_store<kStore, kDim, kBf16, kWaves>(raw, wave, lane, s_k[buf ^ 1], s_v[buf ^ 1]);
+        if (more) put_tile(raw, i + 1, buf ^ 1);
     }
 
     // ---- results: lane (row col, hh) has values 32 d + 8 k + 4 hh .. + 3
@@ -409,6 +440,12 @@ __global__ __launch_bounds__(64 * kWaves) void k_pages_tile(PagesAttend a) {
         const int64_t r = row0 + 32 * c + col;
         const float sum = sum_over_halves(l[c]);
         if (r >= rows) continue;
+        if constexpr (kStore == SALI_STORE_16)
+            if ((up[c] | down[c]) != 0)
+#pragma unroll
+                for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) acc[c][d][x] += found((up[c] >> (16 * d + x) & 1) != 0, (down[c] >> (16 * d + x) & 1) != 0);
         if (unit.part >= 0) {
             float* part = a.partial + (((size_t)unit.part * n_kv + head) * kTileRows + (size_t)(r - (int64_t)unit.row_tile * kTileRows)) * kPitch;
             if (hh == 0) {

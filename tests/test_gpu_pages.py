@@ -178,9 +178,17 @@ def test_tiny_and_infinite_groups(store):
     c.pages.read(0, c.batch([(4, 4)]), back[:, 0], back[:, 1])
     assert np.array_equal(bits_of(back[:, 0]) & 0x7FFF, op.read_back(bits_of(c.k[0]), c.spec) & 0x7FFF)
     assert c.pages.get_status() == 0
-    c.k[0][2, 0, 40] = math.inf
+    for value in (math.inf, -math.inf, math.nan):
+        c.k[0][2, 0, 40] = value
+        c.write([(4, 4)])
+        c.pages.read(0, c.batch([(4, 4)]), back[:, 0], back[:, 1])
+        assert c.pages.get_status() == binding.FAULT_NONFINITE
+        assert np.array_equal(bits_of(back[:, 0]) & 0x7FFF, op.read_back(bits_of(c.k[0]), c.spec) & 0x7FFF)
+        assert bool((back[2, 0, 0, 32:] == 0).all()) and bool((back[2, 0, 0, :32] != 0).any())
+    c.v[0][3, 0, :] = torch.linspace(-3e38, 3e38, 64)        # wider than fp32
     c.write([(4, 4)])
-    assert c.pages.get_status() == binding.FAULT_NONFINITE
+    c.pages.read(0, c.batch([(4, 4)]), back[:, 0], back[:, 1])
+    assert np.array_equal(bits_of(back[:, 1]) & 0x7FFF, op.read_back(bits_of(c.v[0]), c.spec) & 0x7FFF)
 
 
 # ---- attention -------------------------------------------------------------------------------------
@@ -281,7 +289,8 @@ def test_priors_without_weight(new):
 @pytest.mark.parametrize("many", [False, True], ids=["stream", "tile"])
 def test_keys_out_of_sight_do_not_reach_a_token(store, many):
     """Later tokens, and tokens behind the window, that hold infinities and NaN (and the NaN patterns past the end of a sequence, which every test
-    has): the rows that do not see them are those of finite keys, the rows that do are not finite where the values are not."""
+    has): the rows that do not see them are those of finite keys, the rows that do are not finite where the values are not (quantised groups with
+    such values are zeros)."""
     n, t = (100, 150) if many else (6, 150)
     spec = op.PagesSpec(1, 2, 64, 16, "bf16", store)
     c = Cache(spec, [t], 12, history=False)
@@ -294,12 +303,26 @@ def test_keys_out_of_sight_do_not_reach_a_token(store, many):
         c.v[0][p, 0, :] = math.inf
     c.write([(t, t)])
     for window, sinks in ((0, 0), (40, 3)) if store == "16" else ((0, 0),):
-        q, out, lse = c.attend([(n, t)], window=window, sinks=sinks, check=store == "16")
+        q, out, lse = c.attend([(n, t)], window=window, sinks=sinks)
         before = out[:p - (t - n)].float()
         if store == "16" and window == 0:
             before = torch.cat([before[..., :20], before[..., 21:]], -1)
         assert bool(torch.isfinite(before).all()), "a key out of sight reaches a row"
         assert bool(torch.isfinite(lse).all())
+
+
+@pytest.mark.parametrize("heads", [1, 2, 5, 9])
+def test_values_that_are_not_finite_in_view_of_some(heads):
+    """Random infinities and NaN among the last tokens' values, single heads to many rows, several sequences and windows."""
+    for dim, new in ((64, [(9, 60), (1, 33), (3, 130)]), (128, [(40, 90), (100, 100), (1, 70)])):
+        c = Cache(op.PagesSpec(1, heads, dim, 16, "fp16", "16"), [t for _, t in new], 19 + heads, history=False)
+        for s, (n, t) in enumerate(new):
+            for value in (math.inf, -math.inf, math.nan):
+                for _ in range(3):
+                    c.v[s][c.rng.integers(max(0, t - n - 5), t), 0, c.rng.integers(dim)] = value
+        c.write([(t, t) for _, t in new])
+        for window, sinks in ((0, 0), (20, 2)):
+            c.attend(new, window=window, sinks=sinks)
 
 
 @pytest.mark.parametrize("many", [False, True], ids=["stream", "tile"])
