@@ -70,9 +70,9 @@ SALI_BOTH bool sees(int p, int j, int window, int sinks) {
 SALI_BOTH int64_t stretch_start(int64_t b, int64_t total, int64_t blocks) { return b * total / blocks; }
 SALI_BOTH int64_t stretch_of(int64_t tile, int64_t total, int64_t blocks) { return ((tile + 1) * blocks + total - 1) / total - 1; }
 
-constexpr int kTileRows = 256;              // rows of a block of the tile kernel
-constexpr int kTileKeys = 64;               // keys of its steps
-constexpr int kTileShares = 256;            // fair shares that the whole work is cut into: one a compute unit
+constexpr int kTileRows = 128;              // rows of a block of the tile kernel
+constexpr int kTileKeys = 32;               // keys of its steps
+constexpr int kTileShares = 512;            // fair shares that the whole work is cut into
 
 // row tiles of a batch by slots, as those of blocks in append: sequence s owns the slots from first * group / kTileRows + s on
 SALI_BOTH int64_t tile_slots(int64_t n_tokens, int group, int64_t n_seqs) { return n_tokens * group / kTileRows + n_seqs; }

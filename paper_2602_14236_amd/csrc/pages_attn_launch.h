@@ -29,10 +29,9 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
         else go(std::integral_constant<int, 4>{}, stream_blocks(4));
     }
     if (most_rows > 64) {
-        constexpr int kWaves = 8;
         const int64_t units = tile_slots(a.seqs.n_tokens, group, a.seqs.n_seqs) + tile_parts(n_kv);
         hipLaunchKernelGGL(k_pages_plan, dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1);
-        hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16, kWaves>), dim3((unsigned)(units * n_kv)), dim3(64 * kWaves), 0, s, a);
+        hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16>), dim3((unsigned)(units * n_kv)), dim3(64 * kTileWaves), 0, s, a);
         hipLaunchKernelGGL((k_pages_tile_merge<kDim, kBf16>), dim3(tile_parts(n_kv) / 2 * n_kv, kTileRows / 8), dim3(256), 0, s, a);
     }
 }

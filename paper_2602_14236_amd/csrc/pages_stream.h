@@ -242,6 +242,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
                 if ((unsigned)(index - page0) >= 64u) {
                     page0 = index;
                     page_of_lane = index + lane < pages ? table[index + lane] : -1;
+                    asm volatile("" : "+v"(page_of_lane));      // waited for here: a wait behind the branch would be one for K and V too
                 }
                 int page = __builtin_amdgcn_readlane(page_of_lane, index - page0);
                 t.live[j] = min(kBlockTokens, seq.len - block * kBlockTokens);

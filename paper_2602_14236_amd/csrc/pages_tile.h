@@ -1,8 +1,8 @@
 // Attention of many new tokens a sequence (chunks of prompts, whole prompts): tiles of rows on the matrix cores.
 //
-// A block takes kWaves * kSets * 32 rows of one sequence and K/V head and walks the keys they see, 64 at a time.  The 64 keys are brought
-// into LDS once for all waves (dequantised on the way, in the order of the operands) while the 64 before are worked on; a wave
-// multiplies them with its kSets * 32 rows, whose queries stay in registers.
+// A block takes 128 rows of one sequence and K/V head, 32 a wave, and walks the keys they see, 32 at a time.  The keys are brought
+// into LDS once for all waves (dequantised on the way, in the order of the operands) while those before are worked on; a wave
+// multiplies them with its rows, whose queries stay in registers.
 //
 // The causal triangle, windows and ragged batches make blocks of very different length: a planning launch of one block writes the
 // units (rows and a range of key tiles), the longest first, and cuts the keys of those that are longer than a fair share of the whole; the
@@ -15,6 +15,7 @@ namespace sali {
 
 namespace {
 
+constexpr int kTileWaves = kTileRows / 32;
 constexpr int kPlanThreads = 1024;
 constexpr int kUnitBuckets = 64;
 
@@ -140,103 +141,125 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan(PagesAttend a, int 
     if (threadIdx.x == 0) t.plan->n_merges = s_merges;
 }
 
-// ---- bringing 64 keys into LDS: four blocks of 16 tokens, each in the layout of 16-bit blocks (K [D / 8][place][8], V [2][D][8])
-template <int kStore, int kDim, int kWaves>
+// ---- bringing 32 keys into LDS: two blocks of 16 tokens, each in the layout of 16-bit blocks (K [D / 8][place][8], V [2][D][8])
+// Wave w has half w % 2 of block w / 2: half of K's pieces, and of V's those of tokens 8 (w % 2) .. + 7.
+template <int kStore, int kDim>
 struct TileRaw {
-    static constexpr int kPieces = kStore == SALI_STORE_16 ? 2 * kDim : (kStore == SALI_STORE_INT8 ? kDim : kDim / 2);   // of 16 bytes, K or V of a block
-    static constexpr int kShare = kPieces * 4 / kWaves;                 // a wave's: a block, or half of one
+    static constexpr int kShare = (kStore == SALI_STORE_16 ? 2 * kDim : (kStore == SALI_STORE_INT8 ? kDim : kDim / 2)) / 2;   // pieces of 16 bytes, of K or V
     static constexpr int kLoads = (kShare + 63) / 64;
     u32x4 k[kLoads], v[kLoads];
     float ks[kStore == SALI_STORE_16 ? 1 : kLoads];
     Scales8 vs[kStore == SALI_STORE_16 ? 1 : kLoads];
     uint16_t kz[kStore == SALI_STORE_INT4 ? kLoads : 1];
     u32x4 vz[kStore == SALI_STORE_INT4 ? kLoads : 1];
+    static __device__ __forceinline__ bool none(int i, int lane) { return kShare % 64 != 0 && lane + 64 * i >= kShare; }
 };
-template <int kStore, int kDim, int kWaves>
-__device__ __forceinline__ void tile_load(const char* block, int wave, int lane, TileRaw<kStore, kDim, kWaves>& r) {
-    typedef TileRaw<kStore, kDim, kWaves> R;
+template <int kStore, int kDim>
+__device__ __forceinline__ void tile_load_k(const char* block, int half, int lane, TileRaw<kStore, kDim>& r) {
+    typedef TileRaw<kStore, kDim> R;
     constexpr BlockLayout kAt = block_layout(kStore, kDim);
-    const int p0 = wave % (kWaves / 4) * R::kShare;
 #pragma unroll
     for (int i = 0; i < R::kLoads; ++i) {
-        if (R::kShare % 64 != 0 && lane + 64 * i >= R::kShare) continue;
-        const uint32_t p = (uint32_t)(p0 + 64 * i + lane);
+        if (R::none(i, lane)) continue;
+        const uint32_t p = (uint32_t)(half * R::kShare + 64 * i + lane);
         r.k[i] = load16(block + p * 16);
-        r.v[i] = load16(block + kAt.v + p * 16);
-        if constexpr (kStore != SALI_STORE_16) {
-            // K piece: [D / 16 or D / 32][place]; V piece: [2][group][8 pieces of two values or of two bytes], 16 pieces where codes are bytes
-            const uint32_t kg = kStore == SALI_STORE_INT8 ? p >> 5 : p >> 4, place = p & 15;
-            const uint32_t per = kStore == SALI_STORE_INT8 ? 16 : 8, a = p / (kDim / 32 * per), vg = p / per % (kDim / 32);
-            r.ks[i] = *reinterpret_cast<const float*>(block + kAt.ks + (kg * 16 + place) * 4);
-            const f32x4* s = reinterpret_cast<const f32x4*>(block + kAt.vs + (vg * 16 + a * 8) * 4);
-            r.vs[i] = {s[0], s[1]};
-            if constexpr (kStore == SALI_STORE_INT4) {
-                r.kz[i] = *reinterpret_cast<const uint16_t*>(block + kAt.kz + (kg * 16 + place) * 2);
-                r.vz[i] = load16(block + kAt.vz + (vg * 16 + a * 8) * 2);
-            }
+        if constexpr (kStore != SALI_STORE_16) {            // pieces [D / 16 or D / 32][place]
+            const uint32_t at = (kStore == SALI_STORE_INT8 ? p >> 5 : p >> 4) * 16 + (p & 15);
+            r.ks[i] = *reinterpret_cast<const float*>(block + kAt.ks + at * 4);
+            if constexpr (kStore == SALI_STORE_INT4) r.kz[i] = *reinterpret_cast<const uint16_t*>(block + kAt.kz + at * 2);
         }
     }
 }
-// ... with those of its tokens that are alive (the first `live`); V's others become zeros.  Are some of V's 16-bit values not finite?
-template <int kStore, int kDim, bool kBf16, int kWaves>
-__device__ __forceinline__ bool tile_store(TileRaw<kStore, kDim, kWaves>& r, int live, int wave, int lane, bool look, uint8_t* k, uint8_t* v) {
-    typedef TileRaw<kStore, kDim, kWaves> R;
-    const int p0 = wave % (kWaves / 4) * R::kShare, at = wave / (kWaves / 4) * (32 * kDim);
-    bool odd = false;
-    auto put = [](uint8_t* to, const u32x4& x) { *reinterpret_cast<u32x4*>(to) = x; };
+template <int kStore, int kDim>
+__device__ __forceinline__ void tile_load_v(const char* block, int half, int lane, TileRaw<kStore, kDim>& r) {
+    typedef TileRaw<kStore, kDim> R;
+    constexpr BlockLayout kAt = block_layout(kStore, kDim);
 #pragma unroll
     for (int i = 0; i < R::kLoads; ++i) {
-        if (R::kShare % 64 != 0 && lane + 64 * i >= R::kShare) continue;
-        const int p = p0 + 64 * i + lane;
-        if (live < kBlockTokens) {
-            const int mine = live - 8 * (p / (R::kPieces / 2));
-            if constexpr (kStore == SALI_STORE_16) r.v[i] = live_tokens(r.v[i], mine);
-            else r.vs[i] = live_tokens(r.vs[i], mine);
-            if constexpr (kStore == SALI_STORE_INT4) r.vz[i] = live_tokens(r.vz[i], mine);
+        if (R::none(i, lane)) continue;
+        const uint32_t p = (uint32_t)(64 * i + lane);
+        r.v[i] = load16(block + kAt.v + (half * R::kShare + p) * 16);
+        if constexpr (kStore != SALI_STORE_16) {            // pieces of two values (8 bits) or two bytes (4 bits) of a group
+            const uint32_t at = (kStore == SALI_STORE_INT8 ? p >> 4 : p >> 3) * 16 + (uint32_t)half * 8;
+            const f32x4* s = reinterpret_cast<const f32x4*>(block + kAt.vs + at * 4);
+            r.vs[i] = {s[0], s[1]};
+            if constexpr (kStore == SALI_STORE_INT4) r.vz[i] = load16(block + kAt.vz + at * 2);
         }
+    }
+}
+__device__ __forceinline__ void put16(uint8_t* to, const u32x4& x) { *reinterpret_cast<u32x4*>(to) = x; }
+constexpr uint32_t kLowHalves = 0x0F0F0F0Fu;
+// `k`, `v`: where the block lies in LDS
+template <int kStore, int kDim, bool kBf16>
+__device__ __forceinline__ void tile_store_k(const TileRaw<kStore, kDim>& r, int half, int lane, uint8_t* k) {
+    typedef TileRaw<kStore, kDim> R;
+#pragma unroll
+    for (int i = 0; i < R::kLoads; ++i) {
+        if (R::none(i, lane)) continue;
+        const int p = half * R::kShare + 64 * i + lane;
         if constexpr (kStore == SALI_STORE_16) {
-            if (look) odd |= any_not_finite<kBf16>(r.v[i]);
-            put(k + at + p * 16, r.k[i]);
-            put(v + at + p * 16, r.v[i]);
+            put16(k + p * 16, r.k[i]);
         } else if constexpr (kStore == SALI_STORE_INT8) {
-            uint8_t* const kd = k + at + ((p >> 4) * 32 + (p & 15)) * 16;
-            put(kd, values8<kBf16>(r.k[i].x, r.k[i].y, r.ks[i]));
-            put(kd + 256, values8<kBf16>(r.k[i].z, r.k[i].w, r.ks[i]));
-            uint8_t* const vd = v + at + p * 32;
-            put(vd, values8<kBf16>(r.v[i].x, r.v[i].y, r.vs[i]));
-            put(vd + 16, values8<kBf16>(r.v[i].z, r.v[i].w, r.vs[i]));
+            uint8_t* const to = k + ((p >> 4) * 32 + (p & 15)) * 16;
+            put16(to, values8<kBf16>(r.k[i].x, r.k[i].y, r.ks[i]));
+            put16(to + 256, values8<kBf16>(r.k[i].z, r.k[i].w, r.ks[i]));
         } else {
             const float low = low_half<kBf16>(r.kz[i]);
-            constexpr uint32_t kLow = 0x0F0F0F0Fu;
-            uint8_t* const kd = k + at + ((p >> 4) * 64 + (p & 15)) * 16;
-            put(kd, values4<kBf16>(r.k[i].x & kLow, r.k[i].y & kLow, r.ks[i], low));
-            put(kd + 256, values4<kBf16>(r.k[i].z & kLow, r.k[i].w & kLow, r.ks[i], low));
-            put(kd + 512, values4<kBf16>(r.k[i].x >> 4 & kLow, r.k[i].y >> 4 & kLow, r.ks[i], low));
-            put(kd + 768, values4<kBf16>(r.k[i].z >> 4 & kLow, r.k[i].w >> 4 & kLow, r.ks[i], low));
-            uint8_t* const vd = v + at + ((p >> 3) * 32 + (p & 7) * 2) * 16;
-            put(vd, values4<kBf16>(r.v[i].x & kLow, r.v[i].y & kLow, r.vs[i], r.vz[i]));
-            put(vd + 16, values4<kBf16>(r.v[i].z & kLow, r.v[i].w & kLow, r.vs[i], r.vz[i]));
-            put(vd + 256, values4<kBf16>(r.v[i].x >> 4 & kLow, r.v[i].y >> 4 & kLow, r.vs[i], r.vz[i]));
-            put(vd + 272, values4<kBf16>(r.v[i].z >> 4 & kLow, r.v[i].w >> 4 & kLow, r.vs[i], r.vz[i]));
+            uint8_t* const to = k + ((p >> 4) * 64 + (p & 15)) * 16;
+            put16(to, values4<kBf16>(r.k[i].x & kLowHalves, r.k[i].y & kLowHalves, r.ks[i], low));
+            put16(to + 256, values4<kBf16>(r.k[i].z & kLowHalves, r.k[i].w & kLowHalves, r.ks[i], low));
+            put16(to + 512, values4<kBf16>(r.k[i].x >> 4 & kLowHalves, r.k[i].y >> 4 & kLowHalves, r.ks[i], low));
+            put16(to + 768, values4<kBf16>(r.k[i].z >> 4 & kLowHalves, r.k[i].w >> 4 & kLowHalves, r.ks[i], low));
         }
     }
-    return odd;
+}
+template <int kStore, int kDim, bool kBf16>
+__device__ __forceinline__ void tile_store_v(const TileRaw<kStore, kDim>& r, int half, int lane, uint8_t* v) {
+    typedef TileRaw<kStore, kDim> R;
+#pragma unroll
+    for (int i = 0; i < R::kLoads; ++i) {
+        if (R::none(i, lane)) continue;
+        const int p = half * R::kShare + 64 * i + lane;
+        if constexpr (kStore == SALI_STORE_16) {
+            put16(v + p * 16, r.v[i]);
+        } else if constexpr (kStore == SALI_STORE_INT8) {
+            uint8_t* const to = v + p * 32;
+            put16(to, values8<kBf16>(r.v[i].x, r.v[i].y, r.vs[i]));
+            put16(to + 16, values8<kBf16>(r.v[i].z, r.v[i].w, r.vs[i]));
+        } else {
+            uint8_t* const to = v + ((p >> 3) * 32 + (p & 7) * 2) * 16;
+            put16(to, values4<kBf16>(r.v[i].x & kLowHalves, r.v[i].y & kLowHalves, r.vs[i], r.vz[i]));
+            put16(to + 16, values4<kBf16>(r.v[i].z & kLowHalves, r.v[i].w & kLowHalves, r.vs[i], r.vz[i]));
+            put16(to + 256, values4<kBf16>(r.v[i].x >> 4 & kLowHalves, r.v[i].y >> 4 & kLowHalves, r.vs[i], r.vz[i]));
+            put16(to + 272, values4<kBf16>(r.v[i].z >> 4 & kLowHalves, r.v[i].w >> 4 & kLowHalves, r.vs[i], r.vz[i]));
+        }
+    }
 }
 
-template <int kStore, int kDim, bool kBf16, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void k_pages_tile(PagesAttend a) {
-    constexpr int kSets = kTileRows / 32 / kWaves;          // of 32 rows, a wave
+// All waves of the block, LDS accesses before it done by then (global ones may be under way)
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int kStore, int kDim, bool kBf16>
+__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(3, 3))) void k_pages_tile(PagesAttend a) {
     constexpr int kSteps = kDim / 16, kDt = kDim / 32, kPitch = kDim + 4;
-    constexpr int kHalf = kTileKeys * kDim * 2;             // bytes of the tile's K or V
-    __shared__ __align__(16) uint8_t s_k[2][kHalf], s_v[2][kHalf];
-    __shared__ int s_live[2][4];            // of each block of 16 tokens: those that a row may see
-    __shared__ int s_odd[2][kWaves];        // V holds values that are not finite, and some row does not see some key
+    constexpr int kBlock = 32 * kDim;                       // bytes of a block's K or V in LDS
+    __shared__ __align__(16) uint8_t s_k[2][2 * kBlock], s_v[2][2 * kBlock];
+    __shared__ int s_live[2][2];                            // of each block of 16 tokens: those that a row may see
+    // 16-bit tiles that not all rows see whole: V's values that are not finite, +inf or NaN and -inf or NaN, a bit a token; of each wave's
+    // share whether there are any
+    __shared__ uint8_t s_up[2][kStore == SALI_STORE_16 ? kTileWaves : 1][kDim], s_down[2][kStore == SALI_STORE_16 ? kTileWaves : 1][kDim];
+    __shared__ int s_odd[2][kTileWaves];
     const TileScratch t = tile_scratch(a.records, a.geom.n_kv);
     const int n_kv = a.geom.n_kv;
     const int nth = (int)(blockIdx.x / (uint32_t)n_kv), head = (int)blockIdx.x - nth * n_kv;
     if (nth >= t.plan->n_units) return;
     const TileUnit unit = t.units[nth];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 31, hh = lane >> 5;
+    const int half = wave & 1;
     const int group = a.group;
     const PageSeq seq = load_seq(a.seqs, a.geom, unit.seq, false);
     const View view = view_of_rows(seq, unit.row_tile, group, a.window, a.sinks);
@@ -244,240 +267,241 @@ __global__ __launch_bounds__(64 * kWaves) void k_pages_tile(PagesAttend a) {
     const char* const heads = a.geom.pool + (uint64_t)head * a.geom.head_bytes;
     const uint32_t block_bytes = a.geom.head_bytes >> a.geom.blocks_log2;
 
-    // the wave's block of a tile
-    constexpr int kPer = kWaves / 4;                        // waves that share a block
-    auto page_at = [&](int i) -> int {
-        const int block = 4 * tile_at(view, i) + wave / kPer;
-        return block * kBlockTokens < seq.len ? table[block >> a.geom.blocks_log2] : -1;
+    // ---- the wave's share of the tiles: where tile i's block lies, and its tokens
+    typedef TileRaw<kStore, kDim> Raw;
+    Raw raw;
+    auto block_of = [&](int i) { return 2 * tile_at(view, i) + (wave >> 1); };
+    // the pages from `page0` on, one a lane: where this head's part of them lies, and which are none
+    const int pages = (seq.len + (kBlockTokens << a.geom.blocks_log2) - 1) / (kBlockTokens << a.geom.blocks_log2);
+    int page0 = -64;
+    uint64_t at_page = 0, no_page = 0;
+    struct Source {
+        const char* block;
+        int live;
     };
-    int live;
-    auto block_at = [&](int i, int page) -> const char* {
-        const int block = 4 * tile_at(view, i) + wave / kPer;
-        live = max(0, min(kBlockTokens, seq.len - block * kBlockTokens));
-        if ((unsigned)page >= (unsigned)a.geom.n_pages) {
-            if (live > 0 && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
-            live = page = 0;
+    auto source = [&](int i) -> Source {
+        const int block = block_of(i), index = block >> a.geom.blocks_log2;
+        if ((unsigned)(index - page0) >= 64u) {
+            page0 = index;
+            int page = index + lane < pages ? table[index + lane] : -1;
+            const bool none = (unsigned)page >= (unsigned)a.geom.n_pages;
+            no_page = __builtin_amdgcn_ballot_w64(none);
+            at_page = (uint64_t)(none ? 0 : page) * a.geom.page_bytes;
+            asm volatile("" : "+v"(at_page));               // waited for here: a wait behind the branch would be one for K and V too
         }
-        return heads + (uint64_t)page * a.geom.page_bytes + (uint32_t)(block & ((1 << a.geom.blocks_log2) - 1)) * block_bytes;
+        const int nth_page = index - page0;
+        const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at_page, nth_page) |
+                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(at_page >> 32), nth_page) << 32;
+        Source s;
+        s.live = max(0, min(kBlockTokens, seq.len - block * kBlockTokens));
+        if ((no_page >> nth_page & 1) != 0) {
+            if (i < unit.hi && s.live > 0 && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
+            s.live = 0;
+        }
+        s.block = heads + at + (uint32_t)(block & ((1 << a.geom.blocks_log2) - 1)) * block_bytes;
+        return s;
     };
-    auto put_tile = [&](auto& raw, int i, int buf) {
-        const bool look = kStore == SALI_STORE_16 && partly_hidden(view, a.window, a.sinks, tile_at(view, i) * kTileKeys, kTileKeys);
-        const bool odd = tile_store<kStore, kDim, kBf16, kWaves>(raw, live, wave, lane, look, s_k[buf], s_v[buf]);
+    auto put_k = [&](int live, int buf) {
+        tile_store_k<kStore, kDim, kBf16>(raw, half, lane, s_k[buf] + (wave >> 1) * kBlock);
+        if (lane == 0 && half == 0) s_live[buf][wave >> 1] = live;
+    };
+    // V of tile i before it goes to LDS: zeros for the tokens that are nobody's, and what is not finite
+    auto clean_v = [&](int i, int live, int buf) {
+        const int mine = live - 8 * half;
+        if (mine < 8)
+#pragma unroll
+            for (int x = 0; x < Raw::kLoads; ++x) {
+                if constexpr (kStore == SALI_STORE_16) raw.v[x] = live_tokens(raw.v[x], mine);
+                else raw.vs[x] = live_tokens(raw.vs[x], mine);
+                if constexpr (kStore == SALI_STORE_INT4) raw.vz[x] = live_tokens(raw.vz[x], mine);
+            }
         if constexpr (kStore == SALI_STORE_16) {
-            const bool any = __builtin_amdgcn_ballot_w64(odd) != 0;
+            bool any = false;
+            if (partly_hidden(view, a.window, a.sinks, tile_at(view, i) * kTileKeys, kTileKeys)) {
+                bool odd = false;
+#pragma unroll
+                for (int x = 0; x < Raw::kLoads; ++x) odd |= !Raw::none(x, lane) && any_not_finite<kBf16>(raw.v[x]);
+                any = __builtin_amdgcn_ballot_w64(odd) != 0;
+                if (any)
+#pragma unroll
+                    for (int x = 0; x < Raw::kLoads; ++x) {
+                        if (Raw::none(x, lane)) continue;
+                        u32x4 plus, minus;
+                        take_apart<kBf16>(raw.v[x], raw.v[x], plus, minus);
+                        uint32_t up = 0, down = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t p = plus[e], m = minus[e];
+                            up |= ((p & 0xFFFFu) != 0 ? 1u : 0u) << (2 * e) | (p >> 16 != 0 ? 2u : 0u) << (2 * e);
+                            down |= ((m & 0xFFFFu) != 0 ? 1u : 0u) << (2 * e) | (m >> 16 != 0 ? 2u : 0u) << (2 * e);
+                        }
+                        s_up[buf][wave][64 * x + lane] = (uint8_t)up;
+                        s_down[buf][wave][64 * x + lane] = (uint8_t)down;
+                    }
+            }
             if (lane == 0) s_odd[buf][wave] = any ? 1 : 0;
         }
-        if (lane == 0) s_live[buf][wave / kPer] = live;
     };
-    typedef TileRaw<kStore, kDim, kWaves> Raw;
-    Raw raw;
-    int page = __builtin_amdgcn_readfirstlane(page_at(unit.lo));
-    tile_load<kStore, kDim, kWaves>(block_at(unit.lo, page), wave, lane, raw);
-    int page_next = unit.lo + 1 < unit.hi ? page_at(unit.lo + 1) : -1;
+    auto put_v = [&](int buf) { tile_store_v<kStore, kDim, kBf16>(raw, half, lane, s_v[buf] + (wave >> 1) * kBlock); };
 
-    const int64_t row0 = (int64_t)unit.row_tile * kTileRows + wave * 32 * kSets, rows = (int64_t)seq.n * group;
+    Source next = source(unit.lo);
+    tile_load_k<kStore, kDim>(next.block, half, lane, raw);
+    tile_load_v<kStore, kDim>(next.block, half, lane, raw);
+
+    // ---- the wave's rows
+    const int64_t row0 = (int64_t)unit.row_tile * kTileRows + wave * 32, rows = (int64_t)seq.n * group, r = row0 + col;
+    const int token = (int)(r / group), of_group = (int)(r - (int64_t)token * group);
+    const int pos = r < rows ? seq.len - seq.n + token : -1;
     const bool some = row0 < rows;                          // uniform over the wave
     View mine = view;
-    {
-        const int64_t last = min(rows, row0 + 32 * kSets) - 1;
-        mine.first = seq.len - seq.n + (int)(row0 / group);
-        mine.last = seq.len - seq.n + (int)(last / group);
-    }
-    u32x4 q[kSets][kSteps];
-    int pos[kSets];
+    mine.first = seq.len - seq.n + (int)(row0 / group);
+    mine.last = seq.len - seq.n + (int)((least(rows, row0 + 32) - 1) / group);
+    u32x4 q[kSteps];
 #pragma unroll
-    for (int c = 0; c < kSets; ++c) {
-        const int64_t r = row0 + 32 * c + col;
-        const int token = (int)(r / group), g = (int)(r - (int64_t)token * group);
-        pos[c] = r < rows ? seq.len - seq.n + token : -1;
+    for (int s = 0; s < kSteps; ++s) {
+        q[s] = (u32x4){0u, 0u, 0u, 0u};
+        if (r < rows) {
+            const u32x4 v = load16(a.q.d + (int64_t)(seq.first + token) * a.q.token_bytes + (int64_t)(head * group + of_group) * a.q.head_bytes +
+                                   2 * (16 * s + 8 * hh));
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            q[c][s] = (u32x4){0u, 0u, 0u, 0u};
-            if (r < rows) {
-                const u32x4 v = load16(a.q.d + (int64_t)(seq.first + token) * a.q.token_bytes + (int64_t)(head * group + g) * a.q.head_bytes +
-                                       2 * (16 * s + 8 * hh));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) q[c][s][e] = (v[e] & a.q_keep) ^ a.q_flip;
-            }
+            for (int e = 0; e < 4; ++e) q[s][e] = (v[e] & a.q_keep) ^ a.q_flip;
         }
     }
-    float m[kSets], l[kSets];
-    f32x16 acc[kSets][kDt];
-    uint64_t up[kSets], down[kSets];                        // a bit for every value of acc: values that are not finite
+    // keys that all of the wave's rows see: j0 .. j0 + 31 with j0 up to seen_to, and from seen_from on or all of them sinks
+    const int seen_to = mine.first - 31, seen_from = a.window > 0 ? mine.last - a.window + 1 : 0, sunk_to = a.sinks - 32;
+    float m = -INFINITY, l = 0.0f;
+    f32x16 acc[kDt];
 #pragma unroll
-    for (int c = 0; c < kSets; ++c) {
-        m[c] = -INFINITY;
-        l[c] = 0.0f;
-        up[c] = down[c] = 0u;
+    for (int d = 0; d < kDt; ++d)
 #pragma unroll
-        for (int d = 0; d < kDt; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[c][d][r] = 0.0f;
-    }
+        for (int x = 0; x < 16; ++x) acc[d][x] = 0.0f;
+    uint64_t up = 0, down = 0;                              // a bit for every value of acc: values that are not finite
 
-    put_tile(raw, unit.lo, 0);
-    for (int i = unit.lo; i < unit.hi; ++i) {
-        const int buf = (i - unit.lo) & 1;
-        __syncthreads();                                    // this tile is there, and every wave is through with the other buffer
-        const bool more = i + 1 < unit.hi;
-        if (more) {
-            page = __builtin_amdgcn_readfirstlane(page_next);
-            tile_load<kStore, kDim, kWaves>(block_at(i + 1, page), wave, lane, raw);
-            if (i + 2 < unit.hi) page_next = page_at(i + 2);
+    auto step = [&](int tile0, int buf) {
+        const uint8_t* const k = s_k[buf] + (col >> 4) * kBlock + (hh * 16 + (col & 15)) * 16;
+        const uint8_t* const v = s_v[buf] + (hh * kDim + col) * 16;
+        const int live_of_block = s_live[buf][lane & 1];
+        f32x16 st;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) st[x] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) st = Num<kBf16>::mma32(load16(k + s * 512), q[s], st);
+        // lane (row col, hh): register x has token 8 hh + x % 8 of block x / 8
+        if (tile0 > seen_to || (tile0 < seen_from && tile0 > sunk_to) || __builtin_amdgcn_ballot_w64(live_of_block < kBlockTokens) != 0) {
+            const int live0 = __builtin_amdgcn_readlane(live_of_block, 0), live1 = __builtin_amdgcn_readlane(live_of_block, 1);
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+                if ((x < 8 ? live0 : live1) <= 0 || !sees(pos, tile0 + 16 * (x / 8) + 8 * hh + x % 8, a.window, a.sinks)) st[x] = -INFINITY;
         }
-        const int tile0 = tile_at(view, i) * kTileKeys;
-        if constexpr (kStore == SALI_STORE_16) {
-            if (__builtin_amdgcn_ballot_w64(s_odd[buf][lane % kWaves] != 0) != 0) {          // the same for all waves
-                if (some) {
+        float tops[4];
 #pragma unroll
-                    for (int c = 0; c < kSets; ++c)
-#pragma unroll 1
-                        for (int b = 0; b < 4; ++b) {
-                            u32x4 seen;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int j = tile0 + 16 * b + 8 * hh + 2 * e, there = s_live[buf][b] - 8 * hh;
-                                seen[e] = (2 * e < there && sees(pos[c], j, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne : 0u) |
-                                          (2 * e + 1 < there && sees(pos[c], j + 1, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
-                            }
-#pragma unroll 1                                            // not to cost registers
-                            for (int d = 0; d < kDt; ++d) {
-                                u32x4 finite, plus, minus;
-                                take_apart<kBf16>(load16(s_v[buf] + b * (32 * kDim) + (hh * kDim + col + 32 * d) * 16), finite, plus, minus);
-                                f32x16 zero;
-#pragma unroll
-                                for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
-                                const f32x16 ups = Num<kBf16>::mma32(plus, seen, zero), downs = Num<kBf16>::mma32(minus, seen, zero);
-                                uint32_t u = 0, w = 0;
-#pragma unroll
-                                for (int r = 0; r < 16; ++r) {
-                                    u |= ups[r] > 0.0f ? 1u << r : 0u;
-                                    w |= downs[r] > 0.0f ? 1u << r : 0u;
-                                }
-                                up[c] |= (uint64_t)u << (16 * d);
-                                down[c] |= (uint64_t)w << (16 * d);
-                            }
-                        }
-                }
-                __syncthreads();                            // every wave has looked
-                for (int p = (int)threadIdx.x; p < kHalf / 16; p += 64 * kWaves) {
-                    u32x4 finite, plus, minus;
-                    take_apart<kBf16>(load16(s_v[buf] + p * 16), finite, plus, minus);
-                    *reinterpret_cast<u32x4*>(s_v[buf] + p * 16) = finite;
-                }
-                __syncthreads();
-            }
-        }
-#pragma unroll 1
-        for (int sub = 0; sub < 2; ++sub) {
-            const int j0 = tile0 + 32 * sub;
-            if (!some || j0 > mine.last) break;
-            const uint8_t* const kb = s_k[buf] + sub * (64 * kDim), * const vb = s_v[buf] + sub * (64 * kDim);
-            f32x16 s2[kSets];
-#pragma unroll
-            for (int c = 0; c < kSets; ++c)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s2[c][r] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const u32x4 kf = load16(kb + (col >> 4) * (32 * kDim) + ((2 * s + hh) * 16 + (col & 15)) * 16);
-#pragma unroll
-                for (int c = 0; c < kSets; ++c) s2[c] = Num<kBf16>::mma32(kf, q[c][s], s2[c]);
-            }
-            // lane (row col, hh): register r has token 8 hh + r % 8 of block r / 8
-            const int live0 = __builtin_amdgcn_readfirstlane(s_live[buf][2 * sub]), live1 = __builtin_amdgcn_readfirstlane(s_live[buf][2 * sub + 1]);
-            const bool masked = live0 < kBlockTokens || live1 < kBlockTokens || partly_hidden(mine, a.window, a.sinks, j0, 32);
-            if (masked) {
-#pragma unroll
-                for (int c = 0; c < kSets; ++c)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if ((r < 8 ? live0 : live1) <= 0 || !sees(pos[c], j0 + 16 * (r / 8) + 8 * hh + r % 8, a.window, a.sinks)) s2[c][r] = -INFINITY;
-            }
-            u32x4 p[kSets][2];
-#pragma unroll
-            for (int c = 0; c < kSets; ++c) {
-                float top = s2[c][0];
-#pragma unroll
-                for (int r = 1; r < 16; ++r) top = fmaxf(top, s2[c][r]);
-                top = max_over_halves(top) * a.scale2;
-                const float to = top > m[c] + kLag ? top : m[c];
-                if (__builtin_amdgcn_ballot_w64(to != m[c]) != 0) {
-                    const float by = to != m[c] ? __builtin_amdgcn_exp2f(m[c] - to) : 1.0f;
-                    l[c] *= by;
-#pragma unroll
-                    for (int d = 0; d < kDt; ++d)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[c][d][r] *= by;
-                    m[c] = to;
-                }
-                const float ref = m[c] == -INFINITY ? 0.0f : m[c];
-                float e[16];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s2[c][r], a.scale2, -ref));
-                    l[c] += e[r];
-                }
-#pragma unroll
-                for (int r = 0; r < 8; ++r) p[c][r / 4][r % 4] = pack2<kBf16>(e[2 * r], e[2 * r + 1]);
-            }
-            const uint8_t* const vl = vb + (hh * kDim + col) * 16;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int d = 0; d < kDt; ++d) {
-                    const u32x4 vf = load16(vl + b * (32 * kDim) + d * 512);
-#pragma unroll
-                    for (int c = 0; c < kSets; ++c) acc[c][d] = Num<kBf16>::mma32(vf, p[c][b], acc[c][d]);
-                }
-        }
-        if (more) put_tile(raw, i + 1, buf ^ 1);
-    }
-
-    // ---- results: lane (row col, hh) has values 32 d + 8 k + 4 hh .. + 3
-#pragma unroll
-    for (int c = 0; c < kSets; ++c) {
-        const int64_t r = row0 + 32 * c + col;
-        const float sum = sum_over_halves(l[c]);
-        if (r >= rows) continue;
-        if constexpr (kStore == SALI_STORE_16)
-            if ((up[c] | down[c]) != 0)
-#pragma unroll
-                for (int d = 0; d < kDt; ++d)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) acc[c][d][x] += found((up[c] >> (16 * d + x) & 1) != 0, (down[c] >> (16 * d + x) & 1) != 0);
-        if (unit.part >= 0) {
-            float* part = a.partial + (((size_t)unit.part * n_kv + head) * kTileRows + (size_t)(r - (int64_t)unit.row_tile * kTileRows)) * kPitch;
-            if (hh == 0) {
-                part[0] = m[c];
-                part[1] = sum;
-            }
+        for (int x = 0; x < 4; ++x) tops[x] = fmaxf(fmaxf(st[4 * x], st[4 * x + 1]), fmaxf(st[4 * x + 2], st[4 * x + 3]));
+        const float top = max_over_halves(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * a.scale2;
+        const float to = top > m + kLag ? top : m;
+        if (__builtin_amdgcn_ballot_w64(to != m) != 0) {
+            const float by = to != m ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+            l *= by;
 #pragma unroll
             for (int d = 0; d < kDt; ++d)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    *reinterpret_cast<f32x4*>(part + 4 + 32 * d + 8 * k + 4 * hh) =
-                        (f32x4){acc[c][d][4 * k], acc[c][d][4 * k + 1], acc[c][d][4 * k + 2], acc[c][d][4 * k + 3]};
-            continue;
+                for (int x = 0; x < 16; ++x) acc[d][x] *= by;
+            m = to;
         }
-        const int token = (int)(r / group), h = head * group + (int)(r - (int64_t)token * group);
-        const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
-        const RowEnd e = row_end(m[c], sum, a, row);
-        char* const out = a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes;
+        const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) st[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[x], a.scale2, -ref));
+#pragma unroll
+        for (int x = 0; x < 4; ++x) tops[x] = (st[4 * x] + st[4 * x + 1]) + (st[4 * x + 2] + st[4 * x + 3]);
+        l += (tops[0] + tops[1]) + (tops[2] + tops[3]);
+        u32x4 p[2];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) p[x / 4][x % 4] = pack2<kBf16>(st[2 * x], st[2 * x + 1]);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int d = 0; d < kDt; ++d) acc[d] = Num<kBf16>::mma32(load16(v + b * kBlock + d * 512), p[b], acc[d]);
+    };
+    auto look_for_odd = [&](int tile0, int buf) {
+        if constexpr (kStore == SALI_STORE_16) {
+            const int there = s_odd[buf][lane % kTileWaves];
+            if (__builtin_amdgcn_ballot_w64(there != 0) == 0) return;
+#pragma unroll 1
+            for (int w = 0; w < kTileWaves; ++w) {
+                if (s_odd[buf][w] == 0) continue;
+                uint32_t seen = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) seen |= (sees(pos, tile0 + 8 * w + e, a.window, a.sinks) ? 1u : 0u) << e;
+#pragma unroll 1
+                for (int x = 0; x < 16 * kDt; ++x) {
+                    const int d = 32 * (x >> 4) + 8 * (x >> 2 & 3) + 4 * hh + (x & 3);
+                    up |= (uint64_t)((s_up[buf][w][d] & seen) != 0) << x;
+                    down |= (uint64_t)((s_down[buf][w][d] & seen) != 0) << x;
+                }
+            }
+        }
+    };
+
+    put_k(next.live, 0);
+    clean_v(unit.lo, next.live, 0);
+    put_v(0);
+    next = source(unit.lo + 1);
+    tile_load_k<kStore, kDim>(next.block, half, lane, raw);
+    tile_load_v<kStore, kDim>(next.block, half, lane, raw);
+    for (int i = unit.lo; i < unit.hi; ++i) {
+        const int buf = (i - unit.lo) & 1, tile0 = tile_at(view, i) * kTileKeys;
+        lds_barrier();                                      // the tile is there, and all waves are through with the other buffer
+        if (some && tile0 <= mine.last) {
+            step(tile0, buf);
+            look_for_odd(tile0, buf);
+        }
+        if (i + 1 == unit.hi) break;
+        put_k(next.live, buf ^ 1);
+        clean_v(i + 1, next.live, buf ^ 1);
+        put_v(buf ^ 1);
+        next = source(i + 2);
+        tile_load_k<kStore, kDim>(next.block, half, lane, raw);
+        tile_load_v<kStore, kDim>(next.block, half, lane, raw);
+    }
+
+    // ---- results: lane (row col, hh) has values 32 d + 8 k + 4 hh .. + 3
+    const float sum = sum_over_halves(l);
+    if (r >= rows) return;
+    if constexpr (kStore == SALI_STORE_16)
+        if ((up | down) != 0)
+#pragma unroll
+            for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) acc[d][x] += found((up >> (16 * d + x) & 1) != 0, (down >> (16 * d + x) & 1) != 0);
+    if (unit.part >= 0) {
+        float* part = a.partial + (((size_t)unit.part * n_kv + head) * kTileRows + (size_t)(wave * 32 + col)) * kPitch;
+        if (hh == 0) {
+            part[0] = m;
+            part[1] = sum;
+        }
 #pragma unroll
         for (int d = 0; d < kDt; ++d)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                f32x4 pr = {0.0f, 0.0f, 0.0f, 0.0f};
-                const int at = 32 * d + 8 * k + 4 * hh;
-                if (a.prior != nullptr) pr = *reinterpret_cast<const f32x4*>(a.prior + row * kDim + at);
-                float o[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) o[x] = joined(e, acc[c][d][4 * k + x], pr[x]);
-                *reinterpret_cast<u32x2*>(out + 2 * at) = (u32x2){pack2<kBf16>(o[0], o[1]), pack2<kBf16>(o[2], o[3])};
-            }
-        if (hh == 0 && a.lse != nullptr) a.lse[row] = e.lse;
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<f32x4*>(part + 4 + 32 * d + 8 * k + 4 * hh) = (f32x4){acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
+        return;
     }
+    const int h = head * group + of_group;
+    const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
+    const RowEnd e = row_end(m, sum, a, row);
+    char* const out = a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes;
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            f32x4 pr = {0.0f, 0.0f, 0.0f, 0.0f};
+            const int at = 32 * d + 8 * k + 4 * hh;
+            if (a.prior != nullptr) pr = *reinterpret_cast<const f32x4*>(a.prior + row * kDim + at);
+            float o[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] = joined(e, acc[d][4 * k + x], pr[x]);
+            *reinterpret_cast<u32x2*>(out + 2 * at) = (u32x2){pack2<kBf16>(o[0], o[1]), pack2<kBf16>(o[2], o[3])};
+        }
+    if (hh == 0 && a.lse != nullptr) a.lse[row] = e.lse;
 }
 
 // Joins the parts of cut units: grid (merges * n_kv at most, kTileRows / 8), a row per 32 lanes
