@@ -47,12 +47,14 @@ struct PagesAttend {
     int32_t heads, group;                   // query heads, and of one K/V head
     float* partial;
     int32_t* records;
+    uint32_t* arrived;                      // counters, at zero between calls
 };
+constexpr int kMergeParts = 128;            // parts of a pair that a block of the stream may join
 
-// scratch of the pages object: the status word, then the partial results of attention
+// scratch of the pages object: the status word, counters, then the partial results of attention
 constexpr size_t kPagesStatusBytes = 256;
 struct PagesScratch {
-    size_t partial, records, bytes;         // where the two areas start
+    size_t cleared, partial, records, bytes;        // the status word and the counters, which start at zero; where the two areas start
 };
 PagesScratch pages_scratch(int64_t n_pages, int page_tokens, int n_kv, int group, int dim);
 
@@ -62,14 +64,16 @@ hipError_t launch_pages_attend_fp16(int store, int dim, const PagesAttend& a, hi
 hipError_t launch_pages_attend_bf16(int store, int dim, const PagesAttend& a, hipStream_t s);
 
 #ifdef __HIPCC__
-__device__ __forceinline__ PageSeq load_seq(const PageSeqs& q, const PageGeom& g, int s, bool note) {
+__device__ __forceinline__ PageSeq read_seq(const PageSeqs& q, const PageGeom& g, int s, bool& fits) {
     const int64_t a = q.start[s], b = q.start[s + 1], len = q.length[s];
     const int64_t in_table = (int64_t)q.width * (kBlockTokens << g.blocks_log2), room = in_table < q.max_kv ? in_table : q.max_kv;
-    PageSeq r = {(int32_t)a, (int32_t)(b - a), (int32_t)len};
-    if (!page_seq_holds(a, b, len, q.n_tokens, q.max_q, room)) {
-        if (note) atomicOr(q.status, SALI_FAULT_BATCH);
-        r.n = 0;
-    }
+    fits = page_seq_holds(a, b, len, q.n_tokens, q.max_q, room);
+    return {(int32_t)a, fits ? (int32_t)(b - a) : 0, (int32_t)len};
+}
+__device__ __forceinline__ PageSeq load_seq(const PageSeqs& q, const PageGeom& g, int s, bool note) {
+    bool fits;
+    const PageSeq r = read_seq(q, g, s, fits);
+    if (note && !fits) atomicOr(q.status, SALI_FAULT_BATCH);
     return r;
 }
 #endif

@@ -104,8 +104,7 @@ int sali_pages_create(const sali_pages_config* cfg, void* d_pool, void* d_scratc
     p->scratch = static_cast<uint8_t*>(d_scratch);
     p->layout = pages_scratch(cfg->n_pages, cfg->page_tokens, cfg->n_kv_heads, cfg->n_heads / cfg->n_kv_heads, cfg->head_dim);
     p->layer_bytes = layer_bytes_of(*cfg);
-    const uint32_t none = 0;
-    if (hipMemcpy(p->scratch, &none, sizeof(none), hipMemcpyHostToDevice) != hipSuccess) {
+    if (hipMemset(p->scratch, 0, p->layout.cleared) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
         delete p;
         return SALI_ERR_HIP;
     }
@@ -148,6 +147,8 @@ int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch
     if (window < 0 || sinks < 0 || window > (1 << 30) || sinks > (1 << 30)) return SALI_ERR_SHAPE;
     if (!isfinite(softmax_scale * 1.44269504088896340736f)) return SALI_ERR_CONFIG;
     if (nothing_to_do(*batch)) return SALI_OK;
+    // tiles are counted in 31 bits
+    if (((int64_t)batch->max_kv / kTileTokens + 2) * p->cfg.n_kv_heads > 0x7FFFFFFFll / batch->n_seqs) return SALI_ERR_SHAPE;
     PagesAttend a = {};
     a.geom = geom_of(p, layer);
     a.seqs = seqs_of(p, *batch);
@@ -164,6 +165,7 @@ int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch
     a.heads = p->cfg.n_heads;
     a.group = p->cfg.n_heads / p->cfg.n_kv_heads;
     a.partial = reinterpret_cast<float*>(p->scratch + p->layout.partial);
+    a.arrived = reinterpret_cast<uint32_t*>(p->scratch + kPagesStatusBytes);
     a.records = reinterpret_cast<int32_t*>(p->scratch + p->layout.records);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = p->cfg.dtype == SALI_DTYPE_BF16 ? launch_pages_attend_bf16(p->cfg.store, p->cfg.head_dim, a, s)

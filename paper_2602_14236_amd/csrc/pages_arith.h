@@ -66,9 +66,20 @@ SALI_BOTH bool sees(int p, int j, int window, int sinks) {
     return j <= p && (window == 0 || j > p - window || j < sinks);
 }
 
-// the last block of a pair's stretch: blocks of `blocks` equal stretches of `total` tiles; block b starts at tile b * total / blocks
-SALI_BOTH int64_t stretch_start(int64_t b, int64_t total, int64_t blocks) { return b * total / blocks; }
-SALI_BOTH int64_t stretch_of(int64_t tile, int64_t total, int64_t blocks) { return ((tile + 1) * blocks + total - 1) / total - 1; }
+// `total` tiles in `blocks` stretches (blocks <= total) that differ by one at most, the longer ones first
+struct Stretches {
+    uint32_t each, longer;
+    SALI_BOTH Stretches(uint32_t total, uint32_t blocks) : each(total / blocks), longer(total - total / blocks * blocks) {}
+    SALI_BOTH uint32_t start(uint32_t block) const { return block * each + least(block, longer); }
+    SALI_BOTH uint32_t of(uint32_t tile) const {
+        const uint32_t in_longer = longer * (each + 1);
+        return tile < in_longer ? tile / (each + 1) : longer + (tile - in_longer) / each;
+    }
+};
+constexpr int kStreamMinTiles = 4;          // of a stretch
+// A sequence's tiles are the same for all K/V heads, so one pair of sequence and head has at most a head's share of all tiles, and so many stretches
+// have a part of it (they have kStreamMinTiles or more, so the shorter ones are at least four fifths of the others).
+SALI_BOTH int parts_of_pair(int blocks, int n_kv) { return blocks * (kStreamMinTiles + 1) / (n_kv * kStreamMinTiles) + 2; }
 
 constexpr int kTileRows = 128;              // rows of a block of the tile kernel
 constexpr int kTileKeys = 32;               // keys of its steps

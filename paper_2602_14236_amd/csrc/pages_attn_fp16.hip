@@ -14,7 +14,8 @@ PagesScratch pages_scratch(int64_t n_pages, int page_tokens, int n_kv, int group
     const size_t records = max(sizeof(TilePlan) + (size_t)tile_parts(n_kv) * sizeof(TileMerge) + units * sizeof(TileUnit),
                                (size_t)stream_blocks(1) * sizeof(StreamRecord));
     PagesScratch p;
-    p.partial = kPagesStatusBytes;
+    p.cleared = kPagesStatusBytes + (size_t)kStreamMostBlocks * kMergeParts * sizeof(uint32_t);
+    p.partial = align(p.cleared);
     p.records = align(p.partial + parts * row);
     p.bytes = align(p.records + records);
     return p;

@@ -8,6 +8,9 @@ namespace sali {
 
 namespace {
 
+// rows x parts of a pair that the last block joins by itself, at most (by the bound on the parts); more are a launch's work
+constexpr int kMergeRowParts = 512;
+
 template <int kStore, int kDim, bool kBf16>
 void launch_attend(const PagesAttend& a, hipStream_t s) {
     const int n_kv = a.geom.n_kv, group = a.group;
@@ -18,15 +21,20 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
     if (stream_rows > 0) {
         const int64_t reach = a.window > 0 ? (int64_t)a.window + a.seqs.max_q + a.sinks + 3 * kTileTokens : (int64_t)a.seqs.max_kv + kTileTokens;
         const int64_t tiles = min((int64_t)a.seqs.max_kv + kTileTokens, reach) / kTileTokens * a.seqs.n_seqs * n_kv;
-        auto go = [&](auto sets, int most) {
+        auto go = [&](auto sets) {
             constexpr int kSets = decltype(sets)::value;
-            const int blocks = (int)max((int64_t)1, min((int64_t)most, (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
-            hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets>), dim3(blocks), dim3(64 * kStreamWaves), 0, s, a, stream_rows, kStreamMinTiles);
-            hipLaunchKernelGGL((k_pages_stream_merge<kDim, kBf16>), dim3(blocks, (unsigned)min((int64_t)stream_rows, most_rows)), dim3(256), 0, s, a, 16 * kSets);
+            const int blocks = (int)max((int64_t)1, min((int64_t)stream_blocks(kSets), (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
+            const int rows = (int)min((int64_t)stream_rows, most_rows), parts = parts_of_pair(blocks, n_kv);
+            if (parts <= kMergeParts && rows * parts <= kMergeRowParts) {
+                hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, true>), dim3(blocks), dim3(64 * kStreamWaves), 0, s, a, stream_rows, kStreamMinTiles);
+            } else {
+                hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, false>), dim3(blocks), dim3(64 * kStreamWaves), 0, s, a, stream_rows, kStreamMinTiles);
+                hipLaunchKernelGGL((k_pages_stream_merge<kDim, kBf16>), dim3(blocks, (rows + 3) / 4), dim3(256), 0, s, a, 16 * kSets);
+            }
         };
-        if (stream_rows == 16) go(std::integral_constant<int, 1>{}, stream_blocks(1));
-        else if (stream_rows == 32) go(std::integral_constant<int, 2>{}, stream_blocks(2));
-        else go(std::integral_constant<int, 4>{}, stream_blocks(4));
+        if (stream_rows == 16) go(std::integral_constant<int, 1>{});
+        else if (stream_rows == 32) go(std::integral_constant<int, 2>{});
+        else go(std::integral_constant<int, 4>{});
     }
     if (most_rows > 64) {
         const int64_t units = tile_slots(a.seqs.n_tokens, group, a.seqs.n_seqs) + tile_parts(n_kv);

@@ -17,8 +17,9 @@ namespace sali {
 namespace {
 
 constexpr int kStreamWaves = 4;
-constexpr int kStreamMinTiles = 4;          // of a block: one a wave
-constexpr int stream_blocks(int sets) { return sets == 1 ? 768 : (sets == 2 ? 512 : 256); }        // that are resident at once
+constexpr int stream_occupancy(int sets) { return sets == 1 ? 3 : (sets == 2 ? 2 : 1); }           // waves a SIMD: what their registers leave room for
+constexpr int kStreamMostBlocks = 256 * 3;
+constexpr int stream_blocks(int sets) { return 256 * stream_occupancy(sets); }                      // that are resident at once
 
 // A tile of 32 tokens as it lies in memory, a lane's share.  i = lane % 16, hh = lane / 16.
 //   K as the A operand, 16 places of a block in rows: lane (place i, hh) has 8 values of its token a step
@@ -139,88 +140,171 @@ __device__ __forceinline__ int stream_v_value(int f, int i) {
 
 __device__ __forceinline__ bool in_stream(const PageSeq& q, int group, int rows_max) { return q.n > 0 && (int64_t)q.n * group <= rows_max; }
 
-// the record of a block whose last segment is a pair's first part; blocks without one leave parts = 0
+// sums over the lanes up to each
+__device__ __forceinline__ int wave_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // row_bcast 15, 31
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+    return v;
+}
+
+// The parts of a pair, as a block or a launch that joins them finds them: the first in `slot`, the others the first segments of the following
+// blocks.  A block leaves a record of the pair whose first part is its last segment, parts = 0 if there is none.
 struct StreamRecord {
-    int32_t seq, head, slot, parts;         // slot of the first part; the others are the first segments of the following blocks
+    int32_t seq, head, slot, parts;
 };
+__device__ __forceinline__ int slot_of_part(const StreamRecord& r, int i) { return i == 0 ? r.slot : 2 * ((r.slot >> 1) + i); }
 
-template <int kStore, int kDim, bool kBf16, int kSets>
-__global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend a, int rows_max, int min_tiles) {
-    constexpr int kRows = 16 * kSets, kSteps = kDim / 32, kFs = kDim / 16, kPitch = kDim + 4;
-    __shared__ __align__(16) float s_acc[kStreamWaves][kRows][kPitch];
-    __shared__ float s_m[kStreamWaves][kRows], s_l[kStreamWaves][kRows];
-    __shared__ int64_t s_sum[kStreamWaves];
-    __shared__ int s_found;
-    __shared__ int64_t s_before;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 15, hh = lane >> 4;
-    const int n_kv = a.geom.n_kv, group = a.group;
+// Partial results are handed over past the caches that the compute dies do not share: agent-scope accesses, coherent by themselves, so that no
+// fence is needed; a block counts itself in when its own have arrived.
+__device__ __forceinline__ void put_pair(float* p, float a, float b) {
+    const uint64_t v = (uint64_t)__builtin_bit_cast(uint32_t, a) | (uint64_t)__builtin_bit_cast(uint32_t, b) << 32;
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void get_pair(const float* p, float& a, float& b) {
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    a = __builtin_bit_cast(float, (uint32_t)v);
+    b = __builtin_bit_cast(float, (uint32_t)(v >> 32));
+}
 
-    // ---- the block's stretch
-    auto tiles_of_seq = [&](int s) -> int {
-        const PageSeq q = load_seq(a.seqs, a.geom, s, blockIdx.x == 0);
-        return in_stream(q, group, rows_max) ? view_of<kTileTokens>(q.len - q.n, q.len - 1, a.window, a.sinks).tiles : 0;
-    };
-    const int mine = (int)threadIdx.x < a.seqs.n_seqs ? tiles_of_seq(threadIdx.x) : 0;
-    auto sum_block = [&](int64_t v) -> int64_t {            // inclusive over the block's threads; s_sum has the waves'
+// Rows r0, r0 + step, ... of a pair from its parts, by a block of 256 threads: the parts' references and sums give their weights (a wave a row),
+// then a thread takes two values of a row, sixteen parts in flight.  s_weight: [rows][kMostParts], s_sum [rows].
+template <int kDim, bool kBf16, int kMostParts>
+__device__ __forceinline__ void join_parts(const PagesAttend& a, const StreamRecord& rec, const PageSeq& seq, int kernel_rows, int r0, int n_rows,
+                                           float (*s_weight)[kMostParts], float* s_top, float* s_sum) {
+    constexpr int kPitch = kDim + 4;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int x = wave; x < n_rows; x += 4) {
+        float top = -INFINITY, sum = 0.0f;
+        float m[kMostParts / 64], l[kMostParts / 64];
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int64_t u = __shfl_up(v, off);
-            if (lane >= off) v += u;
+        for (int j = 0; j < kMostParts / 64; ++j) {
+            m[j] = -INFINITY;
+            l[j] = 0.0f;
+            const int i = 64 * j + lane;
+            if (i < rec.parts) get_pair(a.partial + ((size_t)slot_of_part(rec, i) * kernel_rows + r0 + x) * kPitch, m[j], l[j]);
         }
-        __syncthreads();
-        if (lane == 63) s_sum[wave] = v;
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) v += s_sum[w];
-        return v;
-    };
-    int64_t own = mine;
-    for (int s = (int)threadIdx.x + 256; s < a.seqs.n_seqs; s += 256) own += tiles_of_seq(s);
-    int64_t upto = sum_block(own);
-    const int64_t per_head = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3], total = per_head * n_kv;
-    const int64_t blocks = max((int64_t)1, min((int64_t)gridDim.x, total / min_tiles));
-    StreamRecord* records = reinterpret_cast<StreamRecord*>(a.records);
-    StreamRecord record = {0, 0, 0, 0};
-    int64_t at = 0, end = 0;
-    if ((int64_t)blockIdx.x < blocks) {
-        at = stretch_start(blockIdx.x, total, blocks);
-        end = stretch_start((int64_t)blockIdx.x + 1, total, blocks);
-    }
-    if (at >= end) {
-        if (threadIdx.x == 0) records[blockIdx.x] = record;
-        return;
-    }
-    if (a.seqs.n_seqs <= 256) {
-        if (at >= (upto - mine) * n_kv && at < upto * n_kv) {
-            s_found = threadIdx.x;
-            s_before = upto - mine;
+#pragma unroll
+        for (int j = 0; j < kMostParts / 64; ++j)
+            if (l[j] != 0.0f) top = fmaxf(top, m[j]);
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+#pragma unroll
+        for (int j = 0; j < kMostParts / 64; ++j) {
+            const float w = l[j] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m[j] - top);
+            sum += l[j] == 0.0f ? 0.0f : l[j] * w;
+            s_weight[x][64 * j + lane] = w;
         }
-    } else {
-        int64_t before = 0;
-        for (int base = 0; base < a.seqs.n_seqs; base += 256) {
-            const int s = base + (int)threadIdx.x, t = s < a.seqs.n_seqs ? tiles_of_seq(s) : 0;
-            upto = before + sum_block(t);
-            if (at >= (upto - t) * n_kv && at < upto * n_kv) {
-                s_found = s;
-                s_before = upto - t;
-            }
-            before += s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-            if (before * n_kv > at) break;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+        if (lane == 0) {
+            s_top[x] = top;
+            s_sum[x] = sum;
         }
     }
     __syncthreads();
-    int s = __builtin_amdgcn_readfirstlane(s_found);
-    PageSeq seq = load_seq(a.seqs, a.geom, s, false);
-    View view = view_of<kTileTokens>(seq.len - seq.n, seq.len - 1, a.window, a.sinks);
-    int head, done;                          // of the sequence: K/V head and its tiles before the block's
-    {
-        const int64_t off = at - s_before * n_kv;
-        head = (int)(off / view.tiles);
-        done = (int)(off - (int64_t)head * view.tiles);
+    for (int idx = threadIdx.x; idx < n_rows * (kDim / 2); idx += 256) {
+        const int x = idx / (kDim / 2), d = idx % (kDim / 2) * 2, r = r0 + x;
+        float o0 = 0.0f, o1 = 0.0f;
+        for (int i0 = 0; i0 < rec.parts; i0 += 16) {
+            float v0[16], v1[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                get_pair(a.partial + ((size_t)slot_of_part(rec, min(i0 + i, rec.parts - 1)) * kernel_rows + r) * kPitch + 4 + d, v0[i], v1[i]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = i0 + i < rec.parts ? s_weight[x][i0 + i] : 0.0f;
+                if (w == 0.0f) continue;                    // nothing seen, or nothing left of it
+                o0 = __builtin_fmaf(v0[i], w, o0);
+                o1 = __builtin_fmaf(v1[i], w, o1);
+            }
+        }
+        const int token = r / a.group, h = rec.head * a.group + (r - token * a.group);
+        const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
+        const RowEnd e = row_end(s_top[x], s_sum[x], a, row);
+        float p0 = 0.0f, p1 = 0.0f;
+        if (a.prior != nullptr) {
+            p0 = a.prior[row * kDim + d];
+            p1 = a.prior[row * kDim + d + 1];
+        }
+        *reinterpret_cast<uint32_t*>(a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes + 2 * d) =
+            pack2<kBf16>(joined(e, o0, p0), joined(e, o1, p1));
+        if (d == 0 && a.lse != nullptr) a.lse[row] = e.lse;
     }
+}
+
+// kMerged: the last block of a pair to finish joins its parts; else a launch of its own does (k_pages_stream_merge)
+template <int kStore, int kDim, bool kBf16, int kSets, bool kMerged>
+__global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(stream_occupancy(kSets), stream_occupancy(kSets)))) void k_pages_stream(
+    PagesAttend a, int rows_max, int min_tiles) {
+    constexpr int kRows = 16 * kSets, kSteps = kDim / 32, kFs = kDim / 16, kPitch = kDim + 4;
+    __shared__ __align__(16) float s_acc[kStreamWaves][kRows][kPitch];
+    __shared__ float s_m[kStreamWaves][kRows], s_l[kStreamWaves][kRows];
+    __shared__ int s_last;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 15, hh = lane >> 4;
+    const int n_kv = a.geom.n_kv, group = a.group;
+
+    // ---- the block's stretch: every wave finds it by itself, a sequence a lane
+    bool bad = false;
+    auto lane_seq = [&](int s) -> PageSeq {
+        PageSeq q = {0, 0, 0};
+        if (s >= a.seqs.n_seqs) return q;
+        bool fits;
+        q = read_seq(a.seqs, a.geom, s, fits);
+        bad |= !fits;
+        return q;
+    };
+    auto tiles_of = [&](const PageSeq& q) { return in_stream(q, group, rows_max) ? view_of<kTileTokens>(q.len - q.n, q.len - 1, a.window, a.sinks).tiles : 0; };
+    const PageSeq first_mine = lane_seq(lane);
+    const int first_tiles = tiles_of(first_mine);
+    int own = first_tiles;
+#pragma unroll 4
+    for (int s = 64 + lane; s < a.seqs.n_seqs; s += 64) own += tiles_of(lane_seq(s));
+    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane(wave_scan(own), 63) * (uint32_t)n_kv;
+    if (bad && blockIdx.x == 0 && wave == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
+    const uint32_t blocks = max(1u, min(gridDim.x, total / (uint32_t)min_tiles));
+    StreamRecord* records = reinterpret_cast<StreamRecord*>(a.records);
+    StreamRecord record = {0, 0, 0, 0};
+    if (blockIdx.x >= blocks || total == 0) {
+        if (!kMerged && threadIdx.x == 0) records[blockIdx.x] = record;
+        return;
+    }
+    const Stretches cut(total, blocks);
+    uint32_t at = __builtin_amdgcn_readfirstlane(cut.start(blockIdx.x));
+    const uint32_t end = __builtin_amdgcn_readfirstlane(cut.start(blockIdx.x + 1));
+    int s = 0;
+    PageSeq seq = {0, 0, 0};
+    uint32_t before = 0;                    // tiles a head of the sequences before it
+    {
+        PageSeq q = first_mine;
+        int t = first_tiles;
+        for (int base = 0;;) {
+            const int upto = wave_scan(t);
+            const uint64_t past = __builtin_amdgcn_ballot_w64((before + (uint32_t)upto) * (uint32_t)n_kv > at);
+            if (past != 0) {
+                const int k = __builtin_ctzll(past);
+                s = base + k;
+                seq = {__builtin_amdgcn_readlane(q.first, k), __builtin_amdgcn_readlane(q.n, k), __builtin_amdgcn_readlane(q.len, k)};
+                before += (uint32_t)(__builtin_amdgcn_readlane(upto, k) - __builtin_amdgcn_readlane(t, k));
+                break;
+            }
+            before += (uint32_t)__builtin_amdgcn_readlane(upto, 63);
+            base += 64;
+            if (base >= a.seqs.n_seqs) return;              // the batch changed while it was read
+            q = lane_seq(base + lane);
+            t = tiles_of(q);
+        }
+    }
+    View view = view_of<kTileTokens>(seq.len - seq.n, seq.len - 1, a.window, a.sinks);
+    int head = __builtin_amdgcn_readfirstlane((int)((at - before * (uint32_t)n_kv) / (uint32_t)view.tiles));
+    int done = (int)(at - before * (uint32_t)n_kv) - head * view.tiles;         // tiles of the pair before the block's
 
     bool first_segment = true;
     while (at < end) {
-        const int todo = (int)min((int64_t)(view.tiles - done), end - at);
+        const int todo = min(view.tiles - done, (int)(end - at));
         const int rows = seq.n * group;
         const int32_t* table = a.seqs.table + (int64_t)s * a.seqs.width;
         const int pages = (seq.len + (kBlockTokens << a.geom.blocks_log2) - 1) / (kBlockTokens << a.geom.blocks_log2);
@@ -256,7 +340,8 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
             return t;
         };
 
-        const int lo = done + (int)((int64_t)todo * wave / kStreamWaves), hi = done + (int)((int64_t)todo * (wave + 1) / kStreamWaves);
+        const int lo = done + (int)((uint32_t)todo / kStreamWaves) * wave + min(wave, todo % kStreamWaves);
+        const int hi = lo + (int)((uint32_t)todo / kStreamWaves) + (wave < todo % kStreamWaves ? 1 : 0);
         StreamRaw<kStore, kDim> raw;
         Tile now = {};
         if (lo < hi) {
@@ -295,8 +380,8 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
 
         for (int i = lo; i < hi; ++i) {
             const int j0 = tile_at(view, i) * kTileTokens;
-            const bool more = i + 1 < hi;
-            const Tile next = more ? locate(i + 1) : now;
+            // behind the last tile the same once more, for nothing: with loads that depend on a branch every wait would be one for all of them
+            const Tile next = locate(min(i + 1, hi - 1));
             f32x4 s2[kSets][2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -309,7 +394,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
                     for (int c = 0; c < kSets; ++c) s2[c][j] = Num<kBf16>::mma16(kf, q[c][t], s2[c][j]);
                 }
             }
-            if (more) stream_load_k<kStore, kDim>(next.b[0], next.b[1], lane, raw);
+            stream_load_k<kStore, kDim>(next.b[0], next.b[1], lane, raw);
             // lane (row col, hh): tokens 8 (hh % 2) + 4 (hh / 2) .. + 3 of each block
             const int t0 = j0 + 8 * (hh & 1) + 4 * (hh >> 1);
             const bool masked = now.live[0] < kBlockTokens || now.live[1] < kBlockTokens || partly_hidden(view, a.window, a.sinks, j0, kTileTokens);
@@ -411,7 +496,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
 #pragma unroll
                 for (int c = 0; c < kSets; ++c) acc[c][f] = Num<kBf16>::mma16(vf, p[c], acc[c][f]);
             }
-            if (more) stream_load_v<kStore, kDim>(next.b[0], next.b[1], lane, raw);
+            stream_load_v<kStore, kDim>(next.b[0], next.b[1], lane, raw);
             now = next;
         }
 
@@ -456,11 +541,9 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
             }
             if (!whole) {
                 float* part = a.partial + ((size_t)slot * kRows + r) * kPitch;
-                *reinterpret_cast<f32x4*>(part + 4 + d) = o;
-                if (d == 0) {
-                    part[0] = top;
-                    part[1] = sum;
-                }
+                put_pair(part + 4 + d, o[0], o[1]);
+                put_pair(part + 6 + d, o[2], o[3]);
+                if (d == 0) put_pair(part, top, sum);
                 continue;
             }
             const int token = r / group, h = head * group + (r - token * group);
@@ -472,12 +555,26 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
             *reinterpret_cast<u32x2*>(a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes + 2 * d) = v;
             if (d == 0 && a.lse != nullptr) a.lse[row] = e.lse;
         }
+        if (!whole) {
+            // the pair's first part is in the block whose stretch has its first tile; that is its last segment, and its only one if it starts there
+            const uint32_t pair0 = at - (uint32_t)done, b0 = __builtin_amdgcn_readfirstlane(cut.of(pair0)), b1 = __builtin_amdgcn_readfirstlane(cut.of(pair0 + (uint32_t)view.tiles - 1u));
+            const StreamRecord pair = {s, head, (int)(2 * b0 + (cut.start(b0) == pair0 ? 0u : 1u)), (int)(b1 - b0) + 1};
+            if constexpr (kMerged) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // every wave: its parts have arrived
+                __syncthreads();
+                if (threadIdx.x == 0)
+                    s_last = last_arrival(atomicInc(a.arrived + (size_t)b0 * kMergeParts + (pair.parts - 1), (uint32_t)pair.parts - 1u), pair.parts) ? 1 : 0;
+                __syncthreads();
+                if (s_last != 0) {
+                    static_assert(sizeof(float[kRows][kMergeParts]) <= sizeof(s_acc), "the weights of the parts");
+                    join_parts<kDim, kBf16, kMergeParts>(a, pair, seq, kRows, 0, rows, reinterpret_cast<float(*)[kMergeParts]>(&s_acc[0][0][0]), s_m[0], s_l[0]);
+                }
+            } else if (done == 0) {
+                record = pair;
+            }
+        }
         __syncthreads();
 
-        if (!whole && done == 0) {                          // a pair's first part: the following blocks have the others
-            const int64_t last = at + view.tiles - 1;
-            record = {s, head, slot, (int)(stretch_of(last, total, blocks) - blockIdx.x) + 1};
-        }
         at += todo;
         first_segment = false;
         done += todo;
@@ -494,65 +591,20 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_pages_stream(PagesAttend 
             }
         }
     }
-    if (threadIdx.x == 0) records[blockIdx.x] = record;
+    if (!kMerged && threadIdx.x == 0) records[blockIdx.x] = record;
 }
 
-// Joins the parts of a pair's row: grid (blocks of the stream, rows), four waves that share the parts.
+// Joins the parts of the pairs, four rows a block: grid (blocks of the stream, rows / 4)
 template <int kDim, bool kBf16>
 __global__ __launch_bounds__(256) void k_pages_stream_merge(PagesAttend a, int kernel_rows) {
-    constexpr int kPitch = kDim + 4, kPer = kDim / 64;
-    __shared__ float s_acc[4][kDim], s_m[4], s_l[4];
+    __shared__ float s_weight[4][kStreamMostBlocks], s_top[4], s_sum[4];
     const StreamRecord rec = reinterpret_cast<const StreamRecord*>(a.records)[blockIdx.x];
     if (rec.parts == 0) return;
-    const PageSeq seq = load_seq(a.seqs, a.geom, rec.seq, false);
-    const int r = blockIdx.y;
-    if (r >= seq.n * a.group) return;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    float m = -INFINITY, l = 0.0f, acc[kPer];
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) acc[e] = 0.0f;
-#pragma unroll 4
-    for (int i = wave; i < rec.parts; i += 4) {
-        const int slot = i == 0 ? rec.slot : 2 * ((rec.slot >> 1) + i);
-        const float* part = a.partial + ((size_t)slot * kernel_rows + r) * kPitch;
-        const float pm = part[0], pl = part[1];
-        float v[kPer];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) v[e] = part[4 + lane * kPer + e];
-        const float to = fmaxf(m, pm);
-        const float ref = to == -INFINITY ? 0.0f : to, by = __builtin_amdgcn_exp2f(m - ref), pby = __builtin_amdgcn_exp2f(pm - ref);
-        if (pl == 0.0f) continue;               // nothing seen
-        const bool none = l == 0.0f;
-        l = (none ? 0.0f : l * by) + pl * pby;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = (none ? 0.0f : acc[e] * by) + v[e] * pby;
-        m = to;
-    }
-    if (lane == 0) {
-        s_m[wave] = m;
-        s_l[wave] = l;
-    }
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) s_acc[wave][lane * kPer + e] = acc[e];
-    __syncthreads();
-    const int d = threadIdx.x;
-    if (d >= kDim) return;
-    const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-    float sum = 0.0f, o = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        if (s_l[w] == 0.0f) continue;
-        const float by = __builtin_amdgcn_exp2f(s_m[w] - top);
-        sum += s_l[w] * by;
-        o += s_acc[w][d] * by;
-    }
-    const int token = r / a.group, h = rec.head * a.group + (r - token * a.group);
-    const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
-    const RowEnd e = row_end(top, sum, a, row);
-    const float pr = a.prior != nullptr ? a.prior[row * kDim + d] : 0.0f;
-    *reinterpret_cast<typename Num<kBf16>::T*>(a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes + 2 * d) =
-        (typename Num<kBf16>::T)joined(e, o, pr);
-    if (d == 0 && a.lse != nullptr) a.lse[row] = e.lse;
+    bool fits;
+    const PageSeq seq = read_seq(a.seqs, a.geom, rec.seq, fits);
+    const int r0 = 4 * (int)blockIdx.y;
+    if (r0 >= seq.n * a.group) return;
+    join_parts<kDim, kBf16, kStreamMostBlocks>(a, rec, seq, kernel_rows, r0, min(4, seq.n * a.group - r0), s_weight, s_top, s_sum);
 }
 
 }  // namespace

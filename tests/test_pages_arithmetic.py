@@ -125,11 +125,18 @@ def test_stretches_and_shares(tmp_path, seed):
 int main() {
     srand(%d);
     for (int round = 0; round < 2000; ++round) {
-        const int64_t total = rand() %% 2 ? rand() %% 3000 + 1 : (int64_t)rand() * 1000 + 1, blocks = least(total, (int64_t)(rand() %% 768 + 1));
-        if (stretch_start(0, total, blocks) != 0 || stretch_start(blocks, total, blocks) != total) return 1;
+        const uint32_t total = rand() %% 2 ? rand() %% 3000 + 1 : (uint32_t)rand() / 2 + 1, blocks = least(total, (uint32_t)(rand() %% 768 + 1));
+        const Stretches cut(total, blocks);
+        if (cut.start(0) != 0 || cut.start(blocks) != total) return 1;
         for (int k = 0; k < 200; ++k) {
-            const int64_t b = rand() %% blocks, lo = stretch_start(b, total, blocks), hi = stretch_start(b + 1, total, blocks);
-            if (lo >= hi || stretch_of(lo, total, blocks) != b || stretch_of(hi - 1, total, blocks) != b) return 2;
+            const uint32_t b = rand() %% blocks, lo = cut.start(b), hi = cut.start(b + 1);
+            if (lo >= hi || cut.of(lo) != b || cut.of(hi - 1) != b) return 2;
+        }
+        const uint32_t n_kv = rand() %% 40 + 1, per_head = total / n_kv;
+        if (per_head * n_kv / kStreamMinTiles >= blocks) {
+            const Stretches all(per_head * n_kv, blocks);
+            const uint32_t head = rand() %% n_kv;
+            if (all.of(per_head * (head + 1) - 1) - all.of(per_head * head) + 1 > (uint32_t)parts_of_pair(blocks, n_kv)) return 5;
         }
     }
     for (int round = 0; round < 3000; ++round) {
