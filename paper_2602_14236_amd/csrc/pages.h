@@ -47,14 +47,12 @@ struct PagesAttend {
     int32_t heads, group;                   // query heads, and of one K/V head
     float* partial;
     int32_t* records;
-    uint32_t* arrived;                      // counters, at zero between calls
 };
-constexpr int kMergeParts = 128;            // parts of a pair that a block of the stream may join
 
-// scratch of the pages object: the status word, counters, then the partial results of attention
+// scratch of the pages object: the status word, then the partial results of attention
 constexpr size_t kPagesStatusBytes = 256;
 struct PagesScratch {
-    size_t cleared, partial, records, bytes;        // the status word and the counters, which start at zero; where the two areas start
+    size_t partial, records, bytes;         // where the two areas start
 };
 PagesScratch pages_scratch(int64_t n_pages, int page_tokens, int n_kv, int group, int dim);
 

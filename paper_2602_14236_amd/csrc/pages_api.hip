@@ -104,7 +104,7 @@ int sali_pages_create(const sali_pages_config* cfg, void* d_pool, void* d_scratc
     p->scratch = static_cast<uint8_t*>(d_scratch);
     p->layout = pages_scratch(cfg->n_pages, cfg->page_tokens, cfg->n_kv_heads, cfg->n_heads / cfg->n_kv_heads, cfg->head_dim);
     p->layer_bytes = layer_bytes_of(*cfg);
-    if (hipMemset(p->scratch, 0, p->layout.cleared) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
+    if (hipMemset(p->scratch, 0, kPagesStatusBytes) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
         delete p;
         return SALI_ERR_HIP;
     }
@@ -165,7 +165,6 @@ int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch
     a.heads = p->cfg.n_heads;
     a.group = p->cfg.n_heads / p->cfg.n_kv_heads;
     a.partial = reinterpret_cast<float*>(p->scratch + p->layout.partial);
-    a.arrived = reinterpret_cast<uint32_t*>(p->scratch + kPagesStatusBytes);
     a.records = reinterpret_cast<int32_t*>(p->scratch + p->layout.records);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = p->cfg.dtype == SALI_DTYPE_BF16 ? launch_pages_attend_bf16(p->cfg.store, p->cfg.head_dim, a, s)

@@ -76,11 +76,7 @@ struct Stretches {
         return tile < in_longer ? tile / (each + 1) : longer + (tile - in_longer) / each;
     }
 };
-constexpr int kStreamMinTiles = 4;          // of a stretch
-// A sequence's tiles are the same for all K/V heads, so one pair of sequence and head has at most a head's share of all tiles, and so many stretches
-// have a part of it (they have kStreamMinTiles or more, so the shorter ones are at least four fifths of the others).
-SALI_BOTH int parts_of_pair(int blocks, int n_kv) { return blocks * (kStreamMinTiles + 1) / (n_kv * kStreamMinTiles) + 2; }
-
+constexpr int kStreamMinTiles = 8;          // of a stretch
 constexpr int kTileRows = 128;              // rows of a block of the tile kernel
 constexpr int kTileKeys = 32;               // keys of its steps
 constexpr int kTileShares = 512;            // fair shares that the whole work is cut into

@@ -9,13 +9,12 @@ PagesScratch pages_scratch(int64_t n_pages, int page_tokens, int n_kv, int group
     auto align = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t row = (size_t)(dim + 4) * sizeof(float);
     size_t parts = (size_t)tile_parts(n_kv) * n_kv * kTileRows;
-    for (int sets = 1; sets <= 4; sets *= 2) parts = max(parts, (size_t)2 * stream_blocks(sets) * 16 * sets);
+    parts = max(parts, (size_t)2 * kStreamMostBlocks * 32);
     const size_t units = (size_t)(tile_slots(n_pages * page_tokens, group, n_pages) + tile_parts(n_kv));
     const size_t records = max(sizeof(TilePlan) + (size_t)tile_parts(n_kv) * sizeof(TileMerge) + units * sizeof(TileUnit),
-                               (size_t)stream_blocks(1) * sizeof(StreamRecord));
+                               (size_t)kStreamMostBlocks * sizeof(StreamRecord));
     PagesScratch p;
-    p.cleared = kPagesStatusBytes + (size_t)kStreamMostBlocks * kMergeParts * sizeof(uint32_t);
-    p.partial = align(p.cleared);
+    p.partial = kPagesStatusBytes;
     p.records = align(p.partial + parts * row);
     p.bytes = align(p.records + records);
     return p;

@@ -8,35 +8,38 @@ namespace sali {
 
 namespace {
 
-// rows x parts of a pair that the last block joins by itself, at most (by the bound on the parts); more are a launch's work
-constexpr int kMergeRowParts = 512;
-
 template <int kStore, int kDim, bool kBf16>
 void launch_attend(const PagesAttend& a, hipStream_t s) {
     const int n_kv = a.geom.n_kv, group = a.group;
     const int64_t most_rows = (int64_t)a.seqs.max_q * group;
     // Rows of a sequence that the stream takes at most.  In a batch that has longer sequences: those of single tokens.
-    int stream_rows = most_rows <= 16 ? 16 : (most_rows <= 32 ? 32 : 64);
-    if (most_rows > 64) stream_rows = a.seqs.n_seqs == 1 || group > 64 ? 0 : (group <= 16 ? 16 : (group <= 32 ? 32 : 64));
+    int stream_rows = most_rows <= 16 ? 16 : 32;
+    if (most_rows > 32) stream_rows = a.seqs.n_seqs == 1 || group > 32 ? 0 : (group <= 16 ? 16 : 32);
     if (stream_rows > 0) {
         const int64_t reach = a.window > 0 ? (int64_t)a.window + a.seqs.max_q + a.sinks + 3 * kTileTokens : (int64_t)a.seqs.max_kv + kTileTokens;
         const int64_t tiles = min((int64_t)a.seqs.max_kv + kTileTokens, reach) / kTileTokens * a.seqs.n_seqs * n_kv;
+        const PageSeqs& q = a.seqs;
         auto go = [&](auto sets) {
             constexpr int kSets = decltype(sets)::value;
-            const int blocks = (int)max((int64_t)1, min((int64_t)stream_blocks(kSets), (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
-            const int rows = (int)min((int64_t)stream_rows, most_rows), parts = parts_of_pair(blocks, n_kv);
-            if (parts <= kMergeParts && rows * parts <= kMergeRowParts) {
-                hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, true>), dim3(blocks), dim3(64 * kStreamWaves), 0, s, a, stream_rows, kStreamMinTiles);
-            } else {
-                hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, false>), dim3(blocks), dim3(64 * kStreamWaves), 0, s, a, stream_rows, kStreamMinTiles);
-                hipLaunchKernelGGL((k_pages_stream_merge<kDim, kBf16>), dim3(blocks, (rows + 3) / 4), dim3(256), 0, s, a, 16 * kSets);
+            auto launch = [&](auto mode, dim3 grid) {
+                hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, decltype(mode)::value>), grid, dim3(64 * kStreamWaves), 0, s, q.start, q.length,
+                                   q.table, q.n_seqs, q.width, q.n_tokens, q.max_q, q.max_kv, a.geom.blocks_log2, a.window, a.sinks, group, n_kv, a,
+                                   stream_rows, kStreamMinTiles);
+            };
+            const int64_t pairs = (int64_t)q.n_seqs * n_kv, tiles_a_pair = tiles / pairs;
+            if (tiles_a_pair <= 4 * kStreamWaves && pairs <= kStreamMostBlocks) {
+                launch(std::integral_constant<StreamMode, StreamMode::pairs>{}, dim3(n_kv, q.n_seqs));
+                return;
             }
+            const int blocks = (int)max((int64_t)1, min((int64_t)kStreamMostBlocks, (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
+            const int rows = (int)min((int64_t)stream_rows, most_rows);
+            launch(std::integral_constant<StreamMode, StreamMode::stretches>{}, dim3(blocks));
+            hipLaunchKernelGGL((k_pages_stream_merge<kDim, kBf16>), dim3(blocks, (rows + 3) / 4), dim3(256), 0, s, a, 16 * kSets);
         };
         if (stream_rows == 16) go(std::integral_constant<int, 1>{});
-        else if (stream_rows == 32) go(std::integral_constant<int, 2>{});
-        else go(std::integral_constant<int, 4>{});
+        else go(std::integral_constant<int, 2>{});
     }
-    if (most_rows > 64) {
+    if (most_rows > 32) {
         const int64_t units = tile_slots(a.seqs.n_tokens, group, a.seqs.n_seqs) + tile_parts(n_kv);
         hipLaunchKernelGGL(k_pages_plan, dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1);
         hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16>), dim3((unsigned)(units * n_kv)), dim3(64 * kTileWaves), 0, s, a);

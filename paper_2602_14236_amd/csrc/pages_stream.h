@@ -1,4 +1,4 @@
-// Attention of few new tokens a sequence (up to 64 rows: single tokens, drafts, short texts): a stream over the pages.
+// Attention of few new tokens a sequence (up to 32 rows: single tokens, drafts, short texts): a stream over the pages.
 //
 // Few rows make the products thin, so the kernel is bound by the bytes of K and V.  Every wave takes tiles of its own straight from memory into the
 // operands of the 16x16x32 products, no LDS and no barrier between tiles; the next tile's K is asked for when this one's has been multiplied, V
@@ -6,8 +6,8 @@
 //
 // The work of all sequences and K/V heads is one row of tiles, cut into equal stretches, one a block: whatever the lengths, all
 // blocks have the same number of tiles, give or take one.  A block's stretch may end inside one pair of sequence and head and hold
-// whole ones; its four waves split each such segment, meet in LDS, and leave a result (whole pairs) or a partial one, of which a block has
-// at most two, at its ends.  The merge kernel joins a pair's partial results.
+// whole ones; its waves split each such segment, meet in LDS, and leave a result (whole pairs) or a partial one, of which a block has
+// at most two, at its ends.  A second launch joins a pair's partial results.
 #pragma once
 
 #include "pages_attn.h"
@@ -16,10 +16,8 @@ namespace sali {
 
 namespace {
 
-constexpr int kStreamWaves = 4;
-constexpr int stream_occupancy(int sets) { return sets == 1 ? 3 : (sets == 2 ? 2 : 1); }           // waves a SIMD: what their registers leave room for
-constexpr int kStreamMostBlocks = 256 * 3;
-constexpr int stream_blocks(int sets) { return 256 * stream_occupancy(sets); }                      // that are resident at once
+constexpr int kStreamWaves = 8;             // of a block, which has a compute unit to itself: their registers leave room for two a SIMD
+constexpr int kStreamMostBlocks = 256;      // compute units
 
 // A tile of 32 tokens as it lies in memory, a lane's share.  i = lane % 16, hh = lane / 16.
 //   K as the A operand, 16 places of a block in rows: lane (place i, hh) has 8 values of its token a step
@@ -46,6 +44,8 @@ struct StreamRaw<SALI_STORE_INT4, kDim> {
     u32x4 vz[kDim / 32];
 };
 
+__device__ __forceinline__ u32x4 stream16(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4*>(p)); }
+
 template <int kStore, int kDim>
 __device__ __forceinline__ void stream_load_k(const char* b0, const char* b1, int lane, StreamRaw<kStore, kDim>& r) {
     constexpr BlockLayout kAt = block_layout(kStore, kDim);
@@ -54,20 +54,20 @@ __device__ __forceinline__ void stream_load_k(const char* b0, const char* b1, in
         const char* b = j == 0 ? b0 : b1;
         if constexpr (kStore == SALI_STORE_16) {
 #pragma unroll
-            for (int t = 0; t < kDim / 32; ++t) r.k[j][t] = load16(b + (uint32_t)(t * 1024 + lane * 16));
+            for (int t = 0; t < kDim / 32; ++t) r.k[j][t] = stream16(b + (uint32_t)(t * 1024 + lane * 16));
         } else if constexpr (kStore == SALI_STORE_INT8) {
 #pragma unroll
             for (int u = 0; u < kDim / 64; ++u) {
-                r.k[j][u] = load16(b + (uint32_t)(u * 1024 + lane * 16));
+                r.k[j][u] = stream16(b + (uint32_t)(u * 1024 + lane * 16));
                 r.ks[j][u] = *reinterpret_cast<const float*>(b + kAt.ks + (uint32_t)((2 * u + (lane >> 5)) * 64 + (lane & 15) * 4));
             }
         } else if constexpr (kDim == 128) {
-            r.k[j] = load16(b + (uint32_t)(lane * 16));
+            r.k[j] = stream16(b + (uint32_t)(lane * 16));
             r.ks[j] = *reinterpret_cast<const float*>(b + kAt.ks + (uint32_t)(lane * 4));
             r.kz[j] = *reinterpret_cast<const uint16_t*>(b + kAt.kz + (uint32_t)(lane * 2));
         } else {
             const uint32_t at = (uint32_t)((lane >> 5) * 16 + (lane & 15));
-            const u32x2 c = *reinterpret_cast<const u32x2*>(b + at * 16 + (uint32_t)(lane >> 4 & 1) * 8);
+            const u32x2 c = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(b + at * 16 + (uint32_t)(lane >> 4 & 1) * 8));
             r.k[j] = (u32x4){c.x, c.y, 0u, 0u};
             r.ks[j] = *reinterpret_cast<const float*>(b + kAt.ks + at * 4);
             r.kz[j] = *reinterpret_cast<const uint16_t*>(b + kAt.kz + at * 2);
@@ -81,12 +81,12 @@ __device__ __forceinline__ void stream_load_v(const char* b0, const char* b1, in
     const uint32_t i = lane & 15, a = lane >> 4 & 1;
     if constexpr (kStore == SALI_STORE_16) {
 #pragma unroll
-        for (int f = 0; f < kDim / 16; ++f) r.v[f] = load16(b + kAt.v + (a * kDim + 16 * f + i) * 16);
+        for (int f = 0; f < kDim / 16; ++f) r.v[f] = stream16(b + kAt.v + (a * kDim + 16 * f + i) * 16);
     } else {
 #pragma unroll
         for (int g = 0; g < kDim / 32; ++g) {
-            if constexpr (kStore == SALI_STORE_INT8) r.v[g] = load16(b + kAt.v + (a * kDim + 32 * g + 2 * i) * 8);
-            else r.v[g] = *reinterpret_cast<const u32x2*>(b + kAt.v + ((a * (kDim / 32) + g) * 16 + i) * 8);
+            if constexpr (kStore == SALI_STORE_INT8) r.v[g] = stream16(b + kAt.v + (a * kDim + 32 * g + 2 * i) * 8);
+            else r.v[g] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(b + kAt.v + ((a * (kDim / 32) + g) * 16 + i) * 8));
             const f32x4* s = reinterpret_cast<const f32x4*>(b + kAt.vs + (g * 16 + 8 * a) * 4);
             r.vs[g] = {s[0], s[1]};
             if constexpr (kStore == SALI_STORE_INT4) r.vz[g] = load16(b + kAt.vz + (g * 16 + 8 * a) * 2);
@@ -151,77 +151,93 @@ __device__ __forceinline__ int wave_scan(int v) {
     return v;
 }
 
-// The parts of a pair, as a block or a launch that joins them finds them: the first in `slot`, the others the first segments of the following
+// The parts of a pair, as the launch that joins them finds them: the first in `slot`, the others the first segments of the following
 // blocks.  A block leaves a record of the pair whose first part is its last segment, parts = 0 if there is none.
 struct StreamRecord {
     int32_t seq, head, slot, parts;
 };
-__device__ __forceinline__ int slot_of_part(const StreamRecord& r, int i) { return i == 0 ? r.slot : 2 * ((r.slot >> 1) + i); }
 
-// Partial results are handed over past the caches that the compute dies do not share: agent-scope accesses, coherent by themselves, so that no
-// fence is needed; a block counts itself in when its own have arrived.
-__device__ __forceinline__ void put_pair(float* p, float a, float b) {
-    const uint64_t v = (uint64_t)__builtin_bit_cast(uint32_t, a) | (uint64_t)__builtin_bit_cast(uint32_t, b) << 32;
-    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void get_pair(const float* p, float& a, float& b) {
-    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    a = __builtin_bit_cast(float, (uint32_t)v);
-    b = __builtin_bit_cast(float, (uint32_t)(v >> 32));
-}
-
-// Rows r0, r0 + step, ... of a pair from its parts, by a block of 256 threads: the parts' references and sums give their weights (a wave a row),
-// then a thread takes two values of a row, sixteen parts in flight.  s_weight: [rows][kMostParts], s_sum [rows].
-template <int kDim, bool kBf16, int kMostParts>
-__device__ __forceinline__ void join_parts(const PagesAttend& a, const StreamRecord& rec, const PageSeq& seq, int kernel_rows, int r0, int n_rows,
-                                           float (*s_weight)[kMostParts], float* s_top, float* s_sum) {
-    constexpr int kPitch = kDim + 4;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int x = wave; x < n_rows; x += 4) {
+// Rows r0 .. r0 + n_rows - 1 of a pair from its parts, by a block of kThreads: groups of threads that have two values of a row each share the parts,
+// sixteen in flight; meanwhile the parts' references and sums give their weights (a wave a row).
+template <int kDim, int kThreads>
+constexpr int join_lds(int rows, int parts) { return rows * (parts + 2) + 2 * (kThreads > rows * (kDim / 2) ? kThreads : rows * (kDim / 2)); }      // floats
+template <int kDim, bool kBf16, int kThreads>
+__device__ __forceinline__ void join_parts(const PagesAttend& a, const StreamRecord& rec, const PageSeq& seq, int kernel_rows, int r0, int n_rows, int tid, float* lds) {
+    constexpr int kPitch = kDim + 4, kPairs = kDim / 2, kFlight = 16;
+    const int wave = tid >> 6, lane = tid & 63;
+    float* const s_top = lds;
+    float* const s_sum = lds + n_rows;
+    float* const s_weight = lds + 2 * n_rows;               // [n_rows][parts]
+    float* const s_part = s_weight + n_rows * rec.parts;    // [groups][n_rows][kDim]
+    const int items = n_rows * kPairs, groups = max(1, kThreads / items);
+    const int group = min(tid / items, groups - 1);
+    // offsets in the area of partial results, which is far below 4 GB
+    const char* const area = reinterpret_cast<const char*>(a.partial);
+    const uint32_t slot_bytes = (uint32_t)kernel_rows * kPitch * 4u, first_at = (uint32_t)rec.slot * slot_bytes, others_at = (uint32_t)(rec.slot & ~1) * slot_bytes;
+    auto row_of_part = [&](int part, int row) { return (part == 0 ? first_at : others_at + (uint32_t)part * (2u * slot_bytes)) + (uint32_t)(r0 + row) * (kPitch * 4u); };
+    float2 v[kFlight];
+    auto ask = [&](int item, int k) {
+        const int row = item / kPairs;
+        const uint32_t in_row = 16u + (uint32_t)(item % kPairs) * 8u;
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i)
+            v[i] = *reinterpret_cast<const float2*>(area + (row_of_part(min(group + groups * (k + i), rec.parts - 1), row) + in_row));
+    };
+    const bool helps = tid < items * groups;
+    const int item0 = tid - group * items;
+    if (helps) ask(min(item0, items - 1), 0);
+    for (int x = wave; x < n_rows; x += kThreads / 64) {
         float top = -INFINITY, sum = 0.0f;
-        float m[kMostParts / 64], l[kMostParts / 64];
-#pragma unroll
-        for (int j = 0; j < kMostParts / 64; ++j) {
-            m[j] = -INFINITY;
-            l[j] = 0.0f;
-            const int i = 64 * j + lane;
-            if (i < rec.parts) get_pair(a.partial + ((size_t)slot_of_part(rec, i) * kernel_rows + r0 + x) * kPitch, m[j], l[j]);
+        for (int i = lane; i < rec.parts; i += 64) {
+            const float2 ml = *reinterpret_cast<const float2*>(area + row_of_part(i, x));
+            const float m = ml.x, l = ml.y;
+            s_weight[x * rec.parts + i] = l == 0.0f ? -INFINITY : m;
+            const float to = l == 0.0f ? top : fmaxf(top, m);
+            if (l != 0.0f) sum = (sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f(top - to)) + l * __builtin_amdgcn_exp2f(m - to);
+            top = to;
         }
+        float all = top;
 #pragma unroll
-        for (int j = 0; j < kMostParts / 64; ++j)
-            if (l[j] != 0.0f) top = fmaxf(top, m[j]);
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
-#pragma unroll
-        for (int j = 0; j < kMostParts / 64; ++j) {
-            const float w = l[j] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m[j] - top);
-            sum += l[j] == 0.0f ? 0.0f : l[j] * w;
-            s_weight[x][64 * j + lane] = w;
-        }
+        for (int off = 1; off < 64; off <<= 1) all = fmaxf(all, __shfl_xor(all, off));
+        sum = sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f(top - all);
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+        for (int i = lane; i < rec.parts; i += 64) {
+            const float m = s_weight[x * rec.parts + i];
+            s_weight[x * rec.parts + i] = m == -INFINITY && sum == sum ? 0.0f : __builtin_amdgcn_exp2f(m - all);
+        }
         if (lane == 0) {
-            s_top[x] = top;
+            s_top[x] = all;
             s_sum[x] = sum;
         }
     }
     __syncthreads();
-    for (int idx = threadIdx.x; idx < n_rows * (kDim / 2); idx += 256) {
-        const int x = idx / (kDim / 2), d = idx % (kDim / 2) * 2, r = r0 + x;
+    for (int item = item0; helps && item < items; item += kThreads) {
+        if (item != item0) ask(item, 0);
+        const float* const weight = s_weight + item / kPairs * rec.parts;
         float o0 = 0.0f, o1 = 0.0f;
-        for (int i0 = 0; i0 < rec.parts; i0 += 16) {
-            float v0[16], v1[16];
+        for (int k = 0; group + groups * k < rec.parts; k += kFlight) {
+            if (k > 0) ask(item, k);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                get_pair(a.partial + ((size_t)slot_of_part(rec, min(i0 + i, rec.parts - 1)) * kernel_rows + r) * kPitch + 4 + d, v0[i], v1[i]);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = i0 + i < rec.parts ? s_weight[x][i0 + i] : 0.0f;
-                if (w == 0.0f) continue;                    // nothing seen, or nothing left of it
-                o0 = __builtin_fmaf(v0[i], w, o0);
-                o1 = __builtin_fmaf(v1[i], w, o1);
+            for (int i = 0; i < kFlight; ++i) {
+                const int part = group + groups * (k + i);
+                const float w = part < rec.parts ? weight[part] : 0.0f;
+                const bool none = w == 0.0f;                // nothing seen, or nothing left of it
+                o0 = __builtin_fmaf(none ? 0.0f : v[i].x, w, o0);
+                o1 = __builtin_fmaf(none ? 0.0f : v[i].y, w, o1);
             }
         }
+        s_part[(group * items + item) * 2] = o0;
+        s_part[(group * items + item) * 2 + 1] = o1;
+    }
+    __syncthreads();
+    for (int item = tid; item < items; item += kThreads) {
+        float o0 = 0.0f, o1 = 0.0f;
+        for (int g = 0; g < groups; ++g) {
+            o0 += s_part[(g * items + item) * 2];
+            o1 += s_part[(g * items + item) * 2 + 1];
+        }
+        const int x = item / kPairs, d = item % kPairs * 2, r = r0 + x;
         const int token = r / a.group, h = rec.head * a.group + (r - token * a.group);
         const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
         const RowEnd e = row_end(s_top[x], s_sum[x], a, row);
@@ -236,49 +252,89 @@ __device__ __forceinline__ void join_parts(const PagesAttend& a, const StreamRec
     }
 }
 
-// kMerged: the last block of a pair to finish joins its parts; else a launch of its own does (k_pages_stream_merge)
-template <int kStore, int kDim, bool kBf16, int kSets, bool kMerged>
-__global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(stream_occupancy(kSets), stream_occupancy(kSets)))) void k_pages_stream(
-    PagesAttend a, int rows_max, int min_tiles) {
+// The kernel's last struct argument once more, for the end of a segment: what is only needed there is not to take registers before
+// (kStreamArgsAt bytes of leading arguments; alignment 8)
+constexpr int kStreamArgsAt = 3 * 8 + 10 * 4;
+static_assert(kStreamArgsAt % alignof(PagesAttend) == 0, "where the struct lies");
+__device__ __forceinline__ PagesAttend late_arguments() {
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef const __attribute__((address_space(4))) char* Constant;
+    Constant p = (Constant)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const __attribute__((address_space(4))) PagesAttend*)(p + kStreamArgsAt);
+#else
+    return {};                              // the host's pass over this file
+#endif
+}
+
+// What a block works on.
+//   pairs: grid (K/V heads, sequences), a block the one pair; for short sequences, where parts and their joining would cost more than they bring
+//   stretches: of all tiles; a launch of its own joins the parts of cut pairs (k_pages_stream_merge)
+enum class StreamMode { pairs, stretches };
+
+// The leading arguments come in registers: what the first loads depend on.
+template <int kStore, int kDim, bool kBf16, int kSets, StreamMode kMode>
+__global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_pages_stream(
+    const int32_t* __restrict__ starts, const int32_t* __restrict__ lengths, const int32_t* __restrict__ tables, int n_seqs, int width, int n_tokens, int max_q,
+    int max_kv, int blocks_log2, int window, int sinks, int group, int n_kv, PagesAttend a, int rows_max, int min_tiles) {
     constexpr int kRows = 16 * kSets, kSteps = kDim / 32, kFs = kDim / 16, kPitch = kDim + 4;
+    constexpr bool kStretches = kMode != StreamMode::pairs;
     __shared__ __align__(16) float s_acc[kStreamWaves][kRows][kPitch];
     __shared__ float s_m[kStreamWaves][kRows], s_l[kStreamWaves][kRows];
-    __shared__ int s_last;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 15, hh = lane >> 4;
-    const int n_kv = a.geom.n_kv, group = a.group;
-
-    // ---- the block's stretch: every wave finds it by itself, a sequence a lane
-    bool bad = false;
-    auto lane_seq = [&](int s) -> PageSeq {
-        PageSeq q = {0, 0, 0};
-        if (s >= a.seqs.n_seqs) return q;
-        bool fits;
-        q = read_seq(a.seqs, a.geom, s, fits);
-        bad |= !fits;
-        return q;
+    const int page_tokens = kBlockTokens << blocks_log2;
+    const int64_t in_table = (int64_t)width * page_tokens, room = in_table < max_kv ? in_table : max_kv;
+    auto read = [&](int s, bool& fits) -> PageSeq {
+        const int first = starts[s], next = starts[s + 1], len = lengths[s];
+        fits = page_seq_holds(first, next, len, n_tokens, max_q, room);
+        return {first, fits ? next - first : 0, len};
     };
-    auto tiles_of = [&](const PageSeq& q) { return in_stream(q, group, rows_max) ? view_of<kTileTokens>(q.len - q.n, q.len - 1, a.window, a.sinks).tiles : 0; };
-    const PageSeq first_mine = lane_seq(lane);
-    const int first_tiles = tiles_of(first_mine);
-    int own = first_tiles;
-#pragma unroll 4
-    for (int s = 64 + lane; s < a.seqs.n_seqs; s += 64) own += tiles_of(lane_seq(s));
-    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane(wave_scan(own), 63) * (uint32_t)n_kv;
-    if (bad && blockIdx.x == 0 && wave == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
-    const uint32_t blocks = max(1u, min(gridDim.x, total / (uint32_t)min_tiles));
-    StreamRecord* records = reinterpret_cast<StreamRecord*>(a.records);
-    StreamRecord record = {0, 0, 0, 0};
-    if (blockIdx.x >= blocks || total == 0) {
-        if (!kMerged && threadIdx.x == 0) records[blockIdx.x] = record;
-        return;
-    }
-    const Stretches cut(total, blocks);
-    uint32_t at = __builtin_amdgcn_readfirstlane(cut.start(blockIdx.x));
-    const uint32_t end = __builtin_amdgcn_readfirstlane(cut.start(blockIdx.x + 1));
-    int s = 0;
+    auto view_of_seq = [&](const PageSeq& q) { return view_of<kTileTokens>(q.len - q.n, q.len - 1, window, sinks); };
+    // the pages from `page0` on, one a lane
+    int page0 = 0, page_of_lane = -1;
+
+    int s, head, done = 0;                  // done: tiles of the pair before the block's
     PageSeq seq = {0, 0, 0};
-    uint32_t before = 0;                    // tiles a head of the sequences before it
-    {
+    uint32_t at = 0, end = 0, total = 0, blocks = 1;
+    StreamRecord record = {0, 0, 0, 0};
+    if constexpr (!kStretches) {
+        head = blockIdx.x;
+        s = blockIdx.y;
+        if (width > 0) page_of_lane = tables[(int64_t)s * width + min(lane, width - 1)];      // on their way with the lengths
+        bool fits;
+        seq = read(s, fits);
+        if (!fits && head == 0 && threadIdx.x == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
+        if (!in_stream(seq, group, rows_max)) return;
+        end = (uint32_t)view_of_seq(seq).tiles;
+    } else {
+        // the block's stretch: every wave finds it by itself, a sequence a lane
+        page0 = -64;
+        bool bad = false;
+        auto lane_seq = [&](int i) -> PageSeq {
+            PageSeq q = {0, 0, 0};
+            if (i >= n_seqs) return q;
+            bool fits;
+            q = read(i, fits);
+            bad |= !fits;
+            return q;
+        };
+        auto tiles_of = [&](const PageSeq& q) { return in_stream(q, group, rows_max) ? view_of_seq(q).tiles : 0; };
+        const PageSeq first_mine = lane_seq(lane);
+        const int first_tiles = tiles_of(first_mine);
+        int own = first_tiles;
+#pragma unroll 4
+        for (int i = 64 + lane; i < n_seqs; i += 64) own += tiles_of(lane_seq(i));
+        total = (uint32_t)__builtin_amdgcn_readlane(wave_scan(own), 63) * (uint32_t)n_kv;
+        if (bad && blockIdx.x == 0 && wave == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
+        blocks = max(1u, min(gridDim.x, total / (uint32_t)min_tiles));
+        if (blockIdx.x >= blocks || total == 0) {
+            if (threadIdx.x == 0) reinterpret_cast<StreamRecord*>(late_arguments().records)[blockIdx.x] = record;
+            return;
+        }
+        const Stretches cut(total, blocks);
+        at = __builtin_amdgcn_readfirstlane(cut.start(blockIdx.x));
+        end = __builtin_amdgcn_readfirstlane(cut.start(blockIdx.x + 1));
+        uint32_t before = 0;                // tiles a head of the sequences before it
         PageSeq q = first_mine;
         int t = first_tiles;
         for (int base = 0;;) {
@@ -293,26 +349,31 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
             }
             before += (uint32_t)__builtin_amdgcn_readlane(upto, 63);
             base += 64;
-            if (base >= a.seqs.n_seqs) return;              // the batch changed while it was read
+            if (base >= n_seqs) return;                     // the batch changed while it was read
             q = lane_seq(base + lane);
             t = tiles_of(q);
         }
+        const int tiles = view_of_seq(seq).tiles;
+        head = (int)((at - before * (uint32_t)n_kv) / (uint32_t)tiles);
+        done = (int)(at - before * (uint32_t)n_kv) - head * tiles;
     }
-    View view = view_of<kTileTokens>(seq.len - seq.n, seq.len - 1, a.window, a.sinks);
-    int head = __builtin_amdgcn_readfirstlane((int)((at - before * (uint32_t)n_kv) / (uint32_t)view.tiles));
-    int done = (int)(at - before * (uint32_t)n_kv) - head * view.tiles;         // tiles of the pair before the block's
 
     bool first_segment = true;
-    while (at < end) {
+    for (;;) {
+        // the same for all lanes, and to be in scalar registers
+        at = __builtin_amdgcn_readfirstlane(at);
+        done = __builtin_amdgcn_readfirstlane(done);
+        s = __builtin_amdgcn_readfirstlane(s);
+        head = __builtin_amdgcn_readfirstlane(head);
+        seq = {__builtin_amdgcn_readfirstlane(seq.first), __builtin_amdgcn_readfirstlane(seq.n), __builtin_amdgcn_readfirstlane(seq.len)};
+        if (at >= end) break;
+        const View view = view_of_seq(seq);
         const int todo = min(view.tiles - done, (int)(end - at));
         const int rows = seq.n * group;
-        const int32_t* table = a.seqs.table + (int64_t)s * a.seqs.width;
-        const int pages = (seq.len + (kBlockTokens << a.geom.blocks_log2) - 1) / (kBlockTokens << a.geom.blocks_log2);
+        const int32_t* table = tables + (int64_t)s * width;
+        const int pages = (seq.len + page_tokens - 1) >> (blocks_log2 + 4);
         const char* const heads = a.geom.pool + (uint64_t)head * a.geom.head_bytes;
-        const uint32_t block_bytes = a.geom.head_bytes >> a.geom.blocks_log2;
-
-        // the pages from `page0` on, one a lane
-        int page0 = -64, page_of_lane = -1;
+        constexpr uint32_t block_bytes = block_layout(kStore, kDim).bytes;
         struct Tile {
             const char* b[2];
             int live[2];                     // tokens of the block that a row may see: none of a page that is none
@@ -322,7 +383,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
             const int tile = tile_at(view, i);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int block = 2 * tile + j, index = block >> a.geom.blocks_log2;
+                const int block = 2 * tile + j, index = block >> blocks_log2;
                 if ((unsigned)(index - page0) >= 64u) {
                     page0 = index;
                     page_of_lane = index + lane < pages ? table[index + lane] : -1;
@@ -330,12 +391,14 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
                 }
                 int page = __builtin_amdgcn_readlane(page_of_lane, index - page0);
                 t.live[j] = min(kBlockTokens, seq.len - block * kBlockTokens);
-                if ((unsigned)page >= (unsigned)a.geom.n_pages) {
-                    if (t.live[j] > 0 && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
+                if (t.live[j] <= 0) {
+                    page = 0;                // behind the sequence's end
+                } else if ((unsigned)page >= (unsigned)a.geom.n_pages) {
+                    if (lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
                     t.live[j] = 0;
                     page = 0;
                 }
-                t.b[j] = heads + (uint64_t)page * a.geom.page_bytes + (uint32_t)(block & ((1 << a.geom.blocks_log2) - 1)) * block_bytes;
+                t.b[j] = heads + (uint64_t)page * a.geom.page_bytes + (uint32_t)(block & ((1 << blocks_log2) - 1)) * block_bytes;
             }
             return t;
         };
@@ -353,7 +416,9 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
         int pos[kSets];
 #pragma unroll
         for (int c = 0; c < kSets; ++c) {
-            const int r = 16 * c + col, token = r / group, g = r - token * group;
+            int r = 16 * c + col;
+            if constexpr (kStretches) asm volatile("" : "+v"(r));       // not worked out before the loop over segments, which would take registers
+            const int token = r / group, g = r - token * group;
             pos[c] = r < rows ? view.first + token : -1;
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
@@ -397,7 +462,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
             stream_load_k<kStore, kDim>(next.b[0], next.b[1], lane, raw);
             // lane (row col, hh): tokens 8 (hh % 2) + 4 (hh / 2) .. + 3 of each block
             const int t0 = j0 + 8 * (hh & 1) + 4 * (hh >> 1);
-            const bool masked = now.live[0] < kBlockTokens || now.live[1] < kBlockTokens || partly_hidden(view, a.window, a.sinks, j0, kTileTokens);
+            const bool masked = now.live[0] < kBlockTokens || now.live[1] < kBlockTokens || partly_hidden(view, window, sinks, j0, kTileTokens);
             if (masked) {
 #pragma unroll
                 for (int c = 0; c < kSets; ++c)
@@ -405,7 +470,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (now.live[j] <= 0 || !sees(pos[c], t0 + 16 * j + r, a.window, a.sinks)) s2[c][j][r] = -INFINITY;
+                            if (now.live[j] <= 0 || !sees(pos[c], t0 + 16 * j + r, window, sinks)) s2[c][j][r] = -INFINITY;
             }
             u32x4 p[kSets];
 #pragma unroll
@@ -461,8 +526,8 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const int j = j0 + 16 * (hh >> 1) + 8 * (hh & 1) + 2 * e;
-                                seen[c][e] = (2 * e < live && sees(pos[c], j, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne : 0u) |
-                                             (2 * e + 1 < live && sees(pos[c], j + 1, a.window, a.sinks) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
+                                seen[c][e] = (2 * e < live && sees(pos[c], j, window, sinks) ? (uint32_t)Num<kBf16>::kOne : 0u) |
+                                             (2 * e + 1 < live && sees(pos[c], j + 1, window, sinks) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
                             }
                         // through the wave's part of LDS, one product at a time: this path is not to cost registers
                         u32x4* const mine = reinterpret_cast<u32x4*>(&s_acc[wave][0][0]) + lane;
@@ -501,9 +566,12 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
         }
 
         // ---- the waves meet
+        // (from here on with a thread number that the compiler does not know: it would work out all of this before the loop and have no registers for it)
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
 #pragma unroll
         for (int c = 0; c < kSets; ++c) {
-            const int r = 16 * c + col;
+            const int r = 16 * c + (tid & 15);
             const float sum = sum_over_quarters(l[c]);
             if (r >= rows) continue;
             if constexpr (kStore == SALI_STORE_16)
@@ -512,19 +580,20 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
                     for (int f = 0; f < kFs; ++f)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[c][f][e] += found((up[c] >> (4 * f + e) & 1) != 0, (down[c] >> (4 * f + e) & 1) != 0);
-            if (hh == 0) {
+            if ((tid >> 4 & 3) == 0) {
                 s_m[wave][r] = m[c];
                 s_l[wave][r] = sum;
             }
 #pragma unroll
             for (int f = 0; f < kFs; ++f)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s_acc[wave][r][stream_v_value<kStore>(f, 4 * hh + e)] = acc[c][f][e];
+                for (int e = 0; e < 4; ++e) s_acc[wave][r][stream_v_value<kStore>(f, 4 * (tid >> 4 & 3) + e)] = acc[c][f][e];
         }
         __syncthreads();
+        const PagesAttend b = late_arguments();
         const bool whole = todo == view.tiles;
         const int slot = 2 * (int)blockIdx.x + (first_segment ? 0 : 1);
-        for (int idx = threadIdx.x; idx < rows * (kDim / 4); idx += 64 * kStreamWaves) {
+        for (int idx = tid; idx < rows * (kDim / 4); idx += 64 * kStreamWaves) {
             const int r = idx / (kDim / 4), d = idx % (kDim / 4) * 4;
             float top = -INFINITY;
 #pragma unroll
@@ -539,40 +608,27 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
                 sum += s_l[w][r] * by;
                 o += *reinterpret_cast<const f32x4*>(&s_acc[w][r][d]) * by;
             }
-            if (!whole) {
-                float* part = a.partial + ((size_t)slot * kRows + r) * kPitch;
-                put_pair(part + 4 + d, o[0], o[1]);
-                put_pair(part + 6 + d, o[2], o[3]);
-                if (d == 0) put_pair(part, top, sum);
+            if (kStretches && !whole) {
+                float* part = b.partial + ((size_t)slot * kRows + r) * kPitch;
+                *reinterpret_cast<f32x4*>(part + 4 + d) = o;
+                if (d == 0) *reinterpret_cast<float2*>(part) = make_float2(top, sum);
                 continue;
             }
             const int token = r / group, h = head * group + (r - token * group);
-            const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
-            const RowEnd e = row_end(top, sum, a, row);
+            const int64_t row = (int64_t)(seq.first + token) * b.heads + h;
+            const RowEnd e = row_end(top, sum, b, row);
             f32x4 pr = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (a.prior != nullptr) pr = *reinterpret_cast<const f32x4*>(a.prior + row * kDim + d);
+            if (b.prior != nullptr) pr = *reinterpret_cast<const f32x4*>(b.prior + row * kDim + d);
             const u32x2 v = {pack2<kBf16>(joined(e, o[0], pr[0]), joined(e, o[1], pr[1])), pack2<kBf16>(joined(e, o[2], pr[2]), joined(e, o[3], pr[3]))};
-            *reinterpret_cast<u32x2*>(a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes + 2 * d) = v;
-            if (d == 0 && a.lse != nullptr) a.lse[row] = e.lse;
+            *reinterpret_cast<u32x2*>(b.out.d + (int64_t)(seq.first + token) * b.out.token_bytes + (int64_t)h * b.out.head_bytes + 2 * d) = v;
+            if (d == 0 && b.lse != nullptr) b.lse[row] = e.lse;
         }
-        if (!whole) {
-            // the pair's first part is in the block whose stretch has its first tile; that is its last segment, and its only one if it starts there
-            const uint32_t pair0 = at - (uint32_t)done, b0 = __builtin_amdgcn_readfirstlane(cut.of(pair0)), b1 = __builtin_amdgcn_readfirstlane(cut.of(pair0 + (uint32_t)view.tiles - 1u));
-            const StreamRecord pair = {s, head, (int)(2 * b0 + (cut.start(b0) == pair0 ? 0u : 1u)), (int)(b1 - b0) + 1};
-            if constexpr (kMerged) {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // every wave: its parts have arrived
-                __syncthreads();
-                if (threadIdx.x == 0)
-                    s_last = last_arrival(atomicInc(a.arrived + (size_t)b0 * kMergeParts + (pair.parts - 1), (uint32_t)pair.parts - 1u), pair.parts) ? 1 : 0;
-                __syncthreads();
-                if (s_last != 0) {
-                    static_assert(sizeof(float[kRows][kMergeParts]) <= sizeof(s_acc), "the weights of the parts");
-                    join_parts<kDim, kBf16, kMergeParts>(a, pair, seq, kRows, 0, rows, reinterpret_cast<float(*)[kMergeParts]>(&s_acc[0][0][0]), s_m[0], s_l[0]);
-                }
-            } else if (done == 0) {
-                record = pair;
-            }
+        if (kStretches && !whole && done == 0) {
+            // the pair's first part, in the block's last segment; the following blocks have the others
+            const Stretches cut(total, blocks);
+            record = {s, head, slot, (int)(cut.of(at + (uint32_t)view.tiles - 1u) - blockIdx.x) + 1};
         }
+        if constexpr (!kStretches) return;
         __syncthreads();
 
         at += todo;
@@ -582,29 +638,30 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
             done = 0;
             if (++head == n_kv) {
                 head = 0;
+                bool fits;
                 do {
-                    if (++s >= a.seqs.n_seqs) break;
-                    seq = load_seq(a.seqs, a.geom, s, false);
+                    if (++s >= n_seqs) break;
+                    seq = read(s, fits);
                 } while (!in_stream(seq, group, rows_max));
-                if (s >= a.seqs.n_seqs) break;
-                view = view_of<kTileTokens>(seq.len - seq.n, seq.len - 1, a.window, a.sinks);
+                if (s >= n_seqs) break;
+                page0 = -64;
             }
         }
     }
-    if (!kMerged && threadIdx.x == 0) records[blockIdx.x] = record;
+    if (threadIdx.x == 0) reinterpret_cast<StreamRecord*>(late_arguments().records)[blockIdx.x] = record;
 }
 
 // Joins the parts of the pairs, four rows a block: grid (blocks of the stream, rows / 4)
 template <int kDim, bool kBf16>
 __global__ __launch_bounds__(256) void k_pages_stream_merge(PagesAttend a, int kernel_rows) {
-    __shared__ float s_weight[4][kStreamMostBlocks], s_top[4], s_sum[4];
+    __shared__ float s_join[join_lds<kDim, 256>(4, kStreamMostBlocks)];
     const StreamRecord rec = reinterpret_cast<const StreamRecord*>(a.records)[blockIdx.x];
     if (rec.parts == 0) return;
     bool fits;
     const PageSeq seq = read_seq(a.seqs, a.geom, rec.seq, fits);
     const int r0 = 4 * (int)blockIdx.y;
     if (r0 >= seq.n * a.group) return;
-    join_parts<kDim, kBf16, kStreamMostBlocks>(a, rec, seq, kernel_rows, r0, min(4, seq.n * a.group - r0), s_weight, s_top, s_sum);
+    join_parts<kDim, kBf16, 256>(a, rec, seq, kernel_rows, r0, min(4, seq.n * a.group - r0), threadIdx.x, s_join);
 }
 
 }  // namespace

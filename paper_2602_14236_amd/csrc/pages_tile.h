@@ -244,7 +244,7 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 template <int kStore, int kDim, bool kBf16>
-__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(3, 3))) void k_pages_tile(PagesAttend a) {
+__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(kStore == SALI_STORE_INT4 ? 2 : 3, 3))) void k_pages_tile(PagesAttend a) {
     constexpr int kSteps = kDim / 16, kDt = kDim / 32, kPitch = kDim + 4;
     constexpr int kBlock = 32 * kDim;                       // bytes of a block's K or V in LDS
     __shared__ __align__(16) uint8_t s_k[2][2 * kBlock], s_v[2][2 * kBlock];
@@ -253,6 +253,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     // share whether there are any
     __shared__ uint8_t s_up[2][kStore == SALI_STORE_16 ? kTileWaves : 1][kDim], s_down[2][kStore == SALI_STORE_16 ? kTileWaves : 1][kDim];
     __shared__ int s_odd[2][kTileWaves];
+    __shared__ uint64_t s_found[2][kStore == SALI_STORE_16 ? 64 * kTileWaves : 1];
     const TileScratch t = tile_scratch(a.records, a.geom.n_kv);
     const int n_kv = a.geom.n_kv;
     const int nth = (int)(blockIdx.x / (uint32_t)n_kv), head = (int)blockIdx.x - nth * n_kv;
@@ -271,10 +272,11 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     typedef TileRaw<kStore, kDim> Raw;
     Raw raw;
     auto block_of = [&](int i) { return 2 * tile_at(view, i) + (wave >> 1); };
-    // the pages from `page0` on, one a lane: where this head's part of them lies, and which are none
+    // the pages from `page0` on, one a lane: their numbers, and which are none
     const int pages = (seq.len + (kBlockTokens << a.geom.blocks_log2) - 1) / (kBlockTokens << a.geom.blocks_log2);
     int page0 = -64;
-    uint64_t at_page = 0, no_page = 0;
+    int page_of_lane = 0;
+    uint64_t no_page = 0;
     struct Source {
         const char* block;
         int live;
@@ -286,12 +288,11 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
             int page = index + lane < pages ? table[index + lane] : -1;
             const bool none = (unsigned)page >= (unsigned)a.geom.n_pages;
             no_page = __builtin_amdgcn_ballot_w64(none);
-            at_page = (uint64_t)(none ? 0 : page) * a.geom.page_bytes;
-            asm volatile("" : "+v"(at_page));               // waited for here: a wait behind the branch would be one for K and V too
+            page_of_lane = none ? 0 : page;
+            asm volatile("" : "+v"(page_of_lane));          // waited for here: a wait behind the branch would be one for K and V too
         }
         const int nth_page = index - page0;
-        const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at_page, nth_page) |
-                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(at_page >> 32), nth_page) << 32;
+        const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(page_of_lane, nth_page) * a.geom.page_bytes;
         Source s;
         s.live = max(0, min(kBlockTokens, seq.len - block * kBlockTokens));
         if ((no_page >> nth_page & 1) != 0) {
@@ -375,7 +376,8 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     for (int d = 0; d < kDt; ++d)
 #pragma unroll
         for (int x = 0; x < 16; ++x) acc[d][x] = 0.0f;
-    uint64_t up = 0, down = 0;                              // a bit for every value of acc: values that are not finite
+    // a bit for every value of acc: infinities found, of either sign (in LDS, since there are hardly ever any)
+    if constexpr (kStore == SALI_STORE_16) s_found[0][threadIdx.x] = s_found[1][threadIdx.x] = 0;
 
     auto step = [&](int tile0, int buf) {
         const uint8_t* const k = s_k[buf] + (col >> 4) * kBlock + (hh * 16 + (col & 15)) * 16;
@@ -425,6 +427,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         if constexpr (kStore == SALI_STORE_16) {
             const int there = s_odd[buf][lane % kTileWaves];
             if (__builtin_amdgcn_ballot_w64(there != 0) == 0) return;
+            uint64_t up = 0, down = 0;
 #pragma unroll 1
             for (int w = 0; w < kTileWaves; ++w) {
                 if (s_odd[buf][w] == 0) continue;
@@ -438,6 +441,8 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
                     down |= (uint64_t)((s_down[buf][w][d] & seen) != 0) << x;
                 }
             }
+            s_found[0][threadIdx.x] |= up;
+            s_found[1][threadIdx.x] |= down;
         }
     };
 
@@ -465,16 +470,24 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 
     // ---- results: lane (row col, hh) has values 32 d + 8 k + 4 hh .. + 3
     const float sum = sum_over_halves(l);
-    if (r >= rows) return;
-    if constexpr (kStore == SALI_STORE_16)
+    // (worked out again, with a lane number that the compiler does not know: through the loop it has no registers for it)
+    int there = lane;
+    asm volatile("" : "+v"(there));
+    const int end_col = there & 31, end_hh = there >> 5;
+    const int64_t end_r = row0 + end_col;
+    if (end_r >= rows) return;
+    const int end_token = (int)(end_r / group), end_of_group = (int)(end_r - (int64_t)end_token * group);
+    if constexpr (kStore == SALI_STORE_16) {
+        const uint64_t up = s_found[0][threadIdx.x], down = s_found[1][threadIdx.x];
         if ((up | down) != 0)
 #pragma unroll
             for (int d = 0; d < kDt; ++d)
 #pragma unroll
                 for (int x = 0; x < 16; ++x) acc[d][x] += found((up >> (16 * d + x) & 1) != 0, (down >> (16 * d + x) & 1) != 0);
+    }
     if (unit.part >= 0) {
-        float* part = a.partial + (((size_t)unit.part * n_kv + head) * kTileRows + (size_t)(wave * 32 + col)) * kPitch;
-        if (hh == 0) {
+        float* part = a.partial + (((size_t)unit.part * n_kv + head) * kTileRows + (size_t)(wave * 32 + end_col)) * kPitch;
+        if (end_hh == 0) {
             part[0] = m;
             part[1] = sum;
         }
@@ -482,26 +495,26 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         for (int d = 0; d < kDt; ++d)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                *reinterpret_cast<f32x4*>(part + 4 + 32 * d + 8 * k + 4 * hh) = (f32x4){acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
+                *reinterpret_cast<f32x4*>(part + 4 + 32 * d + 8 * k + 4 * end_hh) = (f32x4){acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
         return;
     }
-    const int h = head * group + of_group;
-    const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
+    const int h = head * group + end_of_group;
+    const int64_t row = (int64_t)(seq.first + end_token) * a.heads + h;
     const RowEnd e = row_end(m, sum, a, row);
-    char* const out = a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes;
+    char* const out = a.out.d + (int64_t)(seq.first + end_token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes;
 #pragma unroll
     for (int d = 0; d < kDt; ++d)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             f32x4 pr = {0.0f, 0.0f, 0.0f, 0.0f};
-            const int at = 32 * d + 8 * k + 4 * hh;
+            const int at = 32 * d + 8 * k + 4 * end_hh;
             if (a.prior != nullptr) pr = *reinterpret_cast<const f32x4*>(a.prior + row * kDim + at);
             float o[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) o[x] = joined(e, acc[d][4 * k + x], pr[x]);
             *reinterpret_cast<u32x2*>(out + 2 * at) = (u32x2){pack2<kBf16>(o[0], o[1]), pack2<kBf16>(o[2], o[3])};
         }
-    if (hh == 0 && a.lse != nullptr) a.lse[row] = e.lse;
+    if (end_hh == 0 && a.lse != nullptr) a.lse[row] = e.lse;
 }
 
 // Joins the parts of cut units: grid (merges * n_kv at most, kTileRows / 8), a row per 32 lanes

@@ -132,12 +132,6 @@ int main() {
             const uint32_t b = rand() %% blocks, lo = cut.start(b), hi = cut.start(b + 1);
             if (lo >= hi || cut.of(lo) != b || cut.of(hi - 1) != b) return 2;
         }
-        const uint32_t n_kv = rand() %% 40 + 1, per_head = total / n_kv;
-        if (per_head * n_kv / kStreamMinTiles >= blocks) {
-            const Stretches all(per_head * n_kv, blocks);
-            const uint32_t head = rand() %% n_kv;
-            if (all.of(per_head * (head + 1) - 1) - all.of(per_head * head) + 1 > (uint32_t)parts_of_pair(blocks, n_kv)) return 5;
-        }
     }
     for (int round = 0; round < 3000; ++round) {
         const int n_kv = rand() %% 3 ? 1 << rand() %% 7 : rand() %% 300 + 1, units = rand() %% 400 + 1;

@@ -74,3 +74,11 @@ def test_pages_are_on_the_gpu():
     from paper_2602_14236_amd import binding
     with pytest.raises(ValueError):
         binding.SaliPages(config(), "cpu")
+
+
+def test_reports_of_spilled_registers_are_read():
+    from paper_2602_14236_amd import build
+    line = "a.hip:1:1: remark: {} [-Rpass-analysis=kernel-resource-usage]"
+    report = "\n".join(line.format(x) for x in ("Function Name: good", "    SGPRs Spill: 3", "    VGPRs Spill: 0", "Function Name: bad",
+                                                "    SGPRs Spill: 0", "    VGPRs Spill: 12"))
+    assert build.spilled(report) == ["bad"]
