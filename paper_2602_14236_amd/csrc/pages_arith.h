@@ -76,7 +76,7 @@ struct Stretches {
         return tile < in_longer ? tile / (each + 1) : longer + (tile - in_longer) / each;
     }
 };
-constexpr int kStreamMinTiles = 8;          // of a stretch
+constexpr int kStreamMinTiles = 4;          // of a stretch
 constexpr int kTileRows = 128;              // rows of a block of the tile kernel
 constexpr int kTileKeys = 32;               // keys of its steps
 constexpr int kTileShares = 512;            // fair shares that the whole work is cut into

@@ -113,19 +113,36 @@ __device__ __forceinline__ u32x4 values4(uint32_t a, uint32_t b, float scale, fl
     r.w = pack2_after_f32<kBf16>(__builtin_fmaf(code4(b, 2), scale, low), __builtin_fmaf(code4(b, 3), scale, low));
     return r;
 }
-// 8 tokens' codes of one value (V)
+// 8 tokens' codes of one value (V).  The 16 lanes of a row take values of one group, so lane i of them brings the scale (and smallest value) of token
+// i % 8 and the others take it from there, as an operand.
+template <int kLane>
+__device__ __forceinline__ float from_row(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x150 + kLane, 0xF, 0xF, true));        // row_newbcast
+}
+template <bool kBf16>
+__device__ __forceinline__ u32x4 row_values8(uint32_t a, uint32_t b, float s) {
+    asm("" : "+v"(s));         // used once a lane each, so that it is an operand and not a move
+    u32x4 r;
+    r.x = pack2_after_f32<kBf16>(code8(a, 0) * from_row<0>(s), code8(a, 1) * from_row<1>(s));
+    r.y = pack2_after_f32<kBf16>(code8(a, 2) * from_row<2>(s), code8(a, 3) * from_row<3>(s));
+    r.z = pack2_after_f32<kBf16>(code8(b, 0) * from_row<4>(s), code8(b, 1) * from_row<5>(s));
+    r.w = pack2_after_f32<kBf16>(code8(b, 2) * from_row<6>(s), code8(b, 3) * from_row<7>(s));
+    return r;
+}
+template <bool kBf16>
+__device__ __forceinline__ u32x4 row_values4(uint32_t a, uint32_t b, float s, float z) {
+    asm("" : "+v"(s));
+    u32x4 r;
+    r.x = pack2_after_f32<kBf16>(__builtin_fmaf(code4(a, 0), from_row<0>(s), from_row<0>(z)), __builtin_fmaf(code4(a, 1), from_row<1>(s), from_row<1>(z)));
+    r.y = pack2_after_f32<kBf16>(__builtin_fmaf(code4(a, 2), from_row<2>(s), from_row<2>(z)), __builtin_fmaf(code4(a, 3), from_row<3>(s), from_row<3>(z)));
+    r.z = pack2_after_f32<kBf16>(__builtin_fmaf(code4(b, 0), from_row<4>(s), from_row<4>(z)), __builtin_fmaf(code4(b, 1), from_row<5>(s), from_row<5>(z)));
+    r.w = pack2_after_f32<kBf16>(__builtin_fmaf(code4(b, 2), from_row<6>(s), from_row<6>(z)), __builtin_fmaf(code4(b, 3), from_row<7>(s), from_row<7>(z)));
+    return r;
+}
+// the same where a lane has all of them
 struct Scales8 {
     f32x4 a, b;
 };
-template <bool kBf16>
-__device__ __forceinline__ u32x4 values8(uint32_t a, uint32_t b, const Scales8& s) {
-    u32x4 r;
-    r.x = pack2_after_f32<kBf16>(code8(a, 0) * s.a[0], code8(a, 1) * s.a[1]);
-    r.y = pack2_after_f32<kBf16>(code8(a, 2) * s.a[2], code8(a, 3) * s.a[3]);
-    r.z = pack2_after_f32<kBf16>(code8(b, 0) * s.b[0], code8(b, 1) * s.b[1]);
-    r.w = pack2_after_f32<kBf16>(code8(b, 2) * s.b[2], code8(b, 3) * s.b[3]);
-    return r;
-}
 template <bool kBf16>
 __device__ __forceinline__ u32x4 values4(uint32_t a, uint32_t b, const Scales8& s, const u32x4& z) {
     u32x4 r;

@@ -22,16 +22,16 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
         auto go = [&](auto sets) {
             constexpr int kSets = decltype(sets)::value;
             auto launch = [&](auto mode, dim3 grid) {
-                hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, decltype(mode)::value>), grid, dim3(64 * kStreamWaves), 0, s, q.start, q.length,
+                hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, decltype(mode)::value>), grid, dim3(64 * stream_waves(decltype(mode)::value)), 0, s, q.start, q.length,
                                    q.table, q.n_seqs, q.width, q.n_tokens, q.max_q, q.max_kv, a.geom.blocks_log2, a.window, a.sinks, group, n_kv, a,
                                    stream_rows, kStreamMinTiles);
             };
             const int64_t pairs = (int64_t)q.n_seqs * n_kv, tiles_a_pair = tiles / pairs;
-            if (tiles_a_pair <= 4 * kStreamWaves && pairs <= kStreamMostBlocks) {
+            if (tiles_a_pair <= 4 * stream_waves(StreamMode::pairs) && pairs <= kComputeUnits) {
                 launch(std::integral_constant<StreamMode, StreamMode::pairs>{}, dim3(n_kv, q.n_seqs));
                 return;
             }
-            const int blocks = (int)max((int64_t)1, min((int64_t)kStreamMostBlocks, (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
+            const int blocks = (int)max((int64_t)1, min((int64_t)kComputeUnits * stream_occupancy(kStore, kSets, StreamMode::stretches), (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
             const int rows = (int)min((int64_t)stream_rows, most_rows);
             launch(std::integral_constant<StreamMode, StreamMode::stretches>{}, dim3(blocks));
             hipLaunchKernelGGL((k_pages_stream_merge<kDim, kBf16>), dim3(blocks, (rows + 3) / 4), dim3(256), 0, s, a, 16 * kSets);

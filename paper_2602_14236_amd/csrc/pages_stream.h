@@ -16,8 +16,8 @@ namespace sali {
 
 namespace {
 
-constexpr int kStreamWaves = 8;             // of a block, which has a compute unit to itself: their registers leave room for two a SIMD
-constexpr int kStreamMostBlocks = 256;      // compute units
+constexpr int kComputeUnits = 256;
+constexpr int kStreamMostBlocks = 3 * kComputeUnits;
 
 // A tile of 32 tokens as it lies in memory, a lane's share.  i = lane % 16, hh = lane / 16.
 //   K as the A operand, 16 places of a block in rows: lane (place i, hh) has 8 values of its token a step
@@ -32,7 +32,7 @@ template <int kDim>
 struct StreamRaw<SALI_STORE_INT8, kDim> {
     u32x4 k[2][kDim / 64], v[kDim / 32];
     float ks[2][kDim / 64];
-    Scales8 vs[kDim / 32];
+    float vs[kDim / 32];
 };
 template <int kDim>
 struct StreamRaw<SALI_STORE_INT4, kDim> {
@@ -40,8 +40,8 @@ struct StreamRaw<SALI_STORE_INT4, kDim> {
     u32x2 v[kDim / 32];
     float ks[2];
     uint16_t kz[2];
-    Scales8 vs[kDim / 32];
-    u32x4 vz[kDim / 32];
+    float vs[kDim / 32];
+    uint16_t vz[kDim / 32];
 };
 
 __device__ __forceinline__ u32x4 stream16(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4*>(p)); }
@@ -87,9 +87,9 @@ __device__ __forceinline__ void stream_load_v(const char* b0, const char* b1, in
         for (int g = 0; g < kDim / 32; ++g) {
             if constexpr (kStore == SALI_STORE_INT8) r.v[g] = stream16(b + kAt.v + (a * kDim + 32 * g + 2 * i) * 8);
             else r.v[g] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(b + kAt.v + ((a * (kDim / 32) + g) * 16 + i) * 8));
-            const f32x4* s = reinterpret_cast<const f32x4*>(b + kAt.vs + (g * 16 + 8 * a) * 4);
-            r.vs[g] = {s[0], s[1]};
-            if constexpr (kStore == SALI_STORE_INT4) r.vz[g] = load16(b + kAt.vz + (g * 16 + 8 * a) * 2);
+            const uint32_t token = g * 16 + 8 * a + (i & 7);
+            r.vs[g] = *reinterpret_cast<const float*>(b + kAt.vs + token * 4);
+            if constexpr (kStore == SALI_STORE_INT4) r.vz[g] = *reinterpret_cast<const uint16_t*>(b + kAt.vz + token * 2);
         }
     }
 }
@@ -124,11 +124,11 @@ __device__ __forceinline__ u32x4 stream_v(const StreamRaw<kStore, kDim>& r, int 
     else if constexpr (kStore == SALI_STORE_INT8) {
         const u32x4& c = r.v[f / 2];
         const uint32_t lo = f & 1 ? c.z : c.x, hi = f & 1 ? c.w : c.y;
-        return values8<kBf16>(lo, hi, r.vs[f / 2]);
+        return row_values8<kBf16>(lo, hi, r.vs[f / 2]);
     } else {
         const int shift = (f & 1) * 4;
         const uint32_t lo = r.v[f / 2].x, hi = r.v[f / 2].y;
-        return values4<kBf16>(lo >> shift & 0x0F0F0F0Fu, hi >> shift & 0x0F0F0F0Fu, r.vs[f / 2], r.vz[f / 2]);
+        return row_values4<kBf16>(lo >> shift & 0x0F0F0F0Fu, hi >> shift & 0x0F0F0F0Fu, r.vs[f / 2], low_half<kBf16>(r.vz[f / 2]));
     }
 }
 template <int kStore>
@@ -271,13 +271,18 @@ __device__ __forceinline__ PagesAttend late_arguments() {
 //   pairs: grid (K/V heads, sequences), a block the one pair; for short sequences, where parts and their joining would cost more than they bring
 //   stretches: of all tiles; a launch of its own joins the parts of cut pairs (k_pages_stream_merge)
 enum class StreamMode { pairs, stretches };
+// Waves of a block, and waves a SIMD that their registers leave room for.  Stretches: small blocks, several of which share a compute unit, so that one
+// walks on while another is between two pairs.
+constexpr int stream_waves(StreamMode mode) { return mode == StreamMode::pairs ? 8 : 4; }
+constexpr int stream_occupancy(int store, int sets, StreamMode mode) { return store != SALI_STORE_16 && sets == 1 && mode == StreamMode::stretches ? 3 : 2; }
 
 // The leading arguments come in registers: what the first loads depend on.
 template <int kStore, int kDim, bool kBf16, int kSets, StreamMode kMode>
-__global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_pages_stream(
+__global__ __launch_bounds__(64 * stream_waves(kMode)) __attribute__((amdgpu_waves_per_eu(stream_occupancy(kStore, kSets, kMode), stream_occupancy(kStore, kSets, kMode))))
+void k_pages_stream(
     const int32_t* __restrict__ starts, const int32_t* __restrict__ lengths, const int32_t* __restrict__ tables, int n_seqs, int width, int n_tokens, int max_q,
     int max_kv, int blocks_log2, int window, int sinks, int group, int n_kv, PagesAttend a, int rows_max, int min_tiles) {
-    constexpr int kRows = 16 * kSets, kSteps = kDim / 32, kFs = kDim / 16, kPitch = kDim + 4;
+    constexpr int kStreamWaves = stream_waves(kMode), kRows = 16 * kSets, kSteps = kDim / 32, kFs = kDim / 16, kPitch = kDim + 4;
     constexpr bool kStretches = kMode != StreamMode::pairs;
     __shared__ __align__(16) float s_acc[kStreamWaves][kRows][kPitch];
     __shared__ float s_m[kStreamWaves][kRows], s_l[kStreamWaves][kRows];
@@ -417,7 +422,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
 #pragma unroll
         for (int c = 0; c < kSets; ++c) {
             int r = 16 * c + col;
-            if constexpr (kStretches) asm volatile("" : "+v"(r));       // not worked out before the loop over segments, which would take registers
+            asm volatile("" : "+v"(r));     // not worked out ahead of time, which would take registers
             const int token = r / group, g = r - token * group;
             pos[c] = r < rows ? view.first + token : -1;
 #pragma unroll
@@ -509,8 +514,8 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
                 if constexpr (kStore != SALI_STORE_16) {
 #pragma unroll
                     for (int g = 0; g < kDim / 32; ++g) {
-                        raw.vs[g] = live_tokens(raw.vs[g], live);
-                        if constexpr (kStore == SALI_STORE_INT4) raw.vz[g] = live_tokens(raw.vz[g], live);
+                        raw.vs[g] = (lane & 7) < live ? raw.vs[g] : 0.0f;
+                        if constexpr (kStore == SALI_STORE_INT4) raw.vz[g] = (lane & 7) < live ? raw.vz[g] : 0;
                     }
                 } else {
                     bool odd = false;

@@ -149,7 +149,7 @@ struct TileRaw {
     static constexpr int kLoads = (kShare + 63) / 64;
     u32x4 k[kLoads], v[kLoads];
     float ks[kStore == SALI_STORE_16 ? 1 : kLoads];
-    Scales8 vs[kStore == SALI_STORE_16 ? 1 : kLoads];
+    typename std::conditional<kStore == SALI_STORE_INT4, Scales8, float>::type vs[kStore == SALI_STORE_16 ? 1 : kLoads];
     uint16_t kz[kStore == SALI_STORE_INT4 ? kLoads : 1];
     u32x4 vz[kStore == SALI_STORE_INT4 ? kLoads : 1];
     static __device__ __forceinline__ bool none(int i, int lane) { return kShare % 64 != 0 && lane + 64 * i >= kShare; }
@@ -181,9 +181,13 @@ __device__ __forceinline__ void tile_load_v(const char* block, int half, int lan
         r.v[i] = load16(block + kAt.v + (half * R::kShare + p) * 16);
         if constexpr (kStore != SALI_STORE_16) {            // pieces of two values (8 bits) or two bytes (4 bits) of a group
             const uint32_t at = (kStore == SALI_STORE_INT8 ? p >> 4 : p >> 3) * 16 + (uint32_t)half * 8;
-            const f32x4* s = reinterpret_cast<const f32x4*>(block + kAt.vs + at * 4);
-            r.vs[i] = {s[0], s[1]};
-            if constexpr (kStore == SALI_STORE_INT4) r.vz[i] = load16(block + kAt.vz + at * 2);
+            if constexpr (kStore == SALI_STORE_INT8) {
+                r.vs[i] = *reinterpret_cast<const float*>(block + kAt.vs + (at + (p & 7)) * 4);
+            } else {
+                const f32x4* s = reinterpret_cast<const f32x4*>(block + kAt.vs + at * 4);
+                r.vs[i] = {s[0], s[1]};
+                r.vz[i] = load16(block + kAt.vz + at * 2);
+            }
         }
     }
 }
@@ -224,8 +228,8 @@ __device__ __forceinline__ void tile_store_v(const TileRaw<kStore, kDim>& r, int
             put16(v + p * 16, r.v[i]);
         } else if constexpr (kStore == SALI_STORE_INT8) {
             uint8_t* const to = v + p * 32;
-            put16(to, values8<kBf16>(r.v[i].x, r.v[i].y, r.vs[i]));
-            put16(to + 16, values8<kBf16>(r.v[i].z, r.v[i].w, r.vs[i]));
+            put16(to, row_values8<kBf16>(r.v[i].x, r.v[i].y, r.vs[i]));
+            put16(to + 16, row_values8<kBf16>(r.v[i].z, r.v[i].w, r.vs[i]));
         } else {
             uint8_t* const to = v + ((p >> 3) * 32 + (p & 7) * 2) * 16;
             put16(to, values4<kBf16>(r.v[i].x & kLowHalves, r.v[i].y & kLowHalves, r.vs[i], r.vz[i]));
@@ -313,8 +317,11 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
             for (int x = 0; x < Raw::kLoads; ++x) {
                 if constexpr (kStore == SALI_STORE_16) raw.v[x] = live_tokens(raw.v[x], mine);
-                else raw.vs[x] = live_tokens(raw.vs[x], mine);
-                if constexpr (kStore == SALI_STORE_INT4) raw.vz[x] = live_tokens(raw.vz[x], mine);
+                else if constexpr (kStore == SALI_STORE_INT8) raw.vs[x] = (lane & 7) < mine ? raw.vs[x] : 0.0f;
+                else {
+                    raw.vs[x] = live_tokens(raw.vs[x], mine);
+                    raw.vz[x] = live_tokens(raw.vz[x], mine);
+                }
             }
         if constexpr (kStore == SALI_STORE_16) {
             bool any = false;
