@@ -129,9 +129,9 @@ __device__ __forceinline__ u32x4 row_values8(uint32_t a, uint32_t b, float s) {
     r.w = pack2_after_f32<kBf16>(code8(b, 2) * from_row<6>(s), code8(b, 3) * from_row<7>(s));
     return r;
 }
+// (moves here, since a multiply-add takes no such operand; the two halves of a group's bytes share them)
 template <bool kBf16>
 __device__ __forceinline__ u32x4 row_values4(uint32_t a, uint32_t b, float s, float z) {
-    asm("" : "+v"(s));
     u32x4 r;
     r.x = pack2_after_f32<kBf16>(__builtin_fmaf(code4(a, 0), from_row<0>(s), from_row<0>(z)), __builtin_fmaf(code4(a, 1), from_row<1>(s), from_row<1>(z)));
     r.y = pack2_after_f32<kBf16>(__builtin_fmaf(code4(a, 2), from_row<2>(s), from_row<2>(z)), __builtin_fmaf(code4(a, 3), from_row<3>(s), from_row<3>(z)));

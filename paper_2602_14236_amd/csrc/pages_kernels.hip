@@ -11,6 +11,7 @@
 // reads fall on different banks.  Codes are made and expanded on the side of the rows, where a group lies in four adjacent lanes.
 // Blocks that the new tokens do not fill are written value by value, so that no byte of another token is touched.
 
+#include <algorithm>
 #include <type_traits>
 
 #include "pages.h"
@@ -21,6 +22,8 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kEnoughBlocks = 4096;         // of 256 threads: twice what the compute units hold
 
 template <bool kBf16>
 struct Half;
@@ -70,17 +73,16 @@ __device__ __forceinline__ int seq_of_slot(const PageSeqs& q, int64_t slot) {
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// the 16-token block a thread block has: which tokens of it are the batch's, where their rows and the block itself lie
+// What a thread block has: a 16-token block of a sequence, for a run of K/V heads; which tokens of it are the batch's, where their rows and
+// the first head's block lie
 struct BlockWork {
-    char* block;                            // NULL: no such page
+    char* block;                            // of head 0; NULL: no such page
     int32_t row0;                           // row of the block's token 0 (it may lie before the new tokens)
     int32_t t0, t1;                         // the new tokens of the block
-    int32_t head;
+    int32_t head, heads_end;
 };
-__device__ __forceinline__ bool find_work(const PageGeom& g, const PageSeqs& q, BlockWork& w) {
-    const uint32_t id = blockIdx.x;
-    const uint32_t slot = id / (uint32_t)g.n_kv;
-    w.head = (int)(id - slot * (uint32_t)g.n_kv);
+__device__ __forceinline__ bool find_work(const PageGeom& g, const PageSeqs& q, int heads_each, BlockWork& w) {
+    const int64_t slot = blockIdx.x;
     const int s = seq_of_slot(q, slot);
     const PageSeq seq = load_seq(q, g, s, threadIdx.x == 0);
     if (seq.n == 0) return false;
@@ -88,6 +90,8 @@ __device__ __forceinline__ bool find_work(const PageGeom& g, const PageSeqs& q, 
     const int64_t at = (int64_t)(pos0 / kBlockTokens) + (slot - first_slot(seq.first, s));
     if (at * kBlockTokens >= seq.len) return false;         // one of the slots that the sequence has no use for
     const int block = (int)at;
+    w.head = (int)blockIdx.y * heads_each;
+    w.heads_end = min(w.head + heads_each, g.n_kv);
     w.t0 = max(0, pos0 - block * kBlockTokens);
     w.t1 = min(kBlockTokens, seq.len - block * kBlockTokens);
     w.row0 = seq.first + (block * kBlockTokens - pos0);
@@ -95,8 +99,7 @@ __device__ __forceinline__ bool find_work(const PageGeom& g, const PageSeqs& q, 
     w.block = nullptr;
     if (page >= 0 && page < g.n_pages) {
         const int in_page = block & ((1 << g.blocks_log2) - 1);
-        const uint32_t block_bytes = g.head_bytes >> g.blocks_log2;
-        w.block = g.pool + (uint64_t)page * g.page_bytes + (uint64_t)w.head * g.head_bytes + (uint32_t)in_page * block_bytes;
+        w.block = g.pool + (uint64_t)page * g.page_bytes + (uint32_t)in_page * (g.head_bytes >> g.blocks_log2);
     } else if (threadIdx.x == 0) {
         atomicOr(q.status, SALI_FAULT_PAGE);
     }
@@ -112,7 +115,7 @@ struct Rows {
 };
 
 template <int kStore, int kDim, bool kBf16>
-__global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs, RowsIn k, RowsIn v) {
+__global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs, RowsIn k, RowsIn v, int heads_each) {
     typedef Rows<kStore, kDim> R;
     constexpr int kPieces = kDim / 8, kItems = 32 * kPieces;            // 16-byte pieces of a row, of all rows
     constexpr BlockLayout kAt = block_layout(kStore, kDim);
@@ -120,141 +123,149 @@ __global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs,
     __shared__ float s_scale[kStore == SALI_STORE_16 ? 1 : 32 * R::kGroups];
     __shared__ uint16_t s_low[kStore == SALI_STORE_INT4 ? 32 * R::kGroups : 1];
     BlockWork w;
-    if (!find_work(g, seqs, w) || w.block == nullptr) return;
+    if (!find_work(g, seqs, heads_each, w) || w.block == nullptr) return;
 
     Piece<kBf16> x[kItems / 256];
+    auto ask = [&](int head) {
 #pragma unroll
-    for (int i = 0; i < kItems / 256; ++i) {
-        const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces, t = row & 15;
-        const RowsIn& in = row < 16 ? k : v;
-        x[i].u = (u32x4){0u, 0u, 0u, 0u};
-        if (t >= w.t0 && t < w.t1)
-            x[i].u = *reinterpret_cast<const u32x4*>(in.d + (int64_t)(w.row0 + t) * in.token_bytes + (int64_t)w.head * in.head_bytes + c * 16);
-    }
+        for (int i = 0; i < kItems / 256; ++i) {
+            const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces, t = row & 15;
+            const RowsIn& in = row < 16 ? k : v;
+            x[i].u = (u32x4){0u, 0u, 0u, 0u};
+            if (t >= w.t0 && t < w.t1)
+                x[i].u = *reinterpret_cast<const u32x4*>(in.d + (int64_t)(w.row0 + t) * in.token_bytes + (int64_t)head * in.head_bytes + c * 16);
+        }
+    };
+    ask(w.head);
     bool bad = false;
+    for (int head = w.head; head < w.heads_end; ++head) {
+        char* const block = w.block + (uint64_t)head * g.head_bytes;
+        if (head > w.head) __syncthreads();                     // the head before is out of LDS
 #pragma unroll
-    for (int i = 0; i < kItems / 256; ++i) {
-        const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces;
-        if constexpr (kStore == SALI_STORE_16) {
+        for (int i = 0; i < kItems / 256; ++i) {
+            const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces;
+            if constexpr (kStore == SALI_STORE_16) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) bad |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent;
-            *reinterpret_cast<u32x4*>(s_rows + row * R::kPitch + c * 16) = x[i].u;
-        } else {
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = (float)x[i].h[e];
-            float m, low = 0.0f;
-            constexpr float kSteps = kStore == SALI_STORE_INT8 ? 127.0f : 15.0f;
-            if constexpr (kStore == SALI_STORE_INT8) {
-                m = fabsf(f[0]);
-#pragma unroll
-                for (int e = 1; e < 8; ++e) m = fmaxf(m, fabsf(f[e]));
-                m = fmaxf(m, quad_move<kSwap1>(m));
-                m = fmaxf(m, quad_move<kSwap2>(m));
+                for (int e = 0; e < 8; ++e) bad |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent;
+                *reinterpret_cast<u32x4*>(s_rows + row * R::kPitch + c * 16) = x[i].u;
             } else {
-                float high = f[0];
-                low = f[0];
+                float f[8];
 #pragma unroll
-                for (int e = 1; e < 8; ++e) {
-                    low = fminf(low, f[e]);
-                    high = fmaxf(high, f[e]);
+                for (int e = 0; e < 8; ++e) f[e] = (float)x[i].h[e];
+                float m, low = 0.0f;
+                constexpr float kSteps = kStore == SALI_STORE_INT8 ? 127.0f : 15.0f;
+                if constexpr (kStore == SALI_STORE_INT8) {
+                    m = fabsf(f[0]);
+#pragma unroll
+                    for (int e = 1; e < 8; ++e) m = fmaxf(m, fabsf(f[e]));
+                    m = fmaxf(m, quad_move<kSwap1>(m));
+                    m = fmaxf(m, quad_move<kSwap2>(m));
+                } else {
+                    float high = f[0];
+                    low = f[0];
+#pragma unroll
+                    for (int e = 1; e < 8; ++e) {
+                        low = fminf(low, f[e]);
+                        high = fmaxf(high, f[e]);
+                    }
+                    low = fminf(low, quad_move<kSwap1>(low));
+                    low = fminf(low, quad_move<kSwap2>(low));
+                    high = fmaxf(high, quad_move<kSwap1>(high));
+                    high = fmaxf(high, quad_move<kSwap2>(high));
+                    // rounding keeps the order of numbers, so the largest of the rounded differences is this one
+                    m = high - low;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] = f[e] - low;
                 }
-                low = fminf(low, quad_move<kSwap1>(low));
-                low = fminf(low, quad_move<kSwap2>(low));
-                high = fmaxf(high, quad_move<kSwap1>(high));
-                high = fmaxf(high, quad_move<kSwap2>(high));
-                // rounding keeps the order of numbers, so the largest of the rounded differences is this one
-                m = high - low;
+                float inv = kSteps / m;
+                // a group with an infinity or NaN, or one too wide or too small for fp32 steps, is stored as zeros: every value of the pages is finite
+                uint32_t odd = 0u;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = f[e] - low;
-            }
-            float inv = kSteps / m;
-            // a group with an infinity or NaN, or one too wide or too small for fp32 steps, is stored as zeros: every value of the pages is finite
-            uint32_t odd = 0u;
+                for (int e = 0; e < 8; ++e) odd |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent ? 1u : 0u;
+                odd |= m <= 3.402823466e38f ? 0u : 1u;
+                odd |= quad_move<kSwap1>(odd);
+                odd |= quad_move<kSwap2>(odd);
+                bad |= odd != 0u;
+                const bool some = odd == 0u && m > 0.0f && inv <= 3.402823466e38f;
+                const float scale = some ? m / kSteps : 0.0f;
+                inv = some ? inv : 0.0f;
+                if ((c & 3) == 0) {
+                    s_scale[row * R::kGroups + c / 4] = scale;
+                    if constexpr (kStore == SALI_STORE_INT4) {
+                        Piece<kBf16> z;
+                        z.h[0] = (typename Half<kBf16>::type)(odd == 0u ? low : 0.0f);       // exact: one of the values
+                        s_low[row * R::kGroups + c / 4] = z.b16[0];
+                    }
+                }
+                Piece<kBf16> code;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) odd |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent ? 1u : 0u;
-            odd |= m <= 3.402823466e38f ? 0u : 1u;
-            odd |= quad_move<kSwap1>(odd);
-            odd |= quad_move<kSwap2>(odd);
-            bad |= odd != 0u;
-            const bool some = odd == 0u && m > 0.0f && inv <= 3.402823466e38f;
-            const float scale = some ? m / kSteps : 0.0f;
-            inv = some ? inv : 0.0f;
-            if ((c & 3) == 0) {
-                s_scale[row * R::kGroups + c / 4] = scale;
-                if constexpr (kStore == SALI_STORE_INT4) {
-                    Piece<kBf16> z;
-                    z.h[0] = (typename Half<kBf16>::type)(odd == 0u ? low : 0.0f);       // exact: one of the values
-                    s_low[row * R::kGroups + c / 4] = z.b16[0];
+                for (int e = 0; e < 8; ++e) {
+                    const float q = some ? fminf(fmaxf(rintf(f[e] * inv), kStore == SALI_STORE_INT8 ? -kSteps : 0.0f), kSteps) : 0.0f;
+                    code.b8[e] = (uint8_t)(int)q;
+                }
+                if constexpr (kStore == SALI_STORE_INT8) {
+                    *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + c * 8) = (u32x2){code.u.x, code.u.y};
+                } else {
+                    // lanes 0, 1 of a quad hold values 0 .. 15 of the group, lanes 2, 3 the others, which go to the high halves of the same bytes
+                    const uint32_t a = quad_move<kSwap2>(code.u.x) << 4 | code.u.x, b = quad_move<kSwap2>(code.u.y) << 4 | code.u.y;
+                    if ((c & 2) == 0) *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + (c / 4) * 16 + (c & 1) * 8) = (u32x2){a, b};
                 }
             }
-            Piece<kBf16> code;
+        }
+        __syncthreads();
+        if (head + 1 < w.heads_end) ask(head + 1);              // on its way while this one is written
+
+        // K: pieces of 16 bytes, [piece of the row][place]
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float q = some ? fminf(fmaxf(rintf(f[e] * inv), kStore == SALI_STORE_INT8 ? -kSteps : 0.0f), kSteps) : 0.0f;
-                code.b8[e] = (uint8_t)(int)q;
+        for (int i = 0; i < (R::kBytes + 255) / 256; ++i) {
+            const int p = (int)threadIdx.x + 256 * i, t = token_of_place(p & 15);
+            if (p < R::kBytes && t >= w.t0 && t < w.t1)
+                *reinterpret_cast<u32x4*>(block + p * 16) = *reinterpret_cast<const u32x4*>(s_rows + t * R::kPitch + (p >> 4) * 16);
+        }
+        // V: for each half of the block and each element of a row (a value, a code, a byte of two codes) those of eight tokens
+        constexpr int kElem = kStore == SALI_STORE_16 ? 2 : 1, kElems = R::kBytes / kElem;
+#pragma unroll
+        for (int i = 0; i < (2 * kElems + 255) / 256; ++i) {
+            const int p = (int)threadIdx.x + 256 * i, a = p / kElems, e = p % kElems;
+            if (p >= 2 * kElems) continue;
+            Piece<kBf16> o;
+            o.u = (u32x4){0u, 0u, 0u, 0u};
+            const uint8_t* column = s_rows + (16 + 8 * a) * R::kPitch + e * kElem;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                if constexpr (kElem == 2) o.b16[t] = *reinterpret_cast<const uint16_t*>(column + t * R::kPitch);
+                else o.b8[t] = column[t * R::kPitch];
             }
-            if constexpr (kStore == SALI_STORE_INT8) {
-                *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + c * 8) = (u32x2){code.u.x, code.u.y};
+            char* dst = block + kAt.v + (uint32_t)p * (8 * kElem);
+            if (w.t0 <= 8 * a && w.t1 >= 8 * a + 8) {
+                if constexpr (kElem == 2) *reinterpret_cast<u32x4*>(dst) = o.u;
+                else *reinterpret_cast<u32x2*>(dst) = (u32x2){o.u.x, o.u.y};
             } else {
-                // lanes 0, 1 of a quad hold values 0 .. 15 of the group, lanes 2, 3 the others, which go to the high halves of the same bytes
-                const uint32_t a = quad_move<kSwap2>(code.u.x) << 4 | code.u.x, b = quad_move<kSwap2>(code.u.y) << 4 | code.u.y;
-                if ((c & 2) == 0) *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + (c / 4) * 16 + (c & 1) * 8) = (u32x2){a, b};
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    if (8 * a + t < w.t0 || 8 * a + t >= w.t1) continue;
+                    if constexpr (kElem == 2) reinterpret_cast<uint16_t*>(dst)[t] = o.b16[t];
+                    else reinterpret_cast<uint8_t*>(dst)[t] = o.b8[t];
+                }
+            }
+        }
+        if constexpr (kStore != SALI_STORE_16) {
+            const int p = (int)threadIdx.x;                     // [K, V][group][16]
+            if (p < 32 * R::kGroups) {
+                const int side = p / (16 * R::kGroups), group = p / 16 % R::kGroups, t = side == 0 ? token_of_place(p & 15) : p & 15;
+                if (t >= w.t0 && t < w.t1) {
+                    const int from = (16 * side + t) * R::kGroups + group;
+                    reinterpret_cast<float*>(block + kAt.ks)[p] = s_scale[from];
+                    if constexpr (kStore == SALI_STORE_INT4) reinterpret_cast<uint16_t*>(block + kAt.kz)[p] = s_low[from];
+                }
             }
         }
     }
     if (bad) atomicOr(seqs.status, SALI_FAULT_NONFINITE);
-    __syncthreads();
-
-    // K: pieces of 16 bytes, [piece of the row][place]
-#pragma unroll
-    for (int i = 0; i < (R::kBytes + 255) / 256; ++i) {
-        const int p = (int)threadIdx.x + 256 * i, t = token_of_place(p & 15);
-        if (p < R::kBytes && t >= w.t0 && t < w.t1)
-            *reinterpret_cast<u32x4*>(w.block + p * 16) = *reinterpret_cast<const u32x4*>(s_rows + t * R::kPitch + (p >> 4) * 16);
-    }
-    // V: for each half of the block and each element of a row (a value, a code, a byte of two codes) those of eight tokens
-    constexpr int kElem = kStore == SALI_STORE_16 ? 2 : 1, kElems = R::kBytes / kElem;
-#pragma unroll
-    for (int i = 0; i < (2 * kElems + 255) / 256; ++i) {
-        const int p = (int)threadIdx.x + 256 * i, a = p / kElems, e = p % kElems;
-        if (p >= 2 * kElems) continue;
-        Piece<kBf16> o;
-        o.u = (u32x4){0u, 0u, 0u, 0u};
-        const uint8_t* column = s_rows + (16 + 8 * a) * R::kPitch + e * kElem;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            if constexpr (kElem == 2) o.b16[t] = *reinterpret_cast<const uint16_t*>(column + t * R::kPitch);
-            else o.b8[t] = column[t * R::kPitch];
-        }
-        char* dst = w.block + kAt.v + (uint32_t)p * (8 * kElem);
-        if (w.t0 <= 8 * a && w.t1 >= 8 * a + 8) {
-            if constexpr (kElem == 2) *reinterpret_cast<u32x4*>(dst) = o.u;
-            else *reinterpret_cast<u32x2*>(dst) = (u32x2){o.u.x, o.u.y};
-        } else {
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                if (8 * a + t < w.t0 || 8 * a + t >= w.t1) continue;
-                if constexpr (kElem == 2) reinterpret_cast<uint16_t*>(dst)[t] = o.b16[t];
-                else reinterpret_cast<uint8_t*>(dst)[t] = o.b8[t];
-            }
-        }
-    }
-    if constexpr (kStore != SALI_STORE_16) {
-        const int p = (int)threadIdx.x;                     // [K, V][group][16]
-        if (p < 32 * R::kGroups) {
-            const int side = p / (16 * R::kGroups), group = p / 16 % R::kGroups, t = side == 0 ? token_of_place(p & 15) : p & 15;
-            if (t >= w.t0 && t < w.t1) {
-                const int from = (16 * side + t) * R::kGroups + group;
-                reinterpret_cast<float*>(w.block + kAt.ks)[p] = s_scale[from];
-                if constexpr (kStore == SALI_STORE_INT4) reinterpret_cast<uint16_t*>(w.block + kAt.kz)[p] = s_low[from];
-            }
-        }
-    }
 }
 
 template <int kStore, int kDim, bool kBf16>
-__global__ __launch_bounds__(256) void k_pages_read(PageGeom g, PageSeqs seqs, RowsOut k, RowsOut v) {
+__global__ __launch_bounds__(256) void k_pages_read(PageGeom g, PageSeqs seqs, RowsOut k, RowsOut v, int heads_each) {
     typedef Rows<kStore, kDim> R;
     typedef typename Half<kBf16>::type T;
     constexpr int kPieces = kDim / 8, kItems = 32 * kPieces;
@@ -265,20 +276,24 @@ __global__ __launch_bounds__(256) void k_pages_read(PageGeom g, PageSeqs seqs, R
     __shared__ float s_scale[kStore == SALI_STORE_16 ? 1 : 32 * R::kGroups];
     __shared__ uint16_t s_low[kStore == SALI_STORE_INT4 ? 32 * R::kGroups : 1];
     BlockWork w;
-    if (!find_work(g, seqs, w)) return;
-    if (w.block != nullptr) {
-        u32x4 kp[kKLoads];
-        Piece<kBf16> vp[kVLoads];
+    if (!find_work(g, seqs, heads_each, w)) return;
+    u32x4 kp[kKLoads];
+    Piece<kBf16> vp[kVLoads];
+    float scale_in = 0.0f;
+    uint16_t low_in = 0;
+    auto ask = [&](int head) {
+        if (w.block == nullptr) return;
+        const char* const block = w.block + (uint64_t)head * g.head_bytes;
 #pragma unroll
         for (int i = 0; i < kKLoads; ++i) {
             const int p = (int)threadIdx.x + 256 * i;
-            if (p < R::kBytes) kp[i] = *reinterpret_cast<const u32x4*>(w.block + p * 16);
+            if (p < R::kBytes) kp[i] = *reinterpret_cast<const u32x4*>(block + p * 16);
         }
 #pragma unroll
         for (int i = 0; i < kVLoads; ++i) {
             const int p = (int)threadIdx.x + 256 * i;
             if (p >= 2 * kElems) continue;
-            const char* src = w.block + kAt.v + (uint32_t)p * (8 * kElem);
+            const char* src = block + kAt.v + (uint32_t)p * (8 * kElem);
             if constexpr (kElem == 2) {
                 vp[i].u = *reinterpret_cast<const u32x4*>(src);
             } else {
@@ -289,61 +304,75 @@ __global__ __launch_bounds__(256) void k_pages_read(PageGeom g, PageSeqs seqs, R
         if constexpr (kStore != SALI_STORE_16) {
             const int p = (int)threadIdx.x;
             if (p < 32 * R::kGroups) {
-                const int side = p / (16 * R::kGroups), group = p / 16 % R::kGroups, t = side == 0 ? token_of_place(p & 15) : p & 15;
-                const int to = (16 * side + t) * R::kGroups + group;
-                s_scale[to] = reinterpret_cast<const float*>(w.block + kAt.ks)[p];
-                if constexpr (kStore == SALI_STORE_INT4) s_low[to] = reinterpret_cast<const uint16_t*>(w.block + kAt.kz)[p];
+                scale_in = reinterpret_cast<const float*>(block + kAt.ks)[p];
+                if constexpr (kStore == SALI_STORE_INT4) low_in = reinterpret_cast<const uint16_t*>(block + kAt.kz)[p];
             }
         }
-#pragma unroll
-        for (int i = 0; i < kKLoads; ++i) {
-            const int p = (int)threadIdx.x + 256 * i;
-            if (p < R::kBytes) *reinterpret_cast<u32x4*>(s_rows + token_of_place(p & 15) * R::kPitch + (p >> 4) * 16) = kp[i];
-        }
-#pragma unroll
-        for (int i = 0; i < kVLoads; ++i) {
-            const int p = (int)threadIdx.x + 256 * i, a = p / kElems, e = p % kElems;
-            if (p >= 2 * kElems) continue;
-            uint8_t* column = s_rows + (16 + 8 * a) * R::kPitch + e * kElem;
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                if constexpr (kElem == 2) *reinterpret_cast<uint16_t*>(column + t * R::kPitch) = vp[i].b16[t];
-                else column[t * R::kPitch] = vp[i].b8[t];
-            }
-        }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kItems / 256; ++i) {
-        const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces, t = row & 15;
-        if (t < w.t0 || t >= w.t1) continue;
-        Piece<kBf16> o;
-        o.u = (u32x4){0u, 0u, 0u, 0u};
+    };
+    ask(w.head);
+    for (int head = w.head; head < w.heads_end; ++head) {
+        if (head > w.head) __syncthreads();                     // the head before is out of LDS
         if (w.block != nullptr) {
-            if constexpr (kStore == SALI_STORE_16) {
-                o.u = *reinterpret_cast<const u32x4*>(s_rows + row * R::kPitch + c * 16);
-            } else {
-                const float scale = s_scale[row * R::kGroups + c / 4];
-                Piece<kBf16> code;
-                if constexpr (kStore == SALI_STORE_INT8) {
-                    const u32x2 q = *reinterpret_cast<const u32x2*>(s_rows + row * R::kPitch + c * 8);
-                    code.u = (u32x4){q.x, q.y, 0u, 0u};
+            if constexpr (kStore != SALI_STORE_16) {
+                const int p = (int)threadIdx.x;
+                if (p < 32 * R::kGroups) {
+                    const int side = p / (16 * R::kGroups), group = p / 16 % R::kGroups, t = side == 0 ? token_of_place(p & 15) : p & 15;
+                    const int to = (16 * side + t) * R::kGroups + group;
+                    s_scale[to] = scale_in;
+                    if constexpr (kStore == SALI_STORE_INT4) s_low[to] = low_in;
+                }
+            }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o.h[e] = rounded_after_f32<T>((float)(int)(int8_t)code.b8[e] * scale);
-                } else {
-                    Piece<kBf16> z;
-                    z.b16[0] = s_low[row * R::kGroups + c / 4];
-                    const float low = (float)z.h[0];
-                    const u32x2 q = *reinterpret_cast<const u32x2*>(s_rows + row * R::kPitch + (c / 4) * 16 + (c & 1) * 8);
-                    const int shift = (c & 2) * 2;          // values 16 .. 31 of a group lie in the high halves
-                    code.u = (u32x4){q.x >> shift & 0x0F0F0F0Fu, q.y >> shift & 0x0F0F0F0Fu, 0u, 0u};
+            for (int i = 0; i < kKLoads; ++i) {
+                const int p = (int)threadIdx.x + 256 * i;
+                if (p < R::kBytes) *reinterpret_cast<u32x4*>(s_rows + token_of_place(p & 15) * R::kPitch + (p >> 4) * 16) = kp[i];
+            }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o.h[e] = rounded_after_f32<T>(__builtin_fmaf((float)code.b8[e], scale, low));
+            for (int i = 0; i < kVLoads; ++i) {
+                const int p = (int)threadIdx.x + 256 * i, a = p / kElems, e = p % kElems;
+                if (p >= 2 * kElems) continue;
+                uint8_t* column = s_rows + (16 + 8 * a) * R::kPitch + e * kElem;
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    if constexpr (kElem == 2) *reinterpret_cast<uint16_t*>(column + t * R::kPitch) = vp[i].b16[t];
+                    else column[t * R::kPitch] = vp[i].b8[t];
                 }
             }
         }
-        const RowsOut& out = row < 16 ? k : v;
-        *reinterpret_cast<u32x4*>(out.d + (int64_t)(w.row0 + t) * out.token_bytes + (int64_t)w.head * out.head_bytes + c * 16) = o.u;
+        __syncthreads();
+        if (head + 1 < w.heads_end) ask(head + 1);              // on its way while this one is written
+#pragma unroll
+        for (int i = 0; i < kItems / 256; ++i) {
+            const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces, t = row & 15;
+            if (t < w.t0 || t >= w.t1) continue;
+            Piece<kBf16> o;
+            o.u = (u32x4){0u, 0u, 0u, 0u};
+            if (w.block != nullptr) {
+                if constexpr (kStore == SALI_STORE_16) {
+                    o.u = *reinterpret_cast<const u32x4*>(s_rows + row * R::kPitch + c * 16);
+                } else {
+                    const float scale = s_scale[row * R::kGroups + c / 4];
+                    Piece<kBf16> code;
+                    if constexpr (kStore == SALI_STORE_INT8) {
+                        const u32x2 q = *reinterpret_cast<const u32x2*>(s_rows + row * R::kPitch + c * 8);
+                        code.u = (u32x4){q.x, q.y, 0u, 0u};
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o.h[e] = rounded_after_f32<T>((float)(int)(int8_t)code.b8[e] * scale);
+                    } else {
+                        Piece<kBf16> z;
+                        z.b16[0] = s_low[row * R::kGroups + c / 4];
+                        const float low = (float)z.h[0];
+                        const u32x2 q = *reinterpret_cast<const u32x2*>(s_rows + row * R::kPitch + (c / 4) * 16 + (c & 1) * 8);
+                        const int shift = (c & 2) * 2;          // values 16 .. 31 of a group lie in the high halves
+                        code.u = (u32x4){q.x >> shift & 0x0F0F0F0Fu, q.y >> shift & 0x0F0F0F0Fu, 0u, 0u};
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o.h[e] = rounded_after_f32<T>(__builtin_fmaf((float)code.b8[e], scale, low));
+                    }
+                }
+            }
+            const RowsOut& out = row < 16 ? k : v;
+            *reinterpret_cast<u32x4*>(out.d + (int64_t)(w.row0 + t) * out.token_bytes + (int64_t)head * out.head_bytes + c * 16) = o.u;
+        }
     }
 }
 
@@ -363,23 +392,32 @@ hipError_t by_type(int dtype, int store, int dim, const F& go) {
     return hipGetLastError();
 }
 
-uint32_t slot_blocks(const PageGeom& g, const PageSeqs& q) {
-    return (uint32_t)((q.n_tokens / kBlockTokens + 2ll * q.n_seqs) * g.n_kv);
+// Heads of a thread block: as many as leave a few rounds of blocks for the compute units.  Finding the work is a chain of four trips to memory; a block that
+// walks several heads has the next one's data on its way meanwhile.
+struct Shares {
+    int heads_each;
+    dim3 grid;
+};
+Shares shares(const PageGeom& g, const PageSeqs& q) {
+    const int64_t slots = q.n_tokens / kBlockTokens + 2ll * q.n_seqs;
+    const int64_t most = slots * g.n_kv / kEnoughBlocks;
+    const int each = (int)std::max<int64_t>(1, std::min<int64_t>(most, std::min(g.n_kv, 8)));
+    return {each, dim3((unsigned)slots, (unsigned)((g.n_kv + each - 1) / each))};
 }
 
 }  // namespace
 
 hipError_t launch_pages_append(int dtype, int store, int dim, const PageGeom& g, const PageSeqs& seqs, const RowsIn& k, const RowsIn& v, hipStream_t s) {
+    const Shares sh = shares(g, seqs);
     return by_type(dtype, store, dim, [&](auto bf16, auto st, auto d) {
-        hipLaunchKernelGGL((k_pages_append<decltype(st)::value, decltype(d)::value, decltype(bf16)::value>), dim3(slot_blocks(g, seqs)), dim3(256), 0, s,
-                           g, seqs, k, v);
+        hipLaunchKernelGGL((k_pages_append<decltype(st)::value, decltype(d)::value, decltype(bf16)::value>), sh.grid, dim3(256), 0, s, g, seqs, k, v, sh.heads_each);
     });
 }
 
 hipError_t launch_pages_read(int dtype, int store, int dim, const PageGeom& g, const PageSeqs& seqs, const RowsOut& k, const RowsOut& v, hipStream_t s) {
+    const Shares sh = shares(g, seqs);
     return by_type(dtype, store, dim, [&](auto bf16, auto st, auto d) {
-        hipLaunchKernelGGL((k_pages_read<decltype(st)::value, decltype(d)::value, decltype(bf16)::value>), dim3(slot_blocks(g, seqs)), dim3(256), 0, s,
-                           g, seqs, k, v);
+        hipLaunchKernelGGL((k_pages_read<decltype(st)::value, decltype(d)::value, decltype(bf16)::value>), sh.grid, dim3(256), 0, s, g, seqs, k, v, sh.heads_each);
     });
 }
 
