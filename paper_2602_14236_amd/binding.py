@@ -441,7 +441,7 @@ class PageBatch:
             raise ValueError(f"{n} lengths need {n + 1} starts and {n} rows of the table, got {start.shape[0]} and {table.shape[0]}")
         self.tensors = (start, length, table)
         self.tokens = tokens
-        self.device = length.device
+        self.device, self.index = length.device, length.get_device()
         self.c = sali_page_batch(start.data_ptr(), length.data_ptr(), table.data_ptr(), n, table.shape[1], tokens, tokens if max_q is None else max_q,
                                  max_kv, 0)
 
@@ -460,11 +460,13 @@ class SaliPages:
         if pool is not None and (not pool.is_contiguous() or pool.numel() * pool.element_size() < pool_bytes or pool.device.type != "cuda"):
             raise ValueError(f"pool: {pool_bytes} contiguous bytes on the GPU expected")
         self.dtype = torch.bfloat16 if cfg.dtype else torch.float16
+        self.n_heads, self.n_kv_heads, self.head_dim = cfg.n_heads, cfg.n_kv_heads, cfg.head_dim
         self.handle = None
         with torch.cuda.device(self.device):
             self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=self.device) if pool is None else pool
             self.scratch = torch.empty(scratch_bytes, dtype=torch.uint8, device=self.device)
             self.device = self.scratch.device
+            self.index = self.device.index
             h = C.c_void_p()
             _check(self.lib.sali_pages_create(C.byref(cfg), _ptr(self.pool), _ptr(self.scratch), C.byref(h)), "sali_pages_create")
         self.handle = h
@@ -482,44 +484,49 @@ class SaliPages:
             pass
 
     def _rows(self, t: torch.Tensor, batch: PageBatch, heads: int, name: str) -> sali_rows:
-        if t.dtype != self.dtype or t.shape != (batch.tokens, heads, self.cfg.head_dim) or t.stride(2) != 1 or t.device != self.device:
-            raise ValueError(f"{name}: {self.dtype} [{batch.tokens}, {heads}, {self.cfg.head_dim}] on {self.device} with its last dimension side by "
+        token, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if t.dtype is not self.dtype or t.shape != (batch.tokens, heads, self.head_dim) or one != 1 or t.get_device() != self.index:
+            raise ValueError(f"{name}: {self.dtype} [{batch.tokens}, {heads}, {self.head_dim}] on {self.device} with its last dimension side by "
                              f"side expected, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
-        if batch.device != self.device:
+        return sali_rows(t.data_ptr(), token, head)
+
+    def _call(self, batch: PageBatch, stream: Optional[torch.cuda.Stream]) -> int:
+        """The stream of a call on `batch`: the pages' device's current one, if none is given."""
+        if batch.index != self.index:
             raise ValueError(f"the batch lies on {batch.device}, the pages on {self.device}")
-        return sali_rows(t.data_ptr(), t.stride(0), t.stride(1))
+        return torch._C._cuda_getCurrentRawStream(self.index) if stream is None else stream.cuda_stream
 
     def _dense(self, t: Optional[torch.Tensor], shape, name: str):
         if t is None:
             return None
-        if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+        if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() or t.get_device() != self.index:
             raise ValueError(f"{name}: contiguous float32 {list(shape)} on {self.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
     def append(self, layer: int, batch: PageBatch, k: torch.Tensor, v: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """Store the K/V rows of the batch's new tokens, [tokens, n_kv_heads, head_dim]."""
-        n = self.cfg.n_kv_heads
+        n = self.n_kv_heads
         _check(self.lib.sali_pages_append(self.handle, layer, batch.c, self._rows(k, batch, n, "k"), self._rows(v, batch, n, "v"),
-                                          _stream() if stream is None else stream.cuda_stream), "sali_pages_append")
+                                          self._call(batch, stream)), "sali_pages_append")
 
     def read(self, layer: int, batch: PageBatch, k_out: torch.Tensor, v_out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """The rows of the batch's new tokens as the pages hold them."""
-        n = self.cfg.n_kv_heads
+        n = self.n_kv_heads
         _check(self.lib.sali_pages_read(self.handle, layer, batch.c, self._rows(k_out, batch, n, "k_out"), self._rows(v_out, batch, n, "v_out"),
-                                        _stream() if stream is None else stream.cuda_stream), "sali_pages_read")
+                                        self._call(batch, stream)), "sali_pages_read")
 
     def attend(self, layer: int, batch: PageBatch, q: torch.Tensor, softmax_scale: float, out: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
                window: int = 0, sinks: int = 0, prior: Optional[torch.Tensor] = None, prior_lse: Optional[torch.Tensor] = None,
                stream: Optional[torch.cuda.Stream] = None):
         """Causal attention of the batch's new tokens over the pages: q, out [tokens, n_heads, head_dim], lse [tokens, n_heads] in fp32.  prior and
         prior_lse (fp32): attention of the same queries over other keys, joined with this one."""
-        c, n = self.cfg, self.cfg.n_heads
+        n, d = self.n_heads, self.head_dim
         _check(self.lib.sali_pages_attend(self.handle, layer, batch.c, self._rows(q, batch, n, "q"), softmax_scale, window, sinks,
-                                          self._dense(prior, (batch.tokens, n, c.head_dim), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
+                                          self._dense(prior, (batch.tokens, n, d), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
                                           self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"),
-                                          _stream() if stream is None else stream.cuda_stream), "sali_pages_attend")
+                                          self._call(batch, stream)), "sali_pages_attend")
 
     def get_status(self) -> int:
         f = C.c_uint32()
-        _check(self.lib.sali_pages_get_status(self.handle, C.byref(f), _stream()), "sali_pages_get_status")
+        _check(self.lib.sali_pages_get_status(self.handle, C.byref(f), torch._C._cuda_getCurrentRawStream(self.index)), "sali_pages_get_status")
         return f.value

@@ -147,7 +147,8 @@ int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch
     if (window < 0 || sinks < 0 || window > (1 << 30) || sinks > (1 << 30)) return SALI_ERR_SHAPE;
     if (!isfinite(softmax_scale * 1.44269504088896340736f)) return SALI_ERR_CONFIG;
     if (nothing_to_do(*batch)) return SALI_OK;
-    // tiles are counted in 31 bits
+    // rows and tiles are counted in 31 bits
+    if ((int64_t)batch->n_tokens * (p->cfg.n_heads / p->cfg.n_kv_heads) >= 0x7FFFFFFF - 1024) return SALI_ERR_SHAPE;
     if (((int64_t)batch->max_kv / kTileTokens + 2) * p->cfg.n_kv_heads > 0x7FFFFFFFll / batch->n_seqs) return SALI_ERR_SHAPE;
     PagesAttend a = {};
     a.geom = geom_of(p, layer);

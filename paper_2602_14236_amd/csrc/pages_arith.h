@@ -66,6 +66,13 @@ SALI_BOTH bool sees(int p, int j, int window, int sinks) {
     return j <= p && (window == 0 || j > p - window || j < sinks);
 }
 
+// the same for keys counted from j0 on
+struct Sight {
+    int32_t last, from, sunk;               // keys up to `last` that lie behind `from` or before `sunk`
+    SALI_BOTH bool has(int c) const { return c <= last && (c > from || c < sunk); }
+};
+SALI_BOTH Sight sight_of(int p, int j0, int window, int sinks) { return {p - j0, window == 0 ? -2147483647 : p - window - j0, sinks - j0}; }
+
 // `total` tiles in `blocks` stretches (blocks <= total) that differ by one at most, the longer ones first
 struct Stretches {
     uint32_t each, longer;
@@ -77,22 +84,28 @@ struct Stretches {
     }
 };
 constexpr int kStreamMinTiles = 4;          // of a stretch
-constexpr int kTileRows = 128;              // rows of a block of the tile kernel
-constexpr int kTileKeys = 32;               // keys of its steps
-constexpr int kTileShares = 512;            // fair shares that the whole work is cut into
+// Blocks of the tile kernel: 32 rows a wave, and of each step's keys 8 a wave.  A block of twelve waves has a compute unit to itself, of those of four waves
+// three share one.
+constexpr int tile_rows(int waves) { return 32 * waves; }
+constexpr int tile_keys(int waves) { return 8 * waves; }
 
-// row tiles of a batch by slots, as those of blocks in append: sequence s owns the slots from first * group / kTileRows + s on
-SALI_BOTH int64_t tile_slots(int64_t n_tokens, int group, int64_t n_seqs) { return n_tokens * group / kTileRows + n_seqs; }
-// Tiles of a fair share of `sum` tiles a head.  Units longer than one are cut, into at most twice as many parts as they have shares, so there are
-// at most tile_parts of them a head.
-SALI_BOTH int tile_shares(int n_kv) { return (kTileShares + n_kv - 1) / n_kv; }
-SALI_BOTH int fair_share(int64_t sum, int n_kv) { return (int)((most(sum, (int64_t)1) + tile_shares(n_kv) - 1) / tile_shares(n_kv)); }
+// row tiles of a batch by slots, as those of blocks in append: sequence s owns the slots from first * group / rows + s on
+SALI_BOTH int64_t tile_slots(int64_t n_tokens, int group, int64_t n_seqs, int rows) { return n_tokens * group / rows + n_seqs; }
+// The whole work is cut into fair shares.  Units longer than one are cut, into at most twice as many parts as they have shares, so there are at
+// most tile_parts of them a head.
+SALI_BOTH int tile_shares(int n_kv, int waves) { return ((waves == 12 ? 256 : 512) + n_kv - 1) / n_kv; }
+SALI_BOTH int tile_parts(int n_kv, int waves) { return 2 * tile_shares(n_kv, waves); }
+// tiles of a share of `sum` tiles a head
+SALI_BOTH int fair_share(int64_t sum, int shares) { return (int)((most(sum, (int64_t)1) + shares - 1) / shares); }
 SALI_BOTH int parts_of(int tiles, int share) { return tiles > share ? (tiles + share - 1) / share : 1; }
-SALI_BOTH int tile_parts(int n_kv) { return 2 * tile_shares(n_kv); }
 
+// (rows of a batch are counted in 31 bits)
+template <int kWaves>
 SALI_BOTH View view_of_rows(const PageSeq& q, int row_tile, int group, int window, int sinks) {
-    const int first = q.len - q.n, last_row = (int)least((int64_t)q.n * group, (int64_t)(row_tile + 1) * kTileRows) - 1;
-    return view_of<kTileKeys>(first + (int)((int64_t)row_tile * kTileRows / group), first + last_row / group, window, sinks);
+    const uint32_t first_row = (uint32_t)row_tile * (uint32_t)tile_rows(kWaves), rows = (uint32_t)(q.n * group);
+    const uint32_t last_row = least(rows, first_row + (uint32_t)tile_rows(kWaves)) - 1u, g = (uint32_t)group;
+    const int first = q.len - q.n;
+    return view_of<tile_keys(kWaves)>(first + (int)(first_row / g), first + (int)(last_row / g), window, sinks);
 }
 
 }  // namespace sali

@@ -8,11 +8,12 @@ hipError_t launch_pages_attend_fp16(int store, int dim, const PagesAttend& a, hi
 PagesScratch pages_scratch(int64_t n_pages, int page_tokens, int n_kv, int group, int dim) {
     auto align = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t row = (size_t)(dim + 4) * sizeof(float);
-    size_t parts = (size_t)tile_parts(n_kv) * n_kv * kTileRows;
-    parts = max(parts, (size_t)2 * kStreamMostBlocks * 32);
-    const size_t units = (size_t)(tile_slots(n_pages * page_tokens, group, n_pages) + tile_parts(n_kv));
-    const size_t records = max(sizeof(TilePlan) + (size_t)tile_parts(n_kv) * sizeof(TileMerge) + units * sizeof(TileUnit),
-                               (size_t)kStreamMostBlocks * sizeof(StreamRecord));
+    size_t parts = (size_t)2 * kStreamMostBlocks * 32, records = (size_t)kStreamMostBlocks * sizeof(StreamRecord);
+    for (int waves : {4, 12}) {
+        parts = max(parts, (size_t)tile_parts(n_kv, waves) * n_kv * tile_rows(waves));
+        const size_t units = (size_t)(tile_slots(n_pages * page_tokens, group, n_pages, tile_rows(waves)) + tile_parts(n_kv, waves));
+        records = max(records, sizeof(TilePlan) + (size_t)tile_parts(n_kv, waves) * sizeof(TileMerge) + units * sizeof(TileUnit));
+    }
     PagesScratch p;
     p.partial = kPagesStatusBytes;
     p.records = align(p.partial + parts * row);

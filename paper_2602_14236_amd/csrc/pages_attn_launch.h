@@ -8,6 +8,9 @@ namespace sali {
 
 namespace {
 
+// Rows are taken 384 a block where that gives so many blocks, two rounds of one a compute unit, else 128.
+constexpr int kLargeBlocks = 2 * kComputeUnits;
+
 template <int kStore, int kDim, bool kBf16>
 void launch_attend(const PagesAttend& a, hipStream_t s) {
     const int n_kv = a.geom.n_kv, group = a.group;
@@ -40,10 +43,20 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
         else go(std::integral_constant<int, 2>{});
     }
     if (most_rows > 32) {
-        const int64_t units = tile_slots(a.seqs.n_tokens, group, a.seqs.n_seqs) + tile_parts(n_kv);
-        hipLaunchKernelGGL(k_pages_plan, dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1);
-        hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16>), dim3((unsigned)(units * n_kv)), dim3(64 * kTileWaves), 0, s, a);
-        hipLaunchKernelGGL((k_pages_tile_merge<kDim, kBf16>), dim3(tile_parts(n_kv) / 2 * n_kv, kTileRows / 8), dim3(256), 0, s, a);
+        auto go = [&](auto waves) {
+            constexpr int kWaves = decltype(waves)::value;
+            const int64_t units = tile_slots(a.seqs.n_tokens, group, a.seqs.n_seqs, tile_rows(kWaves)) + tile_parts(n_kv, kWaves);
+            hipLaunchKernelGGL((k_pages_plan<kWaves>), dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1);
+            hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16, kWaves>), dim3((unsigned)(units * n_kv)), dim3(64 * kWaves), 0, s, a);
+            hipLaunchKernelGGL((k_pages_tile_merge<kDim, kBf16, kWaves>), dim3(tile_parts(n_kv, kWaves) / 2 * n_kv, tile_rows(kWaves) / 8), dim3(256), 0, s, a);
+        };
+        // (twelve waves of 4-bit rows of 128 values have too few registers)
+        if constexpr (kStore != SALI_STORE_INT4 || kDim == 64)
+            if (most_rows >= tile_rows(12) && (int64_t)a.seqs.n_tokens * group / tile_rows(12) * n_kv >= kLargeBlocks) {
+                go(std::integral_constant<int, 12>{});
+                return;
+            }
+        go(std::integral_constant<int, 4>{});
     }
 }
 

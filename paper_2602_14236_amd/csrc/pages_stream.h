@@ -466,16 +466,20 @@ void k_pages_stream(
             }
             stream_load_k<kStore, kDim>(next.b[0], next.b[1], lane, raw);
             // lane (row col, hh): tokens 8 (hh % 2) + 4 (hh / 2) .. + 3 of each block
-            const int t0 = j0 + 8 * (hh & 1) + 4 * (hh >> 1);
             const bool masked = now.live[0] < kBlockTokens || now.live[1] < kBlockTokens || partly_hidden(view, window, sinks, j0, kTileTokens);
             if (masked) {
+                // relative to the lane's first key, in place
+                int first_key = j0 + 8 * (hh & 1) + 4 * (hh >> 1);
+                asm volatile("" : "+v"(first_key));
 #pragma unroll
-                for (int c = 0; c < kSets; ++c)
+                for (int c = 0; c < kSets; ++c) {
+                    const Sight sight = sight_of(pos[c], first_key, window, sinks);
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (now.live[j] <= 0 || !sees(pos[c], t0 + 16 * j + r, window, sinks)) s2[c][j][r] = -INFINITY;
+                            if (now.live[j] <= 0 || !sight.has(16 * j + r)) s2[c][j][r] = -INFINITY;
+                }
             }
             u32x4 p[kSets];
 #pragma unroll
@@ -527,13 +531,13 @@ void k_pages_stream(
                     if (__builtin_amdgcn_ballot_w64(odd) != 0) {
                         u32x4 seen[kSets];
 #pragma unroll
-                        for (int c = 0; c < kSets; ++c)
+                        for (int c = 0; c < kSets; ++c) {
+                            const Sight sight = sight_of(pos[c], j0 + 16 * (hh >> 1) + 8 * (hh & 1), window, sinks);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int j = j0 + 16 * (hh >> 1) + 8 * (hh & 1) + 2 * e;
-                                seen[c][e] = (2 * e < live && sees(pos[c], j, window, sinks) ? (uint32_t)Num<kBf16>::kOne : 0u) |
-                                             (2 * e + 1 < live && sees(pos[c], j + 1, window, sinks) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
-                            }
+                            for (int e = 0; e < 4; ++e)
+                                seen[c][e] = (2 * e < live && sight.has(2 * e) ? (uint32_t)Num<kBf16>::kOne : 0u) |
+                                             (2 * e + 1 < live && sight.has(2 * e + 1) ? (uint32_t)Num<kBf16>::kOne << 16 : 0u);
+                        }
                         // through the wave's part of LDS, one product at a time: this path is not to cost registers
                         u32x4* const mine = reinterpret_cast<u32x4*>(&s_acc[wave][0][0]) + lane;
                         static_assert(kFs * 1024 <= sizeof(s_acc[0]), "the operands of a tile's V");

@@ -15,7 +15,6 @@ namespace sali {
 
 namespace {
 
-constexpr int kTileWaves = kTileRows / 32;
 constexpr int kPlanThreads = 1024;
 constexpr int kUnitBuckets = 64;
 
@@ -34,24 +33,26 @@ struct TileScratch {
     TileMerge* merges;
     TileUnit* units;
 };
-__host__ __device__ inline TileScratch tile_scratch(int32_t* records, int n_kv) {
+__host__ __device__ inline TileScratch tile_scratch(int32_t* records, int n_kv, int waves) {
     TileScratch t;
     t.plan = reinterpret_cast<TilePlan*>(records);
     t.merges = reinterpret_cast<TileMerge*>(t.plan + 1);
-    t.units = reinterpret_cast<TileUnit*>(t.merges + tile_parts(n_kv));
+    t.units = reinterpret_cast<TileUnit*>(t.merges + tile_parts(n_kv, waves));
     return t;
 }
 
 // one block
+template <int kWaves>
 __global__ __launch_bounds__(kPlanThreads) void k_pages_plan(PagesAttend a, int rows_min) {
     __shared__ int64_t s_sum[kPlanThreads / 64];
     __shared__ int s_longest[kPlanThreads / 64];
     __shared__ int s_count[kUnitBuckets], s_next[kUnitBuckets];
     __shared__ int s_parts, s_merges;
-    const TileScratch t = tile_scratch(a.records, a.geom.n_kv);
+    const TileScratch t = tile_scratch(a.records, a.geom.n_kv, kWaves);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t slots = tile_slots(a.seqs.n_tokens, a.group, a.seqs.n_seqs);
-    auto slot0 = [&](int s) -> int64_t { return (int64_t)max(0, a.seqs.start[s]) * a.group / kTileRows + s; };
+    constexpr int kTileRows = tile_rows(kWaves);
+    const int64_t slots = tile_slots(a.seqs.n_tokens, a.group, a.seqs.n_seqs, kTileRows);
+    auto slot0 = [&](int s) -> int64_t { return (int64_t)((uint32_t)min(max(0, a.seqs.start[s]), a.seqs.n_tokens) * (uint32_t)a.group / (uint32_t)kTileRows) + s; };
     // the unit of slot i before any cut
     auto whole = [&](int64_t i) -> TileUnit {
         int lo = 0, n = a.seqs.n_seqs;
@@ -67,9 +68,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan(PagesAttend a, int 
         TileUnit u = {lo, 0, 0, 0, -1, {0, 0, 0}};
         const PageSeq q = load_seq(a.seqs, a.geom, lo, true);
         const int64_t tile = i - slot0(lo);
-        if (tile < 0 || (int64_t)q.n * a.group < rows_min || tile * kTileRows >= (int64_t)q.n * a.group) return u;
+        if (tile < 0 || q.n * a.group < rows_min || tile * kTileRows >= (int64_t)q.n * a.group) return u;
         u.row_tile = (int)tile;
-        u.hi = view_of_rows(q, u.row_tile, a.group, a.window, a.sinks).tiles;
+        u.hi = view_of_rows<kWaves>(q, u.row_tile, a.group, a.window, a.sinks).tiles;
         return u;
     };
     if (threadIdx.x < kUnitBuckets) s_count[threadIdx.x] = 0;
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan(PagesAttend a, int 
         sum += s_sum[w];
         longest = max(longest, s_longest[w]);
     }
-    const int share = fair_share(sum, a.geom.n_kv);
+    const int share = fair_share(sum, tile_shares(a.geom.n_kv, kWaves));
     const int most = min(share, longest);                   // the longest unit after the cuts
     auto bucket_of = [&](int tiles) { return kUnitBuckets - 1 - min(kUnitBuckets - 1, (int)((int64_t)tiles * (kUnitBuckets - 1) / most)); };
     for (int64_t i = threadIdx.x; i < slots; i += kPlanThreads) {
@@ -247,18 +248,19 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int kStore, int kDim, bool kBf16>
+template <int kStore, int kDim, bool kBf16, int kTileWaves>
 __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(kStore == SALI_STORE_INT4 ? 2 : 3, 3))) void k_pages_tile(PagesAttend a) {
     constexpr int kSteps = kDim / 16, kDt = kDim / 32, kPitch = kDim + 4;
     constexpr int kBlock = 32 * kDim;                       // bytes of a block's K or V in LDS
-    __shared__ __align__(16) uint8_t s_k[2][2 * kBlock], s_v[2][2 * kBlock];
-    __shared__ int s_live[2][2];                            // of each block of 16 tokens: those that a row may see
+    constexpr int kTileRows = tile_rows(kTileWaves), kTileKeys = tile_keys(kTileWaves), kBlocks = kTileKeys / kBlockTokens;
+    __shared__ __align__(16) uint8_t s_k[2][kBlocks * kBlock], s_v[2][kBlocks * kBlock];
+    __shared__ int s_live[2][kBlocks];                            // of each block of 16 tokens: those that a row may see
     // 16-bit tiles that not all rows see whole: V's values that are not finite, +inf or NaN and -inf or NaN, a bit a token; of each wave's
     // share whether there are any
     __shared__ uint8_t s_up[2][kStore == SALI_STORE_16 ? kTileWaves : 1][kDim], s_down[2][kStore == SALI_STORE_16 ? kTileWaves : 1][kDim];
     __shared__ int s_odd[2][kTileWaves];
     __shared__ uint64_t s_found[2][kStore == SALI_STORE_16 ? 64 * kTileWaves : 1];
-    const TileScratch t = tile_scratch(a.records, a.geom.n_kv);
+    const TileScratch t = tile_scratch(a.records, a.geom.n_kv, kTileWaves);
     const int n_kv = a.geom.n_kv;
     const int nth = (int)(blockIdx.x / (uint32_t)n_kv), head = (int)blockIdx.x - nth * n_kv;
     if (nth >= t.plan->n_units) return;
@@ -267,7 +269,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     const int half = wave & 1;
     const int group = a.group;
     const PageSeq seq = load_seq(a.seqs, a.geom, unit.seq, false);
-    const View view = view_of_rows(seq, unit.row_tile, group, a.window, a.sinks);
+    const View view = view_of_rows<kTileWaves>(seq, unit.row_tile, group, a.window, a.sinks);
     const int32_t* table = a.seqs.table + (int64_t)unit.seq * a.seqs.width;
     const char* const heads = a.geom.pool + (uint64_t)head * a.geom.head_bytes;
     const uint32_t block_bytes = a.geom.head_bytes >> a.geom.blocks_log2;
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     // ---- the wave's share of the tiles: where tile i's block lies, and its tokens
     typedef TileRaw<kStore, kDim> Raw;
     Raw raw;
-    auto block_of = [&](int i) { return 2 * tile_at(view, i) + (wave >> 1); };
+    auto block_of = [&](int i) { return kBlocks * tile_at(view, i) + (wave >> 1); };
     // the pages from `page0` on, one a lane: their numbers, and which are none
     const int pages = (seq.len + (kBlockTokens << a.geom.blocks_log2) - 1) / (kBlockTokens << a.geom.blocks_log2);
     int page0 = -64;
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         s.block = heads + at + (uint32_t)(block & ((1 << a.geom.blocks_log2) - 1)) * block_bytes;
         return s;
     };
-    auto put_k = [&](int live, int buf) {
+    auto put_k = [&](int live, int buf, int lane) {
         tile_store_k<kStore, kDim, kBf16>(raw, half, lane, s_k[buf] + (wave >> 1) * kBlock);
         if (lane == 0 && half == 0) s_live[buf][wave >> 1] = live;
     };
@@ -350,20 +352,20 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
             if (lane == 0) s_odd[buf][wave] = any ? 1 : 0;
         }
     };
-    auto put_v = [&](int buf) { tile_store_v<kStore, kDim, kBf16>(raw, half, lane, s_v[buf] + (wave >> 1) * kBlock); };
+    auto put_v = [&](int buf, int lane) { tile_store_v<kStore, kDim, kBf16>(raw, half, lane, s_v[buf] + (wave >> 1) * kBlock); };
 
     Source next = source(unit.lo);
     tile_load_k<kStore, kDim>(next.block, half, lane, raw);
     tile_load_v<kStore, kDim>(next.block, half, lane, raw);
 
     // ---- the wave's rows
-    const int64_t row0 = (int64_t)unit.row_tile * kTileRows + wave * 32, rows = (int64_t)seq.n * group, r = row0 + col;
-    const int token = (int)(r / group), of_group = (int)(r - (int64_t)token * group);
+    const int row0 = unit.row_tile * kTileRows + wave * 32, rows = seq.n * group, r = row0 + col;
+    const int token = (int)((uint32_t)r / (uint32_t)group), of_group = r - token * group;
     const int pos = r < rows ? seq.len - seq.n + token : -1;
     const bool some = row0 < rows;                          // uniform over the wave
     View mine = view;
-    mine.first = seq.len - seq.n + (int)(row0 / group);
-    mine.last = seq.len - seq.n + (int)((least(rows, row0 + 32) - 1) / group);
+    mine.first = seq.len - seq.n + (int)((uint32_t)row0 / (uint32_t)group);
+    mine.last = seq.len - seq.n + (int)((uint32_t)(least(rows, row0 + 32) - 1) / (uint32_t)group);
     u32x4 q[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
@@ -386,21 +388,26 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     // a bit for every value of acc: infinities found, of either sign (in LDS, since there are hardly ever any)
     if constexpr (kStore == SALI_STORE_16) s_found[0][threadIdx.x] = s_found[1][threadIdx.x] = 0;
 
-    auto step = [&](int tile0, int buf) {
-        const uint8_t* const k = s_k[buf] + (col >> 4) * kBlock + (hh * 16 + (col & 15)) * 16;
-        const uint8_t* const v = s_v[buf] + (hh * kDim + col) * 16;
-        const int live_of_block = s_live[buf][lane & 1];
+    // 32 keys from j0 on, those of blocks 2 sub and 2 sub + 1 of the tile in `buf`
+    auto step = [&](int j0, int buf, int sub) {
+        const uint8_t* const k = s_k[buf] + (2 * sub + (col >> 4)) * kBlock + (hh * 16 + (col & 15)) * 16;
+        const uint8_t* const v = s_v[buf] + 2 * sub * kBlock + (hh * kDim + col) * 16;
+        const int live_of_block = s_live[buf][2 * sub + (lane & 1)];
         f32x16 st;
 #pragma unroll
         for (int x = 0; x < 16; ++x) st[x] = 0.0f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) st = Num<kBf16>::mma32(load16(k + s * 512), q[s], st);
         // lane (row col, hh): register x has token 8 hh + x % 8 of block x / 8
-        if (tile0 > seen_to || (tile0 < seen_from && tile0 > sunk_to) || __builtin_amdgcn_ballot_w64(live_of_block < kBlockTokens) != 0) {
+        if (j0 > seen_to || (j0 < seen_from && j0 > sunk_to) || __builtin_amdgcn_ballot_w64(live_of_block < kBlockTokens) != 0) {
             const int live0 = __builtin_amdgcn_readlane(live_of_block, 0), live1 = __builtin_amdgcn_readlane(live_of_block, 1);
+            // relative to the lane's first key, in place (sixteen positions of keys would be sixteen registers through the loop)
+            int first_key = j0 + 8 * hh;
+            asm volatile("" : "+v"(first_key));
+            const Sight sight = sight_of(pos, first_key, a.window, a.sinks);
 #pragma unroll
             for (int x = 0; x < 16; ++x)
-                if ((x < 8 ? live0 : live1) <= 0 || !sees(pos, tile0 + 16 * (x / 8) + 8 * hh + x % 8, a.window, a.sinks)) st[x] = -INFINITY;
+                if ((x < 8 ? live0 : live1) <= 0 || !sight.has(16 * (x / 8) + x % 8)) st[x] = -INFINITY;
         }
         float tops[4];
 #pragma unroll
@@ -432,30 +439,34 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     };
     auto look_for_odd = [&](int tile0, int buf) {
         if constexpr (kStore == SALI_STORE_16) {
-            const int there = s_odd[buf][lane % kTileWaves];
+            const int there = lane < kTileWaves ? s_odd[buf][lane] : 0;
             if (__builtin_amdgcn_ballot_w64(there != 0) == 0) return;
             uint64_t up = 0, down = 0;
+            int tid = threadIdx.x;
+            asm volatile("" : "+v"(tid));                   // worked out here, not kept in registers through the loop
+            const int at_hh = tid >> 5 & 1;
 #pragma unroll 1
             for (int w = 0; w < kTileWaves; ++w) {
                 if (s_odd[buf][w] == 0) continue;
+                const Sight sight = sight_of(pos, tile0 + 8 * w, a.window, a.sinks);
                 uint32_t seen = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) seen |= (sees(pos, tile0 + 8 * w + e, a.window, a.sinks) ? 1u : 0u) << e;
+                for (int e = 0; e < 8; ++e) seen |= (sight.has(e) ? 1u : 0u) << e;
 #pragma unroll 1
                 for (int x = 0; x < 16 * kDt; ++x) {
-                    const int d = 32 * (x >> 4) + 8 * (x >> 2 & 3) + 4 * hh + (x & 3);
+                    const int d = 32 * (x >> 4) + 8 * (x >> 2 & 3) + 4 * at_hh + (x & 3);
                     up |= (uint64_t)((s_up[buf][w][d] & seen) != 0) << x;
                     down |= (uint64_t)((s_down[buf][w][d] & seen) != 0) << x;
                 }
             }
-            s_found[0][threadIdx.x] |= up;
-            s_found[1][threadIdx.x] |= down;
+            s_found[0][tid] |= up;
+            s_found[1][tid] |= down;
         }
     };
 
-    put_k(next.live, 0);
+    put_k(next.live, 0, lane);
     clean_v(unit.lo, next.live, 0);
-    put_v(0);
+    put_v(0, lane);
     next = source(unit.lo + 1);
     tile_load_k<kStore, kDim>(next.block, half, lane, raw);
     tile_load_v<kStore, kDim>(next.block, half, lane, raw);
@@ -463,16 +474,21 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         const int buf = (i - unit.lo) & 1, tile0 = tile_at(view, i) * kTileKeys;
         lds_barrier();                                      // the tile is there, and all waves are through with the other buffer
         if (some && tile0 <= mine.last) {
-            step(tile0, buf);
+            step(tile0, buf, 0);
+            if constexpr (kBlocks > 2)
+#pragma unroll 1
+                for (int sub = 1; sub < kBlocks / 2 && tile0 + 32 * sub <= mine.last; ++sub) step(tile0 + 32 * sub, buf, sub);
             look_for_odd(tile0, buf);
         }
         if (i + 1 == unit.hi) break;
-        put_k(next.live, buf ^ 1);
+        int here = lane;                                    // addresses worked out again, not kept in registers through the step
+        asm volatile("" : "+v"(here));
+        put_k(next.live, buf ^ 1, here);
         clean_v(i + 1, next.live, buf ^ 1);
-        put_v(buf ^ 1);
+        put_v(buf ^ 1, here);
         next = source(i + 2);
-        tile_load_k<kStore, kDim>(next.block, half, lane, raw);
-        tile_load_v<kStore, kDim>(next.block, half, lane, raw);
+        tile_load_k<kStore, kDim>(next.block, half, here, raw);
+        tile_load_v<kStore, kDim>(next.block, half, here, raw);
     }
 
     // ---- results: lane (row col, hh) has values 32 d + 8 k + 4 hh .. + 3
@@ -481,9 +497,9 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     int there = lane;
     asm volatile("" : "+v"(there));
     const int end_col = there & 31, end_hh = there >> 5;
-    const int64_t end_r = row0 + end_col;
+    const int end_r = row0 + end_col;
     if (end_r >= rows) return;
-    const int end_token = (int)(end_r / group), end_of_group = (int)(end_r - (int64_t)end_token * group);
+    const int end_token = (int)((uint32_t)end_r / (uint32_t)group), end_of_group = end_r - end_token * group;
     if constexpr (kStore == SALI_STORE_16) {
         const uint64_t up = s_found[0][threadIdx.x], down = s_found[1][threadIdx.x];
         if ((up | down) != 0)
@@ -524,47 +540,65 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     if (end_hh == 0 && a.lse != nullptr) a.lse[row] = e.lse;
 }
 
-// Joins the parts of cut units: grid (merges * n_kv at most, kTileRows / 8), a row per 32 lanes
-template <int kDim, bool kBf16>
+// Joins the parts of cut units: grid (merges * n_kv at most, rows of a block / 8), a row per 32 lanes
+template <int kDim, bool kBf16, int kWaves>
 __global__ __launch_bounds__(256) void k_pages_tile_merge(PagesAttend a) {
-    constexpr int kPitch = kDim + 4, kPer = kDim / 32;
-    const TileScratch t = tile_scratch(a.records, a.geom.n_kv);
+    constexpr int kPitch = kDim + 4, kPer = kDim / 32, kTileRows = tile_rows(kWaves);
+    const TileScratch t = tile_scratch(a.records, a.geom.n_kv, kWaves);
     const int n_kv = a.geom.n_kv;
     const int nth = (int)(blockIdx.x / (uint32_t)n_kv), head = (int)blockIdx.x - nth * n_kv;
     if (nth >= t.plan->n_merges) return;
     const TileMerge rec = t.merges[nth];
     const PageSeq seq = load_seq(a.seqs, a.geom, rec.seq, false);
     const int in_tile = (int)blockIdx.y * 8 + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int64_t r = (int64_t)rec.row_tile * kTileRows + in_tile;
-    if (r >= (int64_t)seq.n * a.group) return;
+    const int r = rec.row_tile * kTileRows + in_tile;
+    if (r >= seq.n * a.group) return;
+    const int token = (int)((uint32_t)r / (uint32_t)a.group), h = head * a.group + (r - token * a.group);
+    const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
+    float pr[kPer];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) pr[x] = a.prior != nullptr ? a.prior[row * kDim + lane * kPer + x] : 0.0f;
+    constexpr int kFlight = 4;              // parts under way
+    const size_t step = (size_t)n_kv * kTileRows * kPitch;
+    const float* const first = a.partial + (((size_t)rec.part * n_kv + head) * kTileRows + in_tile) * kPitch;
     float m = -INFINITY, l = 0.0f, acc[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) acc[e] = 0.0f;
-#pragma unroll 4
-    for (int i = 0; i < rec.parts; ++i) {
-        const float* part = a.partial + (((size_t)(rec.part + i) * n_kv + head) * kTileRows + in_tile) * kPitch;
-        const float pm = part[0], pl = part[1];
-        float v[kPer];
+    for (int i0 = 0; i0 < rec.parts; i0 += kFlight) {
+        float2 ml[kFlight];
+        float v[kFlight][kPer];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) v[e] = part[4 + lane * kPer + e];
-        if (pl == 0.0f) continue;               // nothing seen
-        const float to = fmaxf(m, pm), by = __builtin_amdgcn_exp2f(m - to), pby = __builtin_amdgcn_exp2f(pm - to);
-        const bool none = l == 0.0f;
-        l = (none ? 0.0f : l * by) + pl * pby;
+        for (int i = 0; i < kFlight; ++i) {
+            const float* const part = first + step * (size_t)min(i0 + i, rec.parts - 1);
+            ml[i] = *reinterpret_cast<const float2*>(part);
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = (none ? 0.0f : acc[e] * by) + v[e] * pby;
+            for (int e = 0; e < kPer; ++e) v[i][e] = part[4 + lane * kPer + e];
+        }
+        float to = m;
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            if (i0 + i >= rec.parts) ml[i].y = 0.0f;
+            to = ml[i].y == 0.0f ? to : fmaxf(to, ml[i].x);         // 0: nothing seen
+        }
+        const float by = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m - to);
+        l = l == 0.0f ? 0.0f : l * by;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] = by == 0.0f ? 0.0f : acc[e] * by;
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const bool none = ml[i].y == 0.0f;
+            const float pby = none ? 0.0f : __builtin_amdgcn_exp2f(ml[i].x - to);
+            l += none ? 0.0f : ml[i].y * pby;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) acc[e] += pby == 0.0f ? 0.0f : v[i][e] * pby;
+        }
         m = to;
     }
-    const int token = (int)(r / a.group), h = head * a.group + (int)(r - (int64_t)token * a.group);
-    const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
     const RowEnd e = row_end(m, l, a, row);
     typename Num<kBf16>::T* out = reinterpret_cast<typename Num<kBf16>::T*>(a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes +
                                                                            (int64_t)h * a.out.head_bytes) + lane * kPer;
 #pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-        const float pr = a.prior != nullptr ? a.prior[row * kDim + lane * kPer + x] : 0.0f;
-        out[x] = (typename Num<kBf16>::T)joined(e, acc[x], pr);
-    }
+    for (int x = 0; x < kPer; ++x) out[x] = (typename Num<kBf16>::T)joined(e, acc[x], pr[x]);
     if (lane == 0 && a.lse != nullptr) a.lse[row] = e.lse;
 }
 

@@ -48,14 +48,14 @@ int main() {
             start[s + 1] = start[s] + fresh;
             len[s] = fresh + rand() %% 300;
         }
-        const int64_t tokens = start[n] + rand() %% 5, slots = tokens / kBlockTokens + 2ll * n, tiles = tile_slots(tokens, group, n);
+        const int64_t tokens = start[n] + rand() %% 5, slots = tokens / kBlockTokens + 2ll * n, rows = rand() %% 2 ? tile_rows(4) : tile_rows(12), tiles = tile_slots(tokens, group, n, rows);
         for (int s = 0; s < n; ++s) {
             const int fresh = start[s + 1] - start[s];
             const int blocks = fresh ? (len[s] - 1) / 16 - (len[s] - fresh) / 16 + 1 : 0;
             const int64_t end = first_slot(start[s], s) + blocks, next = s + 1 < n ? first_slot(start[s + 1], s + 1) : slots;
             if (end > next) { printf("blocks of sequence %%d\\n", s); return 1; }
-            const int64_t t0 = (int64_t)start[s] * group / kTileRows + s, mine = ((int64_t)fresh * group + kTileRows - 1) / kTileRows;
-            const int64_t t1 = s + 1 < n ? (int64_t)start[s + 1] * group / kTileRows + s + 1 : tiles;
+            const int64_t t0 = (int64_t)start[s] * group / rows + s, mine = ((int64_t)fresh * group + rows - 1) / rows;
+            const int64_t t1 = s + 1 < n ? (int64_t)start[s + 1] * group / rows + s + 1 : tiles;
             if (t0 + mine > t1) { printf("tiles of sequence %%d\\n", s); return 1; }
         }
     }
@@ -98,7 +98,11 @@ int check(int first, int last, int window, int sinks) {
         for (int part = 0; part < kTokens; part += 32) {
             bool all = true, any = false;
             for (int j = t * kTokens + part; j < t * kTokens + part + 32; ++j)
-                for (int p = first; p <= last; ++p) (sees(p, j, window, sinks) ? any : all) = sees(p, j, window, sinks);
+                for (int p = first; p <= last; ++p) {
+                    (sees(p, j, window, sinks) ? any : all) = sees(p, j, window, sinks);
+                    const int j0 = j - rand() %% 64;
+                    if (sight_of(p, j0, window, sinks).has(j - j0) != sees(p, j, window, sinks)) return 4;
+                }
             if (any && !times[t]) return 2;
             if (!all && !partly_hidden(v, window, sinks, t * kTokens + part, 32)) return 3;
         }
@@ -109,7 +113,7 @@ int main() {
     for (int round = 0; round < 1500; ++round) {
         const int first = rand() %% 400, last = first + (rand() %% 3 ? rand() %% 20 : rand() %% 200);
         const int window = rand() %% 4 ? rand() %% 150 + 1 : 0, sinks = window && rand() %% 3 ? rand() %% 140 : 0;
-        const int a = check<32>(first, last, window, sinks), b = check<64>(first, last, window, sinks);
+        const int a = check<32>(first, last, window, sinks), b = check<96>(first, last, window, sinks);
         if (a || b) { printf("%%d..%%d window %%d sinks %%d: %%d %%d\\n", first, last, window, sinks, a, b); return 1; }
     }
     return 0;
@@ -139,7 +143,7 @@ int main() {
         int64_t sum = 0;
         const int longest = rand() %% 3000 + 1;
         for (int& t : tiles) sum += t = rand() %% longest + 1;
-        const int share = fair_share(sum, n_kv);
+        const int waves = rand() %% 2 ? 4 : 12, share = fair_share(sum, tile_shares(n_kv, waves));
         int64_t cut = 0;
         for (int t : tiles) {
             const int parts = parts_of(t, share);
@@ -149,7 +153,7 @@ int main() {
                 if (lo >= hi || hi - lo > share) return 3;
             }
         }
-        if (cut > tile_parts(n_kv)) { printf("%%lld parts, room for %%d\\n", (long long)cut, tile_parts(n_kv)); return 4; }
+        if (cut > tile_parts(n_kv, waves)) { printf("%%lld parts, room for %%d\\n", (long long)cut, tile_parts(n_kv, waves)); return 4; }
     }
     return 0;
 }
