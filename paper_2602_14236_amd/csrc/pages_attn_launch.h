@@ -52,7 +52,7 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
         };
         // (twelve waves of 4-bit rows of 128 values have too few registers)
         if constexpr (kStore != SALI_STORE_INT4 || kDim == 64)
-            if (most_rows >= tile_rows(12) && (int64_t)a.seqs.n_tokens * group / tile_rows(12) * n_kv >= kLargeBlocks) {
+            if (most_rows >= tile_rows(12) && (int64_t)a.seqs.n_tokens * group / tile_rows(12) * n_kv >= (kStore == SALI_STORE_16 ? 2 : 1) * kComputeUnits) {
                 go(std::integral_constant<int, 12>{});
                 return;
             }

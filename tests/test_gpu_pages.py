@@ -240,6 +240,28 @@ def test_many_sequences(new):
     c.attend(new)
 
 
+@pytest.mark.parametrize("store,dtype,dim", FORMATS)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 5)])
+def test_chunks_that_fill_the_chip(store, dtype, dim, window, sinks):
+    """Rows enough for the large blocks: lengths around theirs, one history long enough to be cut, single tokens among them, a sequence without
+    pages, and in 16 bits values that are not finite among the last ones."""
+    n_kv, group = 8, 8
+    new = [(48 + s % 14, 48 + s % 14 + 5 * s * (s % 3)) for s in range(64)] + [(61, 400), (1, 90), (60, 60), (4, 300)]
+    c = Cache(op.PagesSpec(n_kv, n_kv * group, dim, 32, dtype, store), [t for _, t in new], 21, history=False)
+    if store == "16":
+        for s in (2, 17, 64):
+            for value in (math.inf, -math.inf, math.nan):
+                c.v[s][c.rng.integers(new[s][1] - 20, new[s][1]), c.rng.integers(n_kv), c.rng.integers(dim)] = value
+    c.write([(t, t) for _, t in new])
+    c.table[66] = -1
+    q, out, lse = c.attend(new, window=window, sinks=sinks, check=False)
+    some = (0, 2, 17, 64, 65, 66, 67)                        # (the oracle's time)
+    start = np.cumsum([0] + [n for n, _ in new])
+    at = torch.from_numpy(np.concatenate([np.arange(start[s], start[s + 1]) for s in some])).to(DEV)
+    c.k, c.v = [c.k[s] for s in some], [c.v[s] for s in some]
+    c.check([new[s] for s in some], q[at], out[at], lse[at], dim ** -0.5, window, sinks, hidden={5: np.ones(60, bool)})
+
+
 @pytest.mark.parametrize("scale", [0.3, -0.2, 0.0, 2.0])
 def test_scales(scale):
     for new in ([(1, 90), (4, 40)], [(90, 200)]):
