@@ -425,7 +425,7 @@ int sali_get_status(sali_ctx* ctx, uint32_t* h_flags, void* stream);
  *   d_start  int32[n_seqs + 1]  new tokens of sequence s are the rows d_start[s] .. d_start[s + 1] - 1 of every
  *                               per-token array of the call (queries, keys, values, outputs); d_start[0] = 0
  *   d_length int32[n_seqs]      tokens of the sequence, the new ones (its last) included
- *   d_table  int32[n_seqs][table_width]  page of tokens p * page_tokens .. of the sequence; not read past its length
+ *   d_table  int32[n_seqs][table_width]  page of tokens p * page_tokens .. of the sequence; entries past its length have no meaning
  *   n_tokens                    rows that the per-token arrays have, d_start[n_seqs] <= n_tokens (rows past it are untouched)
  *   max_q, max_kv               no sequence has more new tokens / more tokens than this
  * A sequence whose numbers contradict each other or these bounds (more new tokens than tokens, rows outside
@@ -515,7 +515,9 @@ int sali_pages_read(sali_pages* p, int32_t layer, const sali_page_batch* batch, 
  *                 keys together.  16-byte aligned.
  * Asynchronous on `stream`.  Calls on one object must not overlap each other (one area of partial results); calls on
  * different objects may share a pool.
- * SALI_ERR_CONFIG for a softmax_scale that is not finite, SALI_ERR_SHAPE for a layer, batch size, window or sinks out of range. */
+ * SALI_ERR_CONFIG for a softmax_scale that is not finite, SALI_ERR_SHAPE for a layer, batch size, window or sinks out of range; more sequences
+ * than pages or more new tokens than the pages hold are out of range, and so are 2^31 query rows (new tokens times queries of a K/V head)
+ * or tiles of 32 tokens (sequences times K/V heads times max_kv / 32). */
 int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, float softmax_scale,
                       int32_t window, int32_t sinks, const float* d_prior_or_null, const float* d_prior_lse_or_null,
                       const sali_rows* out, float* d_lse_or_null, void* stream);
