@@ -91,13 +91,34 @@ constexpr int tile_keys(int waves) { return 8 * waves; }
 
 // row tiles of a batch by slots, as those of blocks in append: sequence s owns the slots from first * group / rows + s on
 SALI_BOTH int64_t tile_slots(int64_t n_tokens, int group, int64_t n_seqs, int rows) { return n_tokens * group / rows + n_seqs; }
-// The whole work is cut into fair shares.  Units longer than one are cut, into at most twice as many parts as they have shares, so there are at
-// most tile_parts of them a head.
+// How the row tiles' work is shared out, one of two ways.
+// Shares: row tiles with more tiles of keys than a fair share of the whole are cut, into at most twice as many parts as they have shares, so there are
+// at most tile_parts of them a head; the pieces are then taken the longest first.
 SALI_BOTH int tile_shares(int n_kv, int waves) { return ((waves == 12 ? 256 : 512) + n_kv - 1) / n_kv; }
 SALI_BOTH int tile_parts(int n_kv, int waves) { return 2 * tile_shares(n_kv, waves); }
 // tiles of a share of `sum` tiles a head
 SALI_BOTH int fair_share(int64_t sum, int shares) { return (int)((most(sum, (int64_t)1) + shares - 1) / shares); }
 SALI_BOTH int parts_of(int tiles, int share) { return tiles > share ? (tiles + share - 1) / share : 1; }
+// Stretches: all tiles of keys of a head in a row, weighted by what they cost, are cut into equal stretches, one a block.
+SALI_BOTH int stretch_blocks(int in_flight, int n_kv) { return most(1, in_flight / n_kv); }
+// What a tile of keys costs a row tile of `rows` rows: bringing it in, and each wave's 32 rows (4, 8 and 12 waves of rows with 96 keys: 3.0, 5.0 and 5.3 us)
+SALI_BOTH int tile_weight(int rows) { return 7 + (rows + 31) / 32; }
+SALI_BOTH uint64_t stretch_length(uint64_t total, int blocks) { return most((total + (uint32_t)blocks - 1u) / (uint32_t)blocks, (uint64_t)(2 * (7 + 12))); }
+// A row tile with `tiles` tiles of keys of weight `weight`, from position `at` of the row on.  A tile of keys is of the stretch that its start lies in.
+struct TileSpan {
+    uint64_t at;
+    int32_t tiles, weight;
+    SALI_BOTH uint64_t end() const { return at + (uint64_t)((uint32_t)tiles * (uint32_t)weight); }
+    // tiles that start before position p
+    SALI_BOTH int before(uint64_t p) const {
+        if (p <= at) return 0;
+        return (int)(((uint32_t)(least(p, end()) - at) + (uint32_t)weight - 1u) / (uint32_t)weight);
+    }
+    SALI_BOTH int first_block(uint64_t length) const { return (int)(at / length); }
+    SALI_BOTH int last_block(uint64_t length) const { return (int)((at + (uint64_t)((uint32_t)(tiles - 1) * (uint32_t)weight)) / length); }
+};
+// The piece of row tile `unit` in block `block`: a block's pieces lie side by side.
+SALI_BOTH int stretch_piece(int unit, int block) { return unit + block; }
 
 // (rows of a batch are counted in 31 bits)
 template <int kWaves>

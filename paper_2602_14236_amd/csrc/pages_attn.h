@@ -250,6 +250,19 @@ __device__ __forceinline__ float joined(const RowEnd& e, float own, float prior)
     return e.by_prior == 0.0f ? a : __builtin_fmaf(prior, e.by_prior, a);
 }
 
+// The kernel's struct argument once more, which lies kAt bytes into its arguments: what is only needed in one place is not to take registers elsewhere
+template <int kAt>
+__device__ __forceinline__ PagesAttend late_arguments() {
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef const __attribute__((address_space(4))) char* Constant;
+    Constant p = (Constant)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const __attribute__((address_space(4))) PagesAttend*)(p + kAt);
+#else
+    return {};                              // the host's pass over this file
+#endif
+}
+
 }  // namespace
 
 }  // namespace sali

@@ -10,9 +10,8 @@ PagesScratch pages_scratch(int64_t n_pages, int page_tokens, int n_kv, int group
     const size_t row = (size_t)(dim + 4) * sizeof(float);
     size_t parts = (size_t)2 * kStreamMostBlocks * 32, records = (size_t)kStreamMostBlocks * sizeof(StreamRecord);
     for (int waves : {4, 12}) {
-        parts = max(parts, (size_t)tile_parts(n_kv, waves) * n_kv * tile_rows(waves));
-        const size_t units = (size_t)(tile_slots(n_pages * page_tokens, group, n_pages, tile_rows(waves)) + tile_parts(n_kv, waves));
-        records = max(records, sizeof(TilePlan) + (size_t)tile_parts(n_kv, waves) * sizeof(TileMerge) + units * sizeof(TileUnit));
+        parts = max(parts, (size_t)tile_parts(n_kv, waves) * n_kv * tile_rows(waves));       // stretches have as many at the most
+        records = max(records, tile_scratch_bytes(tile_slots(n_pages * page_tokens, group, n_pages, tile_rows(waves)), n_kv, waves));
     }
     PagesScratch p;
     p.partial = kPagesStatusBytes;

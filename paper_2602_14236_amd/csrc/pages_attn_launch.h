@@ -43,20 +43,36 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
         else go(std::integral_constant<int, 2>{});
     }
     if (most_rows > 32) {
-        auto go = [&](auto waves) {
+        auto go = [&](auto waves, int stretches) {
             constexpr int kWaves = decltype(waves)::value;
-            const int64_t units = tile_slots(a.seqs.n_tokens, group, a.seqs.n_seqs, tile_rows(kWaves)) + tile_parts(n_kv, kWaves);
-            hipLaunchKernelGGL((k_pages_plan<kWaves>), dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1);
-            hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16, kWaves>), dim3((unsigned)(units * n_kv)), dim3(64 * kWaves), 0, s, a);
-            hipLaunchKernelGGL((k_pages_tile_merge<kDim, kBf16, kWaves>), dim3(tile_parts(n_kv, kWaves) / 2 * n_kv, tile_rows(kWaves) / 8), dim3(256), 0, s, a);
+            const int64_t blocks = stretches > 0 ? stretches : tile_slots(a.seqs.n_tokens, group, a.seqs.n_seqs, tile_rows(kWaves)) + tile_parts(n_kv, kWaves);
+            const int merges = stretches > 0 ? stretches : tile_parts(n_kv, kWaves) / 2;
+            if (kWaves == 12 && stretches > 0) hipLaunchKernelGGL((k_pages_plan_stretches<12>), dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1, stretches);
+            else hipLaunchKernelGGL((k_pages_plan_shares<kWaves>), dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1);
+            hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16, kWaves>), dim3((unsigned)(blocks * n_kv)), dim3(64 * kWaves), 0, s, a);
+            hipLaunchKernelGGL((k_pages_tile_merge<kDim, kBf16, kWaves>), dim3(merges * n_kv, tile_rows(kWaves) / 8), dim3(256), 0, s, a);
         };
-        // (twelve waves of 4-bit rows of 128 values have too few registers)
-        if constexpr (kStore != SALI_STORE_INT4 || kDim == 64)
-            if (most_rows >= tile_rows(12) && (int64_t)a.seqs.n_tokens * group / tile_rows(12) * n_kv >= (kStore == SALI_STORE_16 ? 2 : 1) * kComputeUnits) {
-                go(std::integral_constant<int, 12>{});
+        // Three ways, by how many blocks of 384 rows there are and how many tiles of 96 keys each sees (us, this one against the next best):
+        //   few blocks of many tiles   stretches, since whole ones would leave most of the chip idle and cut ones end at different times.  Not for
+        //                              short ones: the partial results at the ends of 256 stretches take 20 to 40.  1024 new of 12000 tokens, 32 heads
+        //                              over 8, 229 against 291; 512 of 4100, 32 heads, 75 and 81; 2048 new ones alone 96 and 80
+        //   two rounds of blocks       384 rows in shares.  16 bits: 8192 new ones 582, with 128 rows 628; 4096 (1.3 rounds) 206 and 199.
+        //                              Quantised from one round on, since a key is dequantised a third as often: 4096 206 and 219, 2048 95 and 89
+        //   else                       128 rows in shares
+        // (Twelve waves of 4-bit rows of 128 values have too few registers.)
+        if constexpr (kStore != SALI_STORE_INT4 || kDim == 64) {
+            const int64_t reach = a.window > 0 ? min((int64_t)a.seqs.max_kv, (int64_t)a.window + a.sinks) : (int64_t)a.seqs.max_kv - a.seqs.max_q / 2;
+            const int64_t rows = (int64_t)a.seqs.n_tokens * group, units = rows / tile_rows(12), tiles = reach / tile_keys(12), blocks = stretch_blocks(kComputeUnits, n_kv);
+            if (most_rows >= tile_rows(12) && 10 * units <= 7 * blocks && (tiles - 16) * rows >= 4 * blocks * tile_rows(12)) {
+                go(std::integral_constant<int, 12>{}, (int)blocks);
                 return;
             }
-        go(std::integral_constant<int, 4>{});
+            if (most_rows >= tile_rows(12) && units * n_kv >= (kStore == SALI_STORE_16 ? 2 : 1) * kComputeUnits) {
+                go(std::integral_constant<int, 12>{}, 0);
+                return;
+            }
+        }
+        go(std::integral_constant<int, 4>{}, 0);
     }
 }
 

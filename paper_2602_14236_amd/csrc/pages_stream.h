@@ -252,20 +252,9 @@ __device__ __forceinline__ void join_parts(const PagesAttend& a, const StreamRec
     }
 }
 
-// The kernel's last struct argument once more, for the end of a segment: what is only needed there is not to take registers before
-// (kStreamArgsAt bytes of leading arguments; alignment 8)
+// bytes of the kernel's leading arguments, where its struct lies
 constexpr int kStreamArgsAt = 3 * 8 + 10 * 4;
 static_assert(kStreamArgsAt % alignof(PagesAttend) == 0, "where the struct lies");
-__device__ __forceinline__ PagesAttend late_arguments() {
-#ifdef __HIP_DEVICE_COMPILE__
-    typedef const __attribute__((address_space(4))) char* Constant;
-    Constant p = (Constant)__builtin_amdgcn_kernarg_segment_ptr();
-    asm volatile("" : "+s"(p));
-    return *(const __attribute__((address_space(4))) PagesAttend*)(p + kStreamArgsAt);
-#else
-    return {};                              // the host's pass over this file
-#endif
-}
 
 // What a block works on.
 //   pairs: grid (K/V heads, sequences), a block the one pair; for short sequences, where parts and their joining would cost more than they bring
@@ -333,7 +322,7 @@ void k_pages_stream(
         if (bad && blockIdx.x == 0 && wave == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
         blocks = max(1u, min(gridDim.x, total / (uint32_t)min_tiles));
         if (blockIdx.x >= blocks || total == 0) {
-            if (threadIdx.x == 0) reinterpret_cast<StreamRecord*>(late_arguments().records)[blockIdx.x] = record;
+            if (threadIdx.x == 0) reinterpret_cast<StreamRecord*>(late_arguments<kStreamArgsAt>().records)[blockIdx.x] = record;
             return;
         }
         const Stretches cut(total, blocks);
@@ -599,7 +588,7 @@ void k_pages_stream(
                 for (int e = 0; e < 4; ++e) s_acc[wave][r][stream_v_value<kStore>(f, 4 * (tid >> 4 & 3) + e)] = acc[c][f][e];
         }
         __syncthreads();
-        const PagesAttend b = late_arguments();
+        const PagesAttend b = late_arguments<kStreamArgsAt>();
         const bool whole = todo == view.tiles;
         const int slot = 2 * (int)blockIdx.x + (first_segment ? 0 : 1);
         for (int idx = tid; idx < rows * (kDim / 4); idx += 64 * kStreamWaves) {
@@ -657,7 +646,7 @@ void k_pages_stream(
             }
         }
     }
-    if (threadIdx.x == 0) reinterpret_cast<StreamRecord*>(late_arguments().records)[blockIdx.x] = record;
+    if (threadIdx.x == 0) reinterpret_cast<StreamRecord*>(late_arguments<kStreamArgsAt>().records)[blockIdx.x] = record;
 }
 
 // Joins the parts of the pairs, four rows a block: grid (blocks of the stream, rows / 4)

@@ -124,7 +124,7 @@ int main() {
 @pytest.mark.parametrize("seed", range(3))
 def test_stretches_and_shares(tmp_path, seed):
     """Equal stretches cover the tiles and every tile knows its block; parts of cut units cover them, are no longer than a share and no more
-    than there is room for."""
+    than there is room for; stretches of weighted row tiles cover them, every block of a cut one has tiles of it, and a block's pieces lie side by side."""
     run_pages_program(tmp_path, """
 int main() {
     srand(%d);
@@ -154,6 +154,36 @@ int main() {
             }
         }
         if (cut > tile_parts(n_kv, waves)) { printf("%%lld parts, room for %%d\\n", (long long)cut, tile_parts(n_kv, waves)); return 4; }
+    }
+    for (int round = 0; round < 1000; ++round) {
+        const int n_kv = rand() %% 3 ? 1 << rand() %% 7 : rand() %% 900 + 1, units = rand() %% 400 + 1, blocks = stretch_blocks(256, n_kv);
+        if (blocks < 1 || (blocks > 1 && blocks * n_kv > 256)) return 5;
+        std::vector<TileSpan> spans;
+        uint64_t total = 0;
+        const int longest = rand() %% 4 ? rand() %% 300 + 1 : 60000000;
+        for (int u = 0; u < units; ++u) {
+            spans.push_back({total, rand() %% longest + 1, tile_weight(rand() %% 384 + 1)});
+            total = spans.back().end();
+        }
+        const uint64_t length = stretch_length(total, blocks);
+        int block = 0, piece = -1, parts = 0, merges = 0;   // those so far
+        for (int u = 0; u < units; ++u) {
+            const TileSpan& x = spans[u];
+            const int first = x.first_block(length), last = x.last_block(length);
+            if (first < block || first > block + 1 || last >= blocks) return 6;
+            int next = 0;                                   // of the unit's tiles
+            for (int b = first; b <= last; ++b) {
+                const int lo = x.before(b * length), hi = x.before((b + 1) * length), own = stretch_piece(u, b);
+                if (lo != next || hi <= lo) return 7;       // every block of the unit has tiles of it
+                next = hi;
+                if (own <= piece || (b == block && u > 0 && own != piece + 1) || own >= units + blocks) return 8;
+                piece = own;
+                block = b;
+            }
+            if (next != x.tiles) return 9;
+            if (last > first) ++merges, parts += last - first + 1;
+        }
+        if (merges > blocks || parts > tile_parts(n_kv, 12)) return 10;
     }
     return 0;
 }
