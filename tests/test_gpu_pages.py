@@ -262,6 +262,27 @@ def test_chunks_that_fill_the_chip(store, dtype, dim, window, sinks):
     c.check([new[s] for s in some], q[at], out[at], lse[at], dim ** -0.5, window, sinks, hidden={5: np.ones(60, bool)})
 
 
+@pytest.mark.parametrize("store,dtype,dim", [("16", "fp16", 64), ("16", "bf16", 128), ("int8", "fp16", 128), ("int8", "bf16", 64), ("int4", "fp16", 64)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2350, 5)])
+def test_few_chunks_of_long_texts(store, dtype, dim, window, sinks):
+    """Few row tiles that see many keys, whose work is cut into stretches: ends of stretches inside row tiles, single tokens among them, pages
+    that are none, and in 16 bits values that are not finite.  (One K/V head in sixty-four is compared.)"""
+    n_kv, group, head = 64, 16, 37
+    new = [(29, 2400), (1, 900), (25, 1200), (2, 70)]
+    c = Cache(op.PagesSpec(n_kv, n_kv * group, dim, 64, dtype, store), [t for _, t in new], 22, history=False)
+    if store == "16":
+        for s in (0, 2):
+            for value in (math.inf, -math.inf, math.nan):
+                c.v[s][c.rng.integers(new[s][1] - 20, new[s][1]), head, c.rng.integers(dim)] = value
+    c.write([(t, t) for _, t in new])
+    c.table[0, 3] = c.table[2, 18] = -1
+    q, out, lse = c.attend(new, window=window, sinks=sinks, check=False)
+    hidden = {s: np.arange(new[s][1]) // 64 == page for s, page in ((0, 3), (2, 18))}
+    c.k, c.v = [k[:, head:head + 1] for k in c.k], [v[:, head:head + 1] for v in c.v]
+    mine = slice(head * group, (head + 1) * group)
+    c.check(new, q[:, mine], out[:, mine], lse[:, mine], dim ** -0.5, window, sinks, hidden=hidden)
+
+
 @pytest.mark.parametrize("scale", [0.3, -0.2, 0.0, 2.0])
 def test_scales(scale):
     for new in ([(1, 90), (4, 40)], [(90, 200)]):
