@@ -10,6 +10,8 @@
 // (K), so the block is turned over in LDS between 16-byte accesses on both sides: its rows (or their codes), padded so that a column's
 // reads fall on different banks.  Codes are made and expanded on the side of the rows, where a group lies in four adjacent lanes.
 // Blocks that the new tokens do not fill are written value by value, so that no byte of another token is touched.
+// Measured: 2048 tokens of 32 heads in 16 bits, written and read back, 134 MB in 25 us (the caches hold them); in 4 bits 1.37 GB in 280 to 296 us, 4.6 to
+// 4.9 TB/s, the rate of a large copy.
 
 #include <algorithm>
 #include <type_traits>
@@ -23,7 +25,9 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kEnoughBlocks = 4096;         // of 256 threads: twice what the compute units hold
+// Blocks of 256 threads, twice what the compute units hold: where there are more, a block takes several heads, the next one's data on its way meanwhile.
+// Three texts of 12001 tokens, 40 heads, written in 4 bits and read back: 296 us, a head a block 380; 32 single tokens 8.1 us, always eight heads a block 19.
+constexpr int kEnoughBlocks = 4096;
 
 template <bool kBf16>
 struct Half;

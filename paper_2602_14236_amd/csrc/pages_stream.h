@@ -8,6 +8,10 @@
 // blocks have the same number of tiles, give or take one.  A block's stretch may end inside one pair of sequence and head and hold
 // whole ones; its waves split each such segment, meet in LDS, and leave a result (whole pairs) or a partial one, of which a block has
 // at most two, at its ends.  A second launch joins a pair's partial results.
+//
+// Measured: one token over 131072 keys, 8 heads of 128 values in 16 bits, 537 MB in 95 us, 5.6 TB/s (a copy of 2 GiB: 4.9); 48 sequences of up to 8192
+// keys in 8 bits 95 us, 5.2 TB/s.  4 bits are bound by the vector instructions that unpack them, 790 a tile: 16 sequences under a window of 4096
+// keys 41 us, 2.3 TB/s.  Short texts are bound by the chain of a launch, the lengths, the page table, K, V and the joining of the waves: 10.4 us for 777 keys.
 #pragma once
 
 #include "pages_attn.h"
@@ -257,11 +261,13 @@ constexpr int kStreamArgsAt = 3 * 8 + 10 * 4;
 static_assert(kStreamArgsAt % alignof(PagesAttend) == 0, "where the struct lies");
 
 // What a block works on.
-//   pairs: grid (K/V heads, sequences), a block the one pair; for short sequences, where parts and their joining would cost more than they bring
+//   pairs: grid (K/V heads, sequences), a block the one pair; for short sequences, where parts and their joining would cost more than they bring.
+//          us of pairs and of stretches: 8 sequences of 300 keys, 32 heads, 10.4 and 17.6; 1 of 1000, 8 heads, 10.4 and 12.1; 1 of 4000, 8 heads, 20.7
+//          and 15.8; 64 of 300, 32 heads, 89 and 66
 //   stretches: of all tiles; a launch of its own joins the parts of cut pairs (k_pages_stream_merge)
 enum class StreamMode { pairs, stretches };
 // Waves of a block, and waves a SIMD that their registers leave room for.  Stretches: small blocks, several of which share a compute unit, so that one
-// walks on while another is between two pairs.
+// walks on while another is between two pairs: 48 sequences in 8 bits 95 us, with one block of eight waves a compute unit 116.
 constexpr int stream_waves(StreamMode mode) { return mode == StreamMode::pairs ? 8 : 4; }
 constexpr int stream_occupancy(int store, int sets, StreamMode mode) { return store != SALI_STORE_16 && sets == 1 && mode == StreamMode::stretches ? 3 : 2; }
 

@@ -1,12 +1,20 @@
 // Attention of many new tokens a sequence (chunks of prompts, whole prompts): tiles of rows on the matrix cores.
 //
-// A block takes 128 rows of one sequence and K/V head, 32 a wave, and walks the keys they see, 32 at a time.  The keys are brought
-// into LDS once for all waves (dequantised on the way, in the order of the operands) while those before are worked on; a wave
-// multiplies them with its rows, whose queries stay in registers.
+// A block takes a row tile, 384 or 128 rows of one sequence and K/V head, 32 a wave, and walks the keys they see, 96 or 32 at a time.  The
+// keys are brought into LDS once for all waves (dequantised on the way, in the order of the operands) while those before are worked on; a
+// wave multiplies them with its rows, whose queries stay in registers.
 //
-// The causal triangle, windows and ragged batches make blocks of very different length: a planning launch of one block writes the
-// units (rows and a range of key tiles), the longest first, and cuts the keys of those that are longer than a fair share of the whole; the
-// parts of a cut unit leave partial results that a merge launch joins.
+// The causal triangle, windows and ragged batches make row tiles of very different length.  A planning launch of one block writes the pieces
+// that blocks take: in shares, the longest first, with the keys of those cut that are longer than a fair share of the whole; or in
+// stretches, all keys of all row tiles in a row and cut evenly, a block a compute unit (pages_attn_launch.h says which when).  The parts
+// of a cut row tile leave partial results that a merge launch joins.
+//
+// What bounds it.  A wave's 32 rows and 32 keys of 128 values are 16 products of 32x32x16 (512 cycles of the matrix cores), the softmax's
+// vector instructions and 16 KB from LDS.  Matrix products and LDS reads alone ran at 1235 TFLOP/s (a large library product: 1372), with
+// the softmax 1010, with keys brought in through registers 945 to 958: 8192 causal tokens, 32 heads over 8 of 128 values in 574 to 581 us.  Three
+// waves a SIMD hide one wave's softmax behind the others' products (one wave alone issues a vector instruction every 6.4 cycles,
+// several together one every 3); blocks in lockstep of product and softmax phases were slower, 683 to 740 us.  32 rows a wave, since 64
+// take more than the 168 registers that three waves leave each.
 #pragma once
 
 #include "pages_attn.h"
@@ -16,7 +24,6 @@ namespace sali {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-
 constexpr int kUnitBuckets = 64;
 constexpr int kTileMostBlocks = 256;        // of a head in stretches
 constexpr int kTileMostMerges = 1024;
@@ -72,7 +79,7 @@ __device__ __forceinline__ TileUnit tile_unit(const PagesAttend& a, int rows_min
     return u;
 }
 
-// The plan in shares, one block
+// The plan in shares, one block (5 to 8 us: a few trips to memory one after the other)
 template <int kWaves>
 __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend a, int rows_min) {
     __shared__ int64_t s_sum[kPlanThreads / 64];
@@ -153,7 +160,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
     }
 }
 
-// The plan in stretches, `blocks` of a head; one block
+// The plan in stretches, `blocks` of a head; one block (5 to 6 us)
 template <int kWaves>
 __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_stretches(PagesAttend a, int rows_min, int blocks) {
     __shared__ uint64_t s_weight[kPlanThreads / 64];
@@ -230,7 +237,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_stretches(PagesAtte
     }
 }
 
-// ---- bringing 32 keys into LDS: two blocks of 16 tokens, each in the layout of 16-bit blocks (K [D / 8][place][8], V [2][D][8])
+// ---- bringing keys into LDS: blocks of 16 tokens, each in the layout of 16-bit blocks (K [D / 8][place][8], V [2][D][8]), two waves a block
 // Wave w has half w % 2 of block w / 2: half of K's pieces, and of V's those of tokens 8 (w % 2) .. + 7.
 template <int kStore, int kDim>
 struct TileRaw {
@@ -342,6 +349,7 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// (4 bits: two waves a SIMD, as the unpacking takes more registers)
 template <int kStore, int kDim, bool kBf16, int kTileWaves>
 __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(kStore == SALI_STORE_INT4 ? 2 : 3, 3))) void k_pages_tile(PagesAttend args) {
     constexpr int kSteps = kDim / 16, kDt = kDim / 32, kPitch = kDim + 4;
@@ -613,50 +621,51 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         const int end_col = there & 31, end_hh = there >> 5;
         const int end_r = row0 + end_col;
         if (end_r < rows) {
-        const int end_token = (int)((uint32_t)end_r / (uint32_t)b.group), end_of_group = end_r - end_token * b.group;
-        if constexpr (kStore == SALI_STORE_16) {
-            const uint64_t up = s_found[0][thread], down = s_found[1][thread];
-            if ((up | down) != 0)
+            const int end_token = (int)((uint32_t)end_r / (uint32_t)b.group), end_of_group = end_r - end_token * b.group;
+            if constexpr (kStore == SALI_STORE_16) {
+                const uint64_t up = s_found[0][thread], down = s_found[1][thread];
+                if ((up | down) != 0)
+#pragma unroll
+                    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) acc[d][x] += found((up >> (16 * d + x) & 1) != 0, (down >> (16 * d + x) & 1) != 0);
+            }
+            if (part_of_piece >= 0) {
+                float* part = b.partial + (((size_t)part_of_piece * b.geom.n_kv + head) * kTileRows + (size_t)(wave * 32 + end_col)) * kPitch;
+                if (end_hh == 0) {
+                    part[0] = m;
+                    part[1] = sum;
+                }
 #pragma unroll
                 for (int d = 0; d < kDt; ++d)
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) acc[d][x] += found((up >> (16 * d + x) & 1) != 0, (down >> (16 * d + x) & 1) != 0);
-        }
-        if (part_of_piece >= 0) {
-            float* part = b.partial + (((size_t)part_of_piece * b.geom.n_kv + head) * kTileRows + (size_t)(wave * 32 + end_col)) * kPitch;
-            if (end_hh == 0) {
-                part[0] = m;
-                part[1] = sum;
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<f32x4*>(part + 4 + 32 * d + 8 * k + 4 * end_hh) = (f32x4){acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
+            } else {
+                const int h = head * b.group + end_of_group;
+                const int64_t row = (int64_t)(seq.first + end_token) * b.heads + h;
+                const RowEnd e = row_end(m, sum, b, row);
+                char* const out = b.out.d + (int64_t)(seq.first + end_token) * b.out.token_bytes + (int64_t)h * b.out.head_bytes;
+#pragma unroll
+                for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        f32x4 pr = {0.0f, 0.0f, 0.0f, 0.0f};
+                        const int at = 32 * d + 8 * k + 4 * end_hh;
+                        if (b.prior != nullptr) pr = *reinterpret_cast<const f32x4*>(b.prior + row * kDim + at);
+                        float o[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) o[x] = joined(e, acc[d][4 * k + x], pr[x]);
+                        *reinterpret_cast<u32x2*>(out + 2 * at) = (u32x2){pack2<kBf16>(o[0], o[1]), pack2<kBf16>(o[2], o[3])};
+                    }
+                if (end_hh == 0 && b.lse != nullptr) b.lse[row] = e.lse;
             }
-#pragma unroll
-            for (int d = 0; d < kDt; ++d)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    *reinterpret_cast<f32x4*>(part + 4 + 32 * d + 8 * k + 4 * end_hh) = (f32x4){acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
-        } else {
-        const int h = head * b.group + end_of_group;
-        const int64_t row = (int64_t)(seq.first + end_token) * b.heads + h;
-        const RowEnd e = row_end(m, sum, b, row);
-        char* const out = b.out.d + (int64_t)(seq.first + end_token) * b.out.token_bytes + (int64_t)h * b.out.head_bytes;
-#pragma unroll
-        for (int d = 0; d < kDt; ++d)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                f32x4 pr = {0.0f, 0.0f, 0.0f, 0.0f};
-                const int at = 32 * d + 8 * k + 4 * end_hh;
-                if (b.prior != nullptr) pr = *reinterpret_cast<const f32x4*>(b.prior + row * kDim + at);
-                float o[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) o[x] = joined(e, acc[d][4 * k + x], pr[x]);
-                *reinterpret_cast<u32x2*>(out + 2 * at) = (u32x2){pack2<kBf16>(o[0], o[1]), pack2<kBf16>(o[2], o[3])};
-            }
-        if (end_hh == 0 && b.lse != nullptr) b.lse[row] = e.lse;
-        }
         }
     }
 }
 
-// Joins the parts of cut units: grid (merges * n_kv at most, rows of a block / 8), a row per 32 lanes
+// Joins the parts of cut row tiles: grid (merges * n_kv at most, rows of a block / 8), a row per 32 lanes.  Bound by the bytes of the partial results: 11 us
+// for 512 rows by 4100 keys, 32 heads of 128 values in stretches
 template <int kDim, bool kBf16, int kWaves>
 __global__ __launch_bounds__(256) void k_pages_tile_merge(PagesAttend a) {
     constexpr int kPitch = kDim + 4, kPer = kDim / 32, kTileRows = tile_rows(kWaves);
