@@ -18,7 +18,13 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
     // Rows of a sequence that the stream takes at most.  In a batch that has longer sequences: those of single tokens.  (Up to 32 rows against the tiles' 128, us:
     // 32 rows over 8192 keys, 8 heads, 40 and 70; 24 over 512, 32 heads, 14 and 26; 32 over 4096, 32 heads, 47 and 38.)
     int stream_rows = most_rows <= 16 ? 16 : 32;
-    if (most_rows > 32) stream_rows = a.seqs.n_seqs == 1 || group > 32 ? 0 : (group <= 16 ? 16 : 32);
+    if (most_rows > 32) {
+        stream_rows = group <= 16 ? 16 : 32;
+        // None if the batch has no such sequence as far as its sizes tell (one of them would leave the batch short of so many tokens; if there is one all the
+        // same, because rows past the batch were counted, it is the tiles').  Two chunks of 1024 tokens under a window: 85 us, with the stream's empty launches 89.
+        const int64_t short_of = (int64_t)a.seqs.n_seqs * a.seqs.max_q - a.seqs.n_tokens;
+        if (a.seqs.n_seqs == 1 || group > 32 || short_of < a.seqs.max_q - stream_rows / group) stream_rows = 0;
+    }
     if (stream_rows > 0) {
         const int64_t reach = a.window > 0 ? (int64_t)a.window + a.seqs.max_q + a.sinks + 3 * kTileTokens : (int64_t)a.seqs.max_kv + kTileTokens;
         const int64_t tiles = min((int64_t)a.seqs.max_kv + kTileTokens, reach) / kTileTokens * a.seqs.n_seqs * n_kv;
