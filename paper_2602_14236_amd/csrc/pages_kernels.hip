@@ -62,6 +62,17 @@ __device__ __forceinline__ uint32_t quad_move(uint32_t v) { return (uint32_t)__b
 template <int kCtrl>
 __device__ __forceinline__ float quad_move(float v) { return __builtin_bit_cast(float, quad_move<kCtrl>(__builtin_bit_cast(uint32_t, v))); }
 constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E;                 // quad_perm [1,0,3,2], [2,3,0,1]
+constexpr int kFirst = 0x00, kSecond = 0x55, kThird = 0xAA, kFourth = 0xFF;     // [n,n,n,n]
+
+// is one of the eight values infinite or NaN?  (An exponent of all ones and one more carries into the sign's place.)
+template <bool kBf16>
+__device__ __forceinline__ bool not_finite(const u32x4& v) {
+    constexpr uint32_t kExponents = Half<kBf16>::kExponent * 0x10001u, kOnes = (0x8000u - Half<kBf16>::kExponent) * 0x10001u;
+    return ((((v.x & kExponents) + kOnes) | ((v.y & kExponents) + kOnes) | ((v.z & kExponents) + kOnes) | ((v.w & kExponents) + kOnes)) & 0x80008000u) != 0u;
+}
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
+}
 
 // the last sequence whose first slot is not past `slot`; all 64 lanes of a wave, 64 candidates a look
 __device__ __forceinline__ int seq_of_slot(const PageSeqs& q, int64_t slot) {
@@ -145,73 +156,80 @@ __global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs,
     for (int head = w.head; head < w.heads_end; ++head) {
         char* const block = w.block + (uint64_t)head * g.head_bytes;
         if (head > w.head) __syncthreads();                     // the head before is out of LDS
+        constexpr int kOwn = kItems / 256;
+        if constexpr (kStore == SALI_STORE_16) {
 #pragma unroll
-        for (int i = 0; i < kItems / 256; ++i) {
-            const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces;
-            if constexpr (kStore == SALI_STORE_16) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) bad |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent;
+            for (int i = 0; i < kOwn; ++i) {
+                const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces;
+                bad |= not_finite<kBf16>(x[i].u);
                 *reinterpret_cast<u32x4*>(s_rows + row * R::kPitch + c * 16) = x[i].u;
-            } else {
-                float f[8];
+            }
+        } else {
+            constexpr float kSteps = kStore == SALI_STORE_INT8 ? 127.0f : 15.0f;
+            float f[kOwn][8], m[kOwn], low[kOwn];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = (float)x[i].h[e];
-                float m, low = 0.0f;
-                constexpr float kSteps = kStore == SALI_STORE_INT8 ? 127.0f : 15.0f;
+            for (int i = 0; i < kOwn; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[i][e] = (float)x[i].h[e];
+                low[i] = 0.0f;
                 if constexpr (kStore == SALI_STORE_INT8) {
-                    m = fabsf(f[0]);
+                    float top = fabsf(f[i][0]);
 #pragma unroll
-                    for (int e = 1; e < 8; ++e) m = fmaxf(m, fabsf(f[e]));
-                    m = fmaxf(m, quad_move<kSwap1>(m));
-                    m = fmaxf(m, quad_move<kSwap2>(m));
+                    for (int e = 1; e < 8; ++e) top = fmaxf(top, fabsf(f[i][e]));
+                    top = fmaxf(top, quad_move<kSwap1>(top));
+                    m[i] = fmaxf(top, quad_move<kSwap2>(top));
                 } else {
-                    float high = f[0];
-                    low = f[0];
+                    float least = f[i][0], high = f[i][0];
 #pragma unroll
                     for (int e = 1; e < 8; ++e) {
-                        low = fminf(low, f[e]);
-                        high = fmaxf(high, f[e]);
+                        least = fminf(least, f[i][e]);
+                        high = fmaxf(high, f[i][e]);
                     }
-                    low = fminf(low, quad_move<kSwap1>(low));
-                    low = fminf(low, quad_move<kSwap2>(low));
+                    least = fminf(least, quad_move<kSwap1>(least));
+                    least = fminf(least, quad_move<kSwap2>(least));
                     high = fmaxf(high, quad_move<kSwap1>(high));
                     high = fmaxf(high, quad_move<kSwap2>(high));
                     // rounding keeps the order of numbers, so the largest of the rounded differences is this one
-                    m = high - low;
+                    m[i] = high - least;
+                    low[i] = least;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] = f[e] - low;
+                    for (int e = 0; e < 8; ++e) f[i][e] = f[i][e] - least;
                 }
-                float inv = kSteps / m;
-                // a group with an infinity or NaN, or one too wide or too small for fp32 steps, is stored as zeros: every value of the pages is finite
-                uint32_t odd = 0u;
+            }
+            // one division for the quad's four (two groups' steps / m and m / steps): a lane has one of them
+            const float of = (threadIdx.x & 2) != 0 ? m[kOwn - 1] : m[0];
+            const float quotient = (threadIdx.x & 1) != 0 ? of / kSteps : kSteps / of;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) odd |= (x[i].b16[e] & Half<kBf16>::kExponent) == Half<kBf16>::kExponent ? 1u : 0u;
-                odd |= m <= 3.402823466e38f ? 0u : 1u;
+            for (int i = 0; i < kOwn; ++i) {
+                const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces;
+                const float inv = i == 0 ? quad_move<kFirst>(quotient) : quad_move<kThird>(quotient);
+                const float step = i == 0 ? quad_move<kSecond>(quotient) : quad_move<kFourth>(quotient);
+                // a group with an infinity or NaN, or one too wide or too small for fp32 steps, is stored as zeros: every value of the pages is finite
+                uint32_t odd = not_finite<kBf16>(x[i].u) || !(m[i] <= 3.402823466e38f) ? 1u : 0u;
                 odd |= quad_move<kSwap1>(odd);
                 odd |= quad_move<kSwap2>(odd);
                 bad |= odd != 0u;
-                const bool some = odd == 0u && m > 0.0f && inv <= 3.402823466e38f;
-                const float scale = some ? m / kSteps : 0.0f;
-                inv = some ? inv : 0.0f;
+                const bool some = odd == 0u && m[i] > 0.0f && inv <= 3.402823466e38f;
                 if ((c & 3) == 0) {
-                    s_scale[row * R::kGroups + c / 4] = scale;
+                    s_scale[row * R::kGroups + c / 4] = some ? step : 0.0f;
                     if constexpr (kStore == SALI_STORE_INT4) {
                         Piece<kBf16> z;
-                        z.h[0] = (typename Half<kBf16>::type)(odd == 0u ? low : 0.0f);       // exact: one of the values
+                        z.h[0] = (typename Half<kBf16>::type)(odd == 0u ? low[i] : 0.0f);       // exact: one of the values
                         s_low[row * R::kGroups + c / 4] = z.b16[0];
                     }
                 }
-                Piece<kBf16> code;
+                // |f| <= m, so the products lie within the steps (give or take a rounding) and need no clamp; adding 1.5 2^23 rounds to the nearest
+                // even whole number and leaves it in the low byte, in two's complement
+                uint32_t q[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float q = some ? fminf(fmaxf(rintf(f[e] * inv), kStore == SALI_STORE_INT8 ? -kSteps : 0.0f), kSteps) : 0.0f;
-                    code.b8[e] = (uint8_t)(int)q;
-                }
+                for (int e = 0; e < 8; ++e) q[e] = __builtin_bit_cast(uint32_t, f[i][e] * inv + 12582912.0f);
+                const uint32_t keep = some ? 0xFFFFFFFFu : 0u;
+                const u32x2 code = {low_bytes(q[0], q[1], q[2], q[3]) & keep, low_bytes(q[4], q[5], q[6], q[7]) & keep};
                 if constexpr (kStore == SALI_STORE_INT8) {
-                    *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + c * 8) = (u32x2){code.u.x, code.u.y};
+                    *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + c * 8) = code;
                 } else {
                     // lanes 0, 1 of a quad hold values 0 .. 15 of the group, lanes 2, 3 the others, which go to the high halves of the same bytes
-                    const uint32_t a = quad_move<kSwap2>(code.u.x) << 4 | code.u.x, b = quad_move<kSwap2>(code.u.y) << 4 | code.u.y;
+                    const uint32_t a = quad_move<kSwap2>(code.x) << 4 | code.x, b = quad_move<kSwap2>(code.y) << 4 | code.y;
                     if ((c & 2) == 0) *reinterpret_cast<u32x2*>(s_rows + row * R::kPitch + (c / 4) * 16 + (c & 1) * 8) = (u32x2){a, b};
                 }
             }
