@@ -283,6 +283,29 @@ def test_few_chunks_of_long_texts(store, dtype, dim, window, sinks):
     c.check(new, q[:, mine], out[:, mine], lse[:, mine], dim ** -0.5, window, sinks, hidden=hidden)
 
 
+@pytest.mark.parametrize("store", ["16", "int8", "int4"])
+def test_rows_past_a_batch_that_has_single_tokens(store):
+    """So many rows past the batch that its sizes look like those of chunks alone."""
+    new = [(70, 90), (1, 40), (68, 100)]
+    c = Cache(op.PagesSpec(2, 4, 64, 16, "fp16", store), [t for _, t in new], 23)
+    q, out, lse = c.attend(new, room=69)
+    assert bool((out[139:] == 7).all()) and bool((lse[139:] == 7).all())
+
+
+@pytest.mark.parametrize("store,pages", [("16", 9000), ("int4", 30000)])
+def test_pools_past_32_bits(store, pages):
+    """The second layer of a pool of 17 GB and more, pages spread all over it."""
+    new = [(1, 700), (70, 3000), (3, 1000)]
+    c = Cache(op.PagesSpec(8, 8, 128, 256, "bf16", store), [t for _, t in new], 24, layers=2, layer=1, extra_pages=pages)
+    assert c.pages.pool.numel() > 4 << 32
+    c.attend(new)
+    back = torch.empty((74, 2, 8, 128), dtype=torch.bfloat16, device=DEV)
+    c.pages.read(1, c.batch(new), back[:, 0], back[:, 1])
+    for i, rows_of_seq in enumerate((c.k, c.v)):
+        exp = np.concatenate([op.read_back(bits_of(r[t - n:t]), c.spec) for r, (n, t) in zip(rows_of_seq, new)])
+        assert np.array_equal(bits_of(back[:, i]), exp)
+
+
 @pytest.mark.parametrize("scale", [0.3, -0.2, 0.0, 2.0])
 def test_scales(scale):
     for new in ([(1, 90), (4, 40)], [(90, 200)]):
