@@ -57,7 +57,7 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
             if (kWaves == 12 && stretches > 0) hipLaunchKernelGGL((k_pages_plan_stretches<12>), dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1, stretches);
             else hipLaunchKernelGGL((k_pages_plan_shares<kWaves>), dim3(1), dim3(kPlanThreads), 0, s, a, stream_rows + 1);
             hipLaunchKernelGGL((k_pages_tile<kStore, kDim, kBf16, kWaves>), dim3((unsigned)(blocks * n_kv)), dim3(64 * kWaves), 0, s, a);
-            hipLaunchKernelGGL((k_pages_tile_merge<kDim, kBf16, kWaves>), dim3(merges * n_kv, tile_rows(kWaves) / 8), dim3(256), 0, s, a);
+            hipLaunchKernelGGL((k_pages_tile_merge<kDim, kBf16, kWaves>), dim3(merges * n_kv, kWaves * (kDim / 32) / 4), dim3(256), 0, s, a);
         };
         // Three ways, by how many blocks of 384 rows there are and how many tiles of 96 keys each sees (us, this one against the next best):
         //   few blocks of many tiles   stretches, since whole ones would leave most of the chip idle and cut ones end at different times.  Not for

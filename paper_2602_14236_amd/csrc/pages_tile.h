@@ -631,16 +631,15 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
                         for (int x = 0; x < 16; ++x) acc[d][x] += found((up >> (16 * d + x) & 1) != 0, (down >> (16 * d + x) & 1) != 0);
             }
             if (part_of_piece >= 0) {
-                float* part = b.partial + (((size_t)part_of_piece * b.geom.n_kv + head) * kTileRows + (size_t)(wave * 32 + end_col)) * kPitch;
-                if (end_hh == 0) {
-                    part[0] = m;
-                    part[1] = sum;
-                }
+                // as the lanes have them, side by side: the rows' references and sums, then 16 bytes a lane
+                float* const part = b.partial + ((size_t)part_of_piece * b.geom.n_kv + head) * (kTileRows * kPitch);
+                if (end_hh == 0) *reinterpret_cast<float2*>(part + 2 * (wave * 32 + end_col)) = make_float2(m, sum);
+                f32x4* const values = reinterpret_cast<f32x4*>(part + 4 * kTileRows) + wave * (kDt * 4 * 64) + there;
 #pragma unroll
                 for (int d = 0; d < kDt; ++d)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        *reinterpret_cast<f32x4*>(part + 4 + 32 * d + 8 * k + 4 * end_hh) = (f32x4){acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
+                        values[(4 * d + k) * 64] = (f32x4){acc[d][4 * k], acc[d][4 * k + 1], acc[d][4 * k + 2], acc[d][4 * k + 3]};
             } else {
                 const int h = head * b.group + end_of_group;
                 const int64_t row = (int64_t)(seq.first + end_token) * b.heads + h;
@@ -664,40 +663,43 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     }
 }
 
-// Joins the parts of cut row tiles: grid (merges * n_kv at most, rows of a block / 8), a row per 32 lanes.  Bound by the bytes of the partial results: 11 us
-// for 512 rows by 4100 keys, 32 heads of 128 values in stretches
+// Joins the parts of cut row tiles: grid (merges * n_kv at most, a block's waves of 32 rows and 32 values / 4), a lane as in the tile's results.  Bound by the
+// bytes of the partial results: 13 us for 512 rows by 4100 keys, 32 heads of 128 values in stretches (48 MB)
 template <int kDim, bool kBf16, int kWaves>
 __global__ __launch_bounds__(256) void k_pages_tile_merge(PagesAttend a) {
-    constexpr int kPitch = kDim + 4, kPer = kDim / 32, kTileRows = tile_rows(kWaves);
+    constexpr int kPitch = kDim + 4, kDt = kDim / 32, kTileRows = tile_rows(kWaves);
     const TileScratch& t = *reinterpret_cast<const TileScratch*>(a.records);
     const int n_kv = a.geom.n_kv;
     const int nth = (int)(blockIdx.x / (uint32_t)n_kv), head = (int)blockIdx.x - nth * n_kv;
     if (nth >= t.plan.n_merges) return;
     const TileMerge rec = t.merges[nth];
     const PageSeq seq = load_seq(a.seqs, a.geom, rec.seq, false);
-    const int in_tile = (int)blockIdx.y * 8 + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int r = rec.row_tile * kTileRows + in_tile;
+    const int at_wave = (int)blockIdx.y * 4 + (int)(threadIdx.x >> 6), wave = at_wave / kDt, d = at_wave % kDt, lane = threadIdx.x & 63, hh = lane >> 5;
+    const int in_tile = wave * 32 + (lane & 31), r = rec.row_tile * kTileRows + in_tile;
     if (r >= seq.n * a.group) return;
     const int token = (int)((uint32_t)r / (uint32_t)a.group), h = head * a.group + (r - token * a.group);
     const int64_t row = (int64_t)(seq.first + token) * a.heads + h;
-    float pr[kPer];
+    f32x4 pr[4];
 #pragma unroll
-    for (int x = 0; x < kPer; ++x) pr[x] = a.prior != nullptr ? a.prior[row * kDim + lane * kPer + x] : 0.0f;
-    constexpr int kFlight = 4;              // parts under way
+    for (int k = 0; k < 4; ++k)
+        pr[k] = a.prior != nullptr ? *reinterpret_cast<const f32x4*>(a.prior + row * kDim + 32 * d + 8 * k + 4 * hh) : (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kFlight = 3;              // parts under way
     const size_t step = (size_t)n_kv * kTileRows * kPitch;
-    const float* const first = a.partial + (((size_t)rec.part * n_kv + head) * kTileRows + in_tile) * kPitch;
-    float m = -INFINITY, l = 0.0f, acc[kPer];
+    const float* const first = a.partial + ((size_t)rec.part * n_kv + head) * (kTileRows * kPitch);
+    const int values = 4 * kTileRows + 4 * ((wave * kDt + d) * (4 * 64) + lane);
+    float m = -INFINITY, l = 0.0f;
+    f32x4 acc[4];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) acc[e] = 0.0f;
+    for (int k = 0; k < 4; ++k) acc[k] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
     for (int i0 = 0; i0 < rec.parts; i0 += kFlight) {
         float2 ml[kFlight];
-        float v[kFlight][kPer];
+        f32x4 v[kFlight][4];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const float* const part = first + step * (size_t)min(i0 + i, rec.parts - 1);
-            ml[i] = *reinterpret_cast<const float2*>(part);
+            ml[i] = *reinterpret_cast<const float2*>(part + 2 * in_tile);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) v[i][e] = part[4 + lane * kPer + e];
+            for (int k = 0; k < 4; ++k) v[i][k] = *reinterpret_cast<const f32x4*>(part + values + k * 256);
         }
         float to = m;
 #pragma unroll
@@ -708,23 +710,31 @@ __global__ __launch_bounds__(256) void k_pages_tile_merge(PagesAttend a) {
         const float by = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m - to);
         l = l == 0.0f ? 0.0f : l * by;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = by == 0.0f ? 0.0f : acc[e] * by;
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[k][e] = by == 0.0f ? 0.0f : acc[k][e] * by;
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const bool none = ml[i].y == 0.0f;
             const float pby = none ? 0.0f : __builtin_amdgcn_exp2f(ml[i].x - to);
             l += none ? 0.0f : ml[i].y * pby;
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) acc[e] += pby == 0.0f ? 0.0f : v[i][e] * pby;
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[k][e] += pby == 0.0f ? 0.0f : v[i][k][e] * pby;
         }
         m = to;
     }
     const RowEnd e = row_end(m, l, a, row);
-    typename Num<kBf16>::T* out = reinterpret_cast<typename Num<kBf16>::T*>(a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes +
-                                                                           (int64_t)h * a.out.head_bytes) + lane * kPer;
+    char* const out = a.out.d + (int64_t)(seq.first + token) * a.out.token_bytes + (int64_t)h * a.out.head_bytes;
 #pragma unroll
-    for (int x = 0; x < kPer; ++x) out[x] = (typename Num<kBf16>::T)joined(e, acc[x], pr[x]);
-    if (lane == 0 && a.lse != nullptr) a.lse[row] = e.lse;
+    for (int k = 0; k < 4; ++k) {
+        float o[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[x] = joined(e, acc[k][x], pr[k][x]);
+        *reinterpret_cast<u32x2*>(out + 2 * (32 * d + 8 * k + 4 * hh)) = (u32x2){pack2<kBf16>(o[0], o[1]), pack2<kBf16>(o[2], o[3])};
+    }
+    if (d == 0 && hh == 0 && a.lse != nullptr) a.lse[row] = e.lse;
 }
 
 }  // namespace
