@@ -13,8 +13,8 @@
 //
 // Masked keys.  Scores outside a row's view become -inf, whatever they were, and their weights 0.  A weight of 0 does not take
 // out an infinity or NaN in V.  What no token has written (past a sequence's end, pages that are none) is set to zero before the product, by
-// position; quantised values are finite wherever they were written.  16-bit rows are looked at in tiles that are not wholly in view
-// of all rows: values that are not finite are set to zero for the product, two more products count, for every output, the
+// position; quantised values are finite wherever they were written.  16-bit rows are looked at, in tiles (of rows) where they are not wholly in view
+// of all rows, in the stream always: values that are not finite are set to zero for the product, two more products count, for every output, the
 // infinities of each sign in its view (a NaN counts for both), and what was found is added to the result at the end.
 #pragma once
 

@@ -476,7 +476,8 @@ void k_pages_stream(
                             if (now.live[j] <= 0 || !sight.has(16 * j + r)) s2[c][j][r] = -INFINITY;
                 }
             }
-            u32x4 p[kSets];
+            // the weights in two 16-bit numbers each, what the first one's rounding leaves in the second: the matrix cores have time for both
+            u32x4 p[kSets], p_rest[kSets];
 #pragma unroll
             for (int c = 0; c < kSets; ++c) {
                 float top = fmaxf(fmaxf(fmaxf(s2[c][0][0], s2[c][0][1]), fmaxf(s2[c][0][2], s2[c][0][3])),
@@ -491,7 +492,7 @@ void k_pages_stream(
                     m[c] = to;
                 }
                 const float ref = m[c] == -INFINITY ? 0.0f : m[c];
-                uint32_t w[2][2];
+                uint32_t w[2][2], rest[2][2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     float e[4];
@@ -500,15 +501,22 @@ void k_pages_stream(
                         e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s2[c][j][r], a.scale2, -ref));
                         l[c] += e[r];
                     }
-                    w[j][0] = pack2<kBf16>(e[0], e[1]);
-                    w[j][1] = pack2<kBf16>(e[2], e[3]);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        w[j][r] = pack2<kBf16>(e[2 * r], e[2 * r + 1]);
+                        rest[j][r] = pack2<kBf16>(e[2 * r] - low_half<kBf16>(w[j][r]), e[2 * r + 1] - high_half<kBf16>(w[j][r]));
+                    }
                 }
                 // to the lanes that hold the same tokens of V: quarter hh takes tokens 8 (hh % 2) .. + 7 of block hh / 2
                 const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
                 const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
                 p[c] = (u32x4){(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]};
+                const auto xr = __builtin_amdgcn_permlane32_swap(rest[0][0], rest[1][0], false, false);
+                const auto yr = __builtin_amdgcn_permlane32_swap(rest[0][1], rest[1][1], false, false);
+                p_rest[c] = (u32x4){(uint32_t)xr[0], (uint32_t)yr[0], (uint32_t)xr[1], (uint32_t)yr[1]};
             }
-            if (masked) {
+            // (16 bits: every tile, since what the second weight is multiplied with has to be finite in all of them)
+            if (masked || kStore == SALI_STORE_16) {
                 const int live = (hh < 2 ? now.live[0] : now.live[1]) - 8 * (hh & 1);
                 if constexpr (kStore != SALI_STORE_16) {
 #pragma unroll
@@ -520,7 +528,7 @@ void k_pages_stream(
                     bool odd = false;
 #pragma unroll
                     for (int f = 0; f < kFs; ++f) {
-                        raw.v[f] = live_tokens(raw.v[f], live);
+                        if (masked) raw.v[f] = live_tokens(raw.v[f], live);
                         odd |= any_not_finite<kBf16>(raw.v[f]);
                     }
                     if (__builtin_amdgcn_ballot_w64(odd) != 0) {
@@ -563,7 +571,7 @@ void k_pages_stream(
             for (int f = 0; f < kFs; ++f) {
                 const u32x4 vf = stream_v<kStore, kDim, kBf16>(raw, f);
 #pragma unroll
-                for (int c = 0; c < kSets; ++c) acc[c][f] = Num<kBf16>::mma16(vf, p[c], acc[c][f]);
+                for (int c = 0; c < kSets; ++c) acc[c][f] = Num<kBf16>::mma16(vf, p_rest[c], Num<kBf16>::mma16(vf, p[c], acc[c][f]));
             }
             stream_load_v<kStore, kDim>(next.b[0], next.b[1], lane, raw);
             now = next;
