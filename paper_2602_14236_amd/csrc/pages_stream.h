@@ -9,9 +9,9 @@
 // whole ones; its waves split each such segment, meet in LDS, and leave a result (whole pairs) or a partial one, of which a block has
 // at most two, at its ends.  A second launch joins a pair's partial results.
 //
-// Measured: one token over 131072 keys, 8 heads of 128 values in 16 bits, 537 MB in 95 us, 5.6 TB/s (a copy of 2 GiB: 4.9); 48 sequences of up to 8192
-// keys in 8 bits 95 us, 5.2 TB/s.  4 bits are bound by the vector instructions that unpack them, 790 a tile: 16 sequences under a window of 4096
-// keys 41 us, 2.3 TB/s.  Short texts are bound by the chain of a launch, the lengths, the page table, K, V and the joining of the waves: 10.4 us for 777 keys.
+// Measured: one token over 131072 keys, 8 heads of 128 values in 16 bits, 537 MB in 96 us, 5.6 TB/s (a copy of 2 GiB: 4.9); 48 sequences of up to 8192
+// keys in 8 bits 97 us, 5.1 TB/s.  4 bits are bound by the vector instructions that unpack them, 790 a tile: 16 sequences under a window of 4096
+// keys 42 us, 2.2 TB/s.  Short texts are bound by the chain of a launch, the lengths, the page table, K, V and the joining of the waves: 10.4 us for 777 keys.
 #pragma once
 
 #include "pages_attn.h"
@@ -525,12 +525,14 @@ void k_pages_stream(
                         if constexpr (kStore == SALI_STORE_INT4) raw.vz[g] = (lane & 7) < live ? raw.vz[g] : 0;
                     }
                 } else {
-                    bool odd = false;
+                    // the matrix cores look: 0 times an infinity or NaN is a NaN, the sum of all others times 0 is 0
+                    f32x4 zeros = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int f = 0; f < kFs; ++f) {
                         if (masked) raw.v[f] = live_tokens(raw.v[f], live);
-                        odd |= any_not_finite<kBf16>(raw.v[f]);
+                        zeros = Num<kBf16>::mma16(raw.v[f], (u32x4){0u, 0u, 0u, 0u}, zeros);
                     }
+                    const bool odd = !((zeros[0] + zeros[1]) + (zeros[2] + zeros[3]) == 0.0f);
                     if (__builtin_amdgcn_ballot_w64(odd) != 0) {
                         u32x4 seen[kSets];
 #pragma unroll
