@@ -10,8 +10,8 @@
 // (K), so the block is turned over in LDS between 16-byte accesses on both sides: its rows (or their codes), padded so that a column's
 // reads fall on different banks.  Codes are made and expanded on the side of the rows, where a group lies in four adjacent lanes.
 // Blocks that the new tokens do not fill are written value by value, so that no byte of another token is touched.
-// Measured: 2048 tokens of 32 heads in 16 bits, written and read back, 134 MB in 25 us (the caches hold them); in 4 bits 1.37 GB in 280 to 296 us, 4.6 to
-// 4.9 TB/s, the rate of a large copy.
+// Measured: 2048 tokens of 32 heads in 16 bits, written and read back, 134 MB in 25 us (the caches hold them); three of 12001 and
+// 40 heads in 4 bits 1.37 GB in 229 us, 6.0 TB/s (a copy of 2 GiB through the caches: 4.9).
 
 #include <algorithm>
 #include <type_traits>
@@ -26,8 +26,12 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 // Blocks of 256 threads, twice what the compute units hold: where there are more, a block takes several heads, the next one's data on its way meanwhile.
-// Three texts of 12001 tokens, 40 heads, written in 4 bits and read back: 296 us, a head a block 380; 32 single tokens 8.1 us, always eight heads a block 19.
+// Three texts of 12001 tokens, 40 heads, written in 4 bits and read back, through the caches: 296 us, a head a block 380; 32 single tokens 8.1 us, always eight heads a block 19.
 constexpr int kEnoughBlocks = 4096;
+// Bytes of rows, half of what the last cache holds, from which on they go past the caches: longer ones would only push each other out.  Written and read back, us with and
+// without: 10000 tokens of 32 heads (164 MB) 105 and 132 in 16 bits, 83 and 96 in 4, three texts of 12001 tokens and 40 heads in 4 bits 229 and 292; 4096 of 32 heads
+// (67 MB) 46 and 43.
+constexpr int64_t kPastCaches = 128 << 20;
 
 template <bool kBf16>
 struct Half;
@@ -129,7 +133,8 @@ struct Rows {
     static constexpr int kGroups = kDim / kGroup;
 };
 
-template <int kStore, int kDim, bool kBf16>
+// kOnce: see kPastCaches
+template <int kStore, int kDim, bool kBf16, bool kOnce>
 __global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs, RowsIn k, RowsIn v, int heads_each) {
     typedef Rows<kStore, kDim> R;
     constexpr int kPieces = kDim / 8, kItems = 32 * kPieces;            // 16-byte pieces of a row, of all rows
@@ -147,8 +152,10 @@ __global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs,
             const int item = (int)threadIdx.x + 256 * i, row = item / kPieces, c = item % kPieces, t = row & 15;
             const RowsIn& in = row < 16 ? k : v;
             x[i].u = (u32x4){0u, 0u, 0u, 0u};
-            if (t >= w.t0 && t < w.t1)
-                x[i].u = *reinterpret_cast<const u32x4*>(in.d + (int64_t)(w.row0 + t) * in.token_bytes + (int64_t)head * in.head_bytes + c * 16);
+            if (t < w.t0 || t >= w.t1) continue;
+            const u32x4* const from = reinterpret_cast<const u32x4*>(in.d + (int64_t)(w.row0 + t) * in.token_bytes + (int64_t)head * in.head_bytes + c * 16);
+            if constexpr (kOnce) x[i].u = __builtin_nontemporal_load(from);
+            else x[i].u = *from;
         }
     };
     ask(w.head);
@@ -286,7 +293,8 @@ __global__ __launch_bounds__(256) void k_pages_append(PageGeom g, PageSeqs seqs,
     if (bad) atomicOr(seqs.status, SALI_FAULT_NONFINITE);
 }
 
-template <int kStore, int kDim, bool kBf16>
+// kOnce: see kPastCaches
+template <int kStore, int kDim, bool kBf16, bool kOnce>
 __global__ __launch_bounds__(256) void k_pages_read(PageGeom g, PageSeqs seqs, RowsOut k, RowsOut v, int heads_each) {
     typedef Rows<kStore, kDim> R;
     typedef typename Half<kBf16>::type T;
@@ -393,7 +401,9 @@ __global__ __launch_bounds__(256) void k_pages_read(PageGeom g, PageSeqs seqs, R
                 }
             }
             const RowsOut& out = row < 16 ? k : v;
-            *reinterpret_cast<u32x4*>(out.d + (int64_t)(w.row0 + t) * out.token_bytes + (int64_t)head * out.head_bytes + c * 16) = o.u;
+            u32x4* const to = reinterpret_cast<u32x4*>(out.d + (int64_t)(w.row0 + t) * out.token_bytes + (int64_t)head * out.head_bytes + c * 16);
+            if constexpr (kOnce) __builtin_nontemporal_store(o.u, to);
+            else *to = o.u;
         }
     }
 }
@@ -418,28 +428,39 @@ hipError_t by_type(int dtype, int store, int dim, const F& go) {
 // walks several heads has the next one's data on its way meanwhile.
 struct Shares {
     int heads_each;
+    bool once;
     dim3 grid;
 };
-Shares shares(const PageGeom& g, const PageSeqs& q) {
+Shares shares(const PageGeom& g, const PageSeqs& q, int dim) {
     const int64_t slots = q.n_tokens / kBlockTokens + 2ll * q.n_seqs;
     const int64_t most = slots * g.n_kv / kEnoughBlocks;
     const int each = (int)std::max<int64_t>(1, std::min<int64_t>(most, std::min(g.n_kv, 8)));
-    return {each, dim3((unsigned)slots, (unsigned)((g.n_kv + each - 1) / each))};
+    return {each, 4ll * dim * g.n_kv * q.n_tokens >= kPastCaches, dim3((unsigned)slots, (unsigned)((g.n_kv + each - 1) / each))};
 }
 
 }  // namespace
 
 hipError_t launch_pages_append(int dtype, int store, int dim, const PageGeom& g, const PageSeqs& seqs, const RowsIn& k, const RowsIn& v, hipStream_t s) {
-    const Shares sh = shares(g, seqs);
+    const Shares sh = shares(g, seqs, dim);
     return by_type(dtype, store, dim, [&](auto bf16, auto st, auto d) {
-        hipLaunchKernelGGL((k_pages_append<decltype(st)::value, decltype(d)::value, decltype(bf16)::value>), sh.grid, dim3(256), 0, s, g, seqs, k, v, sh.heads_each);
+        auto go = [&](auto once) {
+            hipLaunchKernelGGL((k_pages_append<decltype(st)::value, decltype(d)::value, decltype(bf16)::value, decltype(once)::value>), sh.grid, dim3(256), 0, s, g, seqs, k, v,
+                               sh.heads_each);
+        };
+        if (sh.once) go(std::true_type{});
+        else go(std::false_type{});
     });
 }
 
 hipError_t launch_pages_read(int dtype, int store, int dim, const PageGeom& g, const PageSeqs& seqs, const RowsOut& k, const RowsOut& v, hipStream_t s) {
-    const Shares sh = shares(g, seqs);
+    const Shares sh = shares(g, seqs, dim);
     return by_type(dtype, store, dim, [&](auto bf16, auto st, auto d) {
-        hipLaunchKernelGGL((k_pages_read<decltype(st)::value, decltype(d)::value, decltype(bf16)::value>), sh.grid, dim3(256), 0, s, g, seqs, k, v, sh.heads_each);
+        auto go = [&](auto once) {
+            hipLaunchKernelGGL((k_pages_read<decltype(st)::value, decltype(d)::value, decltype(bf16)::value, decltype(once)::value>), sh.grid, dim3(256), 0, s, g, seqs, k, v,
+                               sh.heads_each);
+        };
+        if (sh.once) go(std::true_type{});
+        else go(std::false_type{});
     });
 }
 

@@ -167,6 +167,41 @@ def test_rows_read_back(store, dtype, dim, page, heads):
     assert c.pages.get_status() == 0
 
 
+@pytest.mark.parametrize("store,dtype,dim", [("16", "fp16", 64), ("int8", "bf16", 128), ("int4", "fp16", 128), ("int4", "bf16", 64)])
+def test_long_batches(store, dtype, dim):
+    """More rows than go through the caches, several heads a block: a few of them by their values, all by what two halves of the batch give."""
+    heads = 40
+    lengths = [(1 << 25) // (heads * dim) + 37, 90]
+    c = Cache(op.PagesSpec(heads, heads, dim, 64, dtype, store), [70, 90], 25, history=False)
+    n = sum(lengths)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    kv = torch.randn((n, 2, heads, dim), generator=g, device=DEV).to(TORCH[dtype])
+    cfg = c.b.make_pages_config(n_kv_heads=heads, n_heads=heads, head_dim=dim, page_tokens=64, n_pages=sum(-(-x // 64) for x in lengths), dtype=TORCH[dtype], store=store)
+    width = -(-lengths[0] // 64)
+    table = np.full((2, width), -1, np.int32)
+    table[0] = np.arange(width)[::-1] + 2
+    table[1, :2] = [1, 0]
+    whole, halves = (c.b.SaliPages(cfg, DEV) for _ in range(2))
+    for p in (whole, halves):
+        p.pool.fill_(0xFF)
+    c.table = table
+
+    def batch(new_and_len):
+        return c.batch(new_and_len)
+
+    whole.append(0, batch([(x, x) for x in lengths]), kv[:, 0], kv[:, 1])
+    cut = lengths[0] // 2 + 5
+    halves.append(0, batch([(cut, cut), (0, 0)]), kv[:cut, 0], kv[:cut, 1])
+    halves.append(0, batch([(lengths[0] - cut, lengths[0]), (90, 90)]), kv[cut:, 0], kv[cut:, 1])
+    assert torch.equal(whole.pool, halves.pool)
+    back = torch.empty_like(kv)
+    whole.read(0, batch([(x, x) for x in lengths]), back[:, 0], back[:, 1])
+    some = np.r_[0:20, cut - 3:cut + 3, n - 95:n]
+    for i in range(2):
+        assert np.array_equal(bits_of(back[some, i]), op.read_back(bits_of(kv[some, i]), c.spec))
+    assert whole.get_status() == 0
+
+
 @pytest.mark.parametrize("store", ["int8", "int4"])
 def test_tiny_and_infinite_groups(store):
     from paper_2602_14236_amd import binding
