@@ -423,10 +423,10 @@ int sali_get_status(sali_ctx* ctx, uint32_t* h_flags, void* stream);
  * A call works on a batch of sequences (sali_page_batch), whose numbers lie in DEVICE memory, so that a captured graph
  * can be replayed with other lengths:
  *   d_start  int32[n_seqs + 1]  new tokens of sequence s are the rows d_start[s] .. d_start[s + 1] - 1 of every
- *                               per-token array of the call (queries, keys, values, outputs); d_start[0] = 0
+ *                               per-token array of the call (queries, keys, values, outputs)
  *   d_length int32[n_seqs]      tokens of the sequence, the new ones (its last) included
  *   d_table  int32[n_seqs][table_width]  page of tokens p * page_tokens .. of the sequence; entries past its length have no meaning
- *   n_tokens                    rows that the per-token arrays have, d_start[n_seqs] <= n_tokens (rows past it are untouched)
+ *   n_tokens                    rows that the per-token arrays have, d_start[n_seqs] <= n_tokens (rows past it, and before d_start[0], are untouched)
  *   max_q, max_kv               no sequence has more new tokens / more tokens than this
  * A sequence whose numbers contradict each other or these bounds (more new tokens than tokens, rows outside
  * 0 .. n_tokens, more tokens than its table row holds) is left out: nothing is read or written for it and

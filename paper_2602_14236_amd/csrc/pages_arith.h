@@ -40,6 +40,11 @@ SALI_BOTH bool page_seq_holds(int64_t a, int64_t b, int64_t len, int64_t n_token
 // most n / 16 + 2 blocks, and up to the next sequence's first slot there are that many, so a slot's sequence is found without a sum over
 // those before it.
 SALI_BOTH int64_t first_slot(int32_t first, int s) { return (int64_t)(first < 0 ? 0 : first) / kBlockTokens + 2ll * s; }
+// The block of its sequence that a slot stands for, -1: none (slots that it has no use for, and those of rows before the batch's first, if that is not row 0).
+SALI_BOTH int block_of_slot(const PageSeq& q, int s, int64_t slot) {
+    const int64_t nth = slot - first_slot(q.first, s), block = (q.len - q.n) / kBlockTokens + nth;
+    return q.n > 0 && nth >= 0 && block * kBlockTokens < q.len ? (int)block : -1;
+}
 
 // The keys a set of rows sees: positions first .. last of the sequence (of the set's first and last token), window and sinks.  Tiles of kTokens
 // tokens that some row sees: the first `head` from the sequence's beginning, then from tile `from` on.

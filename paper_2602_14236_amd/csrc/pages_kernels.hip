@@ -104,11 +104,9 @@ __device__ __forceinline__ bool find_work(const PageGeom& g, const PageSeqs& q, 
     const int64_t slot = blockIdx.x;
     const int s = seq_of_slot(q, slot);
     const PageSeq seq = load_seq(q, g, s, threadIdx.x == 0);
-    if (seq.n == 0) return false;
     const int pos0 = seq.len - seq.n;                       // position of the first new token
-    const int64_t at = (int64_t)(pos0 / kBlockTokens) + (slot - first_slot(seq.first, s));
-    if (at * kBlockTokens >= seq.len) return false;         // one of the slots that the sequence has no use for
-    const int block = (int)at;
+    const int block = block_of_slot(seq, s, slot);
+    if (block < 0) return false;
     w.head = (int)blockIdx.y * heads_each;
     w.heads_end = min(w.head + heads_each, g.n_kv);
     w.t0 = max(0, pos0 - block * kBlockTokens);

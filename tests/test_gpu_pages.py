@@ -593,3 +593,33 @@ def test_refusals():
     c.pages.append(0, none, k[:0], k[:0])
     torch.cuda.synchronize()
     assert c.pages.get_status() == 0
+
+
+@pytest.mark.parametrize("store", ["16", "int8", "int4"])
+@pytest.mark.parametrize("news", [[(30, 75), (1, 40), (16, 16)], [(90, 130), (1, 40), (75, 80)]], ids=["short", "long"])
+def test_batches_that_start_behind_row_0(store, news):
+    """The last sequences of a larger batch, with the larger batch's starts and arrays: rows before theirs are neither read nor written."""
+    spec = op.PagesSpec(2, 4, 64, 16, "fp16", store)
+    c = Cache(spec, [t for _, t in news], 26, extra_pages=40, history=False)     # (a batch has no more rows than the pages hold)
+    c.write([(t - n, t - n) for n, t in news])
+    t, before, behind = sum(n for n, _ in news), 333, 5
+    batch = c.batch(news, room=before + behind)
+    batch.tensors[0].add_(before)
+    row = slice(before, before + t)
+    k, v = (torch.full((before + t + behind, 2, 64), math.nan, dtype=torch.float16, device=DEV) for _ in range(2))
+    k[row], v[row] = c.new_rows(c.k, news), c.new_rows(c.v, news)
+    c.pages.append(0, batch, k, v)
+    back = torch.full((before + t + behind, 2, 2, 64), 9.0, dtype=torch.float16, device=DEV)
+    c.pages.read(0, batch, back[:, 0], back[:, 1])
+    for i, x in ((0, k), (1, v)):
+        got, exp = bits_of(back[row, i]), op.read_back(bits_of(x[row]), spec)
+        assert ((got == exp) | (((got | exp) & 0x7FFF) == 0)).all()
+    q = torch.full((before + t + behind, 4, 64), math.nan, dtype=torch.float16, device=DEV)
+    q[row] = rows(c.rng, t, 4, 64, "fp16").to(DEV)
+    out, lse = torch.full_like(q, 7.0), torch.full((before + t + behind, 4), 7.0, device=DEV)
+    c.pages.attend(0, batch, q, 0.125, out, lse)
+    torch.cuda.synchronize()
+    c.check(news, q[row], out[row], lse[row], 0.125)
+    for rest in (slice(0, before), slice(before + t, None)):
+        assert bool((back[rest] == 9).all()) and bool((out[rest] == 7).all()) and bool((lse[rest] == 7).all())
+    assert c.pages.get_status() == 0

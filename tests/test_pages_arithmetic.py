@@ -188,3 +188,40 @@ int main() {
     return 0;
 }
 """ % seed)
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_slots_of_batches_that_start_behind_row_0(tmp_path, seed):
+    """Parts of larger batches (the first start is not 0): every block of a sequence has one slot, and a slot that stands for none says so, those
+    before the first row too; no block lies before a sequence's new tokens or behind its end."""
+    run_pages_program(tmp_path, """
+int main() {
+    srand(%d);
+    for (int round = 0; round < 3000; ++round) {
+        const int n = rand() %% 20 + 1;
+        std::vector<PageSeq> seqs(n);
+        int row = rand() %% 400;
+        for (PageSeq& q : seqs) {
+            q.n = rand() %% 4 ? rand() %% 40 : rand() %% 700;
+            q.first = row;
+            q.len = q.n + rand() %% 300;
+            row += q.n;
+        }
+        const int64_t slots = (row + rand() %% 5) / kBlockTokens + 2ll * n;
+        std::vector<std::vector<int>> times(n);
+        for (int s = 0; s < n; ++s) times[s].assign(seqs[s].len / kBlockTokens + 1, 0);
+        for (int64_t slot = 0; slot < slots; ++slot) {
+            int s = 0;
+            while (s + 1 < n && first_slot(seqs[s + 1].first, s + 1) <= slot) ++s;
+            const int block = block_of_slot(seqs[s], s, slot);
+            if (block == -1) continue;
+            if (block < (seqs[s].len - seqs[s].n) / kBlockTokens || block * kBlockTokens >= seqs[s].len) return 1;
+            ++times[s][block];
+        }
+        for (int s = 0; s < n; ++s)
+            for (int block = 0; block * kBlockTokens < seqs[s].len; ++block)
+                if (times[s][block] != (seqs[s].n > 0 && (block + 1) * kBlockTokens > seqs[s].len - seqs[s].n)) return 2;
+    }
+    return 0;
+}
+""" % seed)
