@@ -430,7 +430,8 @@ int sali_get_status(sali_ctx* ctx, uint32_t* h_flags, void* stream);
  *   max_q, max_kv               no sequence has more new tokens / more tokens than this
  * A sequence whose numbers contradict each other or these bounds (more new tokens than tokens, rows outside
  * 0 .. n_tokens, more tokens than its table row holds) is left out: nothing is read or written for it and
- * SALI_FAULT_BATCH is set.  An entry of the table that is not a page of the pool sets SALI_FAULT_PAGE: its tokens are not
+ * SALI_FAULT_BATCH is set; so is a whole batch in which a start lies behind the next one, by every call.  (A call whose n_seqs, n_tokens,
+ * max_q or max_kv is 0 has nothing to do and looks at nothing.)  An entry of the table that is not a page of the pool sets SALI_FAULT_PAGE: its tokens are not
  * written, read back as zeros and are invisible to attention.
  *
  * Layout.  The pool is [n_layers][n_pages][n_kv_heads][page_tokens / 16][block]; a block holds 16 tokens of one K/V head
@@ -453,7 +454,7 @@ int sali_get_status(sali_ctx* ctx, uint32_t* h_flags, void* stream);
 
 /* sticky device status bits of the pages (sali_pages_get_status), besides SALI_FAULT_NONFINITE */
 #define SALI_FAULT_PAGE   0x10u   /* a page table entry outside the pool       */
-#define SALI_FAULT_BATCH  0x20u   /* a sequence left out (see above)           */
+#define SALI_FAULT_BATCH  0x20u   /* a sequence or batch left out (see above)  */
 
 typedef struct sali_pages sali_pages;   /* opaque host object; owns no device memory */
 

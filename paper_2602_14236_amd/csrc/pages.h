@@ -62,6 +62,12 @@ hipError_t launch_pages_attend_fp16(int store, int dim, const PagesAttend& a, hi
 hipError_t launch_pages_attend_bf16(int store, int dim, const PagesAttend& a, hipStream_t s);
 
 #ifdef __HIPCC__
+// Does the start of one of the sequences i, i + step .. lie behind the next one's?  Nobody knows then whose rows are whose: the batch is left out whole.
+__device__ __forceinline__ bool some_start_falls(const int32_t* start, int n_seqs, int i, int step) {
+    bool falls = false;
+    for (; i < n_seqs; i += step) falls |= start[i] > start[i + 1];
+    return falls;
+}
 __device__ __forceinline__ PageSeq read_seq(const PageSeqs& q, const PageGeom& g, int s, bool& fits) {
     const int64_t a = q.start[s], b = q.start[s + 1], len = q.length[s];
     const int64_t in_table = (int64_t)q.width * (kBlockTokens << g.blocks_log2), room = in_table < q.max_kv ? in_table : q.max_kv;

@@ -78,18 +78,48 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
 }
 
-// the last sequence whose first slot is not past `slot`; all 64 lanes of a wave, 64 candidates a look
+// The last sequence whose first slot is not past `slot`, -1 if a start of the batch falls; all threads of the block.  All starts are looked at, since a fall
+// anywhere is the whole batch's: up to 256 by every wave for itself, more by all four together and through LDS.  (Us of an append of single tokens, this
+// and a search that looks at some of them: 64 of them, 8 heads, 4.3 and 4.3; 200 7.7 and 7.4; 300 10.6 and 9.7; 4096, one head, 22.7 and 14.7.  65: 4.5, through LDS 4.7.)
 __device__ __forceinline__ int seq_of_slot(const PageSeqs& q, int64_t slot) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, n = q.n_seqs;
-    while (n > 1) {
-        const int step = (n + 63) / 64, i = lane * step;
-        const bool before = i < n && first_slot(q.start[lo + i], lo + i) <= slot;
-        const int c = max(1, (int)__popcll(__ballot(before)));
-        lo += (c - 1) * step;
-        n = min(step, n - (c - 1) * step);
+    __shared__ int s_before[4], s_falls[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), last = q.n_seqs - 1;
+    if (last == 0) return 0;
+    int before = 0;                         // sequences whose first slot is not past it (the last one counted several times)
+    bool falls = false;
+    auto look = [&](int first, int next, int i) {
+        falls |= first > next;
+        before += (int)__popcll(__ballot(max(first, 0) / kBlockTokens <= (int)slot - 2 * i));       // first_slot(first, i) <= slot
+    };
+    // sequences base + thread + step k
+    auto looks = [&](int base, int thread, int step, auto flight) {
+        constexpr int kFlight = decltype(flight)::value;
+        int first[kFlight], next[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            const int i = min(base + step * k + thread, last);
+            first[k] = q.start[i];
+            next[k] = q.start[i + 1];
+        }
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) look(first[k], next[k], base + step * k + thread);
+    };
+    if (q.n_seqs <= 256) {
+        if (q.n_seqs <= 64) looks(0, lane, 64, std::integral_constant<int, 1>{});
+        else looks(0, lane, 64, std::integral_constant<int, 4>{});
+        if (__ballot(falls) != 0) return -1;
+    } else {
+        for (int base = 0; base < q.n_seqs; base += 1024) looks(base, threadIdx.x, 256, std::integral_constant<int, 4>{});
+        const bool any = __ballot(falls) != 0;
+        if (lane == 0) {
+            s_before[wave] = before;
+            s_falls[wave] = any ? 1 : 0;
+        }
+        __syncthreads();
+        if ((s_falls[0] | s_falls[1] | s_falls[2] | s_falls[3]) != 0) return -1;
+        before = s_before[0] + s_before[1] + s_before[2] + s_before[3];
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    return __builtin_amdgcn_readfirstlane(max(min(before, q.n_seqs) - 1, 0));
 }
 
 // What a thread block has: a 16-token block of a sequence, for a run of K/V heads; which tokens of it are the batch's, where their rows and
@@ -103,6 +133,10 @@ struct BlockWork {
 __device__ __forceinline__ bool find_work(const PageGeom& g, const PageSeqs& q, int heads_each, BlockWork& w) {
     const int64_t slot = blockIdx.x;
     const int s = seq_of_slot(q, slot);
+    if (s < 0) {
+        if (threadIdx.x == 0) atomicOr(q.status, SALI_FAULT_BATCH);
+        return false;
+    }
     const PageSeq seq = load_seq(q, g, s, threadIdx.x == 0);
     const int pos0 = seq.len - seq.n;                       // position of the first new token
     const int block = block_of_slot(seq, s, slot);

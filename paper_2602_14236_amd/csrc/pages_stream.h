@@ -303,19 +303,24 @@ void k_pages_stream(
         if (width > 0) page_of_lane = tables[(int64_t)s * width + min(lane, width - 1)];      // on their way with the lengths
         bool fits;
         seq = read(s, fits);
+        if (n_seqs > 1 && __builtin_amdgcn_ballot_w64(some_start_falls(starts, n_seqs, lane, 64)) != 0) {
+            fits = false;
+            seq.n = 0;
+        }
         if (!fits && head == 0 && threadIdx.x == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
         if (!in_stream(seq, group, rows_max)) return;
         end = (uint32_t)view_of_seq(seq).tiles;
     } else {
         // the block's stretch: every wave finds it by itself, a sequence a lane
         page0 = -64;
-        bool bad = false;
+        bool bad = false, falls = false;
         auto lane_seq = [&](int i) -> PageSeq {
             PageSeq q = {0, 0, 0};
             if (i >= n_seqs) return q;
             bool fits;
             q = read(i, fits);
             bad |= !fits;
+            falls |= !fits && starts[i] > starts[i + 1];
             return q;
         };
         auto tiles_of = [&](const PageSeq& q) { return in_stream(q, group, rows_max) ? view_of_seq(q).tiles : 0; };
@@ -325,6 +330,7 @@ void k_pages_stream(
 #pragma unroll 4
         for (int i = 64 + lane; i < n_seqs; i += 64) own += tiles_of(lane_seq(i));
         total = (uint32_t)__builtin_amdgcn_readlane(wave_scan(own), 63) * (uint32_t)n_kv;
+        if (__builtin_amdgcn_ballot_w64(falls) != 0) total = 0;
         if (bad && blockIdx.x == 0 && wave == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
         blocks = max(1u, min(gridDim.x, total / (uint32_t)min_tiles));
         if (blockIdx.x >= blocks || total == 0) {
@@ -349,7 +355,10 @@ void k_pages_stream(
             }
             before += (uint32_t)__builtin_amdgcn_readlane(upto, 63);
             base += 64;
-            if (base >= n_seqs) return;                     // the batch changed while it was read
+            if (base >= n_seqs) {                           // the batch changed while it was read
+                if (threadIdx.x == 0) reinterpret_cast<StreamRecord*>(late_arguments<kStreamArgsAt>().records)[blockIdx.x] = record;
+                return;
+            }
             q = lane_seq(base + lane);
             t = tiles_of(q);
         }

@@ -87,8 +87,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
     __shared__ int s_count[kUnitBuckets], s_next[kUnitBuckets];
     __shared__ int s_parts, s_merges;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t slots = tile_slots(a.seqs.n_tokens, a.group, a.seqs.n_seqs, tile_rows(kWaves));
+    int64_t slots = tile_slots(a.seqs.n_tokens, a.group, a.seqs.n_seqs, tile_rows(kWaves));
     TileScratch& t = *reinterpret_cast<TileScratch*>(a.records);
+    const bool falls = some_start_falls(a.seqs.start, a.seqs.n_seqs, threadIdx.x, kPlanThreads);
+    if (falls) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
     if (threadIdx.x < kUnitBuckets) s_count[threadIdx.x] = 0;
     if (threadIdx.x == 0) s_parts = s_merges = 0;
     int64_t sum = 0;
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
         s_sum[wave] = sum;
         s_longest[wave] = longest;
     }
-    __syncthreads();
+    if (__syncthreads_or(falls) != 0) slots = 0;
     sum = 0;
     for (int w = 0; w < kPlanThreads / 64; ++w) {
         sum += s_sum[w];
@@ -171,6 +173,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_stretches(PagesAtte
     TileScratch& t = *reinterpret_cast<TileScratch*>(a.records);
     TileUnit* const units = reinterpret_cast<TileUnit*>(t.pieces + tile_pieces(slots, a.geom.n_kv, kWaves));
     if (threadIdx.x == 0) s_parts = s_merges = 0;
+    const bool falls = some_start_falls(a.seqs.start, a.seqs.n_seqs, threadIdx.x, kPlanThreads);
+    if (falls) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
     // the units that there are, one behind the other
     uint64_t total = 0;
     int count = 0;
@@ -203,7 +207,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_stretches(PagesAtte
         }
         if (own != 0) units[r] = u;
     }
-    __syncthreads();
+    if (__syncthreads_or(falls) != 0) count = 0;
     const uint64_t length = stretch_length(total, blocks);
     // eight lanes a unit, a lane a block
     const int sub = lane & 7;

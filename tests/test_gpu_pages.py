@@ -623,3 +623,93 @@ def test_batches_that_start_behind_row_0(store, news):
     for rest in (slice(0, before), slice(before + t, None)):
         assert bool((back[rest] == 9).all()) and bool((out[rest] == 7).all()) and bool((lse[rest] == 7).all())
     assert c.pages.get_status() == 0
+
+
+class Calls:
+    """The three calls on a batch, each with arrays of its own and its own look at the status."""
+
+    def __init__(self, c, new, room=0):
+        self.c, self.spec, self.t = c, c.spec, sum(n for n, _ in new) + room
+        self.k, self.v = (rows(c.rng, self.t, c.spec.n_kv_heads, c.spec.head_dim, c.spec.dtype).to(DEV) for _ in range(2))
+        self.q = rows(c.rng, self.t, c.spec.n_heads, c.spec.head_dim, c.spec.dtype).to(DEV)
+
+    def status(self):
+        torch.cuda.synchronize()
+        status = self.c.pages.get_status()
+        self.c.pages.scratch[:4].zero_()
+        return status
+
+    def append(self, batch):
+        before = self.c.pages.pool.clone()
+        self.c.pages.append(0, batch, self.k, self.v)
+        changed = (self.c.pages.pool != before).view(self.c.pages.cfg.n_pages, -1).any(1).cpu().numpy()
+        return np.flatnonzero(changed), self.status()
+
+    def read(self, batch):
+        back = torch.full((self.t, 2, self.spec.n_kv_heads, self.spec.head_dim), 9.0, dtype=TORCH[self.spec.dtype], device=DEV)
+        self.c.pages.read(0, batch, back[:, 0], back[:, 1])
+        return back, self.status()
+
+    def attend(self, batch):
+        out, lse = torch.full_like(self.q, 7.0), torch.full((self.t, self.spec.n_heads), 7.0, device=DEV)
+        self.c.pages.attend(0, batch, self.q, self.spec.head_dim ** -0.5, out, lse)
+        return out, lse, self.status()
+
+
+@pytest.mark.parametrize("new,starts", [
+    ([(70, 90), (70, 100), (70, 80)], [0, 280, 140, 210]), ([(70, 90), (70, 100), (70, 80)], [0, 140, 70, 210]),
+    ([(2, 90), (2, 100), (2, 80)], [0, 8, 4, 6]), ([(2, 90), (2, 100), (2, 80)], [3, 2, 4, 6]),
+    ([(1, 1200 + s) for s in range(9)], [0, 1, 2, 3, 4, 5, 8, 7, 8, 9]),
+    ([(1, 20 + s) for s in range(300)], list(range(298)) + [299, 298, 300]),
+    ([(80, 90)] + [(1, 40)] * 99, [0, 81, 80] + list(range(82, 180)))], ids=["past", "inside", "tokens", "first", "long", "many", "mixed"])
+def test_batches_whose_starts_fall(new, starts):
+    """They are left out whole by every call, and each call notes it."""
+    from paper_2602_14236_amd import binding
+    c = Cache(op.PagesSpec(2, 4, 64, 16, "fp16", "16"), [t for _, t in new], 27)
+    calls = Calls(c, new)
+    batch = c.batch(new)
+    for sound in (True, False):
+        if not sound:
+            batch.tensors[0].copy_(torch.tensor(starts, dtype=torch.int32))
+        want = 0 if sound else binding.FAULT_BATCH
+        pages, status = calls.append(batch)
+        assert status == want and (len(pages) > 0) == sound
+        back, status = calls.read(batch)
+        assert status == want and bool((back == 9).all()) != sound
+        out, lse, status = calls.attend(batch)
+        assert status == want and bool((out == 7).all() and (lse == 7).all()) != sound
+
+
+@pytest.mark.parametrize("many", [False, True], ids=["stream", "tile"])
+@pytest.mark.parametrize("change", [("length", "short"), ("length", 101), ("length", 2 ** 31 - 1), ("length", -5), ("start", "past")], ids=str)
+def test_every_call_leaves_out_what_contradicts_and_nothing_else(many, change):
+    """One sequence whose length contradicts the batch, or whose rows end past the arrays: each call notes it, leaves its rows and pages alone, and
+    does the others."""
+    from paper_2602_14236_amd import binding
+    n = 70 if many else 2
+    new = [(n, 90), (n, 80), (n, 100)]
+    c = Cache(op.PagesSpec(2, 4, 64, 32, "fp16", "16"), [t for _, t in new], 28)
+    calls = Calls(c, new)
+    batch = c.batch(new)
+    out = 2
+    if change[0] == "length":
+        batch.tensors[1][out] = n - 1 if change[1] == "short" else change[1]
+    else:
+        batch.tensors[0][out + 1] = 3 * n + 1
+        batch.c.max_q = n + 1
+    keep = slice(0, 2 * n)
+    pages, status = calls.append(batch)
+    assert status == binding.FAULT_BATCH
+    assert set(pages) == {c.table[s, p // 32] for s, (m, t) in enumerate(new[:2]) for p in range(t - m, t)}
+    for s in range(2):
+        at = slice(s * n, (s + 1) * n)
+        t = new[s][1]
+        c.k[s][t - n:], c.v[s][t - n:] = calls.k[at].cpu(), calls.v[at].cpu()
+    back, status = calls.read(batch)
+    assert status == binding.FAULT_BATCH
+    assert torch.equal(back[keep, 0], calls.k[keep]) and torch.equal(back[keep, 1], calls.v[keep]) and bool((back[2 * n:] == 9).all())
+    o, lse, status = calls.attend(batch)
+    assert status == binding.FAULT_BATCH
+    assert bool((o[2 * n:] == 7).all()) and bool((lse[2 * n:] == 7).all())
+    c.k, c.v = c.k[:2], c.v[:2]
+    c.check(new[:2], calls.q[keep], o[keep], lse[keep], 64 ** -0.5)
