@@ -192,12 +192,12 @@ def bounds(spec, out, lse, mass, reach, length, v_max):
     the D products of a score are summed in fp32, D 2^-24 of the sum of their sizes (reach); scaling and the subtraction of the
     reference, 2^-23 of the score's and reference's sizes, both within reach, once for the row and once for where a reference moves; exp2,
     log2 and divisions, 2^-21 in all; sums over the keys and over partial results in fp32, (keys + 64) 2^-24.  These all move a weight
-    relative to the others: `step`.  Weights are rounded to 16 bits for the product with V (half a step; fp16: 2^-25 at the least, relative to the largest),
-    the result once more."""
+    relative to the others: `step`.  Weights are rounded to 16 bits for the product with V (half a step; fp16: 2^-35 of the largest at the least,
+    since it is 2^10 or more where weights are rounded and fp16's smallest step is 2^-24), the result once more."""
     u = spec.half_step
     step = reach * (spec.head_dim * 2.0 ** -24 + 4 * 2.0 ** -23) + 2.0 ** -21 + (length + 64) * 2.0 ** -24
     d_out = 1.01 * ((2 * step[..., None] + u) * mass + u * np.abs(out)) + 2.0 ** -24
     if spec.dtype == "fp16":
-        d_out = d_out + length * 2.0 ** -25 * v_max
+        d_out = d_out + length * 2.0 ** -35 * v_max
     d_lse = step + 2.0 ** -22 * (1.0 + np.where(np.isfinite(lse), np.abs(lse), 0.0))
     return d_out, d_lse

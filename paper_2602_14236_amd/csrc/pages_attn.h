@@ -7,9 +7,10 @@
 // out in memory as those operands: every load is 16 bytes a lane of contiguous memory, ready for use.
 //
 // Softmax.  Scores are kept in units of log 2 (scale2 = scale * log2 e).  Each row has a reference m and a sum of
-// exp2(s - m); the reference follows the row's maximum only when that is more than 2^kLag above it: until then weights of up
-// to 2^kLag are as good as weights up to 1 (fp32 sums, 16-bit weights of the same relative precision), and nothing has to be rescaled.
-// Nothing seen: m = -inf, sum 0.
+// exp2(s - m).  The reference is set kRaise below the row's maximum and follows it only when that has grown by more than kLag, so the weights of
+// 16 bits reach from 2^kRaise to 2^(kRaise + kLag) and nothing has to be rescaled most of the time.  fp16 has nothing below 2^-24: with weights at 1
+// and below, many weak keys under a strong one (a first token that takes most of the weight) lost their bits or vanished, 20 % of the result at a distance of
+// 17; from 2^10 on that happens 2^34 below the strongest.  bfloat16 has the exponents of fp32 and needs no raise.  Nothing seen: m = -inf, sum 0.
 //
 // Masked keys.  Scores outside a row's view become -inf, whatever they were, and their weights 0.  A weight of 0 does not take
 // out an infinity or NaN in V.  What no token has written (past a sequence's end, pages that are none) is set to zero before the product, by
@@ -33,7 +34,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
 
-constexpr float kLag = 8.0f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // the 16-bit types and their matrix products
@@ -45,6 +45,7 @@ struct Num<false> {
     typedef half8 V8;
     static constexpr uint32_t kExp = 0x7C007C00u, kExpOne = 0x04000400u;
     static constexpr uint16_t kOne = 0x3C00u;
+    static constexpr float kRaise = 10.0f, kLag = 5.0f;         // weights up to 2^15
     static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
     }
@@ -58,6 +59,7 @@ struct Num<true> {
     typedef bhalf8 V8;
     static constexpr uint32_t kExp = 0x7F807F80u, kExpOne = 0x00800080u;
     static constexpr uint16_t kOne = 0x3F80u;
+    static constexpr float kRaise = 0.0f, kLag = 8.0f;
     static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
     }
@@ -178,6 +180,14 @@ __device__ __forceinline__ float sum_over_quarters(float v) {
     const uint32_t u = __builtin_bit_cast(uint32_t, v);
     const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
     return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// the reference that a row's largest score asks for
+template <bool kBf16>
+__device__ __forceinline__ float reference_of(float top, float scale2) {
+    top *= scale2;
+    asm("" : "+v"(top));                    // not one instruction, for which the constant would stay in a vector register
+    return top - Num<kBf16>::kRaise;
 }
 
 // V's values of 8 tokens: those that are finite, and 1 where an infinity of either sign (or a NaN) stands

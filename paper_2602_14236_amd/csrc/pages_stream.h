@@ -491,8 +491,8 @@ void k_pages_stream(
             for (int c = 0; c < kSets; ++c) {
                 float top = fmaxf(fmaxf(fmaxf(s2[c][0][0], s2[c][0][1]), fmaxf(s2[c][0][2], s2[c][0][3])),
                                   fmaxf(fmaxf(s2[c][1][0], s2[c][1][1]), fmaxf(s2[c][1][2], s2[c][1][3])));
-                top = max_over_quarters(top) * a.scale2;
-                const float to = top > m[c] + kLag ? top : m[c];
+                top = reference_of<kBf16>(max_over_quarters(top), a.scale2);
+                const float to = top > m[c] + Num<kBf16>::kLag ? top : m[c];
                 if (__builtin_amdgcn_ballot_w64(to != m[c]) != 0) {
                     const float by = to != m[c] ? __builtin_amdgcn_exp2f(m[c] - to) : 1.0f;
                     l[c] *= by;

@@ -536,8 +536,8 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
             float tops[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) tops[x] = fmaxf(fmaxf(st[4 * x], st[4 * x + 1]), fmaxf(st[4 * x + 2], st[4 * x + 3]));
-            const float top = max_over_halves(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * a.scale2;
-            const float to = top > m + kLag ? top : m;
+            const float top = reference_of<kBf16>(max_over_halves(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))), a.scale2);
+            const float to = top > m + Num<kBf16>::kLag ? top : m;
             if (__builtin_amdgcn_ballot_w64(to != m) != 0) {
                 const float by = to != m ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
                 l *= by;
@@ -553,6 +553,8 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
             for (int x = 0; x < 4; ++x) tops[x] = (st[4 * x] + st[4 * x + 1]) + (st[4 * x + 2] + st[4 * x + 3]);
             l += (tops[0] + tops[1]) + (tops[2] + tops[3]);
+            // the weights once rounded to 16 bits, half a step each, against the sum's fp32: a second number each, as the stream has it, would be half as many
+            // products again where the matrix cores are what a prompt waits for
             u32x4 p[2];
 #pragma unroll
             for (int x = 0; x < 8; ++x) p[x / 4][x % 4] = pack2<kBf16>(st[2 * x], st[2 * x + 1]);

@@ -713,3 +713,29 @@ def test_every_call_leaves_out_what_contradicts_and_nothing_else(many, change):
     assert bool((o[2 * n:] == 7).all()) and bool((lse[2 * n:] == 7).all())
     c.k, c.v = c.k[:2], c.v[:2]
     c.check(new[:2], calls.q[keep], o[keep], lse[keep], 64 ** -0.5)
+
+
+@pytest.mark.parametrize("store,dtype", [("16", "fp16"), ("16", "bf16"), ("int8", "fp16"), ("int4", "fp16")])
+@pytest.mark.parametrize("gap", [12, 17, 18, 20])
+@pytest.mark.parametrize("new", [[(1, 3000), (5, 700)], [(200, 1500), (1, 200)], [(1, 100000)]], ids=["stream", "tile", "long"])
+def test_many_weak_keys_under_a_strong_one_that_brings_nothing(store, dtype, gap, new):
+    """A first token whose score lies `gap` above all others' and whose value is zero: the result is the weak keys' alone, each of weight e^-gap."""
+    long = new[0][1] > 10000
+    spec = op.PagesSpec(1 if long else 4, 2 if long else 16, 64 if long else 128, 64, dtype, store)
+    c = Cache(spec, [t for _, t in new], 29, history=False)
+    scale = spec.head_dim ** -0.5
+    for s, (n, t) in enumerate(new):
+        c.k[s][:] = 0
+        c.k[s][0, :, 0] = 8.0
+        v = 100 * (1 + 0.5 * torch.rand(c.v[s].shape, generator=torch.Generator().manual_seed(s)))
+        v[0] = 0
+        c.v[s] = v.to(TORCH[dtype])
+    c.write([(t, t) for _, t in new])
+    rows_all = sum(n for n, _ in new)
+    q = rows(c.rng, rows_all, spec.n_heads, spec.head_dim, dtype)
+    q[:, :, 0] = gap / (8.0 * scale)
+    q = q.to(DEV)
+    out, lse = torch.empty_like(q), torch.empty((rows_all, spec.n_heads), device=DEV)
+    c.pages.attend(0, c.batch(new), q, scale, out, lse)
+    torch.cuda.synchronize()
+    c.check(new, q, out, lse, scale)
