@@ -420,6 +420,8 @@ int sali_get_status(sali_ctx* ctx, uint32_t* h_flags, void* stream);
  * 32 along head_dim, fp32 scales; symmetric INT8, asymmetric INT4 with the group's smallest value).  sali_attend_decode* give the
  * attention over the frames as (out, lse); sali_pages_attend takes that pair as `prior` and joins the two.
  *
+ * The pool, the scratch and the arrays of a call lie on one GPU, which is the current one whenever a call is made.
+ *
  * A call works on a batch of sequences (sali_page_batch), whose numbers lie in DEVICE memory, so that a captured graph
  * can be replayed with other lengths:
  *   d_start  int32[n_seqs + 1]  new tokens of sequence s are the rows d_start[s] .. d_start[s + 1] - 1 of every

@@ -490,11 +490,21 @@ class SaliPages:
                              f"side expected, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
         return sali_rows(t.data_ptr(), token, head)
 
-    def _call(self, batch: PageBatch, stream: Optional[torch.cuda.Stream]) -> int:
-        """The stream of a call on `batch`: the pages' device's current one, if none is given."""
+    def _call(self, name: str, stream: Optional[torch.cuda.Stream], *args):
+        """The C call with the pages' device as the current one (the default stream's handle is the same on every device, and means the current
+        one's) on its current stream, if none is given."""
+        if torch._C._cuda_getDevice() != self.index:
+            with torch.cuda.device(self.index):
+                return self._call(name, stream, *args)
+        if stream is not None and stream.device_index != self.index:
+            raise ValueError(f"the stream is of {stream.device}, the pages lie on {self.device}")
+        s = torch._C._cuda_getCurrentRawStream(self.index) if stream is None else stream.cuda_stream
+        _check(getattr(self.lib, name)(self.handle, *args, s), name)
+
+    def _batch(self, batch: PageBatch) -> sali_page_batch:
         if batch.index != self.index:
             raise ValueError(f"the batch lies on {batch.device}, the pages on {self.device}")
-        return torch._C._cuda_getCurrentRawStream(self.index) if stream is None else stream.cuda_stream
+        return batch.c
 
     def _dense(self, t: Optional[torch.Tensor], shape, name: str):
         if t is None:
@@ -506,14 +516,12 @@ class SaliPages:
     def append(self, layer: int, batch: PageBatch, k: torch.Tensor, v: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """Store the K/V rows of the batch's new tokens, [tokens, n_kv_heads, head_dim]."""
         n = self.n_kv_heads
-        _check(self.lib.sali_pages_append(self.handle, layer, batch.c, self._rows(k, batch, n, "k"), self._rows(v, batch, n, "v"),
-                                          self._call(batch, stream)), "sali_pages_append")
+        self._call("sali_pages_append", stream, layer, self._batch(batch), self._rows(k, batch, n, "k"), self._rows(v, batch, n, "v"))
 
     def read(self, layer: int, batch: PageBatch, k_out: torch.Tensor, v_out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """The rows of the batch's new tokens as the pages hold them."""
         n = self.n_kv_heads
-        _check(self.lib.sali_pages_read(self.handle, layer, batch.c, self._rows(k_out, batch, n, "k_out"), self._rows(v_out, batch, n, "v_out"),
-                                        self._call(batch, stream)), "sali_pages_read")
+        self._call("sali_pages_read", stream, layer, self._batch(batch), self._rows(k_out, batch, n, "k_out"), self._rows(v_out, batch, n, "v_out"))
 
     def attend(self, layer: int, batch: PageBatch, q: torch.Tensor, softmax_scale: float, out: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
                window: int = 0, sinks: int = 0, prior: Optional[torch.Tensor] = None, prior_lse: Optional[torch.Tensor] = None,
@@ -521,12 +529,11 @@ class SaliPages:
         """Causal attention of the batch's new tokens over the pages: q, out [tokens, n_heads, head_dim], lse [tokens, n_heads] in fp32.  prior and
         prior_lse (fp32): attention of the same queries over other keys, joined with this one."""
         n, d = self.n_heads, self.head_dim
-        _check(self.lib.sali_pages_attend(self.handle, layer, batch.c, self._rows(q, batch, n, "q"), softmax_scale, window, sinks,
-                                          self._dense(prior, (batch.tokens, n, d), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
-                                          self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"),
-                                          self._call(batch, stream)), "sali_pages_attend")
+        self._call("sali_pages_attend", stream, layer, self._batch(batch), self._rows(q, batch, n, "q"), softmax_scale, window, sinks,
+                   self._dense(prior, (batch.tokens, n, d), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
+                   self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"))
 
     def get_status(self) -> int:
         f = C.c_uint32()
-        _check(self.lib.sali_pages_get_status(self.handle, C.byref(f), torch._C._cuda_getCurrentRawStream(self.index)), "sali_pages_get_status")
+        self._call("sali_pages_get_status", None, C.byref(f))
         return f.value

@@ -82,3 +82,57 @@ def test_reports_of_spilled_registers_are_read():
     report = "\n".join(line.format(x) for x in ("Function Name: good", "    SGPRs Spill: 3", "    VGPRs Spill: 0", "Function Name: bad",
                                                 "    SGPRs Spill: 0", "    VGPRs Spill: 12"))
     assert build.spilled(report) == ["bad"]
+
+
+@pytest.fixture
+def pages_elsewhere(monkeypatch):
+    """A SaliPages whose GPU (number -1, as CPU tensors have it) is not the current one, over a library that notes the device and stream of its calls."""
+    from types import SimpleNamespace
+    from paper_2602_14236_amd import binding
+    state = SimpleNamespace(device=0, calls=[])
+
+    class On:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            self.before, state.device = state.device, self.device
+
+        def __exit__(self, *_):
+            state.device = self.before
+
+    monkeypatch.setattr(torch.cuda, "device", On)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: state.device, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 1000 + index, raising=False)
+    pages = object.__new__(binding.SaliPages)
+
+    def entry(name):
+        def call(*args):
+            state.calls.append((name, state.device, args[-1]))
+            return 0
+        return call
+
+    names = ("sali_pages_append", "sali_pages_read", "sali_pages_attend", "sali_pages_get_status")
+    pages.lib = SimpleNamespace(**{name: entry(name) for name in names})
+    pages.handle, pages.index, pages.device, pages.dtype = None, -1, torch.device("cpu"), torch.float16
+    pages.n_heads, pages.n_kv_heads, pages.head_dim = 4, 2, 64
+    return pages, state
+
+
+def test_calls_run_on_the_pages_gpu(pages_elsewhere):
+    from types import SimpleNamespace
+    from paper_2602_14236_amd.binding import PageBatch
+    pages, state = pages_elsewhere
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    batch = PageBatch(i(2), i(1), i(1, 5), 3, max_kv=80)
+    kv, q = torch.zeros((3, 2, 64), dtype=torch.float16), torch.zeros((3, 4, 64), dtype=torch.float16)
+    for stream, handle in ((None, 999), (SimpleNamespace(cuda_stream=77, device_index=-1), 77)):
+        pages.append(0, batch, kv, kv, stream=stream)
+        pages.read(0, batch, kv, kv, stream=stream)
+        pages.attend(0, batch, q, 1.0, q, stream=stream)
+        assert state.calls == [(f"sali_pages_{name}", -1, handle) for name in ("append", "read", "attend")]
+        state.calls.clear()
+    pages.get_status()
+    assert state.calls == [("sali_pages_get_status", -1, 999)] and state.device == 0
+    with pytest.raises(ValueError):
+        pages.append(0, batch, kv, kv, stream=SimpleNamespace(cuda_stream=77, device_index=0, device="cuda:0"))
