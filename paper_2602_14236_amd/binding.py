@@ -456,16 +456,17 @@ class SaliPages:
         self.device = torch.device(device)
         if self.device.type != "cuda":
             raise ValueError("libsali runs on the GPU only")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         pool_bytes, scratch_bytes = pages_bytes(cfg)
-        if pool is not None and (not pool.is_contiguous() or pool.numel() * pool.element_size() < pool_bytes or pool.device.type != "cuda"):
-            raise ValueError(f"pool: {pool_bytes} contiguous bytes on the GPU expected")
+        if pool is not None and (not pool.is_contiguous() or pool.numel() * pool.element_size() < pool_bytes or pool.device != self.device):
+            raise ValueError(f"pool: {pool_bytes} contiguous bytes on {self.device} expected, got {pool.numel() * pool.element_size()} on {pool.device}")
         self.dtype = torch.bfloat16 if cfg.dtype else torch.float16
         self.n_heads, self.n_kv_heads, self.head_dim = cfg.n_heads, cfg.n_kv_heads, cfg.head_dim
         self.handle = None
         with torch.cuda.device(self.device):
             self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=self.device) if pool is None else pool
             self.scratch = torch.empty(scratch_bytes, dtype=torch.uint8, device=self.device)
-            self.device = self.scratch.device
             self.index = self.device.index
             h = C.c_void_p()
             _check(self.lib.sali_pages_create(C.byref(cfg), _ptr(self.pool), _ptr(self.scratch), C.byref(h)), "sali_pages_create")

@@ -136,3 +136,19 @@ def test_calls_run_on_the_pages_gpu(pages_elsewhere):
     assert state.calls == [("sali_pages_get_status", -1, 999)] and state.device == 0
     with pytest.raises(ValueError):
         pages.append(0, batch, kv, kv, stream=SimpleNamespace(cuda_stream=77, device_index=0, device="cuda:0"))
+
+
+def test_a_pool_lies_on_the_pages_gpu(monkeypatch):
+    from types import SimpleNamespace
+    from paper_2602_14236_amd import binding
+    cfg = config()
+    need = binding.pages_bytes(cfg)[0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+
+    def pool(device, size=need):
+        return SimpleNamespace(is_contiguous=lambda: True, numel=lambda: size, element_size=lambda: 1, device=torch.device(device))
+
+    for device, bad in (("cuda:0", pool("cuda:1")), ("cuda:1", pool("cuda:0")), ("cuda", pool("cuda:0")), ("cuda:0", pool("cpu")),
+                        ("cuda:0", pool("cuda:0", need - 1))):
+        with pytest.raises(ValueError):
+            binding.SaliPages(cfg, device, pool=bad)
