@@ -739,3 +739,48 @@ def test_many_weak_keys_under_a_strong_one_that_brings_nothing(store, dtype, gap
     c.pages.attend(0, c.batch(new), q, scale, out, lse)
     torch.cuda.synchronize()
     c.check(new, q, out, lse, scale)
+
+
+# ---- 17 to 32 query rows a sequence ------------------------------------------------------------------
+DRAFTS = {
+    "pairs": ((8, 2), [(8, 500), (5, 33), (6, 6), (7, 300), (1, 64), (8, 8)]),
+    "stretches": ((8, 2), [(8, 1500), (5, 2000), (6, 64), (8, 8), (1, 700), (0, 5), (7, 1201)]),
+    "many": ((8, 2), [(5 + s % 4, 20 + s) for s in range(140)]),
+    "one": ((32, 1), [(1, 1300)]),
+    "beside longer": ((24, 1), [(1, 700), (60, 100), (1, 90)]),
+}
+
+
+@pytest.mark.parametrize("store,dtype,dim", FORMATS)
+@pytest.mark.parametrize("window,sinks,prior", [(0, 0, False), (70, 5, True)])
+@pytest.mark.parametrize("name", DRAFTS)
+def test_drafts_of_17_to_32_rows(store, dtype, dim, window, sinks, prior, name):
+    (heads, kv), new = DRAFTS[name]
+    c = Cache(op.PagesSpec(kv, heads, dim, 32, dtype, store), [t for _, t in new], 30)
+    c.attend(new, window=window, sinks=sinks, prior=prior)
+    assert c.pages.get_status() == 0
+
+
+@pytest.mark.parametrize("dtype,dim", [("fp16", 64), ("fp16", 128), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("new", [[(8, 600), (5, 33)], [(8, 3000), (6, 1400), (3, 40)]], ids=["pairs", "stretches"])
+def test_drafts_over_values_that_are_not_finite(dtype, dim, new):
+    """Some among the last tokens, which not all rows see, some early ones, in other parts of a cut pair than those."""
+    c = Cache(op.PagesSpec(2, 8, dim, 16, dtype, "16"), [t for _, t in new], 31, history=False)
+    for s, (n, t) in enumerate(new):
+        for lo, hi in ((0, t // 3), (t - n, t)):
+            for value in (math.inf, -math.inf, math.nan):
+                c.v[s][c.rng.integers(lo, hi), c.rng.integers(2), c.rng.integers(dim)] = value
+    c.write([(t, t) for _, t in new])
+    for window, sinks in ((0, 0), (90, 3)):
+        c.attend(new, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("store", ["16", "int8", "int4"])
+def test_drafts_of_pages_that_are_none(store):
+    from paper_2602_14236_amd import binding
+    new = [(8, 1600), (5, 300), (6, 40)]
+    c = Cache(op.PagesSpec(1, 4, 64, 32, "bf16", store), [t for _, t in new], 32)
+    c.table[0, 7], c.table[2, :2] = -1, c.pages.cfg.n_pages
+    q, out, lse = c.attend(new, hidden={0: np.arange(1600) // 32 == 7, 2: np.ones(40, bool)})
+    assert c.pages.get_status() == binding.FAULT_PAGE
+    assert bool((out[13:] == 0).all()) and bool(torch.isneginf(lse[13:]).all())
