@@ -491,21 +491,19 @@ class SaliPages:
                              f"side expected, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
         return sali_rows(t.data_ptr(), token, head)
 
-    def _call(self, name: str, stream: Optional[torch.cuda.Stream], *args):
-        """The C call with the pages' device as the current one (the default stream's handle is the same on every device, and means the current
-        one's) on its current stream, if none is given."""
-        if torch._C._cuda_getDevice() != self.index:
-            with torch.cuda.device(self.index):
-                return self._call(name, stream, *args)
-        if stream is not None and stream.device_index != self.index:
-            raise ValueError(f"the stream is of {stream.device}, the pages lie on {self.device}")
-        s = torch._C._cuda_getCurrentRawStream(self.index) if stream is None else stream.cuda_stream
-        _check(getattr(self.lib, name)(self.handle, *args, s), name)
+    def _elsewhere(self) -> bool:
+        """Is another GPU than the pages' the current one?  (The default stream's handle is the same on every GPU, and means the current one's.)"""
+        return torch._C._cuda_getDevice() != self.index
 
-    def _batch(self, batch: PageBatch) -> sali_page_batch:
+    def _call(self, batch: PageBatch, stream: Optional[torch.cuda.Stream]) -> int:
+        """The stream of a call on `batch`: the pages' GPU's current one, if none is given."""
         if batch.index != self.index:
             raise ValueError(f"the batch lies on {batch.device}, the pages on {self.device}")
-        return batch.c
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.index)
+        if stream.device_index != self.index:
+            raise ValueError(f"the stream is of {stream.device}, the pages lie on {self.device}")
+        return stream.cuda_stream
 
     def _dense(self, t: Optional[torch.Tensor], shape, name: str):
         if t is None:
@@ -516,25 +514,40 @@ class SaliPages:
 
     def append(self, layer: int, batch: PageBatch, k: torch.Tensor, v: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """Store the K/V rows of the batch's new tokens, [tokens, n_kv_heads, head_dim]."""
+        if self._elsewhere():
+            with torch.cuda.device(self.index):
+                return self.append(layer, batch, k, v, stream)
         n = self.n_kv_heads
-        self._call("sali_pages_append", stream, layer, self._batch(batch), self._rows(k, batch, n, "k"), self._rows(v, batch, n, "v"))
+        _check(self.lib.sali_pages_append(self.handle, layer, batch.c, self._rows(k, batch, n, "k"), self._rows(v, batch, n, "v"),
+                                          self._call(batch, stream)), "sali_pages_append")
 
     def read(self, layer: int, batch: PageBatch, k_out: torch.Tensor, v_out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """The rows of the batch's new tokens as the pages hold them."""
+        if self._elsewhere():
+            with torch.cuda.device(self.index):
+                return self.read(layer, batch, k_out, v_out, stream)
         n = self.n_kv_heads
-        self._call("sali_pages_read", stream, layer, self._batch(batch), self._rows(k_out, batch, n, "k_out"), self._rows(v_out, batch, n, "v_out"))
+        _check(self.lib.sali_pages_read(self.handle, layer, batch.c, self._rows(k_out, batch, n, "k_out"), self._rows(v_out, batch, n, "v_out"),
+                                        self._call(batch, stream)), "sali_pages_read")
 
     def attend(self, layer: int, batch: PageBatch, q: torch.Tensor, softmax_scale: float, out: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
                window: int = 0, sinks: int = 0, prior: Optional[torch.Tensor] = None, prior_lse: Optional[torch.Tensor] = None,
                stream: Optional[torch.cuda.Stream] = None):
         """Causal attention of the batch's new tokens over the pages: q, out [tokens, n_heads, head_dim], lse [tokens, n_heads] in fp32.  prior and
         prior_lse (fp32): attention of the same queries over other keys, joined with this one."""
+        if self._elsewhere():
+            with torch.cuda.device(self.index):
+                return self.attend(layer, batch, q, softmax_scale, out, lse, window=window, sinks=sinks, prior=prior, prior_lse=prior_lse, stream=stream)
         n, d = self.n_heads, self.head_dim
-        self._call("sali_pages_attend", stream, layer, self._batch(batch), self._rows(q, batch, n, "q"), softmax_scale, window, sinks,
-                   self._dense(prior, (batch.tokens, n, d), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
-                   self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"))
+        _check(self.lib.sali_pages_attend(self.handle, layer, batch.c, self._rows(q, batch, n, "q"), softmax_scale, window, sinks,
+                                          self._dense(prior, (batch.tokens, n, d), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
+                                          self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"),
+                                          self._call(batch, stream)), "sali_pages_attend")
 
     def get_status(self) -> int:
+        if self._elsewhere():
+            with torch.cuda.device(self.index):
+                return self.get_status()
         f = C.c_uint32()
-        self._call("sali_pages_get_status", None, C.byref(f))
+        _check(self.lib.sali_pages_get_status(self.handle, C.byref(f), torch._C._cuda_getCurrentRawStream(self.index)), "sali_pages_get_status")
         return f.value
