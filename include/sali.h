@@ -508,7 +508,8 @@ int sali_pages_read(sali_pages* p, int32_t layer, const sali_page_batch* batch, 
  * of the token at position p of its sequence, over the positions j <= p with  window == 0,  or  j > p - window,  or  j < sinks:
  *     s_j = softmax_scale * <q_h, K_j>,   out_h = sum_j softmax(s)_j V_j,   lse_h = log sum_j exp(s_j).
  * K, V are the rows as sali_pages_read returns them; scores, softmax and sums in fp32, its weights rounded to the 16-bit type for
- * the product with V (for sequences of up to 32 query rows a K/V head, alone in their batch, or 16 next to longer ones: to the sum of two).  Keys that a token does not see do not reach it, whatever they hold.
+ * the product with V (for sequences of up to 32 query rows a K/V head, alone in their batch, or 16 next to longer ones: to the sum of two).  Keys that a token does not see do not reach it, whatever they hold;
+ * an infinity or NaN among the values that it sees does, however small its weight.
  *   q             n_heads heads
  *   out           n_heads heads, 16-bit; zeros where nothing is seen
  *   d_lse_or_null fp32 [n_tokens][n_heads]; -inf where nothing is seen

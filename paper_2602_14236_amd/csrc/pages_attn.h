@@ -14,9 +14,10 @@
 //
 // Masked keys.  Scores outside a row's view become -inf, whatever they were, and their weights 0.  A weight of 0 does not take
 // out an infinity or NaN in V.  What no token has written (past a sequence's end, pages that are none) is set to zero before the product, by
-// position; quantised values are finite wherever they were written.  16-bit rows are looked at, in tiles (of rows) where they are not wholly in view
-// of all rows, in the stream always: values that are not finite are set to zero for the product, two more products count, for every output, the
-// infinities of each sign in its view (a NaN counts for both), and what was found is added to the result at the end.
+// position; quantised values are finite wherever they were written.  16-bit rows are looked at, in the stream always: values that are not finite are set to zero for the product, two more products count, for
+// every output, the infinities of each sign in its view (a NaN counts for both), and what was found is added to the result at the end.  Tiles look at keys that
+// not all of their rows see; where all do, the product shows what is there, an infinity, or a NaN where its weight was rounded to zero, and a
+// piece of work with a NaN in its results is done again with a look at all keys.
 #pragma once
 
 #include <type_traits>
@@ -230,6 +231,9 @@ __device__ __forceinline__ void take_apart(const u32x4 v, u32x4& finite, u32x4& 
     }
 }
 
+// A factor that joins results, of what sees something: the smallest number where fp32 has none that is small enough, so that an infinity stays one.
+__device__ __forceinline__ float not_zero(float by) { return fmaxf(by, 1.4e-45f); }
+
 // A row's result from its sum (out and lse still apart): joined with the prior and rounded.  `out` is one value of the unnormalised sum.
 struct RowEnd {
     float lse, by_own, by_prior;            // out = out * by_own + prior * by_prior
@@ -248,13 +252,13 @@ __device__ __forceinline__ RowEnd row_end(float m, float l, const PagesAttend& a
     if (top == -INFINITY && lse == lse && lp == lp) return r;
     const float w1 = expf(lse - top), w2 = expf(lp - top), sum = w1 + w2;
     r.lse = top + logf(sum);
-    r.by_own = own * (w1 / sum);
+    r.by_own = some ? not_zero(own * (w1 / sum)) : 0.0f;
     r.by_prior = w2 / sum;
     return r;
 }
 // what values that are not finite add to a result
 __device__ __forceinline__ float found(bool up, bool down) { return (up ? INFINITY : 0.0f) + (down ? -INFINITY : 0.0f); }
-// a weight of zero takes out whatever the other factor is
+// a weight of zero takes out whatever the other factor is: what sees nothing
 __device__ __forceinline__ float joined(const RowEnd& e, float own, float prior) {
     const float a = e.by_own == 0.0f ? 0.0f : own * e.by_own;
     return e.by_prior == 0.0f ? a : __builtin_fmaf(prior, e.by_prior, a);

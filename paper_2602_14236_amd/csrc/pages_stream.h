@@ -208,7 +208,7 @@ __device__ __forceinline__ void join_parts(const PagesAttend& a, const StreamRec
         for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
         for (int i = lane; i < rec.parts; i += 64) {
             const float m = s_weight[x * rec.parts + i];
-            s_weight[x * rec.parts + i] = m == -INFINITY && sum == sum ? 0.0f : __builtin_amdgcn_exp2f(m - all);
+            s_weight[x * rec.parts + i] = m == -INFINITY && sum == sum ? 0.0f : not_zero(__builtin_amdgcn_exp2f(m - all));
         }
         if (lane == 0) {
             s_top[x] = all;
@@ -226,7 +226,7 @@ __device__ __forceinline__ void join_parts(const PagesAttend& a, const StreamRec
             for (int i = 0; i < kFlight; ++i) {
                 const int part = group + groups * (k + i);
                 const float w = part < rec.parts ? weight[part] : 0.0f;
-                const bool none = w == 0.0f;                // nothing seen, or nothing left of it
+                const bool none = w == 0.0f;                // nothing seen
                 o0 = __builtin_fmaf(none ? 0.0f : v[i].x, w, o0);
                 o1 = __builtin_fmaf(none ? 0.0f : v[i].y, w, o1);
             }
@@ -627,7 +627,7 @@ void k_pages_stream(
             for (int w = 0; w < kStreamWaves; ++w) {
                 const float mw = s_m[w][r];
                 if (s_l[w][r] == 0.0f) continue;
-                const float by = __builtin_amdgcn_exp2f(mw - top);
+                const float by = not_zero(__builtin_amdgcn_exp2f(mw - top));
                 sum += s_l[w][r] * by;
                 o += *reinterpret_cast<const f32x4*>(&s_acc[w][r][d]) * by;
             }

@@ -366,6 +366,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
     __shared__ uint8_t s_up[2][kStore == SALI_STORE_16 ? kTileWaves : 1][kDim], s_down[2][kStore == SALI_STORE_16 ? kTileWaves : 1][kDim];
     __shared__ int s_odd[2][kTileWaves];
     __shared__ uint64_t s_found[2][kStore == SALI_STORE_16 ? 64 * kTileWaves : 1];
+    __shared__ int s_nan[kTileWaves];                             // of each wave: is there one in its results
     const int nth = (int)(blockIdx.x / (uint32_t)args.geom.n_kv);
     int piece = nth, pieces_end = nth + 1;
     {
@@ -377,8 +378,9 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         }
     }
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = wave & 1;
+    bool look = false, again = false;                             // 16 bits: the piece's second time, with a look at all keys; the wave needs it
 #pragma unroll 1
-    for (; piece < pieces_end; ++piece) {
+    while (piece < pieces_end) {
         // arguments and the thread's number: anew for every piece, not kept in registers through the loop
         const PagesAttend a = late_arguments<0>();
         uint32_t all = ~0u;
@@ -393,6 +395,8 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         const uint32_t block_bytes = a.geom.head_bytes >> a.geom.blocks_log2;
         const int32_t* const table = a.seqs.table + (int64_t)uniform(unit.seq) * a.seqs.width;
         const View view = view_of_rows<kTileWaves>(seq, unit.row_tile, group, a.window, a.sinks);
+        View to_look_at = view;             // keys that not all rows see, or all keys
+        if (look) to_look_at.first = -1;
 
         // ---- the wave's share of the tiles: where tile i's block lies, and its tokens
         typedef TileRaw<kStore, kDim> Raw;
@@ -447,7 +451,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
                 }
             if constexpr (kStore == SALI_STORE_16) {
                 bool any = false;
-                if (partly_hidden(view, a.window, a.sinks, tile_at(view, i) * kTileKeys, kTileKeys)) {
+                if (partly_hidden(to_look_at, a.window, a.sinks, tile_at(view, i) * kTileKeys, kTileKeys)) {
                     bool odd = false;
 #pragma unroll
                     for (int x = 0; x < Raw::kLoads; ++x) odd |= !Raw::none(x, lane) && any_not_finite<kBf16>(raw.v[x]);
@@ -618,6 +622,20 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
             tile_load_v<kStore, kDim>(next.block, half, here, raw);
         }
 
+        // Results with a NaN wait for the second time.  (A look at every key would be a tenth of a step's vector instructions; this costs 1 % of 333 of 4000
+        // tokens, 8 heads, 163 and 165 us, and nothing measurable of 8192.)
+        if constexpr (kStore == SALI_STORE_16) {
+            if (!look) {
+                float any[4] = {};
+#pragma unroll
+                for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) any[x % 4] += acc[d][x];
+                any[0] = (any[0] + any[1]) + (any[2] + any[3]);
+                again = __builtin_amdgcn_ballot_w64(any[0] != any[0]) != 0;
+            }
+        }
+        const bool writes = again == look;
         // ---- results: lane (row col, hh) has values 32 d + 8 k + 4 hh .. + 3
         const PagesAttend b = late_arguments<0>();
         const float sum = sum_over_halves(l);
@@ -626,7 +644,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         asm volatile("" : "+v"(there));
         const int end_col = there & 31, end_hh = there >> 5;
         const int end_r = row0 + end_col;
-        if (end_r < rows) {
+        if (end_r < rows && writes) {
             const int end_token = (int)((uint32_t)end_r / (uint32_t)b.group), end_of_group = end_r - end_token * b.group;
             if constexpr (kStore == SALI_STORE_16) {
                 const uint64_t up = s_found[0][thread], down = s_found[1][thread];
@@ -666,6 +684,16 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
                 if (end_hh == 0 && b.lse != nullptr) b.lse[row] = e.lse;
             }
         }
+        if constexpr (kStore == SALI_STORE_16) {
+            if (!look) {
+                if (there == 0) s_nan[wave] = again ? 1 : 0;
+                lds_barrier();
+                look = __builtin_amdgcn_ballot_w64((there < kTileWaves ? s_nan[there] : 0) != 0) != 0;
+                if (look) continue;
+            }
+            look = again = false;
+        }
+        ++piece;
     }
 }
 
@@ -713,7 +741,7 @@ __global__ __launch_bounds__(256) void k_pages_tile_merge(PagesAttend a) {
             if (i0 + i >= rec.parts) ml[i].y = 0.0f;
             to = ml[i].y == 0.0f ? to : fmaxf(to, ml[i].x);         // 0: nothing seen
         }
-        const float by = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m - to);
+        const float by = l == 0.0f ? 0.0f : not_zero(__builtin_amdgcn_exp2f(m - to));
         l = l == 0.0f ? 0.0f : l * by;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -722,7 +750,7 @@ __global__ __launch_bounds__(256) void k_pages_tile_merge(PagesAttend a) {
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const bool none = ml[i].y == 0.0f;
-            const float pby = none ? 0.0f : __builtin_amdgcn_exp2f(ml[i].x - to);
+            const float pby = none ? 0.0f : not_zero(__builtin_amdgcn_exp2f(ml[i].x - to));
             l += none ? 0.0f : ml[i].y * pby;
 #pragma unroll
             for (int k = 0; k < 4; ++k)

@@ -784,3 +784,34 @@ def test_drafts_of_pages_that_are_none(store):
     q, out, lse = c.attend(new, hidden={0: np.arange(1600) // 32 == 7, 2: np.ones(40, bool)})
     assert c.pages.get_status() == binding.FAULT_PAGE
     assert bool((out[13:] == 0).all()) and bool(torch.isneginf(lse[13:]).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("gap", [30, 150])
+@pytest.mark.parametrize("strong_first", [True, False])
+@pytest.mark.parametrize("new,heads", [([(1, 100), (5, 300)], (4, 2)), ([(1, 5000), (8, 3000)], (4, 1)), ([(200, 1500)], (4, 2)), ([(150, 700)] * 12, (32, 8)),
+                                       ([(29, 2400), (1, 900)], (1024, 64))], ids=["pairs", "stretches", "tile", "tiles", "few tiles"])
+def test_an_infinity_reaches_every_row_that_sees_it(dtype, gap, strong_first, new, heads):
+    """However small its weight: a key that all others' scores are `gap` below, before or behind it."""
+    spec = op.PagesSpec(heads[1], heads[0], 64, 32, dtype, "16")
+    c = Cache(spec, [t for _, t in new], 33, history=False)
+    for s, (n, t) in enumerate(new):
+        at = t // 2
+        c.k[s][:] = 0
+        c.k[s][0 if strong_first else t - n, :, 0] = 8.0
+        c.v[s][at, :, 5], c.v[s][at, :, 6], c.v[s][at, :, 7] = math.inf, -math.inf, math.nan
+    c.write([(t, t) for _, t in new])
+    total = sum(n for n, _ in new)
+    q = rows(c.rng, total, spec.n_heads, 64, dtype)
+    q[:, :, 0] = gap
+    q = q.to(DEV)
+    for prior in (False, True):
+        pr, pl = (torch.ones((total, spec.n_heads, 64), device=DEV), torch.full((total, spec.n_heads), 400.0, device=DEV)) if prior else (None, None)
+        out, lse = torch.full_like(q, 7.0), torch.empty((total, spec.n_heads), device=DEV)
+        c.pages.attend(0, c.batch(new), q, 0.125, out, lse, prior=pr, prior_lse=pl)
+        torch.cuda.synchronize()
+        assert bool((out[..., 5] == math.inf).all()) and bool((out[..., 6] == -math.inf).all()) and bool(torch.isnan(out[..., 7]).all())
+        rest = torch.cat([out[..., :5], out[..., 8:]], -1)
+        assert bool(torch.isfinite(rest).all()) and bool(torch.isfinite(lse).all())
+        if prior:
+            assert bool((rest == 1).all())
