@@ -519,9 +519,10 @@ int sali_pages_read(sali_pages* p, int32_t layer, const sali_page_batch* batch, 
  *                 keys together.  16-byte aligned.
  * Asynchronous on `stream`.  Calls on one object must not overlap each other (one area of partial results); calls on
  * different objects may share a pool.
- * SALI_ERR_CONFIG for a softmax_scale that is not finite, SALI_ERR_SHAPE for a layer, batch size, window or sinks out of range; more sequences
- * than pages or more new tokens than the pages hold are out of range, and so are 2^31 query rows (new tokens times queries of a K/V head)
- * or tiles of 32 tokens (sequences times K/V heads times max_kv / 32). */
+ * `out` is none of the other arrays.
+ * SALI_ERR_CONFIG for a softmax_scale that is not finite, SALI_ERR_SHAPE for a layer, batch size, window or sinks out of range.  In every call more
+ * sequences than pages, more new tokens than the pages hold and more than 2^31 - 1025 tokens of a sequence (by max_kv and table_width) are out of range, here 2^31
+ * query rows (new tokens times queries of a K/V head) and tiles of 32 tokens (sequences times K/V heads times max_kv / 32) too. */
 int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, float softmax_scale,
                       int32_t window, int32_t sinks, const float* d_prior_or_null, const float* d_prior_lse_or_null,
                       const sali_rows* out, float* d_lse_or_null, void* stream);

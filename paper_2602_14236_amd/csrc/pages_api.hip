@@ -1,5 +1,6 @@
 // C ABI of the paged cache of text tokens (sali.h): argument checks and launches.
 #include <math.h>
+#include <algorithm>
 #include <new>
 
 #include "pages.h"
@@ -40,6 +41,8 @@ int check_batch(const sali_pages* p, int32_t layer, const sali_page_batch* b) {
     if (p == nullptr || b == nullptr) return SALI_ERR_NULL;
     if (layer < 0 || layer >= p->cfg.n_layers) return SALI_ERR_SHAPE;
     if (b->n_seqs < 0 || b->n_tokens < 0 || b->table_width < 0 || b->max_q < 0 || b->max_kv < 0) return SALI_ERR_SHAPE;
+    // positions, and those of the tiles asked for behind a sequence's last, are counted in 31 bits
+    if (std::min((int64_t)b->max_kv, (int64_t)b->table_width * p->cfg.page_tokens) > kMostPositions) return SALI_ERR_SHAPE;
     if (b->n_seqs > p->cfg.n_pages || b->n_tokens > (int64_t)p->cfg.n_pages * p->cfg.page_tokens) return SALI_ERR_SHAPE;
     if (b->n_seqs > 0 && (b->d_start == nullptr || b->d_length == nullptr || (b->d_table == nullptr && b->table_width > 0))) return SALI_ERR_NULL;
     if (((uintptr_t)b->d_start | (uintptr_t)b->d_length | (uintptr_t)b->d_table) % 4 != 0) return SALI_ERR_ALIGN;

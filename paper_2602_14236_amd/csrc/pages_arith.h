@@ -7,6 +7,7 @@
 namespace sali {
 
 constexpr int kBlockTokens = 16;            // tokens of a block, the unit of the layout
+constexpr int kMostPositions = 0x7FFFFFFF - 1024;       // tokens of a sequence
 constexpr int kTileTokens = 32;             // tokens of a step of the attention: two blocks
 
 // bytes of a block's parts, in their order

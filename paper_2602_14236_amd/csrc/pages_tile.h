@@ -622,8 +622,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
             tile_load_v<kStore, kDim>(next.block, half, here, raw);
         }
 
-        // Results with a NaN wait for the second time.  (A look at every key would be a tenth of a step's vector instructions; this costs 1 % of 333 of 4000
-        // tokens, 8 heads, 163 and 165 us, and nothing measurable of 8192.)
+        // Results with a NaN wait for the second time.  (Without it 333 of 4000 tokens six times, 8 heads, 163 us, with it 165; no difference for 8192.)
         if constexpr (kStore == SALI_STORE_16) {
             if (!look) {
                 float any[4] = {};

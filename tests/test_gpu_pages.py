@@ -815,3 +815,21 @@ def test_an_infinity_reaches_every_row_that_sees_it(dtype, gap, strong_first, ne
         assert bool(torch.isfinite(rest).all()) and bool(torch.isfinite(lse).all())
         if prior:
             assert bool((rest == 1).all())
+
+
+def test_lengths_past_31_bits_are_refused():
+    """No sequence can be that long by the table's width and max_kv together, or the call is refused; either alone may be as large as it likes."""
+    from paper_2602_14236_amd import binding
+    c = Cache(op.PagesSpec(1, 2, 64, 256, "fp16", "16"), [20], 34)
+    c.table = np.concatenate([c.table, np.full((1, (1 << 23) - 1), -1, np.int32)], 1)
+    calls = Calls(c, [(1, 20)])
+    for width, most, good in ((1 << 23, 2 ** 31 - 1, False), (1 << 23, 2 ** 31 - 1024, False), (1 << 23, 2 ** 31 - 1025, True), (1, 2 ** 31 - 1, True), (1 << 23, 20, True)):
+        batch = c.batch([(1, 20)])
+        batch.c.table_width, batch.c.max_kv = width, most
+        for call in (calls.append, calls.read, calls.attend):
+            if good:
+                assert call(batch)[-1] == 0
+            else:
+                with pytest.raises(binding.SaliError) as e:
+                    call(batch)
+                assert e.value.code == -2
