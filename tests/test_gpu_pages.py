@@ -833,3 +833,20 @@ def test_lengths_past_31_bits_are_refused():
                 with pytest.raises(binding.SaliError) as e:
                     call(batch)
                 assert e.value.code == -2
+
+
+@pytest.mark.parametrize("store", ["16", "int8"])
+@pytest.mark.parametrize("new,heads", [([(1, 100), (5, 300)], (4, 2)), ([(1, 5000), (8, 3000)], (4, 1)), ([(200, 1500)], (4, 2)), ([(29, 2400), (1, 900)], (128, 8))],
+                         ids=["pairs", "stretches", "tile", "tiles"])
+def test_values_near_the_largest_of_bfloat16(store, new, heads):
+    """Weighted means of finite values are finite: sums of many of them, not yet divided, have to be too."""
+    spec = op.PagesSpec(heads[1], heads[0], 64, 32, "bf16", store)
+    c = Cache(spec, [t for _, t in new], 35, history=False)
+    for s, (n, t) in enumerate(new):
+        v = 3.3e38 * (1 - 0.1 * torch.rand(c.v[s].shape, generator=torch.Generator().manual_seed(s)))
+        v[..., 32:] *= -1
+        c.v[s] = v.to(torch.bfloat16)
+    c.write([(t, t) for _, t in new])
+    q, out, lse = c.attend(new)
+    assert bool(torch.isfinite(out).all())
+    c.attend(new, window=70, sinks=3, prior=True)
