@@ -10,8 +10,9 @@
 // exp2(s - m).  The reference is set kRaise below the row's maximum and follows it only when that has grown by more than kLag, so the weights of
 // 16 bits reach from 2^kRaise to 2^(kRaise + kLag) and nothing has to be rescaled most of the time.  fp16 has nothing below 2^-24: with weights at 1
 // and below, many weak keys under a strong one (a first token that takes most of the weight) lost their bits or vanished, 20 % of the result at a distance of
-// 17; from 2^10 on that happens 2^34 below the strongest.  bfloat16 has the exponents of fp32, as its values have: weights are lowered there, so that
-// 2^24 of the largest values have a sum.  Nothing seen: m = -inf, sum 0.
+// 17; from 2^10 on that happens 2^34 below the strongest.  bfloat16 has the exponents of fp32, as its values have: weights are lowered there, to about
+// what a text's normalised weights are, so that 2^24 equal ones of the largest values have a sum (2^16 that lie kLag above the reference).
+// Values down to 2^-112 give the results of larger ones but for single last places.  Nothing seen: m = -inf, sum 0.
 //
 // Masked keys.  Scores outside a row's view become -inf, whatever they were, and their weights 0.  A weight of 0 does not take
 // out an infinity or NaN in V.  What no token has written (past a sequence's end, pages that are none) is set to zero before the product, by
@@ -61,7 +62,7 @@ struct Num<true> {
     typedef bhalf8 V8;
     static constexpr uint32_t kExp = 0x7F807F80u, kExpOne = 0x00800080u;
     static constexpr uint16_t kOne = 0x3F80u;
-    static constexpr float kRaise = -32.0f, kLag = 8.0f;         // and down to 2^-126
+    static constexpr float kRaise = -24.0f, kLag = 8.0f;         // and down to 2^-126
     static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
     }
