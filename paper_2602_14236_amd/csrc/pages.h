@@ -63,11 +63,22 @@ hipError_t launch_pages_attend_bf16(int store, int dim, const PagesAttend& a, hi
 
 #ifdef __HIPCC__
 // Does the start of one of the sequences i, i + step .. lie behind the next one's?  Nobody knows then whose rows are whose: the batch is left out whole.
-__device__ __forceinline__ bool some_start_falls(const int32_t* start, int n_seqs, int i, int step) {
-    bool falls = false;
-    for (; i < n_seqs; i += step) falls |= start[i] > start[i + 1];
-    return falls;
-}
+// (The first of them is asked for when this is made; a sequence that is alone has it checked with its other numbers.)
+struct StartFalls {
+    const int32_t* start;
+    int n_seqs, i, step, first, next;
+    __device__ __forceinline__ StartFalls(const int32_t* start, int n_seqs, int i, int step) : start(start), n_seqs(n_seqs), i(i), step(step), first(0), next(0) {
+        if (n_seqs > 1 && i < n_seqs) {
+            first = start[i];
+            next = start[i + 1];
+        }
+    }
+    __device__ __forceinline__ bool some() const {
+        bool falls = first > next;
+        for (int k = i + step; k < n_seqs; k += step) falls |= start[k] > start[k + 1];
+        return falls;
+    }
+};
 __device__ __forceinline__ PageSeq read_seq(const PageSeqs& q, const PageGeom& g, int s, bool& fits) {
     const int64_t a = q.start[s], b = q.start[s + 1], len = q.length[s];
     const int64_t in_table = (int64_t)q.width * (kBlockTokens << g.blocks_log2), room = in_table < q.max_kv ? in_table : q.max_kv;

@@ -297,16 +297,13 @@ void k_pages_stream(
     PageSeq seq = {0, 0, 0};
     uint32_t at = 0, end = 0, total = 0, blocks = 1;
     StreamRecord record = {0, 0, 0, 0};
+    const StartFalls falls_of_pair(starts, kStretches ? 0 : n_seqs, lane, 64);
     if constexpr (!kStretches) {
         head = blockIdx.x;
         s = blockIdx.y;
         if (width > 0) page_of_lane = tables[(int64_t)s * width + min(lane, width - 1)];      // on their way with the lengths
         bool fits;
         seq = read(s, fits);
-        if (n_seqs > 1 && __builtin_amdgcn_ballot_w64(some_start_falls(starts, n_seqs, lane, 64)) != 0) {
-            fits = false;
-            seq.n = 0;
-        }
         if (!fits && head == 0 && threadIdx.x == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
         if (!in_stream(seq, group, rows_max)) return;
         end = (uint32_t)view_of_seq(seq).tiles;
@@ -420,6 +417,12 @@ void k_pages_stream(
             now = locate(lo);
             stream_load_k<kStore, kDim>(now.b[0], now.b[1], lane, raw);
             stream_load_v<kStore, kDim>(now.b[0], now.b[1], lane, raw);
+        }
+        if constexpr (!kStretches) {        // the starts are here since the page table is
+            if (__builtin_amdgcn_ballot_w64(falls_of_pair.some()) != 0) {
+                if (threadIdx.x == 0) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
+                return;
+            }
         }
         u32x4 q[kSets][kSteps];
         int pos[kSets];

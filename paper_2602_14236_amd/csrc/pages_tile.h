@@ -83,14 +83,13 @@ __device__ __forceinline__ TileUnit tile_unit(const PagesAttend& a, int rows_min
 template <int kWaves>
 __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend a, int rows_min) {
     __shared__ int64_t s_sum[kPlanThreads / 64];
-    __shared__ int s_longest[kPlanThreads / 64];
+    __shared__ int s_longest[kPlanThreads / 64], s_falls[kPlanThreads / 64];
     __shared__ int s_count[kUnitBuckets], s_next[kUnitBuckets];
     __shared__ int s_parts, s_merges;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     int64_t slots = tile_slots(a.seqs.n_tokens, a.group, a.seqs.n_seqs, tile_rows(kWaves));
     TileScratch& t = *reinterpret_cast<TileScratch*>(a.records);
-    const bool falls = some_start_falls(a.seqs.start, a.seqs.n_seqs, threadIdx.x, kPlanThreads);
-    if (falls) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
+    const StartFalls starts(a.seqs.start, a.seqs.n_seqs, threadIdx.x, kPlanThreads);
     if (threadIdx.x < kUnitBuckets) s_count[threadIdx.x] = 0;
     if (threadIdx.x == 0) s_parts = s_merges = 0;
     int64_t sum = 0;
@@ -107,16 +106,22 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
         sum += __shfl_xor(sum, off);
         longest = max(longest, __shfl_xor(longest, off));
     }
+    const bool falls = __builtin_amdgcn_ballot_w64(starts.some()) != 0;
     if (lane == 0) {
         s_sum[wave] = sum;
         s_longest[wave] = longest;
+        s_falls[wave] = falls ? 1 : 0;
+        if (falls) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
     }
-    if (__syncthreads_or(falls) != 0) slots = 0;
+    __syncthreads();
     sum = 0;
+    int some_falls = 0;
     for (int w = 0; w < kPlanThreads / 64; ++w) {
         sum += s_sum[w];
         longest = max(longest, s_longest[w]);
+        some_falls |= s_falls[w];
     }
+    if (some_falls != 0) slots = 0;
     const int share = fair_share(sum, tile_shares(a.geom.n_kv, kWaves));
     const int most_tiles = min(share, longest);             // of the longest piece
     auto bucket_of = [&](int tiles) { return kUnitBuckets - 1 - min(kUnitBuckets - 1, (int)((int64_t)tiles * (kUnitBuckets - 1) / most_tiles)); };
@@ -167,14 +172,13 @@ template <int kWaves>
 __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_stretches(PagesAttend a, int rows_min, int blocks) {
     __shared__ uint64_t s_weight[kPlanThreads / 64];
     __shared__ int s_units[kPlanThreads / 64];
-    __shared__ int s_parts, s_merges;
+    __shared__ int s_parts, s_merges, s_falls;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t slots = tile_slots(a.seqs.n_tokens, a.group, a.seqs.n_seqs, tile_rows(kWaves));
     TileScratch& t = *reinterpret_cast<TileScratch*>(a.records);
     TileUnit* const units = reinterpret_cast<TileUnit*>(t.pieces + tile_pieces(slots, a.geom.n_kv, kWaves));
-    if (threadIdx.x == 0) s_parts = s_merges = 0;
-    const bool falls = some_start_falls(a.seqs.start, a.seqs.n_seqs, threadIdx.x, kPlanThreads);
-    if (falls) atomicOr(a.seqs.status, SALI_FAULT_BATCH);
+    if (threadIdx.x == 0) s_parts = s_merges = s_falls = 0;
+    const StartFalls starts(a.seqs.start, a.seqs.n_seqs, threadIdx.x, kPlanThreads);
     // the units that there are, one behind the other
     uint64_t total = 0;
     int count = 0;
@@ -207,7 +211,12 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_stretches(PagesAtte
         }
         if (own != 0) units[r] = u;
     }
-    if (__syncthreads_or(falls) != 0) count = 0;
+    if (starts.some()) {
+        s_falls = 1;
+        atomicOr(a.seqs.status, SALI_FAULT_BATCH);
+    }
+    __syncthreads();
+    if (s_falls != 0) count = 0;
     const uint64_t length = stretch_length(total, blocks);
     // eight lanes a unit, a lane a block
     const int sub = lane & 7;
