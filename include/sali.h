@@ -446,7 +446,8 @@ int sali_get_status(sali_ctx* ctx, uint32_t* h_flags, void* stream);
  *                                                       holds value e of a group in its low half, value e + 16 in its high half
  * Quantised values are those of sali_kv_compress / sali_kv_decompress, in the pool's 16-bit type (a group of bfloat16 values
  * that are all below 2^-121 is stored as zeros: 127 and 15 divided by it are no fp32 numbers).  A group that holds an inf or NaN
- * sets SALI_FAULT_NONFINITE; SALI_STORE_16 keeps it as it is, the others store zeros for it.
+ * sets SALI_FAULT_NONFINITE; SALI_STORE_16 keeps it as it is, the others store zeros for it.  So does SALI_STORE_INT4, bit and zeros, with a group of
+ * bfloat16 values whose largest and smallest lie further apart than fp32's largest number.
  * ------------------------------------------------------------------------------------------------- */
 #define SALI_DTYPE_FP16  0
 #define SALI_DTYPE_BF16  1
@@ -507,9 +508,10 @@ int sali_pages_read(sali_pages* p, int32_t layer, const sali_page_batch* batch, 
 /* Causal attention of the batch's new tokens over the pages, which hold them already (sali_pages_append): for query head h
  * of the token at position p of its sequence, over the positions j <= p with  window == 0,  or  j > p - window,  or  j < sinks:
  *     s_j = softmax_scale * <q_h, K_j>,   out_h = sum_j softmax(s)_j V_j,   lse_h = log sum_j exp(s_j).
- * K, V are the rows as sali_pages_read returns them; scores, softmax and sums in fp32, its weights rounded to the 16-bit type for
- * the product with V (for sequences of up to 32 query rows a K/V head, alone in their batch, or 16 next to longer ones: to the sum of two).  Keys that a token does not see do not reach it, whatever they hold;
- * an infinity or NaN among the values that it sees does, however small its weight.
+ * K, V are the rows as sali_pages_read returns them; scores, softmax and sums in fp32, its weights rounded to the 16-bit type once for the product
+ * with V.  (Where a sequence's rows are few, its kernel may keep a second number of each weight, what the rounding leaves.  Which sequences those are depends on
+ * the batch's n_seqs, n_tokens and max_q, so a token's last places may depend on the batch that it comes in.)  Keys that a token does not see do not
+ * reach it, whatever they hold; an infinity or NaN among the values that it sees does, however small its weight.
  *   q             n_heads heads
  *   out           n_heads heads, 16-bit; zeros where nothing is seen
  *   d_lse_or_null fp32 [n_tokens][n_heads]; -inf where nothing is seen

@@ -428,7 +428,8 @@ def pages_bytes(cfg: sali_pages_config):
 class PageBatch:
     """The sequences of a step, for all layers: int32 tensors start [n + 1], length [n] and table [n, width] on one GPU, as sali_page_batch has
     them.  `tokens` is the number of rows of the per-token arrays; max_q (if not given, tokens) and max_kv bound the new tokens and the tokens of a
-    sequence.  The tensors are read when a call's kernels run: a captured call takes what they hold at its replay."""
+    sequence.  Attention chooses its kernels by them: a batch of single tokens without max_q=1 is taken for one that may hold a long sequence,
+    which is three more launches a call (48 of them 7 to 9 us).  The tensors are read when a call's kernels run: a captured call takes what they hold at its replay."""
 
     def __init__(self, start: torch.Tensor, length: torch.Tensor, table: torch.Tensor, tokens: int, *, max_q: Optional[int] = None, max_kv: int):
         for name, t, dims in (("start", start, 1), ("length", length, 1), ("table", table, 2)):

@@ -5,13 +5,13 @@
 //   INT4  low = min x           m = max (x - low)      scale = m / 15     code = rne((x - low) * (15 / m))    value = code * scale + low, rounded once
 // and the value is then rounded to the pool's 16-bit type.
 //
-// Both kernels move every byte once and are bound by memory; a block of 256 threads has one 16-token block of one K/V head.  Rows are
-// contiguous along the head's values, the layout has eight tokens of one value side by side (V) or a token's pieces 16 tokens apart
-// (K), so the block is turned over in LDS between 16-byte accesses on both sides: its rows (or their codes), padded so that a column's
-// reads fall on different banks.  Codes are made and expanded on the side of the rows, where a group lies in four adjacent lanes.
+// Both kernels move every byte once and are bound by memory; a block of 256 threads has one 16-token block of one K/V head, or in long batches of up to eight
+// heads one after the other.  Rows are contiguous along the head's values, the layout has eight tokens of one value side by side (V) or a token's
+// pieces 16 tokens apart (K), so the block is turned over in LDS between 16-byte accesses on both sides: its rows (or their codes), padded so that
+// a column's reads fall on different banks.  Codes are made and expanded on the side of the rows, where a group lies in four adjacent lanes.
 // Blocks that the new tokens do not fill are written value by value, so that no byte of another token is touched.
 // Measured: 2048 tokens of 32 heads in 16 bits, written and read back, 134 MB in 25 us (the caches hold them); three of 12001 and
-// 40 heads in 4 bits 1.37 GB in 229 us, 6.0 TB/s (a copy of 2 GiB through the caches: 4.9).
+// 40 heads in 4 bits 1.37 GB in 262 us, 5.2 TB/s (229 us with the same rows again; a copy of 2 GiB through the caches: 4.9).
 
 #include <algorithm>
 #include <type_traits>

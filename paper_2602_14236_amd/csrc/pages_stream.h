@@ -10,8 +10,9 @@
 // at most two, at its ends.  A second launch joins a pair's partial results.
 //
 // Measured: one token over 131072 keys, 8 heads of 128 values in 16 bits, 537 MB in 96 us, 5.6 TB/s (a copy of 2 GiB: 4.9); 48 sequences of up to 8192
-// keys in 8 bits 97 us, 5.1 TB/s.  4 bits are bound by the vector instructions that unpack them, 790 a tile: 16 sequences under a window of 4096
-// keys 42 us, 2.2 TB/s.  Short texts are bound by the chain of a launch, the lengths, the page table, K, V and the joining of the waves: 10.4 us for 777 keys.
+// keys in 8 bits 96 us, 5.1 TB/s.  4 bits: 16 sequences under a window of 4096 keys 42 us, 2.2 TB/s; the 800 vector instructions a tile that unpack them
+// keep the vector units busy for half of that, waves wait for a third of it, and neither is the bound alone.  Short texts are bound by the chain of a launch,
+// the lengths, the page table, K, V and the joining of the waves: 10.8 us for 777 keys.
 #pragma once
 
 #include "pages_attn.h"

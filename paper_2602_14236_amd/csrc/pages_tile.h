@@ -11,7 +11,7 @@
 //
 // What bounds it.  A wave's 32 rows and 32 keys of 128 values are 16 products of 32x32x16 (512 cycles of the matrix cores), the softmax's
 // vector instructions and 16 KB from LDS.  Matrix products and LDS reads alone ran at 1235 TFLOP/s (a large library product: 1372), with
-// the softmax 1010, with keys brought in through registers 945 to 958: 8192 causal tokens, 32 heads over 8 of 128 values in 574 to 581 us.  Three
+// the softmax 1010, with keys brought in through registers 945 to 958: 8192 causal tokens, 32 heads over 8 of 128 values in 570 to 588 us.  Three
 // waves a SIMD hide one wave's softmax behind the others' products (one wave alone issues a vector instruction every 6.4 cycles,
 // several together one every 3); blocks in lockstep of product and softmax phases were slower, 683 to 740 us.  32 rows a wave, since 64
 // take more than the 168 registers that three waves leave each.

@@ -850,3 +850,17 @@ def test_values_near_the_largest_of_bfloat16(store, new, heads):
     q, out, lse = c.attend(new)
     assert bool(torch.isfinite(out).all())
     c.attend(new, window=70, sinks=3, prior=True)
+
+
+def test_groups_wider_than_fp32():
+    """bfloat16 values whose difference is no fp32 number, in 4 bits: zeros, and the bit of values that are not finite; 8 bits hold them."""
+    from paper_2602_14236_amd import binding
+    for store, status in (("int4", binding.FAULT_NONFINITE), ("int8", 0)):
+        c = Cache(op.PagesSpec(1, 1, 64, 16, "bf16", store), [3], 37, history=False)
+        c.v[0][1, 0, :32] = torch.linspace(-1, 1, 32) * 3e38       # (torch.linspace(-3e38, 3e38, n) is not finite itself)
+        c.write([(3, 3)])
+        back = torch.full((3, 2, 1, 64), 9.0, dtype=torch.bfloat16, device=DEV)
+        c.pages.read(0, c.batch([(3, 3)]), back[:, 0], back[:, 1])
+        assert c.pages.get_status() == status
+        assert bool((back[1, 1, 0, :32] == 0).all()) == (store == "int4") and bool((back[1, 1, 0, 32:] != 0).any())
+        assert np.array_equal(bits_of(back[:, 1]) & 0x7FFF, op.read_back(bits_of(c.v[0]), c.spec) & 0x7FFF)
