@@ -449,7 +449,8 @@ class PageBatch:
 
 class SaliPages:
     """Owns the pool (or works in the caller's) and the scratch of a paged cache and forwards the C calls.  Per-token tensors are [tokens, heads,
-    head_dim] with values side by side; tokens and heads may be strided (slices of one projection's output)."""
+    head_dim] with values side by side; tokens and heads may be strided (slices of one projection's output).  Where another GPU is the current one,
+    a call makes the pages' current for itself: the default stream's handle is the same on every GPU, and means the current one's."""
 
     def __init__(self, cfg: sali_pages_config, device="cuda:0", pool: Optional[torch.Tensor] = None):
         self.lib = load_library()
@@ -492,10 +493,6 @@ class SaliPages:
                              f"side expected, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
         return sali_rows(t.data_ptr(), token, head)
 
-    def _elsewhere(self) -> bool:
-        """Is another GPU than the pages' the current one?  (The default stream's handle is the same on every GPU, and means the current one's.)"""
-        return torch._C._cuda_getDevice() != self.index
-
     def _call(self, batch: PageBatch, stream: Optional[torch.cuda.Stream]) -> int:
         """The stream of a call on `batch`: the pages' GPU's current one, if none is given."""
         if batch.index != self.index:
@@ -515,7 +512,7 @@ class SaliPages:
 
     def append(self, layer: int, batch: PageBatch, k: torch.Tensor, v: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """Store the K/V rows of the batch's new tokens, [tokens, n_kv_heads, head_dim]."""
-        if self._elsewhere():
+        if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.append(layer, batch, k, v, stream)
         n = self.n_kv_heads
@@ -524,7 +521,7 @@ class SaliPages:
 
     def read(self, layer: int, batch: PageBatch, k_out: torch.Tensor, v_out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """The rows of the batch's new tokens as the pages hold them."""
-        if self._elsewhere():
+        if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.read(layer, batch, k_out, v_out, stream)
         n = self.n_kv_heads
@@ -536,7 +533,7 @@ class SaliPages:
                stream: Optional[torch.cuda.Stream] = None):
         """Causal attention of the batch's new tokens over the pages: q, out [tokens, n_heads, head_dim], lse [tokens, n_heads] in fp32.  prior and
         prior_lse (fp32): attention of the same queries over other keys, joined with this one."""
-        if self._elsewhere():
+        if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.attend(layer, batch, q, softmax_scale, out, lse, window=window, sinks=sinks, prior=prior, prior_lse=prior_lse, stream=stream)
         n, d = self.n_heads, self.head_dim
@@ -546,7 +543,7 @@ class SaliPages:
                                           self._call(batch, stream)), "sali_pages_attend")
 
     def get_status(self) -> int:
-        if self._elsewhere():
+        if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.get_status()
         f = C.c_uint32()
