@@ -65,7 +65,9 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
         //                              batches: chunks of 128 to 2048 tokens, 8 and 32 K/V heads, histories of 1000 to 9000, and windows of as many, which
         //                              leave the shorter tiles an even share.  Stretches and 128 rows in shares, 32 heads over 8, 16 bits: 512 new of 2000
         //                              tokens 56.4 and 51.8, of 2500 55.6 and 56.7, of 3600 67 and 69; 2048 of 2500 102 and 95, of 3000 111 and 116, of
-        //                              3600 132 and 141; 2048 of 9000 under a window of 2500 141 and 134, of 4096 201 and 201, of 6000 274 and 282
+        //                              3600 132 and 141; 2048 of 9000 under a window of 2500 141 and 134, of 4096 201 and 201, of 6000 274 and 282.  And how many
+        //                              row tiles a block, of 144 more: 0.78 (2400 of 7000 tokens) 264 and 312, 0.88 (2700) 355 and 324, 0.97 (3000)
+        //                              358 and 340; over 8 bits and 64 values too 0.78 18 % apart, 0.88 and 0.97 1 to 2
         //   two rounds of blocks       384 rows in shares.  16 bits: 8192 new ones 582, with 128 rows 628; 4096 (1.3 rounds) 206 and 199.
         //                              Quantised from one round on, since a key is dequantised a third as often: 4096 206 and 219, 2048 95 and 89
         //   else                       128 rows in shares
@@ -73,7 +75,7 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
         if constexpr (kStore != SALI_STORE_INT4 || kDim == 64) {
             const int64_t reach = a.window > 0 ? min((int64_t)a.seqs.max_kv, (int64_t)a.window + a.sinks) : (int64_t)a.seqs.max_kv - a.seqs.max_q / 2;
             const int64_t rows = (int64_t)a.seqs.n_tokens * group, units = rows / tile_rows(12), tiles = reach / tile_keys(12), blocks = stretch_blocks(kComputeUnits, n_kv);
-            if (most_rows >= tile_rows(12) && 10 * units <= 7 * blocks && 2 * (tiles - 12) * rows >= (a.window > 0 ? 18 : 5) * blocks * tile_rows(12)) {
+            if (most_rows >= tile_rows(12) && 10 * units <= 8 * blocks && 2 * (tiles - 12) * rows >= (a.window > 0 ? 18 : 5) * blocks * tile_rows(12)) {
                 go(std::integral_constant<int, 12>{}, (int)blocks);
                 return;
             }
