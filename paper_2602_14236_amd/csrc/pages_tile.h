@@ -566,8 +566,8 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
             for (int x = 0; x < 4; ++x) tops[x] = (st[4 * x] + st[4 * x + 1]) + (st[4 * x + 2] + st[4 * x + 3]);
             l += (tops[0] + tops[1]) + (tops[2] + tops[3]);
-            // the weights once rounded to 16 bits, half a step each, against the sum's fp32: a second number each, as the stream has it, would be half as many
-            // products again where the matrix cores are what a prompt waits for
+            // the weights once rounded to 16 bits, half a step each, against the sum's fp32: a second number each, as the stream has it, is half as many
+            // products again where the matrix cores are what a prompt waits for, and registers that three waves a SIMD do not leave (they spill)
             u32x4 p[2];
 #pragma unroll
             for (int x = 0; x < 8; ++x) p[x / 4][x % 4] = pack2<kBf16>(st[2 * x], st[2 * x + 1]);
