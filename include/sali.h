@@ -529,6 +529,69 @@ int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch
                       int32_t window, int32_t sinks, const float* d_prior_or_null, const float* d_prior_lse_or_null,
                       const sali_rows* out, float* d_lse_or_null, void* stream);
 
+/* Rotary positions: queries and keys of new tokens turned by their positions, before keys are stored (sali_pages_append, sali_step; a frame's keys
+ * [head][576][head_dim] are rows too, with head_stride = 576 * head_dim).  For pair i of a row, values i and i + pairs or (adjacent) 2 i and 2 i + 1,
+ *     angle = position[axis of i][row] * frequency[i],   y1 = x1 cos - x2 sin,   y2 = x2 cos + x1 sin   (inverse: by -angle, which is also its gradient).
+ * Angles are taken in 64 bits, the rest in fp32, rounded once to the 16-bit type; values that are in no pair are copied as they are.  Several axes are for patches
+ * of images and videos (frame, row, column); one for text. */
+typedef struct sali_rotary {
+    const double* d_frequency;       /* fp64[pairs], radians per position; DEVICE                       */
+    int32_t pairs;                   /* 1 .. head_dim / 2                                               */
+    int32_t axes;                    /* 1 .. 4                                                          */
+    int32_t section[4];              /* pairs of each axis, the first axis' first; their sum is pairs   */
+    int32_t adjacent;                /* 0: pairs of values i, i + pairs; else 2 i, 2 i + 1              */
+    int32_t reserved;
+} sali_rotary;
+
+/* q has n_heads heads, k n_kv_heads; either may be left out with its output.  An output is its input (the same rows) or none of the inputs.
+ *   d_position   int32[axes][n_tokens]
+ * Asynchronous on `stream`.  SALI_ERR_CONFIG for pairs, axes or sections out of range, SALI_ERR_SHAPE for 2^24 tokens. */
+int sali_pages_rotate(sali_pages* p, const sali_rotary* rotary, const int32_t* d_position, int32_t n_tokens, int32_t inverse,
+                      const sali_rows* q_or_null, const sali_rows* k_or_null, const sali_rows* q_out_or_null, const sali_rows* k_out_or_null,
+                      void* stream);
+
+/* Attention of drafted tokens, several guesses of what follows at once: the batch's new tokens are a draft of up to 64 tokens a sequence, which the pages hold
+ * already (sali_pages_append).  A drafted token sees all tokens before the draft, and of the draft those that its mask names:
+ *   d_seen        uint64[n_tokens], bit i of a row: the draft's i-th token (itself too only if its bit is set); bits of more tokens than the draft has mean nothing
+ * and nothing else; what else there is, is as in sali_pages_attend.  SALI_ERR_SHAPE for a max_q above 64 too.  What was accepted of the draft is moved together by
+ * sali_pages_keep. */
+int sali_pages_attend_tree(sali_pages* p, int32_t layer, const sali_page_batch* batch, const uint64_t* d_seen, const sali_rows* q,
+                           float softmax_scale, const float* d_prior_or_null, const float* d_prior_lse_or_null, const sali_rows* out,
+                           float* d_lse_or_null, void* stream);
+
+/* What attention weight keys had, by which a text can be cut down (sali_pages_select, sali_pages_keep): for every position j of a sequence and K/V head
+ *     w_j = sum of exp(softmax_scale * <q_h, K_j> - lse_h)   over the batch's new tokens that see j and the query heads h of the K/V head,
+ * in fp32, always in the same order for the same batch.  softmax_scale, window and sinks as in sali_pages_attend; d_lse fp32[n_tokens][n_heads] as it gave them (with a
+ * prior: shares of all keys together).  A row whose lse is -inf adds nothing.
+ *   d_weights     fp32[n_pages][n_kv_heads][page_tokens], of this layer: the caller keeps one for every layer
+ *   add           0: the weights of all of the sequence's positions are set to w; else w is added to the weights of positions before the new tokens, and those of the
+ *                 new tokens are set (their pages may have been others' before)
+ * Weights of other positions, and of pages that are none, are not touched.  No two sequences of a batch may share a page.  Asynchronous on `stream`.
+ * Errors as sali_pages_attend's; n_seqs * n_kv_heads * (max_kv / 128 rounded up) is below 2^24 (SALI_ERR_SHAPE). */
+int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, float softmax_scale, int32_t window,
+                     int32_t sinks, const float* d_lse, int32_t add, float* d_weights, void* stream);
+
+/* Which of a sequence's last n = d_start[s + 1] - d_start[s] tokens stay (n = d_length[s]: of all), for each K/V head by itself: the first `sinks` and the last `recent` of
+ * them, and of the others those of most weight, the first ones of equal weight, `budget` in all; all n if there are no more.  A NaN counts as more than
+ * all numbers; tokens of a page that is none as less.
+ *   d_weights     as above
+ *   d_keep        int32[n_seqs][n_kv_heads][budget]: their places among the n, rising; -1 behind the last
+ * Asynchronous on `stream`.  SALI_ERR_SHAPE for a budget below 1 or below sinks + recent, and for 2^22 sequences times K/V heads. */
+int sali_pages_select(sali_pages* p, const sali_page_batch* batch, const float* d_weights, int32_t budget, int32_t sinks, int32_t recent,
+                      int32_t* d_keep, void* stream);
+
+/* Moves rows together, as they are stored: the i-th entry of a list names the one of the sequence's last n tokens (n as above) whose K/V rows, and weight if d_weights
+ * is given, go to position d_length[s] - n + i.  An entry below 0 moves nothing.  The caller's lengths are then smaller; rows keep the rotary positions they had.
+ *   d_keep        int32[n_seqs][keep_heads][keep_width], keep_heads = n_kv_heads, or 1: one list for all heads.  Of a list, the first n entries count.
+ *   d_to_or_null  NULL: in the sequence's own pages; entries are then not below their place in the list (as rising ones are).  Else int32[n_seqs][to_width], a page table of
+ *                 where rows go (as d_table, by position), none of whose pages the batch's d_table names: for texts whose pages others share
+ * An entry that is out of range (n or more, below its place in the list if in place, or of a position that the table is too narrow for) moves nothing and sets
+ * SALI_FAULT_BATCH; rows of a page that is none become zeros (weight 0), rows to one are not written; both set SALI_FAULT_PAGE.
+ * In place and elsewhere, no two sequences of a batch may write the same page.  Asynchronous on `stream`.  SALI_ERR_SHAPE for keep_heads or widths out of
+ * range, and for 2^24 thread blocks: n_seqs * n_kv_heads * (head_dim / 16 + 1), and elsewhere that for every 64 rows. */
+int sali_pages_keep(sali_pages* p, int32_t layer, const sali_page_batch* batch, const int32_t* d_keep, int32_t keep_heads, int32_t keep_width,
+                    const int32_t* d_to_or_null, int32_t to_width, float* d_weights_or_null, void* stream);
+
 /* Copies the status bits to host memory and waits for `stream`. */
 int sali_pages_get_status(sali_pages* p, uint32_t* h_status, void* stream);
 

@@ -147,18 +147,33 @@ def block_bytes_of(spec, k_bits, v_bits, block, own):
 
 
 # ---- attention -------------------------------------------------------------------------------------
-def attend(q, k, v, length, scale, window=0, sinks=0, prior=None, prior_lse=None, hidden=None):
-    """One sequence: q [n, n_heads, D], k, v [length, n_kv, D] (float64) -> out [n, n_heads, D], lse [n, n_heads], and, for error bounds,
-    weights' sum over |V| and the largest sum of |q k|, alike.  hidden: positions that nobody sees (pages that are none)."""
-    n, hq, d = q.shape
-    group = hq // k.shape[1]
-    pos = np.arange(length - n, length)[:, None]
-    j = np.arange(length)[None]
+def visible(n, length, window=0, sinks=0):
+    """[n, length]: which positions the last n tokens see."""
+    pos, j = np.arange(length - n, length)[:, None], np.arange(length)[None]
     seen = j <= pos
     if window > 0:
         seen &= (j > pos - window) | (j < sinks)
+    return seen
+
+
+def drafted(masks, length):
+    """The same for a draft of len(masks) tokens: everything before it, and what each one's mask names."""
+    n = len(masks)
+    seen = np.ones((n, length), bool)
+    for t, m in enumerate(masks):
+        seen[t, length - n:] = [int(m) >> i & 1 == 1 for i in range(n)]
+    return seen
+
+
+def attend(q, k, v, length, scale, window=0, sinks=0, prior=None, prior_lse=None, hidden=None, seen=None):
+    """One sequence: q [n, n_heads, D], k, v [length, n_kv, D] (float64) -> out [n, n_heads, D], lse [n, n_heads], and, for error bounds,
+    weights' sum over |V| and the largest sum of |q k|, alike.  hidden: positions that nobody sees (pages that are none).  seen [n, length]: what
+    each row sees, in place of causality, window and sinks."""
+    n, hq, d = q.shape
+    group = hq // k.shape[1]
+    seen = visible(n, length, window, sinks) if seen is None else seen
     if hidden is not None:
-        seen &= ~hidden[None, :length]
+        seen = seen & ~hidden[None, :length]
     out, lse = np.zeros((n, hq, d)), np.full((n, hq), -np.inf)
     mass, reach = np.zeros((n, hq, d)), np.zeros((n, hq))
     for h in range(hq):
@@ -201,3 +216,78 @@ def bounds(spec, out, lse, mass, reach, length, v_max):
         d_out = d_out + length * 2.0 ** -35 * v_max
     d_lse = step + 2.0 ** -22 * (1.0 + np.where(np.isfinite(lse), np.abs(lse), 0.0))
     return d_out, d_lse
+
+
+# ---- rotary positions ------------------------------------------------------------------------------
+def rotate(x, position, frequency, sections, adjacent=False, inverse=False):
+    """x [T, heads, D] (float64), position [axes, T] -> the turned rows, and for error bounds the sum of the sizes that each value is made of."""
+    m = len(frequency)
+    out, size = x.copy(), np.abs(x)
+    axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    for i in range(m):
+        a = position[axis[i]].astype(np.float64) * frequency[i] * (-1 if inverse else 1)
+        c, s = np.cos(a)[:, None], np.sin(a)[:, None]
+        p, q = (2 * i, 2 * i + 1) if adjacent else (i, i + m)
+        with np.errstate(invalid="ignore", over="ignore"):
+            out[..., p] = x[..., p] * c - x[..., q] * s
+            out[..., q] = x[..., q] * c + x[..., p] * s
+        size[..., p] = size[..., q] = np.abs(x[..., p]) + np.abs(x[..., q])
+    return out, size
+
+
+# ---- weights of keys, and cutting a text down ------------------------------------------------------
+def weigh(q, k, length, scale, lse, window=0, sinks=0, hidden=None):
+    """w [length, n_kv]: exp(s - lse) summed over the rows that see a position and the heads of a group, and how far a right result may be from it: the D products of
+    a score in fp32, D 2^-24 of the sum of their sizes, the scale's two roundings and the products' 2^-22 of it; lse times log2 e 2^-23 of it, their difference 2^-23 of it; exp2
+    2^-22; the sum over the rows and lanes, a rounding each.  Weights below fp32's normal numbers may be zero."""
+    n, hq, d = q.shape
+    group = hq // k.shape[1]
+    seen = visible(n, length, window, sinks)
+    if hidden is not None:
+        seen &= ~hidden[None, :length]
+    w, far = np.zeros((length, k.shape[1])), np.zeros((length, k.shape[1]))
+    for h in range(hq):
+        kh, l = k[:length, h // group], lse[:, h, None]
+        with np.errstate(all="ignore"):
+            s = scale * (q[:, h] @ kh.T)
+            some = seen & ~np.isneginf(l)
+            e = np.where(some, np.exp(s - l), 0.0)
+            reach = np.abs(scale) * (np.abs(q[:, h]) @ np.abs(kh).T)
+            step = reach * ((d + 4) * 2.0 ** -24) + np.abs(l) * 2.0 ** -23 + np.abs(s - l) * 2.0 ** -23 + 2.0 ** -22 + (n * group + 64) * 2.0 ** -24
+            w[:, h // group] += e.sum(0)
+            far[:, h // group] += (np.where(some & (e > 0), 1.01 * e * step, 0.0) + np.where(some, 2.0 ** -126, 0.0)).sum(0)
+    return w, far
+
+
+def select(w, budget, sinks=0, recent=0):
+    """Places of [n] weights that stay, rising: the definition by counting what comes before each of the others."""
+    n = len(w)
+    if n <= budget:
+        return list(range(n))
+    rest = range(sinks, n - recent)
+    stay = [i for i in range(n) if i < sinks or i >= n - recent]
+    value = [np.inf if np.isnan(w[i]) else w[i] for i in range(n)]
+    for i in rest:
+        better = sum(1 for j in rest if (np.isnan(w[j]) and not np.isnan(w[i])) or
+                     (np.isnan(w[j]) == np.isnan(w[i]) and (value[j] > value[i] or (value[j] == value[i] and j < i))))
+        if better < budget - sinks - recent:
+            stay.append(i)
+    return sorted(stay)
+
+
+def bytes_of_token(spec, t):
+    """Offsets of all of a block's bytes that are token t's, in an order that is the same for every token."""
+    at, parts, d = [], _parts(spec), spec.head_dim
+    for side in (0, 1):
+        for e in range(d):
+            byte, shift = byte_of(spec, side, t, e)
+            if shift == 0:
+                at.append(byte)
+            if spec.store == "16":
+                at.append(byte + 1)
+        for g in range(0 if spec.store == "16" else d // GROUP):
+            slot = g * 16 + (place(t) if side == 0 else t)
+            at += [parts[2 + side] + slot * 4 + i for i in range(4)]
+            if spec.store == "int4":
+                at += [parts[4 + side] + slot * 2 + i for i in range(2)]
+    return np.array(at)

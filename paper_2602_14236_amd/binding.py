@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional
+from typing import Optional, Sequence
 
 import numpy as np
 import torch   # imported before the library is loaded so that both share one HIP runtime
@@ -80,6 +80,11 @@ class sali_rows(C.Structure):
     _fields_ = [("d", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
+class sali_rotary(C.Structure):
+    _fields_ = [("d_frequency", C.c_void_p), ("pairs", C.c_int32), ("axes", C.c_int32), ("section", C.c_int32 * 4), ("adjacent", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 EXPORTS = {
     "sali_workspace_bytes": (C.c_int, [C.POINTER(sali_config), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t),
                                        C.POINTER(C.c_size_t)]),
@@ -126,6 +131,15 @@ EXPORTS = {
     "sali_pages_read": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(sali_page_batch), C.POINTER(sali_rows), C.POINTER(sali_rows), C.c_void_p]),
     "sali_pages_attend": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(sali_page_batch), C.POINTER(sali_rows), C.c_float, C.c_int32, C.c_int32,
                                     C.c_void_p, C.c_void_p, C.POINTER(sali_rows), C.c_void_p, C.c_void_p]),
+    "sali_pages_rotate": (C.c_int, [C.c_void_p, C.POINTER(sali_rotary), C.c_void_p, C.c_int32, C.c_int32, C.POINTER(sali_rows), C.POINTER(sali_rows),
+                                    C.POINTER(sali_rows), C.POINTER(sali_rows), C.c_void_p]),
+    "sali_pages_attend_tree": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(sali_page_batch), C.c_void_p, C.POINTER(sali_rows), C.c_float, C.c_void_p,
+                                         C.c_void_p, C.POINTER(sali_rows), C.c_void_p, C.c_void_p]),
+    "sali_pages_weigh": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(sali_page_batch), C.POINTER(sali_rows), C.c_float, C.c_int32, C.c_int32, C.c_void_p,
+                                   C.c_int32, C.c_void_p, C.c_void_p]),
+    "sali_pages_select": (C.c_int, [C.c_void_p, C.POINTER(sali_page_batch), C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
+    "sali_pages_keep": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(sali_page_batch), C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p,
+                                  C.c_void_p]),
     "sali_pages_get_status": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint32), C.c_void_p]),
 }
 
@@ -447,6 +461,34 @@ class PageBatch:
                                  max_kv, 0)
 
 
+def draft_masks(parents: Sequence[int]):
+    """What the tokens of a drafted tree see of it, as attend_tree takes it (bits of a signed 64-bit number): themselves and all that they follow.  parents: of each
+    token the place of the one before it in the draft, which lies before its own, or -1 for those that follow the text."""
+    if len(parents) > 64:
+        raise ValueError(f"a draft has 64 tokens at most, not {len(parents)}")
+    masks = []
+    for i, p in enumerate(parents):
+        if not -1 <= p < i:
+            raise ValueError(f"token {i} of a draft follows one before it or the text (-1), not {p}")
+        masks.append((masks[p] if p >= 0 else 0) | 1 << i)
+    return [m - (1 << 64) if m >> 63 else m for m in masks]
+
+
+class Rotary:
+    """Which pairs of a row turn how fast: frequency, float64 [pairs] on the GPU (radians per position), and how many of them belong to each axis of the
+    positions (if not given, all to one).  adjacent: values 2 i and 2 i + 1 are a pair, else i and i + pairs."""
+
+    def __init__(self, frequency: torch.Tensor, sections: Optional[Sequence[int]] = None, *, adjacent: bool = False):
+        if frequency.dtype is not torch.float64 or frequency.dim() != 1 or not frequency.is_contiguous():
+            raise ValueError(f"frequency: contiguous float64 tensor of one dimension expected, got {frequency.dtype} {tuple(frequency.shape)}")
+        sections = [frequency.shape[0]] if sections is None else list(sections)
+        if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) != frequency.shape[0]:
+            raise ValueError(f"one to four sections of {frequency.shape[0]} pairs in all expected, got {sections}")
+        self.frequency = frequency
+        self.device, self.index, self.axes = frequency.device, frequency.get_device(), len(sections)
+        self.c = sali_rotary(frequency.data_ptr(), frequency.shape[0], len(sections), (C.c_int32 * 4)(*sections), int(adjacent), 0)
+
+
 class SaliPages:
     """Owns the pool (or works in the caller's) and the scratch of a paged cache and forwards the C calls.  Per-token tensors are [tokens, heads,
     head_dim] with values side by side; tokens and heads may be strided (slices of one projection's output).  Where another GPU is the current one,
@@ -465,6 +507,7 @@ class SaliPages:
             raise ValueError(f"pool: {pool_bytes} contiguous bytes on {self.device} expected, got {pool.numel() * pool.element_size()} on {pool.device}")
         self.dtype = torch.bfloat16 if cfg.dtype else torch.float16
         self.n_heads, self.n_kv_heads, self.head_dim = cfg.n_heads, cfg.n_kv_heads, cfg.head_dim
+        self._weights_shape = (cfg.n_pages, cfg.n_kv_heads, cfg.page_tokens)
         self.handle = None
         with torch.cuda.device(self.device):
             self.pool = torch.empty(pool_bytes, dtype=torch.uint8, device=self.device) if pool is None else pool
@@ -493,10 +536,25 @@ class SaliPages:
                              f"side expected, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
         return sali_rows(t.data_ptr(), token, head)
 
+    def _token_rows(self, t: torch.Tensor, tokens: int, heads: int, name: str) -> sali_rows:
+        token, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if t.dtype is not self.dtype or t.shape != (tokens, heads, self.head_dim) or one != 1 or t.get_device() != self.index:
+            raise ValueError(f"{name}: {self.dtype} [{tokens}, {heads}, {self.head_dim}] on {self.device} with its last dimension side by "
+                             f"side expected, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
+        return sali_rows(t.data_ptr(), token, head)
+
     def _call(self, batch: PageBatch, stream: Optional[torch.cuda.Stream]) -> int:
         """The stream of a call on `batch`: the pages' GPU's current one, if none is given."""
         if batch.index != self.index:
             raise ValueError(f"the batch lies on {batch.device}, the pages on {self.device}")
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.index)
+        if stream.device_index != self.index:
+            raise ValueError(f"the stream is of {stream.device}, the pages lie on {self.device}")
+        return stream.cuda_stream
+
+    def _stream_of(self, stream: Optional[torch.cuda.Stream]) -> int:
+        """The same for a call without a batch."""
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self.index)
         if stream.device_index != self.index:
@@ -541,6 +599,84 @@ class SaliPages:
                                           self._dense(prior, (batch.tokens, n, d), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
                                           self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"),
                                           self._call(batch, stream)), "sali_pages_attend")
+
+    def _ints(self, t: torch.Tensor, dtype, dims, name: str):
+        """dims: sizes, None where any will do"""
+        if t.dtype is not dtype or t.dim() != len(dims) or any(d is not None and d != n for d, n in zip(dims, t.shape)) or not t.is_contiguous() or \
+                t.get_device() != self.index:
+            raise ValueError(f"{name}: contiguous {dtype} {list(dims)} on {self.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def rotate(self, rotary: Rotary, position: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor] = None,
+               k_out: Optional[torch.Tensor] = None, *, inverse: bool = False, stream: Optional[torch.cuda.Stream] = None):
+        """Turn queries [tokens, n_heads, head_dim] and keys [tokens, n_kv_heads, head_dim], or one of the two, by their positions, int32 [axes, tokens] (or [tokens]
+        for one axis); in place where no output is given.  inverse: back."""
+        if torch._C._cuda_getDevice() != self.index:
+            with torch.cuda.device(self.index):
+                return self.rotate(rotary, position, q, k, q_out, k_out, inverse=inverse, stream=stream)
+        if rotary.index != self.index:
+            raise ValueError(f"the frequencies lie on {rotary.device}, the pages on {self.device}")
+        if position.dim() == 1:
+            position = position[None]
+        at = self._ints(position, torch.int32, (rotary.axes, None), "position")
+        n = position.shape[1]
+        rows = []
+        for x, out, heads, name in ((q, q_out, self.n_heads, "q"), (k, k_out, self.n_kv_heads, "k")):
+            if x is None and out is not None:
+                raise ValueError(f"{name}_out is given without {name}")
+            rows.append(None if x is None else (self._token_rows(x, n, heads, name), self._token_rows(x if out is None else out, n, heads, name + "_out")))
+        q, k = rows
+        _check(self.lib.sali_pages_rotate(self.handle, rotary.c, at, n, inverse, q and q[0], k and k[0], q and q[1], k and k[1], self._stream_of(stream)),
+               "sali_pages_rotate")
+
+    def attend_tree(self, layer: int, batch: PageBatch, seen: torch.Tensor, q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
+                    lse: Optional[torch.Tensor] = None, *, prior: Optional[torch.Tensor] = None, prior_lse: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None):
+        """Attention of drafted tokens, the batch's new ones (64 a sequence at most): each sees what came before the draft, and of the draft the tokens whose bits are
+        set in its mask (`seen`, int64 [tokens]; draft_masks makes them from a tree).  The others as in attend."""
+        if torch._C._cuda_getDevice() != self.index:
+            with torch.cuda.device(self.index):
+                return self.attend_tree(layer, batch, seen, q, softmax_scale, out, lse, prior=prior, prior_lse=prior_lse, stream=stream)
+        n, d = self.n_heads, self.head_dim
+        _check(self.lib.sali_pages_attend_tree(self.handle, layer, batch.c, self._ints(seen, torch.int64, (batch.tokens,), "seen"),
+                                               self._rows(q, batch, n, "q"), softmax_scale, self._dense(prior, (batch.tokens, n, d), "prior"),
+                                               self._dense(prior_lse, (batch.tokens, n), "prior_lse"), self._rows(out, batch, n, "out"),
+                                               self._dense(lse, (batch.tokens, n), "lse"), self._call(batch, stream)), "sali_pages_attend_tree")
+
+    def weigh(self, layer: int, batch: PageBatch, q: torch.Tensor, softmax_scale: float, lse: torch.Tensor, weights: torch.Tensor, *, add: bool = True,
+              window: int = 0, sinks: int = 0, stream: Optional[torch.cuda.Stream] = None):
+        """What attention weight each key had from the batch's new tokens, summed over them and the query heads of its K/V head, into `weights`, fp32 [n_pages,
+        n_kv_heads, page_tokens] of this layer: added to those of earlier tokens (add), or set.  q, lse, window and sinks: of the attention."""
+        if torch._C._cuda_getDevice() != self.index:
+            with torch.cuda.device(self.index):
+                return self.weigh(layer, batch, q, softmax_scale, lse, weights, add=add, window=window, sinks=sinks, stream=stream)
+        _check(self.lib.sali_pages_weigh(self.handle, layer, batch.c, self._rows(q, batch, self.n_heads, "q"), softmax_scale, window, sinks,
+                                         self._dense(lse, (batch.tokens, self.n_heads), "lse"), add,
+                                         self._dense(weights, self._weights_shape, "weights"), self._call(batch, stream)), "sali_pages_weigh")
+
+    def select(self, batch: PageBatch, weights: torch.Tensor, budget: int, keep: torch.Tensor, *, sinks: int = 0, recent: int = 0,
+               stream: Optional[torch.cuda.Stream] = None):
+        """Which of each sequence's new tokens (all, if it has no others) stay: the first `sinks`, the last `recent`, and those of most weight, `budget` in all.  Their places go
+        to `keep`, int32 [sequences, n_kv_heads, budget], rising, -1 behind the last."""
+        if torch._C._cuda_getDevice() != self.index:
+            with torch.cuda.device(self.index):
+                return self.select(batch, weights, budget, keep, sinks=sinks, recent=recent, stream=stream)
+        _check(self.lib.sali_pages_select(self.handle, batch.c, self._dense(weights, self._weights_shape, "weights"), budget, sinks, recent,
+                                          self._ints(keep, torch.int32, (batch.c.n_seqs, self.n_kv_heads, budget), "keep"),
+                                          self._call(batch, stream)), "sali_pages_select")
+
+    def keep(self, layer: int, batch: PageBatch, keep: torch.Tensor, *, to: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None):
+        """Move the rows (and weights) of those of each sequence's new tokens that `keep` names, int32 [sequences, n_kv_heads or 1, width], to the places from the first
+        new token on: in its own pages, or in those of the page table `to`, int32 [sequences, width], which are none of the batch's."""
+        if torch._C._cuda_getDevice() != self.index:
+            with torch.cuda.device(self.index):
+                return self.keep(layer, batch, keep, to=to, weights=weights, stream=stream)
+        n = batch.c.n_seqs
+        at = self._ints(keep, torch.int32, (n, None, None), "keep")
+        _check(self.lib.sali_pages_keep(self.handle, layer, batch.c, at, keep.shape[1], keep.shape[2],
+                                        None if to is None else self._ints(to, torch.int32, (n, None), "to"), 0 if to is None else to.shape[1],
+                                        self._dense(weights, self._weights_shape, "weights"), self._call(batch, stream)), "sali_pages_keep")
 
     def get_status(self) -> int:
         if torch._C._cuda_getDevice() != self.index:

@@ -35,11 +35,16 @@ SOURCES = {
     "pages_kernels.hip": ["-ffp-contract=off"],
     "pages_attn_fp16.hip": ["-ffp-contract=fast"],
     "pages_attn_bf16.hip": ["-ffp-contract=fast"],
+    "pages_tree_fp16.hip": ["-ffp-contract=fast"],
+    "pages_tree_bf16.hip": ["-ffp-contract=fast"],
+    "pages_weigh.hip": ["-ffp-contract=fast"],
+    "pages_keep.hip": [],
+    "rotary_kernels.hip": ["-ffp-contract=fast"],
 }
 
 # Kernels whose registers have to suffice.  Where a vector register was spilled in one of them, the compiler put the store at the head of a block ahead of
 # the instruction that brings the masked lanes back, and waves reloaded what they had never stored; the build refuses such code.
-NO_SPILLS = ("pages_attn_fp16.hip", "pages_attn_bf16.hip")
+NO_SPILLS = ("pages_attn_fp16.hip", "pages_attn_bf16.hip", "pages_tree_fp16.hip", "pages_tree_bf16.hip", "pages_weigh.hip", "pages_keep.hip")
 REPORT = ["-Rpass-analysis=kernel-resource-usage"]
 
 

@@ -47,6 +47,47 @@ struct PagesAttend {
     int32_t heads, group;                   // query heads, and of one K/V head
     float* partial;
     int32_t* records;
+    const uint64_t* seen;                   // of drafted tokens, a mask each
+};
+
+// rotary positions of queries and keys
+struct Rotate {
+    RowsIn q, k;
+    RowsOut q_out, k_out;
+    const double* frequency;
+    const int32_t* position;
+    int64_t axis_stride;
+    int32_t q_heads, k_heads, dim, pairs, adjacent, inverse, n_tokens;
+    int32_t until[3];                       // first pair of the second, third and fourth axis
+};
+
+// attention weights of keys, summed
+struct PagesWeigh {
+    PageGeom geom;
+    PageSeqs seqs;
+    RowsIn q;
+    const float* lse;
+    float* weights;                         // [page][K/V head][token]
+    float scale2;                           // as PagesAttend has them
+    uint32_t q_keep, q_flip;
+    int32_t window, sinks, heads, group, add;
+};
+
+struct PagesSelect {
+    PageGeom geom;
+    PageSeqs seqs;
+    const float* weights;
+    int32_t* keep;
+    int32_t budget, sinks, recent;
+};
+
+struct PagesKeep {
+    PageGeom geom;
+    PageSeqs seqs;
+    const int32_t* keep;
+    const int32_t* to;                      // table of the places where rows go
+    float* weights;                         // or NULL
+    int32_t width, keep_heads, to_width, in_place;
 };
 
 // scratch of the pages object: the status word, then the partial results of attention
@@ -60,6 +101,21 @@ hipError_t launch_pages_append(int dtype, int store, int dim, const PageGeom& g,
 hipError_t launch_pages_read(int dtype, int store, int dim, const PageGeom& g, const PageSeqs& seqs, const RowsOut& k, const RowsOut& v, hipStream_t s);
 hipError_t launch_pages_attend_fp16(int store, int dim, const PagesAttend& a, hipStream_t s);
 hipError_t launch_pages_attend_bf16(int store, int dim, const PagesAttend& a, hipStream_t s);
+hipError_t launch_pages_attend_tree_fp16(int store, int dim, const PagesAttend& a, hipStream_t s);
+hipError_t launch_pages_attend_tree_bf16(int store, int dim, const PagesAttend& a, hipStream_t s);
+constexpr int kWeighTokens = 128;           // keys of a thread block
+inline int64_t weigh_blocks(const PageSeqs& q) { return ((int64_t)q.max_kv + kWeighTokens - 1) / kWeighTokens; }
+constexpr int kKeepTokens = 64;             // rows of a thread block, if they go to other pages
+inline int64_t keep_chunks(const PageSeqs& q, int32_t width, bool in_place) {
+    // (a sequence's first place may lie inside a block of 16)
+    return in_place ? 1 : (least((int64_t)width, (int64_t)q.max_q) + kBlockTokens - 1 + kKeepTokens - 1) / kKeepTokens;
+}
+inline int keep_strips(int dim, bool weights) { return 2 * (dim / 32) + (weights ? 1 : 0); }
+constexpr int64_t kMostBlocks = (1 << 24) - 1;      // thread blocks of 256 threads that a launch takes
+hipError_t launch_rotate(int dtype, const Rotate& r, hipStream_t s);
+hipError_t launch_pages_weigh(int dtype, int store, int dim, const PagesWeigh& a, hipStream_t s);
+hipError_t launch_pages_select(const PagesSelect& a, hipStream_t s);
+hipError_t launch_pages_keep(int store, int dim, const PagesKeep& a, hipStream_t s);
 
 #ifdef __HIPCC__
 // Does the start of one of the sequences i, i + step .. lie behind the next one's?  Nobody knows then whose rows are whose: the batch is left out whole.

@@ -76,6 +76,49 @@ R rows_of(const sali_rows& r) {
     return {static_cast<decltype(R::d)>(r.d), r.token_stride * 2, r.head_stride * 2};
 }
 
+// what both forms of attention need besides their masks
+int check_attend(const sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, const float* prior, const float* prior_lse,
+                 const sali_rows* out, const float* lse) {
+    int rc = check_batch(p, layer, batch);
+    if (rc == SALI_OK) rc = check_rows(q, batch->n_tokens > 0);
+    if (rc == SALI_OK) rc = check_rows(out, batch->n_tokens > 0);
+    if (rc != SALI_OK) return rc;
+    if ((prior == nullptr) != (prior_lse == nullptr)) return SALI_ERR_NULL;
+    if ((uintptr_t)prior % 16 != 0 || ((uintptr_t)prior_lse | (uintptr_t)lse) % 4 != 0) return SALI_ERR_ALIGN;
+    return SALI_OK;
+}
+int check_window(int32_t window, int32_t sinks) { return window < 0 || sinks < 0 || window > (1 << 30) || sinks > (1 << 30) ? SALI_ERR_SHAPE : SALI_OK; }
+int check_scale(float softmax_scale) { return isfinite(softmax_scale * 1.44269504088896340736f) ? SALI_OK : SALI_ERR_CONFIG; }
+// rows and tiles are counted in 31 bits
+int check_sizes(const sali_pages* p, const sali_page_batch& b) {
+    if ((int64_t)b.n_tokens * (p->cfg.n_heads / p->cfg.n_kv_heads) >= 0x7FFFFFFF - 1024) return SALI_ERR_SHAPE;
+    if (((int64_t)b.max_kv / kTileTokens + 2) * p->cfg.n_kv_heads > 0x7FFFFFFFll / b.n_seqs) return SALI_ERR_SHAPE;
+    return SALI_OK;
+}
+
+float scale2_of(float softmax_scale) { return softmax_scale == 0.0f ? 1.0f : fabsf(softmax_scale) * 1.44269504088896340736f; }
+uint32_t keep_of(float softmax_scale) { return softmax_scale == 0.0f ? 0u : ~0u; }
+uint32_t flip_of(float softmax_scale) { return softmax_scale < 0.0f ? 0x80008000u : 0u; }
+PagesAttend attend_of(sali_pages* p, int32_t layer, const sali_page_batch& batch, const sali_rows& q, float softmax_scale, const float* prior,
+                      const float* prior_lse, const sali_rows& out, float* lse) {
+    PagesAttend a = {};
+    a.geom = geom_of(p, layer);
+    a.seqs = seqs_of(p, batch);
+    a.q = rows_of<RowsIn>(q);
+    a.out = rows_of<RowsOut>(out);
+    a.lse = lse;
+    a.prior = prior;
+    a.prior_lse = prior_lse;
+    a.scale2 = scale2_of(softmax_scale);
+    a.q_keep = keep_of(softmax_scale);
+    a.q_flip = flip_of(softmax_scale);
+    a.heads = p->cfg.n_heads;
+    a.group = p->cfg.n_heads / p->cfg.n_kv_heads;
+    a.partial = reinterpret_cast<float*>(p->scratch + p->layout.partial);
+    a.records = reinterpret_cast<int32_t*>(p->scratch + p->layout.records);
+    return a;
+}
+
 }  // namespace
 
 }  // namespace sali
@@ -141,39 +184,150 @@ int sali_pages_read(sali_pages* p, int32_t layer, const sali_page_batch* batch, 
 
 int sali_pages_attend(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, float softmax_scale, int32_t window, int32_t sinks,
                       const float* d_prior_or_null, const float* d_prior_lse_or_null, const sali_rows* out, float* d_lse_or_null, void* stream) {
-    int rc = check_batch(p, layer, batch);
-    if (rc == SALI_OK) rc = check_rows(q, batch->n_tokens > 0);
-    if (rc == SALI_OK) rc = check_rows(out, batch->n_tokens > 0);
+    int rc = check_attend(p, layer, batch, q, d_prior_or_null, d_prior_lse_or_null, out, d_lse_or_null);
+    if (rc == SALI_OK) rc = check_window(window, sinks);
+    if (rc == SALI_OK) rc = check_scale(softmax_scale);
     if (rc != SALI_OK) return rc;
-    if ((d_prior_or_null == nullptr) != (d_prior_lse_or_null == nullptr)) return SALI_ERR_NULL;
-    if ((uintptr_t)d_prior_or_null % 16 != 0 || ((uintptr_t)d_prior_lse_or_null | (uintptr_t)d_lse_or_null) % 4 != 0) return SALI_ERR_ALIGN;
-    if (window < 0 || sinks < 0 || window > (1 << 30) || sinks > (1 << 30)) return SALI_ERR_SHAPE;
-    if (!isfinite(softmax_scale * 1.44269504088896340736f)) return SALI_ERR_CONFIG;
     if (nothing_to_do(*batch)) return SALI_OK;
-    // rows and tiles are counted in 31 bits
-    if ((int64_t)batch->n_tokens * (p->cfg.n_heads / p->cfg.n_kv_heads) >= 0x7FFFFFFF - 1024) return SALI_ERR_SHAPE;
-    if (((int64_t)batch->max_kv / kTileTokens + 2) * p->cfg.n_kv_heads > 0x7FFFFFFFll / batch->n_seqs) return SALI_ERR_SHAPE;
-    PagesAttend a = {};
-    a.geom = geom_of(p, layer);
-    a.seqs = seqs_of(p, *batch);
-    a.q = rows_of<RowsIn>(*q);
-    a.out = rows_of<RowsOut>(*out);
-    a.lse = d_lse_or_null;
-    a.prior = d_prior_or_null;
-    a.prior_lse = d_prior_lse_or_null;
-    a.scale2 = softmax_scale == 0.0f ? 1.0f : fabsf(softmax_scale) * 1.44269504088896340736f;
-    a.q_keep = softmax_scale == 0.0f ? 0u : ~0u;
-    a.q_flip = softmax_scale < 0.0f ? 0x80008000u : 0u;
+    rc = check_sizes(p, *batch);
+    if (rc != SALI_OK) return rc;
+    PagesAttend a = attend_of(p, layer, *batch, *q, softmax_scale, d_prior_or_null, d_prior_lse_or_null, *out, d_lse_or_null);
     a.window = window;
     a.sinks = window > 0 ? sinks : 0;
-    a.heads = p->cfg.n_heads;
-    a.group = p->cfg.n_heads / p->cfg.n_kv_heads;
-    a.partial = reinterpret_cast<float*>(p->scratch + p->layout.partial);
-    a.records = reinterpret_cast<int32_t*>(p->scratch + p->layout.records);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = p->cfg.dtype == SALI_DTYPE_BF16 ? launch_pages_attend_bf16(p->cfg.store, p->cfg.head_dim, a, s)
                                                          : launch_pages_attend_fp16(p->cfg.store, p->cfg.head_dim, a, s);
     return e == hipSuccess ? SALI_OK : SALI_ERR_HIP;
+}
+
+int sali_pages_attend_tree(sali_pages* p, int32_t layer, const sali_page_batch* batch, const uint64_t* d_seen, const sali_rows* q, float softmax_scale,
+                           const float* d_prior_or_null, const float* d_prior_lse_or_null, const sali_rows* out, float* d_lse_or_null, void* stream) {
+    int rc = check_attend(p, layer, batch, q, d_prior_or_null, d_prior_lse_or_null, out, d_lse_or_null);
+    if (rc == SALI_OK) rc = check_scale(softmax_scale);
+    if (rc != SALI_OK) return rc;
+    if (batch->max_q > kMostDrafted) return SALI_ERR_SHAPE;
+    if (d_seen == nullptr && batch->n_tokens > 0) return SALI_ERR_NULL;
+    if ((uintptr_t)d_seen % 8 != 0) return SALI_ERR_ALIGN;
+    if (nothing_to_do(*batch)) return SALI_OK;
+    rc = check_sizes(p, *batch);
+    if (rc != SALI_OK) return rc;
+    PagesAttend a = attend_of(p, layer, *batch, *q, softmax_scale, d_prior_or_null, d_prior_lse_or_null, *out, d_lse_or_null);
+    a.seen = d_seen;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t e = p->cfg.dtype == SALI_DTYPE_BF16 ? launch_pages_attend_tree_bf16(p->cfg.store, p->cfg.head_dim, a, s)
+                                                         : launch_pages_attend_tree_fp16(p->cfg.store, p->cfg.head_dim, a, s);
+    return e == hipSuccess ? SALI_OK : SALI_ERR_HIP;
+}
+
+int sali_pages_rotate(sali_pages* p, const sali_rotary* rotary, const int32_t* d_position, int32_t n_tokens, int32_t inverse, const sali_rows* q_or_null,
+                      const sali_rows* k_or_null, const sali_rows* q_out_or_null, const sali_rows* k_out_or_null, void* stream) {
+    if (p == nullptr || rotary == nullptr) return SALI_ERR_NULL;
+    if ((q_or_null == nullptr) != (q_out_or_null == nullptr) || (k_or_null == nullptr) != (k_out_or_null == nullptr)) return SALI_ERR_NULL;
+    if (rotary->pairs < 1 || rotary->pairs > p->cfg.head_dim / 2 || rotary->axes < 1 || rotary->axes > 4) return SALI_ERR_CONFIG;
+    int64_t pairs = 0;
+    for (int i = 0; i < rotary->axes; ++i) {
+        if (rotary->section[i] < 0) return SALI_ERR_CONFIG;
+        pairs += rotary->section[i];
+    }
+    if (pairs != rotary->pairs) return SALI_ERR_CONFIG;
+    if (n_tokens < 0 || n_tokens > kMostBlocks) return SALI_ERR_SHAPE;
+    if (n_tokens > 0 && (d_position == nullptr || rotary->d_frequency == nullptr)) return SALI_ERR_NULL;
+    if ((uintptr_t)d_position % 4 != 0 || (uintptr_t)rotary->d_frequency % 8 != 0) return SALI_ERR_ALIGN;
+    for (const sali_rows* r : {q_or_null, k_or_null, q_out_or_null, k_out_or_null}) {
+        const int rc = r == nullptr ? SALI_OK : check_rows(r, n_tokens > 0);
+        if (rc != SALI_OK) return rc;
+    }
+    if (n_tokens == 0 || (q_or_null == nullptr && k_or_null == nullptr)) return SALI_OK;
+    Rotate r = {};
+    if (q_or_null != nullptr) {
+        r.q = rows_of<RowsIn>(*q_or_null);
+        r.q_out = rows_of<RowsOut>(*q_out_or_null);
+        r.q_heads = p->cfg.n_heads;
+    }
+    if (k_or_null != nullptr) {
+        r.k = rows_of<RowsIn>(*k_or_null);
+        r.k_out = rows_of<RowsOut>(*k_out_or_null);
+        r.k_heads = p->cfg.n_kv_heads;
+    }
+    r.frequency = rotary->d_frequency;
+    r.position = d_position;
+    r.axis_stride = n_tokens;
+    r.dim = p->cfg.head_dim;
+    r.pairs = rotary->pairs;
+    r.adjacent = rotary->adjacent != 0;
+    r.inverse = inverse != 0;
+    r.n_tokens = n_tokens;
+    for (int i = 0, upto = 0; i < 3; ++i) {
+        upto += i < rotary->axes ? rotary->section[i] : 0;
+        r.until[i] = i + 1 < rotary->axes ? upto : 0x7FFFFFFF;
+    }
+    return launch_rotate(p->cfg.dtype, r, static_cast<hipStream_t>(stream)) == hipSuccess ? SALI_OK : SALI_ERR_HIP;
+}
+
+int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, float softmax_scale, int32_t window, int32_t sinks,
+                     const float* d_lse, int32_t add, float* d_weights, void* stream) {
+    int rc = check_batch(p, layer, batch);
+    if (rc == SALI_OK) rc = check_rows(q, batch->n_tokens > 0);
+    if (rc == SALI_OK) rc = check_window(window, sinks);
+    if (rc == SALI_OK) rc = check_scale(softmax_scale);
+    if (rc != SALI_OK) return rc;
+    if (batch->n_tokens > 0 && (d_lse == nullptr || d_weights == nullptr)) return SALI_ERR_NULL;
+    if (((uintptr_t)d_lse | (uintptr_t)d_weights) % 4 != 0) return SALI_ERR_ALIGN;
+    if (nothing_to_do(*batch)) return SALI_OK;
+    rc = check_sizes(p, *batch);
+    if (rc != SALI_OK) return rc;
+    PagesWeigh a = {};
+    a.geom = geom_of(p, layer);
+    a.seqs = seqs_of(p, *batch);
+    if (weigh_blocks(a.seqs) * p->cfg.n_kv_heads > kMostBlocks / batch->n_seqs) return SALI_ERR_SHAPE;
+    a.q = rows_of<RowsIn>(*q);
+    a.lse = d_lse;
+    a.weights = d_weights;
+    a.scale2 = scale2_of(softmax_scale);
+    a.q_keep = keep_of(softmax_scale);
+    a.q_flip = flip_of(softmax_scale);
+    a.window = window;
+    a.sinks = window > 0 ? sinks : 0;
+    a.heads = p->cfg.n_heads;
+    a.group = p->cfg.n_heads / p->cfg.n_kv_heads;
+    a.add = add != 0;
+    const hipError_t e = launch_pages_weigh(p->cfg.dtype, p->cfg.store, p->cfg.head_dim, a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SALI_OK : SALI_ERR_HIP;
+}
+
+int sali_pages_select(sali_pages* p, const sali_page_batch* batch, const float* d_weights, int32_t budget, int32_t sinks, int32_t recent, int32_t* d_keep,
+                      void* stream) {
+    const int rc = check_batch(p, 0, batch);
+    if (rc != SALI_OK) return rc;
+    if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return SALI_ERR_SHAPE;
+    if (batch->n_tokens > 0 && (d_weights == nullptr || d_keep == nullptr)) return SALI_ERR_NULL;
+    if (((uintptr_t)d_weights | (uintptr_t)d_keep) % 4 != 0) return SALI_ERR_ALIGN;
+    if (nothing_to_do(*batch)) return SALI_OK;
+    if (4ll * p->cfg.n_kv_heads > kMostBlocks / batch->n_seqs) return SALI_ERR_SHAPE;        // of 1024 threads
+    const PagesSelect a = {geom_of(p, 0), seqs_of(p, *batch), d_weights, d_keep, budget, sinks, recent};
+    return launch_pages_select(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SALI_OK : SALI_ERR_HIP;
+}
+
+int sali_pages_keep(sali_pages* p, int32_t layer, const sali_page_batch* batch, const int32_t* d_keep, int32_t keep_heads, int32_t keep_width,
+                    const int32_t* d_to_or_null, int32_t to_width, float* d_weights_or_null, void* stream) {
+    const int rc = check_batch(p, layer, batch);
+    if (rc != SALI_OK) return rc;
+    if ((keep_heads != 1 && keep_heads != p->cfg.n_kv_heads) || keep_width < 0 || to_width < 0) return SALI_ERR_SHAPE;
+    if (batch->n_tokens > 0 && keep_width > 0 && d_keep == nullptr) return SALI_ERR_NULL;
+    if (((uintptr_t)d_keep | (uintptr_t)d_to_or_null | (uintptr_t)d_weights_or_null) % 4 != 0) return SALI_ERR_ALIGN;
+    if (nothing_to_do(*batch) || keep_width == 0) return SALI_OK;
+    PagesKeep a = {};
+    a.geom = geom_of(p, layer);
+    a.seqs = seqs_of(p, *batch);
+    a.keep = d_keep;
+    a.in_place = d_to_or_null == nullptr;
+    a.to = a.in_place ? batch->d_table : d_to_or_null;
+    a.weights = d_weights_or_null;
+    a.width = keep_width;
+    a.keep_heads = keep_heads;
+    a.to_width = a.in_place ? batch->table_width : to_width;
+    if (keep_chunks(a.seqs, a.width, a.in_place != 0) * p->cfg.n_kv_heads * keep_strips(p->cfg.head_dim, true) > kMostBlocks / batch->n_seqs) return SALI_ERR_SHAPE;
+    return launch_pages_keep(p->cfg.store, p->cfg.head_dim, a, static_cast<hipStream_t>(stream)) == hipSuccess ? SALI_OK : SALI_ERR_HIP;
 }
 
 int sali_pages_get_status(sali_pages* p, uint32_t* h_status, void* stream) {

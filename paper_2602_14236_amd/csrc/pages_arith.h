@@ -79,6 +79,23 @@ struct Sight {
 };
 SALI_BOTH Sight sight_of(int p, int j0, int window, int sinks) { return {p - j0, window == 0 ? -2147483647 : p - window - j0, sinks - j0}; }
 
+// The keys that drafted tokens see: the history, and of the draft what each token's mask names, so all of them see the keys up to the history's last and some of
+// them may see those up to the sequence's last.
+template <int kTokens>
+SALI_BOTH View view_of_draft(const PageSeq& q) { return {q.len - q.n - 1, q.len - 1, 0, 0, (q.len - 1) / kTokens + 1}; }
+// what a mask of the draft's tokens, of which there are n, shows of 32 keys; `from`: the first of them, counted from the draft's first token
+struct DraftSight {
+    uint32_t word;
+    SALI_BOTH bool has(int c) const { return (word >> c & 1u) != 0u; }
+};
+SALI_BOTH DraftSight draft_sight(uint64_t mask, int n, int from) {
+    if (n < 64) mask &= (1ull << n) - 1ull;
+    if (from >= 64) return {0u};
+    if (from >= 0) return {(uint32_t)(mask >> from)};
+    if (from <= -32) return {~0u};
+    return {(uint32_t)(mask << -from) | ((1u << -from) - 1u)};
+}
+
 // `total` tiles in `blocks` stretches (blocks <= total) that differ by one at most, the longer ones first
 struct Stretches {
     uint32_t each, longer;
@@ -125,6 +142,8 @@ struct TileSpan {
 };
 // The piece of row tile `unit` in block `block`: a block's pieces lie side by side.
 SALI_BOTH int stretch_piece(int unit, int block) { return unit + block; }
+
+constexpr int kMostDrafted = 64;            // tokens of a draft: bits of a mask
 
 // (rows of a batch are counted in 31 bits)
 template <int kWaves>

@@ -11,6 +11,28 @@ namespace {
 // Rows are taken 384 a block where that gives so many blocks, two rounds of one a compute unit, else 128.
 constexpr int kLargeBlocks = 2 * kComputeUnits;
 
+// The stream over sequences of up to stream_rows rows (16 kSets), which see up to `reach` keys as far as the batch's sizes tell
+template <int kStore, int kDim, bool kBf16, int kSets, bool kTree>
+void launch_stream(const PagesAttend& a, int stream_rows, int64_t reach, hipStream_t s) {
+    const PageSeqs& q = a.seqs;
+    const int group = a.group, n_kv = a.geom.n_kv;
+    const int64_t tiles = min((int64_t)q.max_kv + kTileTokens, reach) / kTileTokens * q.n_seqs * n_kv;
+    auto launch = [&](auto mode, dim3 grid) {
+        hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, decltype(mode)::value, kTree>), grid, dim3(64 * stream_waves(decltype(mode)::value)), 0, s, q.start,
+                           q.length, q.table, q.n_seqs, q.width, q.n_tokens, q.max_q, q.max_kv, a.geom.blocks_log2, a.window, a.sinks, group, n_kv, a,
+                           stream_rows, kStreamMinTiles);
+    };
+    const int64_t pairs = (int64_t)q.n_seqs * n_kv, tiles_a_pair = tiles / pairs;
+    if (tiles_a_pair <= 4 * stream_waves(StreamMode::pairs) && pairs <= kComputeUnits) {
+        launch(std::integral_constant<StreamMode, StreamMode::pairs>{}, dim3(n_kv, q.n_seqs));
+        return;
+    }
+    const int blocks = (int)max((int64_t)1, min((int64_t)kComputeUnits * stream_occupancy(kStore, kSets, StreamMode::stretches), (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
+    const int rows = (int)min((int64_t)stream_rows, (int64_t)q.max_q * group);
+    launch(std::integral_constant<StreamMode, StreamMode::stretches>{}, dim3(blocks));
+    hipLaunchKernelGGL((k_pages_stream_merge<kDim, kBf16>), dim3(blocks, (rows + 3) / 4), dim3(256), 0, s, a, 16 * kSets);
+}
+
 template <int kStore, int kDim, bool kBf16>
 void launch_attend(const PagesAttend& a, hipStream_t s) {
     const int n_kv = a.geom.n_kv, group = a.group;
@@ -27,27 +49,8 @@ void launch_attend(const PagesAttend& a, hipStream_t s) {
     }
     if (stream_rows > 0) {
         const int64_t reach = a.window > 0 ? (int64_t)a.window + a.seqs.max_q + a.sinks + 3 * kTileTokens : (int64_t)a.seqs.max_kv + kTileTokens;
-        const int64_t tiles = min((int64_t)a.seqs.max_kv + kTileTokens, reach) / kTileTokens * a.seqs.n_seqs * n_kv;
-        const PageSeqs& q = a.seqs;
-        auto go = [&](auto sets) {
-            constexpr int kSets = decltype(sets)::value;
-            auto launch = [&](auto mode, dim3 grid) {
-                hipLaunchKernelGGL((k_pages_stream<kStore, kDim, kBf16, kSets, decltype(mode)::value>), grid, dim3(64 * stream_waves(decltype(mode)::value)), 0, s, q.start, q.length,
-                                   q.table, q.n_seqs, q.width, q.n_tokens, q.max_q, q.max_kv, a.geom.blocks_log2, a.window, a.sinks, group, n_kv, a,
-                                   stream_rows, kStreamMinTiles);
-            };
-            const int64_t pairs = (int64_t)q.n_seqs * n_kv, tiles_a_pair = tiles / pairs;
-            if (tiles_a_pair <= 4 * stream_waves(StreamMode::pairs) && pairs <= kComputeUnits) {
-                launch(std::integral_constant<StreamMode, StreamMode::pairs>{}, dim3(n_kv, q.n_seqs));
-                return;
-            }
-            const int blocks = (int)max((int64_t)1, min((int64_t)kComputeUnits * stream_occupancy(kStore, kSets, StreamMode::stretches), (tiles + kStreamMinTiles - 1) / kStreamMinTiles));
-            const int rows = (int)min((int64_t)stream_rows, most_rows);
-            launch(std::integral_constant<StreamMode, StreamMode::stretches>{}, dim3(blocks));
-            hipLaunchKernelGGL((k_pages_stream_merge<kDim, kBf16>), dim3(blocks, (rows + 3) / 4), dim3(256), 0, s, a, 16 * kSets);
-        };
-        if (stream_rows == 16) go(std::integral_constant<int, 1>{});
-        else go(std::integral_constant<int, 2>{});
+        if (stream_rows == 16) launch_stream<kStore, kDim, kBf16, 1, false>(a, stream_rows, reach, s);
+        else launch_stream<kStore, kDim, kBf16, 2, false>(a, stream_rows, reach, s);
     }
     if (most_rows > 32) {
         auto go = [&](auto waves, int stretches) {

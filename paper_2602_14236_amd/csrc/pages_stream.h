@@ -273,7 +273,8 @@ constexpr int stream_waves(StreamMode mode) { return mode == StreamMode::pairs ?
 constexpr int stream_occupancy(int store, int sets, StreamMode mode) { return store != SALI_STORE_16 && sets == 1 && mode == StreamMode::stretches ? 3 : 2; }
 
 // The leading arguments come in registers: what the first loads depend on.
-template <int kStore, int kDim, bool kBf16, int kSets, StreamMode kMode>
+// kTree: drafted tokens, whose masks say what they see of the draft; the masks are read where a tile has keys of it
+template <int kStore, int kDim, bool kBf16, int kSets, StreamMode kMode, bool kTree = false>
 __global__ __launch_bounds__(64 * stream_waves(kMode)) __attribute__((amdgpu_waves_per_eu(stream_occupancy(kStore, kSets, kMode), stream_occupancy(kStore, kSets, kMode))))
 void k_pages_stream(
     const int32_t* __restrict__ starts, const int32_t* __restrict__ lengths, const int32_t* __restrict__ tables, int n_seqs, int width, int n_tokens, int max_q,
@@ -290,7 +291,20 @@ void k_pages_stream(
         fits = page_seq_holds(first, next, len, n_tokens, max_q, room);
         return {first, fits ? next - first : 0, len};
     };
-    auto view_of_seq = [&](const PageSeq& q) { return view_of<kTileTokens>(q.len - q.n, q.len - 1, window, sinks); };
+    auto view_of_seq = [&](const PageSeq& q) -> View {
+        if constexpr (kTree) return view_of_draft<kTileTokens>(q);
+        else return view_of<kTileTokens>(q.len - q.n, q.len - 1, window, sinks);
+    };
+    // what row c's token sees from key `from` of the sequence on
+    auto sight_of_row = [&](int c, int pos, const PageSeq& q, int from) {
+        if constexpr (kTree) {
+            const int r = 16 * c + col;
+            const uint64_t mask = r < q.n * group ? a.seen[q.first + r / group] : 0ull;
+            return draft_sight(mask, q.n, from - (q.len - q.n));
+        } else {
+            return sight_of(pos, from, window, sinks);
+        }
+    };
     // the pages from `page0` on, one a lane
     int page0 = 0, page_of_lane = -1;
 
@@ -481,7 +495,7 @@ void k_pages_stream(
                 asm volatile("" : "+v"(first_key));
 #pragma unroll
                 for (int c = 0; c < kSets; ++c) {
-                    const Sight sight = sight_of(pos[c], first_key, window, sinks);
+                    const auto sight = sight_of_row(c, pos[c], seq, first_key);
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -550,7 +564,7 @@ void k_pages_stream(
                         u32x4 seen[kSets];
 #pragma unroll
                         for (int c = 0; c < kSets; ++c) {
-                            const Sight sight = sight_of(pos[c], j0 + 16 * (hh >> 1) + 8 * (hh & 1), window, sinks);
+                            const auto sight = sight_of_row(c, pos[c], seq, j0 + 16 * (hh >> 1) + 8 * (hh & 1));
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
                                 seen[c][e] = (2 * e < live && sight.has(2 * e) ? (uint32_t)Num<kBf16>::kOne : 0u) |

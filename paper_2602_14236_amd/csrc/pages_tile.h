@@ -55,8 +55,15 @@ __host__ inline size_t tile_scratch_bytes(int64_t slots, int n_kv, int waves) {
     return offsetof(TileScratch, pieces) + (size_t)tile_pieces(slots, n_kv, waves) * sizeof(TilePiece) + (size_t)slots * sizeof(TileUnit);
 }
 
+// the keys that a row tile's rows see
+template <int kWaves, bool kTree>
+__device__ __forceinline__ View view_of_row_tile(const PageSeq& q, int row_tile, const PagesAttend& a) {
+    if constexpr (kTree) return view_of_draft<tile_keys(kWaves)>(q);
+    else return view_of_rows<kWaves>(q, row_tile, a.group, a.window, a.sinks);
+}
+
 // the row tile in a slot, or none (no tiles)
-template <int kWaves>
+template <int kWaves, bool kTree = false>
 __device__ __forceinline__ TileUnit tile_unit(const PagesAttend& a, int rows_min, int64_t slot) {
     constexpr int kTileRows = tile_rows(kWaves);
     auto slot0 = [&](int s) -> int64_t { return (int64_t)((uint32_t)min(max(0, a.seqs.start[s]), a.seqs.n_tokens) * (uint32_t)a.group / (uint32_t)kTileRows) + s; };
@@ -74,13 +81,13 @@ __device__ __forceinline__ TileUnit tile_unit(const PagesAttend& a, int rows_min
     const int64_t tile = slot - slot0(lo), rows = (int64_t)q.n * a.group;
     TileUnit u = {{0, 0, 0}, lo, (int)tile, q.first, q.n, q.len, {0, 0, 0}};
     if (tile < 0 || rows < rows_min || tile * kTileRows >= rows) return u;
-    u.span.tiles = view_of_rows<kWaves>(q, u.row_tile, a.group, a.window, a.sinks).tiles;
+    u.span.tiles = view_of_row_tile<kWaves, kTree>(q, u.row_tile, a).tiles;
     u.span.weight = tile_weight((int)min((int64_t)kTileRows, rows - tile * kTileRows));
     return u;
 }
 
 // The plan in shares, one block (5 to 8 us: a few trips to memory one after the other)
-template <int kWaves>
+template <int kWaves, bool kTree = false>
 __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend a, int rows_min) {
     __shared__ int64_t s_sum[kPlanThreads / 64];
     __shared__ int s_longest[kPlanThreads / 64], s_falls[kPlanThreads / 64];
@@ -96,7 +103,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
     int longest = 1;
     TileUnit first = {{0, 0, 0}, 0, 0, 0, 0, 0, {0, 0, 0}};
     for (int64_t i = threadIdx.x; i < slots; i += kPlanThreads) {
-        const TileUnit u = tile_unit<kWaves>(a, rows_min, i);
+        const TileUnit u = tile_unit<kWaves, kTree>(a, rows_min, i);
         if (i == threadIdx.x) first = u;
         sum += u.span.tiles;
         longest = max(longest, u.span.tiles);
@@ -126,7 +133,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
     const int most_tiles = min(share, longest);             // of the longest piece
     auto bucket_of = [&](int tiles) { return kUnitBuckets - 1 - min(kUnitBuckets - 1, (int)((int64_t)tiles * (kUnitBuckets - 1) / most_tiles)); };
     for (int64_t i = threadIdx.x; i < slots; i += kPlanThreads) {
-        const TileUnit u = i == threadIdx.x ? first : tile_unit<kWaves>(a, rows_min, i);
+        const TileUnit u = i == threadIdx.x ? first : tile_unit<kWaves, kTree>(a, rows_min, i);
         const int tiles = u.span.tiles;
         if (tiles == 0) continue;
         const int parts = parts_of(tiles, share);
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
     }
     __syncthreads();
     for (int64_t i = threadIdx.x; i < slots; i += kPlanThreads) {
-        const TileUnit u = i == threadIdx.x ? first : tile_unit<kWaves>(a, rows_min, i);
+        const TileUnit u = i == threadIdx.x ? first : tile_unit<kWaves, kTree>(a, rows_min, i);
         const int tiles = u.span.tiles;
         if (tiles == 0) continue;
         const int parts = parts_of(tiles, share);
@@ -363,7 +370,7 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // (4 bits: two waves a SIMD, as the unpacking takes more registers)
-template <int kStore, int kDim, bool kBf16, int kTileWaves>
+template <int kStore, int kDim, bool kBf16, int kTileWaves, bool kTree = false>
 __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(kStore == SALI_STORE_INT4 ? 2 : 3, 3))) void k_pages_tile(PagesAttend args) {
     constexpr int kSteps = kDim / 16, kDt = kDim / 32, kPitch = kDim + 4;
     constexpr int kBlock = 32 * kDim;                       // bytes of a block's K or V in LDS
@@ -403,7 +410,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         const char* const heads = a.geom.pool + (uint64_t)head * a.geom.head_bytes;
         const uint32_t block_bytes = a.geom.head_bytes >> a.geom.blocks_log2;
         const int32_t* const table = a.seqs.table + (int64_t)uniform(unit.seq) * a.seqs.width;
-        const View view = view_of_rows<kTileWaves>(seq, unit.row_tile, group, a.window, a.sinks);
+        const View view = view_of_row_tile<kTileWaves, kTree>(seq, unit.row_tile, a);
         View to_look_at = view;             // keys that not all rows see, or all keys
         if (look) to_look_at.first = -1;
 
@@ -497,8 +504,15 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
         const int pos = r < rows ? seq.len - seq.n + token : -1;
         const bool some = row0 < rows;                          // uniform over the wave
         View mine = view;
-        mine.first = seq.len - seq.n + (int)((uint32_t)row0 / (uint32_t)group);
-        mine.last = seq.len - seq.n + (int)((uint32_t)(least(rows, row0 + 32) - 1) / (uint32_t)group);
+        if constexpr (!kTree) {
+            mine.first = seq.len - seq.n + (int)((uint32_t)row0 / (uint32_t)group);
+            mine.last = seq.len - seq.n + (int)((uint32_t)(least(rows, row0 + 32) - 1) / (uint32_t)group);
+        }
+        // what the lane's row sees from key `from` of the sequence on
+        auto sight_of_row = [&](int from) {
+            if constexpr (kTree) return draft_sight(pos >= 0 ? a.seen[seq.first + token] : 0ull, seq.n, from - (seq.len - seq.n));
+            else return sight_of(pos, from, a.window, a.sinks);
+        };
         u32x4 q[kSteps];
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
@@ -541,7 +555,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
                 // relative to the lane's first key, in place (sixteen positions of keys would be sixteen registers through the loop)
                 int first_key = j0 + 8 * hh;
                 asm volatile("" : "+v"(first_key));
-                const Sight sight = sight_of(pos, first_key, a.window, a.sinks);
+                const auto sight = sight_of_row(first_key);
 #pragma unroll
                 for (int x = 0; x < 16; ++x)
                     if ((x < 8 ? live0 : live1) <= 0 || !sight.has(16 * (x / 8) + x % 8)) st[x] = -INFINITY;
@@ -587,7 +601,7 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 #pragma unroll 1
                 for (int w = 0; w < kTileWaves; ++w) {
                     if (s_odd[buf][w] == 0) continue;
-                    const Sight sight = sight_of(pos, tile0 + 8 * w, a.window, a.sinks);
+                    const auto sight = sight_of_row(tile0 + 8 * w);
                     uint32_t seen = 0;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) seen |= (sight.has(e) ? 1u : 0u) << e;
