@@ -71,6 +71,8 @@ struct PagesWeigh {
     float scale2;                           // as PagesAttend has them
     uint32_t q_keep, q_flip;
     int32_t window, sinks, heads, group, add;
+    float* partial;                         // room for sums of chunks of rows
+    size_t partial_bytes;
 };
 
 struct PagesSelect {

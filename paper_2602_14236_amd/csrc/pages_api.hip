@@ -291,6 +291,8 @@ int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch,
     a.heads = p->cfg.n_heads;
     a.group = p->cfg.n_heads / p->cfg.n_kv_heads;
     a.add = add != 0;
+    a.partial = reinterpret_cast<float*>(p->scratch + p->layout.partial);
+    a.partial_bytes = p->layout.records - p->layout.partial;
     const hipError_t e = launch_pages_weigh(p->cfg.dtype, p->cfg.store, p->cfg.head_dim, a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SALI_OK : SALI_ERR_HIP;
 }
