@@ -188,6 +188,16 @@ __device__ __forceinline__ void weigh_keys(const char* block, int place, int hh,
     }
 }
 
+// kSteps products with 48 vector instructions between them
+template <int kSteps>
+__device__ __forceinline__ void side_by_side() {
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 48 / kSteps, 0);
+    }
+}
+
 // `blocks` thread blocks of 256 keys a sequence and head, times `chunks` of `chunk_rows` rows.  With several chunks the sums go to `partial`, [chunk][sequence, head, block][256].
 template <int kStore, int kDim, bool kBf16>
 __global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_eu(2))) void k_pages_weigh_tile(PagesWeigh a, int blocks, int chunks, int chunk_rows) {
@@ -232,6 +242,11 @@ __global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_e
             float* unused;
             weigh_keys<kStore, kDim, kBf16>(w.block(a, head, block, page, unused), col & 15, hh, k[set]);
         }
+        // waited for here: in the loop a wait for them would be one for the next queries too
+#pragma unroll
+        for (int set = 0; set < 2; ++set)
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) asm volatile("" : "+v"(k[set][t]));
     }
     f32x16 sum[2];
 #pragma unroll
@@ -239,35 +254,45 @@ __global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll
         for (int x = 0; x < 16; ++x) sum[set][x] = 0.0f;
 
-    // rows in (token, head of the group), which move on by 32 rows a step
+    // Rows, which move on by 32 a step: by tokens and heads of the group.  A lane has the addresses of the pieces that it brings and of its own row's log-sum.
     const int by_token = kWeighRows / group, by_head = kWeighRows - by_token * group;
+    const int64_t q_step = by_token * a.q.token_bytes + by_head * a.q.head_bytes, q_wrap = a.q.token_bytes - group * a.q.head_bytes;
+    const int lse_step = by_token * a.heads + by_head, lse_wrap = a.heads - group;
     struct Row {
         int token, of_group;
     };
     auto row_at = [&](int r) -> Row { return {(int)((uint32_t)r / (uint32_t)group), (int)((uint32_t)r % (uint32_t)group)}; };
+    // does it go on to another token than by_token further?
     auto move_on = [&](Row& r) {
         r.token += by_token;
         r.of_group += by_head;
-        if (r.of_group >= group) {
-            r.of_group -= group;
-            ++r.token;
-        }
+        const bool wraps = r.of_group >= group;
+        r.of_group -= wraps ? group : 0;
+        r.token += wraps ? 1 : 0;
+        return wraps;
     };
-    Row bring[kOwn], mine = row_at(lo + col);
+    Row bring[kOwn], mine = row_at(lo + col), first_row = row_at(lo), last_row = row_at(lo + kWeighRows - 1);
+    const char* from[kOwn];
+    const float* lse_from = a.lse + (int64_t)(seq.first + mine.token) * a.heads + head * group + mine.of_group;
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) bring[i] = row_at(lo + ((int)threadIdx.x + 64 * kWeighWaves * i) / kPieces);
+    for (int i = 0; i < kOwn; ++i) {
+        bring[i] = row_at(lo + ((int)threadIdx.x + 64 * kWeighWaves * i) / kPieces);
+        from[i] = a.q.d + (int64_t)(seq.first + bring[i].token) * a.q.token_bytes + (int64_t)(head * group + bring[i].of_group) * a.q.head_bytes + 16 * ((int)threadIdx.x % kPieces);
+    }
     u32x4 x[kOwn];
     float lse = -INFINITY;
+    Row asked = mine;                       // the row whose log-sum is on its way
+    // (Behind the sequence's last row another one instead, which nobody looks at: without branches the step is one stretch of code.)
+    const char* const some_row = a.q.d + (int64_t)seq.first * a.q.token_bytes + (int64_t)(head * group) * a.q.head_bytes;
+    const float* const some_lse = a.lse + (int64_t)seq.first * a.heads + head * group;
     auto ask = [&]() {
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-            const int c = (int)threadIdx.x % kPieces;
-            x[i] = (u32x4){0u, 0u, 0u, 0u};
-            if (bring[i].token < seq.n)
-                x[i] = load16(a.q.d + (int64_t)(seq.first + bring[i].token) * a.q.token_bytes + (int64_t)(head * group + bring[i].of_group) * a.q.head_bytes + 16 * c);
-            move_on(bring[i]);
+            x[i] = load16(bring[i].token < seq.n ? from[i] : some_row);
+            from[i] += q_step + (move_on(bring[i]) ? q_wrap : 0);
         }
-        lse = mine.token < seq.n ? a.lse[(int64_t)(seq.first + mine.token) * a.heads + head * group + mine.of_group] : -INFINITY;
+        lse = *(asked.token < seq.n ? lse_from : some_lse);
+        lse_from += lse_step + (move_on(asked) ? lse_wrap : 0);
     };
     auto put = [&](int buf) {
 #pragma unroll
@@ -279,49 +304,92 @@ __global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_e
             *reinterpret_cast<u32x4*>(s_q[buf] + c * kPitch + r * 16) = v;
         }
     };
-    if (lo < hi) ask();
-    for (int r0 = lo, buf = 0; r0 < hi; r0 += kWeighRows, buf ^= 1) {
+    // A step's beginning: its rows to LDS, the next ones' on their way.  What the step's lanes have:
+    int r0 = lo, buf = 1, pos = 0, first_pos = 0, last_pos = 0;             // positions of its first and last token (the last may lie behind the sequence's last)
+    bool some = false;
+    float lse2 = 0.0f;
+    auto begin = [&]() {
+        buf ^= 1;
         put(buf);
-        const int pos = w.first + mine.token;
-        const bool some = mine.token < seq.n && lse != -INFINITY;
-        const float lse2 = lse * kLog2e;
+        pos = w.first + mine.token;
+        some = mine.token < seq.n && lse != -INFINITY;
+        lse2 = lse * kLog2e;
         move_on(mine);
-        if (r0 + kWeighRows < hi) ask();
+        ask();
+        first_pos = w.first + first_row.token;
+        last_pos = w.first + last_row.token;
+        move_on(first_row);
+        move_on(last_row);
         __syncthreads();                    // the rows are there, and all waves are through with the other buffer
-        // the step's first and last token (the last may lie behind the sequence's last)
-        const int first_pos = w.first + (int)((uint32_t)r0 / (uint32_t)group), last_pos = w.first + (int)((uint32_t)(r0 + kWeighRows - 1) / (uint32_t)group);
-        if (last_pos < j0 || (a.window > 0 && j0 >= a.sinks && first_pos - a.window >= j0 + 63)) continue;
-        f32x16 st[2];
+    };
+    // do all of the step's rows see all of the wave's keys?
+    auto plain = [&]() {
+        return first_pos >= j0 + 63 && (a.window == 0 || last_pos - a.window < j0 || j0 + 64 <= a.sinks) && __builtin_amdgcn_ballot_w64(!some) == 0;
+    };
+    auto add = [&](f32x16& to, const f32x16& st, float lse2) {
 #pragma unroll
-        for (int set = 0; set < 2; ++set)
+        for (int e = 0; e < 16; ++e) to[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], a.scale2, -lse2));
 #pragma unroll
-            for (int e = 0; e < 16; ++e) st[set][e] = 0.0f;
-        const uint8_t* const at = s_q[buf] + hh * kPitch + col * 16;
+        for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(to[e]));        // here, and not moved behind the barrier
+    };
+    auto queries = [&](int t) { return load16(s_q[buf] + (2 * t + hh) * kPitch + col * 16); };
+    if (lo < hi) {
+        ask();
+        begin();
+    }
+    while (r0 < hi) {
+        if (plain()) {
+            // Products and weights of different sets side by side: the second set's weights wait for the next step's products of the first
+            f32x16 held;
+            float held_lse2 = 0.0f;
 #pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-            const u32x4 q = load16(at + 2 * t * kPitch);
+            for (int e = 0; e < 16; ++e) held[e] = -INFINITY;
+            do {
+                u32x4 q[kSteps];
 #pragma unroll
-            for (int set = 0; set < 2; ++set) st[set] = Num<kBf16>::mma32(k[set][t], q, st[set]);
+                for (int t = 0; t < kSteps; ++t) q[t] = queries(t);
+                f32x16 st;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) st[e] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < kSteps; ++t) st = Num<kBf16>::mma32(k[0][t], q[t], st);
+                add(sum[1], held, held_lse2);
+                side_by_side<kSteps>();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) held[e] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < kSteps; ++t) held = Num<kBf16>::mma32(k[1][t], q[t], held);
+                add(sum[0], st, lse2);
+                side_by_side<kSteps>();
+                held_lse2 = lse2;
+                r0 += kWeighRows;
+                if (r0 >= hi) break;
+                begin();
+            } while (plain());
+            add(sum[1], held, held_lse2);
+            if (r0 >= hi) break;
         }
-        // lane (row col, hh): register e of a set has token 8 hh + e % 8 of block e / 8
-        const bool all = first_pos >= j0 + 63 && (a.window == 0 || last_pos - a.window < j0 || j0 + 64 <= a.sinks) && __builtin_amdgcn_ballot_w64(!some) == 0;
-        if (all) {
-#pragma unroll
-            for (int set = 0; set < 2; ++set)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sum[set][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(st[set][e], a.scale2, -lse2));
-        } else {
+        if (last_pos >= j0 && !(a.window > 0 && j0 >= a.sinks && first_pos - a.window >= j0 + 63)) {
             int first_key = j0 + 8 * hh;
             asm volatile("" : "+v"(first_key));
             const Sight sight = sight_of(pos, first_key, a.window, a.sinks);
 #pragma unroll
-            for (int set = 0; set < 2; ++set)
+            for (int set = 0; set < 2; ++set) {
+                f32x16 st;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) st[e] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < kSteps; ++t) st = Num<kBf16>::mma32(k[set][t], queries(t), st);
+                // lane (row col, hh): register e has token 8 hh + e % 8 of the set's block e / 8
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(st[set][e], a.scale2, -lse2));
+                    const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], a.scale2, -lse2));
                     sum[set][e] += some && sight.has(32 * set + 16 * (e / 8) + e % 8) ? v : 0.0f;
                 }
+            }
         }
+        r0 += kWeighRows;
+        if (r0 < hi) begin();
     }
     // ---- over the 32 rows' lanes
 #pragma unroll
