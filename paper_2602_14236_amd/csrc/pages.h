@@ -68,8 +68,7 @@ struct PagesWeigh {
     RowsIn q;
     const float* lse;
     float* weights;                         // [page][K/V head][token]
-    float scale2;                           // as PagesAttend has them
-    uint32_t q_keep, q_flip;
+    float scale2;                           // softmax_scale * log2(e)
     int32_t window, sinks, heads, group, add;
     float* partial;                         // room for sums of chunks of rows
     size_t partial_bytes;

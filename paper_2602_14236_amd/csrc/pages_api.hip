@@ -283,9 +283,7 @@ int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch,
     a.q = rows_of<RowsIn>(*q);
     a.lse = d_lse;
     a.weights = d_weights;
-    a.scale2 = scale2_of(softmax_scale);
-    a.q_keep = keep_of(softmax_scale);
-    a.q_flip = flip_of(softmax_scale);
+    a.scale2 = softmax_scale * 1.44269504088896340736f;
     a.window = window;
     a.sinks = window > 0 ? sinks : 0;
     a.heads = p->cfg.n_heads;

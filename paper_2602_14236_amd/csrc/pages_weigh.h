@@ -107,11 +107,7 @@ __global__ __launch_bounds__(64 * kWeighStreamWaves) void k_pages_weigh_stream(P
         const float lse = a.lse[(int64_t)(seq.first + token) * a.heads + head * a.group + g];
         const char* const at = a.q.d + (int64_t)(seq.first + token) * a.q.token_bytes + (int64_t)(head * a.group + g) * a.q.head_bytes;
 #pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-            const u32x4 v = load16(at + 2 * stream_k_value<kStore, kDim>(t, hh));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) q[c][t][e] = (v[e] & a.q_keep) ^ a.q_flip;
-        }
+        for (int t = 0; t < kSteps; ++t) q[c][t] = load16(at + 2 * stream_k_value<kStore, kDim>(t, hh));
         lse2[c] = lse * kLog2e;
         if (lse != -INFINITY) pos[c] = w.first + token;
     }
@@ -158,10 +154,10 @@ __global__ __launch_bounds__(64 * kWeighStreamWaves) void k_pages_weigh_stream(P
 }
 
 // ---- more rows
-constexpr int kWeighWaves = 4, kWeighKeys = 64 * kWeighWaves;
-constexpr int kWeighRows = 32;              // of a step
+constexpr int kWeighWaves = 4, kWeighKeys = 32 * kWeighWaves;
+constexpr int kWeighRows = 64;              // of a step: two products'
 
-// a wave's 64 keys as the A operand of 32x32x16 products: two sets of two blocks; lane (place col % 16 of block col / 16, hh) has values 16 step + 8 hh .. + 7
+// a wave's 32 keys, two blocks, as the A operand of 32x32x16 products: lane (place col % 16 of block col / 16, hh) has values 16 step + 8 hh .. + 7
 template <int kStore, int kDim, bool kBf16>
 __device__ __forceinline__ void weigh_keys(const char* block, int place, int hh, u32x4* k) {
     constexpr BlockLayout kAt = block_layout(kStore, kDim);
@@ -198,15 +194,24 @@ __device__ __forceinline__ void side_by_side() {
     }
 }
 
-// `blocks` thread blocks of 256 keys a sequence and head, times `chunks` of `chunk_rows` rows.  With several chunks the sums go to `partial`, [chunk][sequence, head, block][256].
-template <int kStore, int kDim, bool kBf16>
-__global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_eu(2))) void k_pages_weigh_tile(PagesWeigh a, int blocks, int chunks, int chunk_rows) {
+// Rows of the kernel: a token has as many as the group has heads, filled up to a divisor of 64 or a multiple of it, so that all rows of a step of 64 move on by the same.
+__host__ __device__ inline int weigh_padded(int group) {
+    if (group >= kWeighRows) return (group + kWeighRows - 1) / kWeighRows * kWeighRows;
+    int n = 1;
+    while (n < group) n *= 2;
+    return n;
+}
+
+// `blocks` thread blocks of 128 keys a sequence and head, times `chunks` of `chunk_rows` rows.  With several chunks the sums go to `partial`, [chunk][sequence, head, block][128].
+// kPad: some rows are none.
+template <int kStore, int kDim, bool kBf16, bool kPad>
+__global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_eu(3))) void k_pages_weigh_tile(PagesWeigh a, int blocks, int chunks, int64_t chunk_rows) {
     constexpr int kSteps = kDim / 16, kPieces = kDim / 8, kPitch = 16 * kWeighRows + 16;
     constexpr int kOwn = kWeighRows * kPieces / (64 * kWeighWaves);         // pieces of 16 bytes that a thread brings
     __shared__ __align__(16) uint8_t s_q[2][kPieces * kPitch];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 31, hh = lane >> 5;
     const uint32_t units = gridDim.x / (uint32_t)chunks, unit = blockIdx.x % units;
-    const int chunk = (int)(blockIdx.x / units);
+    const int chunk = chunks - 1 - (int)(blockIdx.x / units);               // rows that see most keys first
     const int head = (int)(unit % (uint32_t)a.geom.n_kv), nth = (int)(unit / (uint32_t)a.geom.n_kv), s = nth / blocks, nth_of_seq = nth - s * blocks;
     const bool notes = chunk == 0 && nth_of_seq == 0 && head == 0;
     const StartFalls falls(a.seqs.start, a.seqs.n_seqs, lane, 64);
@@ -218,203 +223,219 @@ __global__ __launch_bounds__(64 * kWeighWaves) __attribute__((amdgpu_waves_per_e
     const int key0 = nth_of_seq * kWeighKeys;
     if (seq.n == 0 || key0 >= seq.len) return;
     const WeighSeq w = {a.seqs.table + (int64_t)s * a.seqs.width, seq.len, seq.len - seq.n};
-    const int rows = seq.n * a.group, group = a.group;
+    const int group = a.group, padded = kPad ? weigh_padded(group) : group;
+    const int64_t rows = (int64_t)seq.n * padded;
     // rows that see some of the block's keys: from the one at position key0 on, and under a window up to the last one that has the block's last key in its window
-    int lo = max(0, key0 - w.first) * group, hi = rows;
-    if (a.window > 0 && key0 >= a.sinks) hi = (int)max((int64_t)0, min((int64_t)rows, ((int64_t)key0 + kWeighKeys - 1 + a.window - w.first) * group));
-    lo = max(lo & ~(kWeighRows - 1), chunk * chunk_rows);
-    hi = min(hi, (int)min((int64_t)0x7FFFFFFF, (int64_t)(chunk + 1) * chunk_rows));
-    const int j0 = key0 + 64 * wave;
-    u32x4 k[2][kSteps];
-    float* to[4];                           // of the wave's blocks of 16 keys
+    int64_t lo = (int64_t)max(0, key0 - w.first) * padded, hi = rows;
+    if (a.window > 0 && key0 >= a.sinks) hi = max((int64_t)0, min(rows, ((int64_t)key0 + kWeighKeys - 1 + a.window - w.first) * padded));
+    lo = max(lo & ~(int64_t)(kWeighRows - 1), (int64_t)chunk * chunk_rows);
+    hi = min(hi, (int64_t)(chunk + 1) * chunk_rows);
+    const int steps = (int)max((int64_t)0, (hi - lo + kWeighRows - 1) / kWeighRows);
+    const int j0 = key0 + 32 * wave;
+    u32x4 k[kSteps];
+    float* to[2];                           // of the wave's blocks of 16 keys
+    {
+        const char* at[2];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        const int block = j0 / kBlockTokens + b;
-        const int page = block * kBlockTokens < seq.len ? w.table[block >> a.geom.blocks_log2] : -1;
-        w.block(a, head, block, page, to[b]);
-        if (to[b] == nullptr && block * kBlockTokens < seq.len && chunk == 0 && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
-    }
-    if (lo < hi) {
-#pragma unroll
-        for (int set = 0; set < 2; ++set) {
-            const int block = j0 / kBlockTokens + 2 * set + (col >> 4);
+        for (int b = 0; b < 2; ++b) {
+            const int block = j0 / kBlockTokens + b;
             const int page = block * kBlockTokens < seq.len ? w.table[block >> a.geom.blocks_log2] : -1;
-            float* unused;
-            weigh_keys<kStore, kDim, kBf16>(w.block(a, head, block, page, unused), col & 15, hh, k[set]);
+            at[b] = w.block(a, head, block, page, to[b]);
+            if (to[b] == nullptr && block * kBlockTokens < seq.len && chunk == 0 && lane == 0) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
         }
+        weigh_keys<kStore, kDim, kBf16>(col < 16 ? at[0] : at[1], col & 15, hh, k);
         // waited for here: in the loop a wait for them would be one for the next queries too
 #pragma unroll
-        for (int set = 0; set < 2; ++set)
-#pragma unroll
-            for (int t = 0; t < kSteps; ++t) asm volatile("" : "+v"(k[set][t]));
+        for (int t = 0; t < kSteps; ++t) asm volatile("" : "+v"(k[t]));
     }
-    f32x16 sum[2];
+    f32x16 sum;
 #pragma unroll
-    for (int set = 0; set < 2; ++set)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) sum[set][x] = 0.0f;
+    for (int x = 0; x < 16; ++x) sum[x] = 0.0f;
 
-    // Rows, which move on by 32 a step: by tokens and heads of the group.  A lane has the addresses of the pieces that it brings and of its own row's log-sum.
-    const int by_token = kWeighRows / group, by_head = kWeighRows - by_token * group;
-    const int64_t q_step = by_token * a.q.token_bytes + by_head * a.q.head_bytes, q_wrap = a.q.token_bytes - group * a.q.head_bytes;
-    const int lse_step = by_token * a.heads + by_head, lse_wrap = a.heads - group;
-    struct Row {
-        int token, of_group;
+    // A step's rows: those of 64 / padded tokens, or 64 of a token's.  A thread has the addresses of the pieces that it brings and of its own rows' log-sums; all move on by the same.
+    const int by_token = padded >= kWeighRows ? 1 : kWeighRows / padded, phases = padded > kWeighRows ? padded / kWeighRows : 1;
+    const int64_t q_step = by_token * a.q.token_bytes, lse_step = (int64_t)by_token * a.heads;
+    int phase = (int)(lo % padded) / kWeighRows, token0 = (int)(lo / padded);       // 64 rows of the first token's from 64 phase on
+    auto of_step = [&](int r, int& of_group) {                              // of the step's row r: tokens behind its first one, head of the group without the phase
+        of_group = padded >= kWeighRows ? r : r & (padded - 1);
+        return padded >= kWeighRows ? 0 : r / padded;
     };
-    auto row_at = [&](int r) -> Row { return {(int)((uint32_t)r / (uint32_t)group), (int)((uint32_t)r % (uint32_t)group)}; };
-    // does it go on to another token than by_token further?
-    auto move_on = [&](Row& r) {
-        r.token += by_token;
-        r.of_group += by_head;
-        const bool wraps = r.of_group >= group;
-        r.of_group -= wraps ? group : 0;
-        r.token += wraps ? 1 : 0;
-        return wraps;
-    };
-    Row bring[kOwn], mine = row_at(lo + col), first_row = row_at(lo), last_row = row_at(lo + kWeighRows - 1);
     const char* from[kOwn];
-    const float* lse_from = a.lse + (int64_t)(seq.first + mine.token) * a.heads + head * group + mine.of_group;
+    const float* lse_from[2];
+    int behind[2], row_head[2];             // of the lane's rows
+    // (Instead of a row that is none another one, which nobody looks at.)
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-        bring[i] = row_at(lo + ((int)threadIdx.x + 64 * kWeighWaves * i) / kPieces);
-        from[i] = a.q.d + (int64_t)(seq.first + bring[i].token) * a.q.token_bytes + (int64_t)(head * group + bring[i].of_group) * a.q.head_bytes + 16 * ((int)threadIdx.x % kPieces);
+        int g;
+        const int t = of_step(((int)threadIdx.x + 64 * kWeighWaves * i) / kPieces, g);
+        from[i] = a.q.d + (int64_t)(seq.first + token0 + t) * a.q.token_bytes + (int64_t)(head * group + 64 * phase + (kPad ? min(g, group - 1 - 64 * phase) : g)) * a.q.head_bytes +
+                  16 * ((int)threadIdx.x % kPieces);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        behind[i] = of_step(32 * i + col, row_head[i]);
+        lse_from[i] = a.lse + (int64_t)(seq.first + token0 + behind[i]) * a.heads + head * group + 64 * phase + (kPad ? min(row_head[i], group - 1 - 64 * phase) : row_head[i]);
     }
     u32x4 x[kOwn];
-    float lse = -INFINITY;
-    Row asked = mine;                       // the row whose log-sum is on its way
-    // (Behind the sequence's last row another one instead, which nobody looks at: without branches the step is one stretch of code.)
-    const char* const some_row = a.q.d + (int64_t)seq.first * a.q.token_bytes + (int64_t)(head * group) * a.q.head_bytes;
-    const float* const some_lse = a.lse + (int64_t)seq.first * a.heads + head * group;
+    float lse[2];
+    int asked_token = token0, asked_phase = phase;
     auto ask = [&]() {
+        // tokens behind the last one: the last one's rows
+        const int most = seq.n - 1 - asked_token;
+        if (by_token - 1 <= most) {
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-            x[i] = load16(bring[i].token < seq.n ? from[i] : some_row);
-            from[i] += q_step + (move_on(bring[i]) ? q_wrap : 0);
+            for (int i = 0; i < kOwn; ++i) x[i] = load16(from[i]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) lse[i] = *lse_from[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                int g;
+                const int t = of_step(((int)threadIdx.x + 64 * kWeighWaves * i) / kPieces, g);
+                x[i] = load16(from[i] - (int64_t)max(0, t - most) * a.q.token_bytes);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) lse[i] = *(lse_from[i] - (int64_t)max(0, behind[i] - most) * a.heads);
         }
-        lse = *(asked.token < seq.n ? lse_from : some_lse);
-        lse_from += lse_step + (move_on(asked) ? lse_wrap : 0);
-    };
-    auto put = [&](int buf) {
+        // on to the next rows
+        int64_t q_by = q_step, lse_by = lse_step;
+        if (phases > 1) {
+            const bool next = ++asked_phase == phases;
+            // 64 heads on; from the last ones back to the token's first (where rows are filled up, those of the last phase stay within the group)
+            const int heads = next ? -(phases - 1) * kWeighRows : kWeighRows;
+            if (next) asked_phase = 0;
+            q_by = (next ? a.q.token_bytes : 0) + heads * a.q.head_bytes;
+            lse_by = (next ? a.heads : 0) + heads;
+            asked_token += next ? 1 : 0;
+            if constexpr (kPad) {
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-            const int p = (int)threadIdx.x + 64 * kWeighWaves * i, c = p % kPieces, r = p / kPieces;
-            u32x4 v;
+                for (int i = 0; i < kOwn; ++i) {
+                    const int g = ((int)threadIdx.x + 64 * kWeighWaves * i) / kPieces;
+                    from[i] = a.q.d + (int64_t)(seq.first + asked_token) * a.q.token_bytes + (int64_t)(head * group + min(64 * asked_phase + g, group - 1)) * a.q.head_bytes +
+                              16 * ((int)threadIdx.x % kPieces);
+                }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (x[i][e] & a.q_keep) ^ a.q_flip;
-            *reinterpret_cast<u32x4*>(s_q[buf] + c * kPitch + r * 16) = v;
+                for (int i = 0; i < 2; ++i) lse_from[i] = a.lse + (int64_t)(seq.first + asked_token) * a.heads + head * group + min(64 * asked_phase + 32 * i + col, group - 1);
+                return;
+            }
+        } else {
+            asked_token += by_token;
         }
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) from[i] += q_by;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) lse_from[i] += lse_by;
     };
-    // A step's beginning: its rows to LDS, the next ones' on their way.  What the step's lanes have:
-    int r0 = lo, buf = 1, pos = 0, first_pos = 0, last_pos = 0;             // positions of its first and last token (the last may lie behind the sequence's last)
-    bool some = false;
-    float lse2 = 0.0f;
+    // A step's beginning: its rows to LDS, the next ones' on their way.  What the step has: its first row's token and phase, and the log-sums of the lane's rows
+    int left = steps, buf = 1, token = 0, next_token = token0;
+    int step_phase = 0, next_phase = phase;
+    float lse2[2] = {0.0f, 0.0f};
     auto begin = [&]() {
         buf ^= 1;
-        put(buf);
-        pos = w.first + mine.token;
-        some = mine.token < seq.n && lse != -INFINITY;
-        lse2 = lse * kLog2e;
-        move_on(mine);
-        ask();
-        first_pos = w.first + first_row.token;
-        last_pos = w.first + last_row.token;
-        move_on(first_row);
-        move_on(last_row);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int p = (int)threadIdx.x + 64 * kWeighWaves * i;
+            *reinterpret_cast<u32x4*>(s_q[buf] + p % kPieces * kPitch + p / kPieces * 16) = x[i];
+        }
+        token = next_token;
+        step_phase = next_phase;
+        lse2[0] = lse[0] * kLog2e;
+        lse2[1] = lse[1] * kLog2e;
+        next_token = asked_token;
+        next_phase = asked_phase;
+        if (left > 1) ask();
         __syncthreads();                    // the rows are there, and all waves are through with the other buffer
     };
-    // do all of the step's rows see all of the wave's keys?
+    // Is the lane's row one, whatever its log-sum?
+    auto is_row = [&](int i) { return token + behind[i] < seq.n && (!kPad || 64 * step_phase + row_head[i] < group); };
+    // Do all of the step's rows see all of the wave's keys, and have they seen something?  (Rows that fill up groups do not count.)
     auto plain = [&]() {
-        return first_pos >= j0 + 63 && (a.window == 0 || last_pos - a.window < j0 || j0 + 64 <= a.sinks) && __builtin_amdgcn_ballot_w64(!some) == 0;
+        const int first_pos = w.first + token, last_pos = first_pos + by_token - 1;
+        if (first_pos < j0 + 31 || token + by_token > seq.n || !(a.window == 0 || last_pos - a.window < j0 || j0 + 32 <= a.sinks)) return false;
+        return __builtin_amdgcn_ballot_w64(fminf(lse2[0], lse2[1]) == -INFINITY) == 0;
     };
-    auto add = [&](f32x16& to, const f32x16& st, float lse2) {
+    auto add = [&](f32x16& to, const f32x16& st, float lse2, bool is) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) to[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], a.scale2, -lse2));
+        for (int e = 0; e < 16; ++e) {
+            const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], a.scale2, -lse2));
+            to[e] += !kPad || is ? v : 0.0f;
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(to[e]));        // here, and not moved behind the barrier
     };
-    auto queries = [&](int t) { return load16(s_q[buf] + (2 * t + hh) * kPitch + col * 16); };
-    if (lo < hi) {
+    auto queries = [&](int half, int t) { return load16(s_q[buf] + (2 * t + hh) * kPitch + half * 512 + col * 16); };
+    if (left > 0) {
         ask();
         begin();
     }
-    while (r0 < hi) {
+    while (left > 0) {
         if (plain()) {
-            // Products and weights of different sets side by side: the second set's weights wait for the next step's products of the first
+            // Products and weights of different rows side by side: the weights of a step's second half wait for the next products
             f32x16 held;
-            float held_lse2 = 0.0f;
+            float held_lse2 = INFINITY;             // weights of 0
+            bool held_is = true;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) held[e] = -INFINITY;
+            for (int e = 0; e < 16; ++e) held[e] = 0.0f;
             do {
-                u32x4 q[kSteps];
-#pragma unroll
-                for (int t = 0; t < kSteps; ++t) q[t] = queries(t);
                 f32x16 st;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) st[e] = 0.0f;
 #pragma unroll
-                for (int t = 0; t < kSteps; ++t) st = Num<kBf16>::mma32(k[0][t], q[t], st);
-                add(sum[1], held, held_lse2);
+                for (int t = 0; t < kSteps; ++t) st = Num<kBf16>::mma32(k[t], queries(0, t), st);
+                add(sum, held, held_lse2, held_is);
                 side_by_side<kSteps>();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) held[e] = 0.0f;
 #pragma unroll
-                for (int t = 0; t < kSteps; ++t) held = Num<kBf16>::mma32(k[1][t], q[t], held);
-                add(sum[0], st, lse2);
+                for (int t = 0; t < kSteps; ++t) held = Num<kBf16>::mma32(k[t], queries(1, t), held);
+                add(sum, st, lse2[0], is_row(0));
                 side_by_side<kSteps>();
-                held_lse2 = lse2;
-                r0 += kWeighRows;
-                if (r0 >= hi) break;
+                held_lse2 = lse2[1];
+                held_is = is_row(1);
+                if (--left == 0) break;
                 begin();
             } while (plain());
-            add(sum[1], held, held_lse2);
-            if (r0 >= hi) break;
+            add(sum, held, held_lse2, held_is);
+            if (left == 0) break;
         }
-        if (last_pos >= j0 && !(a.window > 0 && j0 >= a.sinks && first_pos - a.window >= j0 + 63)) {
+        if (w.first + token + by_token - 1 >= j0 && !(a.window > 0 && j0 >= a.sinks && w.first + token - a.window >= j0 + 31)) {
             int first_key = j0 + 8 * hh;
             asm volatile("" : "+v"(first_key));
-            const Sight sight = sight_of(pos, first_key, a.window, a.sinks);
 #pragma unroll
-            for (int set = 0; set < 2; ++set) {
+            for (int half = 0; half < 2; ++half) {
+                const Sight sight = sight_of(w.first + token + behind[half], first_key, a.window, a.sinks);
+                const bool some = is_row(half) && lse2[half] != -INFINITY;     // a row that saw nothing has no weights
                 f32x16 st;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) st[e] = 0.0f;
 #pragma unroll
-                for (int t = 0; t < kSteps; ++t) st = Num<kBf16>::mma32(k[set][t], queries(t), st);
-                // lane (row col, hh): register e has token 8 hh + e % 8 of the set's block e / 8
+                for (int t = 0; t < kSteps; ++t) st = Num<kBf16>::mma32(k[t], queries(half, t), st);
+                // lane (row col, hh): register e has token 8 hh + e % 8 of block e / 8
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], a.scale2, -lse2));
-                    sum[set][e] += some && sight.has(32 * set + 16 * (e / 8) + e % 8) ? v : 0.0f;
+                    const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e], a.scale2, -lse2[half]));
+                    sum[e] += some && sight.has(16 * (e / 8) + e % 8) ? v : 0.0f;
                 }
             }
         }
-        r0 += kWeighRows;
-        if (r0 < hi) begin();
+        if (--left > 0) begin();
     }
     // ---- over the 32 rows' lanes
 #pragma unroll
-    for (int set = 0; set < 2; ++set)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const uint32_t u = __builtin_bit_cast(uint32_t, sum_over_row(sum[set][e]));
-            const auto both = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-            sum[set][e] = __builtin_bit_cast(float, (uint32_t)both[0]) + __builtin_bit_cast(float, (uint32_t)both[1]);
-        }
-    if (col != 0) return;
-    if (chunks > 1) {
-        f32x4* const part = reinterpret_cast<f32x4*>(a.partial + ((int64_t)chunk * units + unit) * kWeighKeys + 64 * wave + 8 * hh);
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) part[4 * b + i] = *(reinterpret_cast<const f32x4*>(&sum[b / 2]) + 2 * (b % 2) + i);
-        return;
+    for (int e = 0; e < 16; ++e) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, sum_over_row(sum[e]));
+        const auto both = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        sum[e] = __builtin_bit_cast(float, (uint32_t)both[0]) + __builtin_bit_cast(float, (uint32_t)both[1]);
     }
+    if (col != 0) return;
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int e = 8 * (b % 2) + 4 * i;
-            w.put(a, to[b], j0 + 16 * b + 8 * hh + 4 * i, (f32x4){sum[b / 2][e], sum[b / 2][e + 1], sum[b / 2][e + 2], sum[b / 2][e + 3]});
+            const int e = 8 * b + 4 * i;
+            const f32x4 four = {sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+            if (chunks > 1) *reinterpret_cast<f32x4*>(a.partial + ((int64_t)chunk * units + unit) * kWeighKeys + 32 * wave + 16 * b + 8 * hh + 4 * i) = four;
+            else w.put(a, to[b], j0 + 16 * b + 8 * hh + 4 * i, four);
         }
 }
 

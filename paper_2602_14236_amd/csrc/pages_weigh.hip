@@ -19,12 +19,16 @@ void launch_weigh(const PagesWeigh& a, hipStream_t s) {
         return;
     }
     const int64_t blocks = ((int64_t)a.seqs.max_kv + kWeighKeys - 1) / kWeighKeys, units = blocks * lines;
-    // rows in chunks where keys alone are too few blocks: eight a compute unit, of 256 rows at least, as far as there is room for their sums
-    int64_t chunks = max((int64_t)1, min((8 * kComputeUnits + units - 1) / units, most_rows / 256));
+    // rows in chunks where keys alone are too few blocks: sixteen a compute unit, of 256 rows at least, as far as there is room for their sums
+    const bool pad = weigh_padded(a.group) != a.group;
+    const int64_t rows = (int64_t)a.seqs.max_q * weigh_padded(a.group);
+    int64_t chunks = max((int64_t)1, min((16 * kComputeUnits + units - 1) / units, rows / 256));
     chunks = max((int64_t)1, min(chunks, (int64_t)(a.partial_bytes / (units * kWeighKeys * sizeof(float)))));
-    const int chunk_rows = (int)((most_rows + chunks - 1) / chunks + kWeighRows - 1) / kWeighRows * kWeighRows;
-    chunks = (most_rows + chunk_rows - 1) / chunk_rows;
-    hipLaunchKernelGGL((k_pages_weigh_tile<kStore, kDim, kBf16>), dim3((unsigned)(units * chunks)), dim3(64 * kWeighWaves), 0, s, a, (int)blocks, (int)chunks, chunk_rows);
+    const int64_t chunk_rows = ((rows + chunks - 1) / chunks + kWeighRows - 1) / kWeighRows * kWeighRows;
+    chunks = (rows + chunk_rows - 1) / chunk_rows;
+    const dim3 grid((unsigned)(units * chunks));
+    if (pad) hipLaunchKernelGGL((k_pages_weigh_tile<kStore, kDim, kBf16, true>), grid, dim3(64 * kWeighWaves), 0, s, a, (int)blocks, (int)chunks, chunk_rows);
+    else hipLaunchKernelGGL((k_pages_weigh_tile<kStore, kDim, kBf16, false>), grid, dim3(64 * kWeighWaves), 0, s, a, (int)blocks, (int)chunks, chunk_rows);
     if (chunks > 1) hipLaunchKernelGGL(k_pages_weigh_merge, dim3((unsigned)units), dim3(kWeighKeys / 4), 0, s, a, (int)blocks, (int)chunks);
 }
 

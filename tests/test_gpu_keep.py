@@ -90,6 +90,18 @@ def test_weights_of_long_texts(store):
         weigh(c, batch, add=True)
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(3, 1), (10, 2), (40, 1), (64, 1), (70, 1), (128, 1), (384, 2)])
+def test_weights_of_wide_groups(heads, kv_heads):
+    """Groups that do not divide a step's rows, fill it, or take several; rows in chunks; windows."""
+    c = Cache(op.PagesSpec(kv_heads, heads, 64, 16, "fp16", "int8"), [333, 30, 90], 22)
+    lse = (c.rng.standard_normal((400, heads)) + 4).astype(np.float32)
+    lse[5, heads // 2], lse[60] = float("-inf"), float("-inf")
+    for batch in ([(1, 333), (1, 30), (1, 90)], [(200, 300), (9, 29), (90, 90)], [(33, 300), (0, 29), (1, 90)]):
+        for window in (0, 50):
+            t = sum(n for n, _ in batch)
+            weigh(c, batch, window=window, sinks=3, lse=torch.from_numpy(lse[:t]).to(DEV))
+
+
 def test_shares_of_attention():
     """With the attention's own log-sums the weights of a row sum to one: for each K/V head as many as rows."""
     c = Cache(op.PagesSpec(2, 8, 128, 16, "fp16", "16"), [500], 4)
