@@ -18,17 +18,33 @@ void launch_weigh(const PagesWeigh& a, hipStream_t s) {
         else hipLaunchKernelGGL((k_pages_weigh_stream<kStore, kDim, kBf16, 2>), grid, dim3(64 * kWeighStreamWaves), 0, s, a, blocks, each);
         return;
     }
+    const int padded = weigh_padded(a.group);
+    const int64_t steps = ((int64_t)a.seqs.max_q * padded + kWeighRows - 1) / kWeighRows;
+    auto by_kind = [&](auto launch) {
+        if (a.group > kWeighRows) launch(std::integral_constant<WeighRows, WeighRows::wide>{});
+        else if (padded != a.group) launch(std::integral_constant<WeighRows, WeighRows::filled>{});
+        else launch(std::integral_constant<WeighRows, WeighRows::even>{});
+    };
+    if (steps <= kWeighFewSteps) {
+        const int64_t tiles = ((int64_t)a.seqs.max_kv + kTileTokens - 1) / kTileTokens;
+        const int each = (int)max((int64_t)1, min((int64_t)16, tiles * lines / (kComputeUnits * 3 * kWeighFewWaves)));
+        const int blocks = (int)((tiles + each * kWeighFewWaves - 1) / (each * kWeighFewWaves));
+        by_kind([&](auto kind) {
+            hipLaunchKernelGGL((k_pages_weigh_few<kStore, kDim, kBf16, decltype(kind)::value>), dim3((unsigned)(blocks * lines)), dim3(64 * kWeighFewWaves),
+                               (unsigned)(steps * (WeighLayout<kDim>::kBytes + 4 * kWeighRows)), s, a, blocks, each, (int)steps);
+        });
+        return;
+    }
     const int64_t blocks = ((int64_t)a.seqs.max_kv + kWeighKeys - 1) / kWeighKeys, units = blocks * lines;
     // rows in chunks where keys alone are too few blocks: sixteen a compute unit, of 256 rows at least, as far as there is room for their sums
-    const bool pad = weigh_padded(a.group) != a.group;
-    const int64_t rows = (int64_t)a.seqs.max_q * weigh_padded(a.group);
-    int64_t chunks = max((int64_t)1, min((16 * kComputeUnits + units - 1) / units, rows / 256));
+    int64_t chunks = max((int64_t)1, min((16 * kComputeUnits + units - 1) / units, steps / 4));
     chunks = max((int64_t)1, min(chunks, (int64_t)(a.partial_bytes / (units * kWeighKeys * sizeof(float)))));
-    const int64_t chunk_rows = ((rows + chunks - 1) / chunks + kWeighRows - 1) / kWeighRows * kWeighRows;
-    chunks = (rows + chunk_rows - 1) / chunk_rows;
-    const dim3 grid((unsigned)(units * chunks));
-    if (pad) hipLaunchKernelGGL((k_pages_weigh_tile<kStore, kDim, kBf16, true>), grid, dim3(64 * kWeighWaves), 0, s, a, (int)blocks, (int)chunks, chunk_rows);
-    else hipLaunchKernelGGL((k_pages_weigh_tile<kStore, kDim, kBf16, false>), grid, dim3(64 * kWeighWaves), 0, s, a, (int)blocks, (int)chunks, chunk_rows);
+    const int chunk_steps = (int)((steps + chunks - 1) / chunks);
+    chunks = (steps + chunk_steps - 1) / chunk_steps;
+    by_kind([&](auto kind) {
+        hipLaunchKernelGGL((k_pages_weigh_tile<kStore, kDim, kBf16, decltype(kind)::value>), dim3((unsigned)(units * chunks)), dim3(64 * kWeighWaves), 0, s, a, (int)blocks,
+                           (int)chunks, chunk_steps);
+    });
     if (chunks > 1) hipLaunchKernelGGL(k_pages_weigh_merge, dim3((unsigned)units), dim3(kWeighKeys / 4), 0, s, a, (int)blocks, (int)chunks);
 }
 
