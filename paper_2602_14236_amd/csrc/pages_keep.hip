@@ -11,6 +11,7 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kDigits[3] = {21, 10, 0};     // lowest bit of each digit: 11, 11 and 10 bits
@@ -50,13 +51,16 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
     }
     const int shift = a.geom.blocks_log2 + 4, page_tokens = 1 << shift;
     const int32_t* const table = a.seqs.table + (int64_t)s * a.seqs.width;
+    auto page_at = [&](int pos) {
+        const int page = table[pos >> shift];
+        return (unsigned)page < (unsigned)a.geom.n_pages ? page : -1;
+    };
+    auto weights_at = [&](int page, int pos) { return a.weights + ((((int64_t)page * a.geom.n_kv + head) << shift) + (pos & (page_tokens - 1))); };
     auto key_in_pages = [&](int i) -> uint32_t {            // of the i-th of the sequence's new tokens
-        const int pos = base + i, page = table[pos >> shift];
-        if ((unsigned)page >= (unsigned)a.geom.n_pages) {
-            atomicOr(a.seqs.status, SALI_FAULT_PAGE);
-            return 0u;
-        }
-        return key_of(a.weights[((int64_t)page * a.geom.n_kv + head) * page_tokens + (pos & (page_tokens - 1))]);
+        const int page = page_at(base + i);
+        if (page >= 0) return key_of(*weights_at(page, base + i));
+        atomicOr(a.seqs.status, SALI_FAULT_PAGE);
+        return 0u;
     };
     // those that are chosen from: first .. first + m - 1
     const int first = a.sinks, m = n - a.sinks - a.recent;
@@ -64,7 +68,29 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
     auto key = [&](int j) { return j < kInLds ? s_keys[j] : key_in_pages(first + j); };
     uint32_t at = 0xFFFFFFFFu, ties = 0;                    // keys above `at` stay, and the first `ties` of those at it
     if (room > 0) {
-        for (int j = tid; j < min(m, kInLds); j += kSelectThreads) s_keys[j] = key_in_pages(first + j);
+        // four at a time, aligned as the pages are, and several of them on their way together
+        const int pos_end = base + first + min(m, kInLds), quad0 = (base + first) & ~3;
+        constexpr int kFlight = 8;
+        for (int64_t pos0 = quad0; pos0 < pos_end; pos0 += 4 * kFlight * kSelectThreads) {
+            int page[kFlight];
+            f32x4 w[kFlight];
+#pragma unroll
+            for (int i = 0; i < kFlight; ++i) {
+                const int64_t pos = pos0 + 4 * (kSelectThreads * i + tid);
+                page[i] = pos < pos_end ? page_at((int)pos) : -2;
+            }
+#pragma unroll
+            for (int i = 0; i < kFlight; ++i)
+                w[i] = page[i] >= 0 ? *reinterpret_cast<const f32x4*>(weights_at(page[i], (int)(pos0 + 4 * (kSelectThreads * i + tid)))) : (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < kFlight; ++i) {
+                if (page[i] == -1) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
+                const int64_t pos = pos0 + 4 * (kSelectThreads * i + tid);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (pos + e >= base + first && pos + e < pos_end) s_keys[(int)(pos + e) - base - first] = page[i] >= 0 ? key_of(w[i][e]) : 0u;
+            }
+        }
         uint32_t prefix = 0;
         for (int d = 0; d < 3; ++d) {
             const int low = kDigits[d], high = d == 0 ? 32 : kDigits[d - 1];
@@ -159,10 +185,10 @@ struct Strip {
     static constexpr int kElems = kStore == SALI_STORE_INT4 ? 16 : 32;
 };
 
-template <int kStore, int kDim, bool kInPlace>
+// kTokens: of a chunk
+template <int kStore, int kDim, bool kInPlace, int kTokens>
 __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int chunks) {
     typedef Strip<kStore, kDim> S;
-    constexpr int kTokens = kInPlace ? 256 : kKeepTokens;
     constexpr BlockLayout kAt = block_layout(kStore, kDim);
     constexpr int kKItems = kTokens * S::kPieces, kVItems = kTokens / 8 * S::kElems;
     constexpr int kKOwn = (kKItems + kKeepThreads - 1) / kKeepThreads, kVOwn = (kVItems + kKeepThreads - 1) / kKeepThreads;
@@ -347,8 +373,13 @@ hipError_t launch_pages_keep(int store, int dim, const PagesKeep& a, hipStream_t
     const int chunks = (int)keep_chunks(a.seqs, a.width, a.in_place != 0);
     const dim3 grid((unsigned)(a.seqs.n_seqs * (int64_t)chunks * a.geom.n_kv * keep_strips(dim, a.weights != nullptr)));
     auto go = [&](auto st, auto d) {
-        if (a.in_place) hipLaunchKernelGGL((k_pages_keep<decltype(st)::value, decltype(d)::value, true>), grid, dim3(kKeepThreads), 0, s, a, chunks);
-        else hipLaunchKernelGGL((k_pages_keep<decltype(st)::value, decltype(d)::value, false>), grid, dim3(kKeepThreads), 0, s, a, chunks);
+        auto launch = [&](auto in_place, auto tokens) {
+            hipLaunchKernelGGL((k_pages_keep<decltype(st)::value, decltype(d)::value, decltype(in_place)::value, decltype(tokens)::value>), grid, dim3(kKeepThreads), 0, s, a, chunks);
+        };
+        // in place a chunk waits for the one before: large ones, where there are several
+        if (!a.in_place) launch(std::false_type{}, std::integral_constant<int, kKeepTokens>{});
+        else if (std::min(a.width, a.seqs.max_q) + kBlockTokens - 1 <= kKeepTokens) launch(std::true_type{}, std::integral_constant<int, kKeepTokens>{});
+        else launch(std::true_type{}, std::integral_constant<int, 256>{});
     };
     auto with_dim = [&](auto st) {
         if (dim == 64) go(st, std::integral_constant<int, 64>{});
