@@ -600,34 +600,39 @@ class SaliPages:
                                           self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"),
                                           self._call(batch, stream)), "sali_pages_attend")
 
-    def _ints(self, t: torch.Tensor, dtype, dims, name: str):
-        """dims: sizes, None where any will do"""
-        if t.dtype is not dtype or t.dim() != len(dims) or any(d is not None and d != n for d, n in zip(dims, t.shape)) or not t.is_contiguous() or \
-                t.get_device() != self.index:
-            raise ValueError(f"{name}: contiguous {dtype} {list(dims)} on {self.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
+    def _wrong(self, name: str, t: torch.Tensor, dtype, dims):
+        return ValueError(f"{name}: contiguous {dtype} {dims} on {self.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
     def rotate(self, rotary: Rotary, position: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor] = None,
                k_out: Optional[torch.Tensor] = None, *, inverse: bool = False, stream: Optional[torch.cuda.Stream] = None):
         """Turn queries [tokens, n_heads, head_dim] and keys [tokens, n_kv_heads, head_dim], or one of the two, by their positions, int32 [axes, tokens] (or [tokens]
         for one axis); in place where no output is given.  inverse: back."""
-        if torch._C._cuda_getDevice() != self.index:
-            with torch.cuda.device(self.index):
+        index = self.index
+        if torch._C._cuda_getDevice() != index:
+            with torch.cuda.device(index):
                 return self.rotate(rotary, position, q, k, q_out, k_out, inverse=inverse, stream=stream)
-        if rotary.index != self.index:
+        if rotary.index != index:
             raise ValueError(f"the frequencies lie on {rotary.device}, the pages on {self.device}")
-        if position.dim() == 1:
-            position = position[None]
-        at = self._ints(position, torch.int32, (rotary.axes, None), "position")
-        n = position.shape[1]
-        rows = []
-        for x, out, heads, name in ((q, q_out, self.n_heads, "q"), (k, k_out, self.n_kv_heads, "k")):
-            if x is None and out is not None:
-                raise ValueError(f"{name}_out is given without {name}")
-            rows.append(None if x is None else (self._token_rows(x, n, heads, name), self._token_rows(x if out is None else out, n, heads, name + "_out")))
-        q, k = rows
-        _check(self.lib.sali_pages_rotate(self.handle, rotary.c, at, n, inverse, q and q[0], k and k[0], q and q[1], k and k[1], self._stream_of(stream)),
-               "sali_pages_rotate")
+        shape = position.shape
+        n = shape[-1]
+        if position.dtype is not torch.int32 or (shape != (rotary.axes, n) and (rotary.axes != 1 or len(shape) != 1)) or not position.is_contiguous() or \
+                position.get_device() != index:
+            raise self._wrong("position", position, torch.int32, [rotary.axes, "tokens"])
+        if (q is None and q_out is not None) or (k is None and k_out is not None):
+            raise ValueError("an output is given without its input")
+        q_rows = k_rows = q_to = k_to = None
+        if q is not None:
+            q_rows = q_to = self._token_rows(q, n, self.n_heads, "q")
+            if q_out is not None:
+                q_to = self._token_rows(q_out, n, self.n_heads, "q_out")
+        if k is not None:
+            k_rows = k_to = self._token_rows(k, n, self.n_kv_heads, "k")
+            if k_out is not None:
+                k_to = self._token_rows(k_out, n, self.n_kv_heads, "k_out")
+        code = self.lib.sali_pages_rotate(self.handle, rotary.c, position.data_ptr(), n, inverse, q_rows, k_rows, q_to, k_to,
+                                          torch._C._cuda_getCurrentRawStream(index) if stream is None else self._stream_of(stream))
+        if code != 0:
+            raise SaliError(code, "sali_pages_rotate")
 
     def attend_tree(self, layer: int, batch: PageBatch, seen: torch.Tensor, q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
                     lse: Optional[torch.Tensor] = None, *, prior: Optional[torch.Tensor] = None, prior_lse: Optional[torch.Tensor] = None,
@@ -638,8 +643,9 @@ class SaliPages:
             with torch.cuda.device(self.index):
                 return self.attend_tree(layer, batch, seen, q, softmax_scale, out, lse, prior=prior, prior_lse=prior_lse, stream=stream)
         n, d = self.n_heads, self.head_dim
-        _check(self.lib.sali_pages_attend_tree(self.handle, layer, batch.c, self._ints(seen, torch.int64, (batch.tokens,), "seen"),
-                                               self._rows(q, batch, n, "q"), softmax_scale, self._dense(prior, (batch.tokens, n, d), "prior"),
+        if seen.dtype is not torch.int64 or seen.shape != (batch.tokens,) or not seen.is_contiguous() or seen.get_device() != self.index:
+            raise self._wrong("seen", seen, torch.int64, [batch.tokens])
+        _check(self.lib.sali_pages_attend_tree(self.handle, layer, batch.c, seen.data_ptr(), self._rows(q, batch, n, "q"), softmax_scale, self._dense(prior, (batch.tokens, n, d), "prior"),
                                                self._dense(prior_lse, (batch.tokens, n), "prior_lse"), self._rows(out, batch, n, "out"),
                                                self._dense(lse, (batch.tokens, n), "lse"), self._call(batch, stream)), "sali_pages_attend_tree")
 
@@ -661,8 +667,9 @@ class SaliPages:
         if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.select(batch, weights, budget, keep, sinks=sinks, recent=recent, stream=stream)
-        _check(self.lib.sali_pages_select(self.handle, batch.c, self._dense(weights, self._weights_shape, "weights"), budget, sinks, recent,
-                                          self._ints(keep, torch.int32, (batch.c.n_seqs, self.n_kv_heads, budget), "keep"),
+        if keep.dtype is not torch.int32 or keep.shape != (batch.c.n_seqs, self.n_kv_heads, budget) or not keep.is_contiguous() or keep.get_device() != self.index:
+            raise self._wrong("keep", keep, torch.int32, [batch.c.n_seqs, self.n_kv_heads, budget])
+        _check(self.lib.sali_pages_select(self.handle, batch.c, self._dense(weights, self._weights_shape, "weights"), budget, sinks, recent, keep.data_ptr(),
                                           self._call(batch, stream)), "sali_pages_select")
 
     def keep(self, layer: int, batch: PageBatch, keep: torch.Tensor, *, to: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
@@ -672,10 +679,15 @@ class SaliPages:
         if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.keep(layer, batch, keep, to=to, weights=weights, stream=stream)
-        n = batch.c.n_seqs
-        at = self._ints(keep, torch.int32, (n, None, None), "keep")
-        _check(self.lib.sali_pages_keep(self.handle, layer, batch.c, at, keep.shape[1], keep.shape[2],
-                                        None if to is None else self._ints(to, torch.int32, (n, None), "to"), 0 if to is None else to.shape[1],
+        n, shape, to_at, to_width = batch.c.n_seqs, keep.shape, None, 0
+        if keep.dtype is not torch.int32 or len(shape) != 3 or shape[0] != n or shape[1] not in (1, self.n_kv_heads) or not keep.is_contiguous() or \
+                keep.get_device() != self.index:
+            raise self._wrong("keep", keep, torch.int32, [n, f"{self.n_kv_heads} or 1", "width"])
+        if to is not None:
+            if to.dtype is not torch.int32 or to.dim() != 2 or to.shape[0] != n or not to.is_contiguous() or to.get_device() != self.index:
+                raise self._wrong("to", to, torch.int32, [n, "width"])
+            to_at, to_width = to.data_ptr(), to.shape[1]
+        _check(self.lib.sali_pages_keep(self.handle, layer, batch.c, keep.data_ptr(), shape[1], shape[2], to_at, to_width,
                                         self._dense(weights, self._weights_shape, "weights"), self._call(batch, stream)), "sali_pages_keep")
 
     def get_status(self) -> int:
