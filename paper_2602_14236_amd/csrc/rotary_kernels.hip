@@ -19,6 +19,8 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRotaryThreads = 256;
+// Bytes of rows, half of what the last cache holds, from which on they go past the caches: longer ones would only push each other out.
+constexpr int64_t kPastCaches = 128 << 20;
 
 template <bool kBf16>
 struct Row16;
@@ -45,7 +47,8 @@ __device__ __forceinline__ void turn(typename Row16<kBf16>::T& a, typename Row16
 }
 
 // kAdjacent: pairs 2 i, 2 i + 1.  kPieces: else, pairs come in whole pieces of eight values (pairs a multiple of 8), two pieces at a time; otherwise value by value.
-template <bool kBf16, bool kAdjacent, bool kPieces>
+// kOnce: see kPastCaches
+template <bool kBf16, bool kAdjacent, bool kPieces, bool kOnce>
 __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
     typedef typename Row16<kBf16>::T T;
     __shared__ float2 s_turn[64];
@@ -69,13 +72,21 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
         return {r.k.d + (int64_t)token * r.k.token_bytes + (int64_t)h * r.k.head_bytes, r.k_out.d + (int64_t)token * r.k_out.token_bytes + (int64_t)h * r.k_out.head_bytes, at};
     };
     Eight<kBf16> a, b;
+    auto get = [](const char* from) -> u32x4 {
+        if constexpr (kOnce) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from));
+        else return *reinterpret_cast<const u32x4*>(from);
+    };
+    auto put = [](char* to, u32x4 v) {
+        if constexpr (kOnce) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to));
+        else *reinterpret_cast<u32x4*>(to) = v;
+    };
     auto ask = [&](const Place& p) {
         if constexpr (kAdjacent) {
-            a.u = *reinterpret_cast<const u32x4*>(p.from + 16 * p.at);
+            a.u = get(p.from + 16 * p.at);
         } else if constexpr (kPieces) {
             const bool turns = p.at < turning;
-            a.u = *reinterpret_cast<const u32x4*>(p.from + 16 * (turns ? p.at : p.at + turning));
-            if (turns) b.u = *reinterpret_cast<const u32x4*>(p.from + 16 * (p.at + turning));
+            a.u = get(p.from + 16 * (turns ? p.at : p.at + turning));
+            if (turns) b.u = get(p.from + 16 * (p.at + turning));
         } else {
             const bool turns = p.at < turning;
             a.h[0] = *reinterpret_cast<const T*>(p.from + 2 * (turns ? p.at : p.at + turning));
@@ -104,15 +115,15 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (4 * p.at + e < r.pairs) turn<kBf16>(a.h[2 * e], a.h[2 * e + 1], s_turn[4 * p.at + e]);
-            *reinterpret_cast<u32x4*>(p.to + 16 * p.at) = a.u;
+            put(p.to + 16 * p.at, a.u);
         } else if constexpr (kPieces) {
             if (p.at < turning) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) turn<kBf16>(a.h[e], b.h[e], s_turn[8 * p.at + e]);
-                *reinterpret_cast<u32x4*>(p.to + 16 * p.at) = a.u;
-                *reinterpret_cast<u32x4*>(p.to + 16 * (p.at + turning)) = b.u;
+                put(p.to + 16 * p.at, a.u);
+                put(p.to + 16 * (p.at + turning), b.u);
             } else {
-                *reinterpret_cast<u32x4*>(p.to + 16 * (p.at + turning)) = a.u;
+                put(p.to + 16 * (p.at + turning), a.u);
             }
         } else {
             if (p.at < turning) {
@@ -139,8 +150,10 @@ hipError_t launch_rotate(int dtype, const Rotate& r, hipStream_t s) {
     // few tokens: their heads over several blocks, a thread's work each
     const int splits = r.n_tokens >= 1024 ? 1 : std::max(1, std::min((total + kRotaryThreads - 1) / kRotaryThreads, 1024 / r.n_tokens));
     const dim3 grid((unsigned)r.n_tokens, (unsigned)splits);
+    const bool once = 2ll * r.dim * (r.q_heads + r.k_heads) * r.n_tokens >= kPastCaches;
     auto go = [&](auto bf16, auto adjacent, auto whole) {
-        hipLaunchKernelGGL((k_rotate<decltype(bf16)::value, decltype(adjacent)::value, decltype(whole)::value>), grid, dim3(kRotaryThreads), 0, s, r);
+        if (once) hipLaunchKernelGGL((k_rotate<decltype(bf16)::value, decltype(adjacent)::value, decltype(whole)::value, true>), grid, dim3(kRotaryThreads), 0, s, r);
+        else hipLaunchKernelGGL((k_rotate<decltype(bf16)::value, decltype(adjacent)::value, decltype(whole)::value, false>), grid, dim3(kRotaryThreads), 0, s, r);
     };
     auto by_layout = [&](auto bf16) {
         if (r.adjacent) go(bf16, std::true_type{}, std::true_type{});

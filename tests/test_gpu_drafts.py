@@ -85,6 +85,27 @@ def test_long_histories(store, dtype, n):
         attend(c, batch, trees(c.rng, batch), prior=n % 8 == 0)
 
 
+@pytest.mark.parametrize("store,dtype,dim", FORMATS)
+@pytest.mark.parametrize("n,group", [(9, 4), (11, 5), (16, 4), (33, 2), (25, 8), (64, 4), (64, 6)])
+def test_row_sets(store, dtype, dim, n, group):
+    """33 to 256 rows, in every number of sets of 32, and more; alone, among others of fewer rows, in one block and in stretches."""
+    c = Cache(op.PagesSpec(2, 2 * group, dim, 16, dtype, store), [700, 150, n, 66], n * group)
+    for batch in ([(n, 700), (max(1, n // 3), 150), (n, n), (2, 66)], [(0, 0), (n, 150), (0, 0), (n, 66)]):
+        attend(c, batch, trees(c.rng, batch), prior=group == 4)
+    assert c.pages.get_status() == 0
+
+
+@pytest.mark.parametrize("group", [2, 12])
+def test_infinities_of_small_weight(group):
+    """An infinity or NaN in V far below the strongest key, where its weight is rounded to zero: it reaches every row that sees it, and only values of its own."""
+    n = 20
+    c = Cache(op.PagesSpec(1, group, 64, 16, "fp16", "16"), [300], 9, history=False)
+    c.k[0][7, 0] *= 20
+    c.v[0][100, 0, 5], c.v[0][200, 0, 6], c.v[0][30, 0, 60] = float("inf"), float("-inf"), float("nan")
+    c.write([(300, 300)])
+    attend(c, [(n, 300)], trees(c.rng, [(n, 300)]), scale=1.0)
+
+
 @pytest.mark.parametrize("dtype", ("fp16", "bf16"))
 @pytest.mark.parametrize("n,total", [(6, 6), (6, 100), (64, 64), (64, 200), (20, 50)])
 def test_masks(dtype, n, total):
@@ -117,7 +138,7 @@ def test_a_chain_is_a_causal_text(n):
     c.check(batch, q, out, lse, 128 ** -0.5)
 
 
-@pytest.mark.parametrize("n,heads", [(5, 2), (40, 4)])
+@pytest.mark.parametrize("n,heads", [(5, 2), (12, 4), (40, 4)])
 def test_keys_out_of_sight_are_not_finite(n, heads):
     """Infinities and NaN in K and V of drafted tokens reach those that see them, and nobody else."""
     c = Cache(op.PagesSpec(1, heads, 64, 16, "fp16", "16"), [90], 3, history=False)
