@@ -71,7 +71,6 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
         const int h = head - r.q_heads;
         return {r.k.d + (int64_t)token * r.k.token_bytes + (int64_t)h * r.k.head_bytes, r.k_out.d + (int64_t)token * r.k_out.token_bytes + (int64_t)h * r.k_out.head_bytes, at};
     };
-    Eight<kBf16> a, b;
     auto get = [](const char* from) -> u32x4 {
         if constexpr (kOnce) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from));
         else return *reinterpret_cast<const u32x4*>(from);
@@ -80,24 +79,28 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
         if constexpr (kOnce) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to));
         else *reinterpret_cast<u32x4*>(to) = v;
     };
-    auto ask = [&](const Place& p) {
-        if constexpr (kAdjacent) {
-            a.u = get(p.from + 16 * p.at);
-        } else if constexpr (kPieces) {
-            const bool turns = p.at < turning;
-            a.u = get(p.from + 16 * (turns ? p.at : p.at + turning));
-            if (turns) b.u = get(p.from + 16 * (p.at + turning));
-        } else {
-            const bool turns = p.at < turning;
-            a.h[0] = *reinterpret_cast<const T*>(p.from + 2 * (turns ? p.at : p.at + turning));
-            if (turns) b.h[0] = *reinterpret_cast<const T*>(p.from + 2 * (p.at + turning));
+    constexpr int kFlight = kPieces ? 2 : 1;        // items of a thread on their way together
+    Eight<kBf16> a[kFlight], b[kFlight];
+    Place p[kFlight];
+    auto ask = [&](int first) {
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            if (first + kRotaryThreads * i >= end) continue;
+            p[i] = place(first + kRotaryThreads * i);
+            if constexpr (kAdjacent) {
+                a[i].u = get(p[i].from + 16 * p[i].at);
+            } else if constexpr (kPieces) {
+                const bool turns = p[i].at < turning;
+                a[i].u = get(p[i].from + 16 * (turns ? p[i].at : p[i].at + turning));
+                if (turns) b[i].u = get(p[i].from + 16 * (p[i].at + turning));
+            } else {
+                const bool turns = p[i].at < turning;
+                a[i].h[0] = *reinterpret_cast<const T*>(p[i].from + 2 * (turns ? p[i].at : p[i].at + turning));
+                if (turns) b[i].h[0] = *reinterpret_cast<const T*>(p[i].from + 2 * (p[i].at + turning));
+            }
         }
     };
-    Place p = {};
-    if (item < end) {
-        p = place(item);
-        ask(p);
-    }
+    ask(item);
     if ((int)threadIdx.x < r.pairs) {
         const int i = threadIdx.x;
         int axis = 0;
@@ -110,35 +113,34 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
         s_turn[i] = make_float2(cosine, r.inverse ? -sine : sine);
     }
     __syncthreads();
-    while (item < end) {
-        if constexpr (kAdjacent) {
+    for (; item < end; item += kFlight * kRotaryThreads) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (4 * p.at + e < r.pairs) turn<kBf16>(a.h[2 * e], a.h[2 * e + 1], s_turn[4 * p.at + e]);
-            put(p.to + 16 * p.at, a.u);
-        } else if constexpr (kPieces) {
-            if (p.at < turning) {
+        for (int i = 0; i < kFlight; ++i) {
+            if (item + kRotaryThreads * i >= end) continue;
+            const int at = p[i].at;
+            if constexpr (kAdjacent) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) turn<kBf16>(a.h[e], b.h[e], s_turn[8 * p.at + e]);
-                put(p.to + 16 * p.at, a.u);
-                put(p.to + 16 * (p.at + turning), b.u);
+                for (int e = 0; e < 4; ++e)
+                    if (4 * at + e < r.pairs) turn<kBf16>(a[i].h[2 * e], a[i].h[2 * e + 1], s_turn[4 * at + e]);
+                put(p[i].to + 16 * at, a[i].u);
+            } else if constexpr (kPieces) {
+                if (at < turning) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) turn<kBf16>(a[i].h[e], b[i].h[e], s_turn[8 * at + e]);
+                    put(p[i].to + 16 * at, a[i].u);
+                    put(p[i].to + 16 * (at + turning), b[i].u);
+                } else {
+                    put(p[i].to + 16 * (at + turning), a[i].u);
+                }
+            } else if (at < turning) {
+                turn<kBf16>(a[i].h[0], b[i].h[0], s_turn[at]);
+                *reinterpret_cast<T*>(p[i].to + 2 * at) = a[i].h[0];
+                *reinterpret_cast<T*>(p[i].to + 2 * (at + turning)) = b[i].h[0];
             } else {
-                put(p.to + 16 * (p.at + turning), a.u);
-            }
-        } else {
-            if (p.at < turning) {
-                turn<kBf16>(a.h[0], b.h[0], s_turn[p.at]);
-                *reinterpret_cast<T*>(p.to + 2 * p.at) = a.h[0];
-                *reinterpret_cast<T*>(p.to + 2 * (p.at + turning)) = b.h[0];
-            } else {
-                *reinterpret_cast<T*>(p.to + 2 * (p.at + turning)) = a.h[0];
+                *reinterpret_cast<T*>(p[i].to + 2 * (at + turning)) = a[i].h[0];
             }
         }
-        item += kRotaryThreads;
-        if (item < end) {
-            p = place(item);
-            ask(p);
-        }
+        ask(item + kFlight * kRotaryThreads);
     }
 }
 
