@@ -3,15 +3,11 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "pages.h"
+#include "pages_stream.h"
 
 namespace sali {
 
 namespace {
-
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kDigits[3] = {21, 10, 0};     // lowest bit of each digit: 11, 11 and 10 bits
@@ -32,7 +28,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
     __shared__ uint32_t s_bins[kBins];
     __shared__ uint32_t s_wave[2][kSelectWaves];
     __shared__ uint32_t s_found[2];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int s = (int)(blockIdx.x / (uint32_t)a.geom.n_kv), head = (int)(blockIdx.x % (uint32_t)a.geom.n_kv);
     const StartFalls falls(a.seqs.start, a.seqs.n_seqs, tid, kSelectThreads);
     const PageSeq seq = load_seq(a.seqs, a.geom, s, head == 0 && tid == 0);
@@ -62,111 +58,125 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
         atomicOr(a.seqs.status, SALI_FAULT_PAGE);
         return 0u;
     };
+    // sum over the waves before this one
+    auto before_wave = [&](const uint32_t* of_wave) {
+        const int upto = wave_scan(lane < kSelectWaves ? (int)of_wave[lane] : 0);
+        return wave == 0 ? 0u : (uint32_t)__builtin_amdgcn_readlane(upto, wave - 1);
+    };
     // those that are chosen from: first .. first + m - 1
     const int first = a.sinks, m = n - a.sinks - a.recent;
     uint32_t room = (uint32_t)(a.budget - a.sinks - a.recent);
-    auto key = [&](int j) { return j < kInLds ? s_keys[j] : key_in_pages(first + j); };
-    uint32_t at = 0xFFFFFFFFu, ties = 0;                    // keys above `at` stay, and the first `ties` of those at it
-    if (room > 0) {
-        // four at a time, aligned as the pages are, and several of them on their way together
-        const int pos_end = base + first + min(m, kInLds), quad0 = (base + first) & ~3;
-        constexpr int kFlight = 8;
-        for (int64_t pos0 = quad0; pos0 < pos_end; pos0 += 4 * kFlight * kSelectThreads) {
-            int page[kFlight];
-            f32x4 w[kFlight];
+    // (Where all are in LDS, reading them takes no branch, and several are on their way together.)
+    auto choose = [&](auto all_in_lds) {
+        auto key = [&](int j) {
+            if constexpr (decltype(all_in_lds)::value) return s_keys[j];
+            else return j < kInLds ? s_keys[j] : key_in_pages(first + j);
+        };
+        uint32_t at = 0xFFFFFFFFu, ties = 0;                    // keys above `at` stay, and the first `ties` of those at it
+        if (room > 0) {
+            // four at a time, aligned as the pages are, and several of them on their way together
+            const int pos_end = base + first + min(m, kInLds), quad0 = (base + first) & ~3;
+            constexpr int kFlight = 8;
+            for (int64_t pos0 = quad0; pos0 < pos_end; pos0 += 4 * kFlight * kSelectThreads) {
+                int page[kFlight];
+                f32x4 w[kFlight];
 #pragma unroll
-            for (int i = 0; i < kFlight; ++i) {
-                const int64_t pos = pos0 + 4 * (kSelectThreads * i + tid);
-                page[i] = pos < pos_end ? page_at((int)pos) : -2;
+                for (int i = 0; i < kFlight; ++i) {
+                    const int64_t pos = pos0 + 4 * (kSelectThreads * i + tid);
+                    page[i] = pos < pos_end ? page_at((int)pos) : -2;
+                }
+#pragma unroll
+                for (int i = 0; i < kFlight; ++i)
+                    w[i] = page[i] >= 0 ? *reinterpret_cast<const f32x4*>(weights_at(page[i], (int)(pos0 + 4 * (kSelectThreads * i + tid)))) : (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < kFlight; ++i) {
+                    if (page[i] == -1) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
+                    const int64_t pos = pos0 + 4 * (kSelectThreads * i + tid);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (pos + e >= base + first && pos + e < pos_end) s_keys[(int)(pos + e) - base - first] = page[i] >= 0 ? key_of(w[i][e]) : 0u;
+                }
             }
+            uint32_t prefix = 0;
+            for (int d = 0; d < 3; ++d) {
+                const int low = kDigits[d], high = d == 0 ? 32 : kDigits[d - 1];
+                for (int b = tid; b < kBins; b += kSelectThreads) s_bins[b] = 0;
+                __syncthreads();
+                // several keys on their way together: the loop is a chain of trips to LDS
+                constexpr int kKeys = 4;
+                for (int j0 = tid; j0 < m; j0 += kKeys * kSelectThreads) {
+                    uint32_t k[kKeys];
 #pragma unroll
-            for (int i = 0; i < kFlight; ++i)
-                w[i] = page[i] >= 0 ? *reinterpret_cast<const f32x4*>(weights_at(page[i], (int)(pos0 + 4 * (kSelectThreads * i + tid)))) : (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int i = 0; i < kKeys; ++i) k[i] = key(min(j0 + kSelectThreads * i, m - 1));
 #pragma unroll
-            for (int i = 0; i < kFlight; ++i) {
-                if (page[i] == -1) atomicOr(a.seqs.status, SALI_FAULT_PAGE);
-                const int64_t pos = pos0 + 4 * (kSelectThreads * i + tid);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (pos + e >= base + first && pos + e < pos_end) s_keys[(int)(pos + e) - base - first] = page[i] >= 0 ? key_of(w[i][e]) : 0u;
+                    for (int i = 0; i < kKeys; ++i)
+                        if (j0 + kSelectThreads * i < m && (d == 0 || k[i] >> high == prefix)) atomicAdd(&s_bins[k[i] >> low & (kBins - 1) & ((1u << (high - low)) - 1u)], 1u);
+                }
+                __syncthreads();
+                // tokens from the highest bin down: thread t has bins kBins - 1 - 2 t and the one below
+                const uint32_t upper = s_bins[kBins - 1 - 2 * tid], lower = s_bins[kBins - 2 - 2 * tid];
+                uint32_t sum = (uint32_t)wave_scan((int)(upper + lower));
+                if (lane == 63) s_wave[0][wave] = sum;
+                __syncthreads();
+                sum += before_wave(s_wave[0]);
+                const uint32_t before = sum - upper - lower;
+                if (before < room && sum >= room) {
+                    const bool in_upper = before + upper >= room;
+                    s_found[0] = (uint32_t)(kBins - 1 - 2 * tid - (in_upper ? 0 : 1));
+                    s_found[1] = room - before - (in_upper ? 0u : upper);
+                }
+                __syncthreads();
+                prefix = prefix << (high - low) | s_found[0];
+                room = s_found[1];
             }
+            at = prefix;
+            ties = room;
         }
-        uint32_t prefix = 0;
-        for (int d = 0; d < 3; ++d) {
-            const int low = kDigits[d], high = d == 0 ? 32 : kDigits[d - 1];
-            for (int b = tid; b < kBins; b += kSelectThreads) s_bins[b] = 0;
-            __syncthreads();
-            for (int j = tid; j < m; j += kSelectThreads) {
-                const uint32_t k = key(j);
-                if (d > 0 && k >> high != prefix) continue;
-                atomicAdd(&s_bins[k >> low & (kBins - 1) & ((1u << (high - low)) - 1u)], 1u);
-            }
-            __syncthreads();
-            // tokens from the highest bin down: thread t has bins kBins - 1 - 2 t and the one below
-            const uint32_t upper = s_bins[kBins - 1 - 2 * tid], lower = s_bins[kBins - 2 - 2 * tid];
-            uint32_t sum = upper + lower;
+        // every wave a stretch of the sequence's tokens
+        const int stretch = ((n + kSelectWaves - 1) / kSelectWaves + 63) & ~63, lo = (int)min((int64_t)n, (int64_t)stretch * wave), hi = (int)min((int64_t)n, (int64_t)lo + stretch);
+        constexpr int kLooks = 8;               // of a lane, on their way together
+        auto each = [&](auto look) {
+            for (int64_t i0 = lo; i0 < hi; i0 += 64 * kLooks) {
+                uint32_t k[kLooks];
 #pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const uint32_t x = __shfl_up(sum, off);
-                if (lane >= off) sum += x;
+                for (int x = 0; x < kLooks; ++x) {
+                    const int64_t i = i0 + 64 * x + lane;
+                    k[x] = decltype(all_in_lds)::value || ties > 0 ? key((int)min(max(i - first, (int64_t)0), (int64_t)m - 1)) : 0u;
+                }
+#pragma unroll
+                for (int x = 0; x < kLooks; ++x) {
+                    const int64_t i = i0 + 64 * x + lane;
+                    const bool from = i >= first && i < first + m;
+                    look((int)i, i < hi && (!from || (ties > 0 && k[x] > at)), ties > 0 && i < hi && from && k[x] == at);
+                }
             }
-            if (lane == 63) s_wave[0][wave] = sum;
-            __syncthreads();
-            for (int w = 0; w < wave; ++w) sum += s_wave[0][w];
-            const uint32_t before = sum - upper - lower;
-            if (before < room && sum >= room) {
-                const bool in_upper = before + upper >= room;
-                s_found[0] = (uint32_t)(kBins - 1 - 2 * tid - (in_upper ? 0 : 1));
-                s_found[1] = room - before - (in_upper ? 0u : upper);
-            }
-            __syncthreads();
-            prefix = prefix << (high - low) | s_found[0];
-            room = s_found[1];
+        };
+        uint32_t sure = 0, tied = 0;
+        each([&](int, bool stays, bool tie) {
+            sure += (uint32_t)__popcll(__ballot(stays));
+            tied += (uint32_t)__popcll(__ballot(tie));
+        });
+        __syncthreads();                                        // s_wave has been read
+        if (lane == 0) {
+            s_wave[0][wave] = sure;
+            s_wave[1][wave] = tied;
         }
-        at = prefix;
-        ties = room;
-    }
-    // every wave a stretch of the sequence's tokens
-    const int stretch = ((n + kSelectWaves - 1) / kSelectWaves + 63) & ~63, lo = (int)min((int64_t)n, (int64_t)stretch * wave), hi = (int)min((int64_t)n, (int64_t)lo + stretch);
-    auto look = [&](int i, bool& stays, bool& tie) {
-        stays = i < hi && (i < first || i >= first + m);
-        tie = false;
-        if (i < hi && !stays && ties > 0) {
-            const uint32_t k = key(i - first);
-            stays = k > at;
-            tie = k == at;
-        }
+        __syncthreads();
+        sure = before_wave(s_wave[0]);
+        tied = before_wave(s_wave[1]);
+        uint32_t next = sure + min(tied, ties);
+        const uint64_t lanes_before = (1ull << lane) - 1ull;
+        each([&](int i, bool stays, bool tie) {
+            const uint64_t all_ties = __ballot(tie);
+            stays |= tie && tied + (uint32_t)__popcll(all_ties & lanes_before) < ties;
+            tied += (uint32_t)__popcll(all_ties);
+            const uint64_t all = __ballot(stays);
+            if (stays) out[next + (uint32_t)__popcll(all & lanes_before)] = i;
+            next += (uint32_t)__popcll(all);
+        });
     };
-    uint32_t sure = 0, tied = 0;
-    for (int i0 = lo; i0 < hi; i0 += 64) {
-        bool stays, tie;
-        look(i0 + lane, stays, tie);
-        sure += (uint32_t)__popcll(__ballot(stays));
-        tied += (uint32_t)__popcll(__ballot(tie));
-    }
-    __syncthreads();                                        // s_wave has been read
-    if (lane == 0) {
-        s_wave[0][wave] = sure;
-        s_wave[1][wave] = tied;
-    }
-    __syncthreads();
-    sure = tied = 0;
-    for (int w = 0; w < wave; ++w) {
-        sure += s_wave[0][w];
-        tied += s_wave[1][w];
-    }
-    uint32_t next = sure + min(tied, ties);
-    const uint64_t lanes_before = (1ull << lane) - 1ull;
-    for (int i0 = lo; i0 < hi; i0 += 64) {
-        bool stays, tie;
-        look(i0 + lane, stays, tie);
-        const uint64_t all_ties = __ballot(tie);
-        stays |= tie && tied + (uint32_t)__popcll(all_ties & lanes_before) < ties;
-        tied += (uint32_t)__popcll(all_ties);
-        const uint64_t all = __ballot(stays);
-        if (stays) out[next + (uint32_t)__popcll(all & lanes_before)] = i0 + lane;
-        next += (uint32_t)__popcll(all);
-    }
+    if (m <= kInLds) choose(std::true_type{});
+    else choose(std::false_type{});
 }
 
 // ---- moving rows

@@ -32,7 +32,7 @@ def check(got, x, position, pairs, sections, adjacent, inverse, dtype):
     got = op.to_f32(bits_of(got), dtype).astype(np.float64)
     # sine and cosine in fp32 (2^-22), two products and their sum (2^-23), the angle (2^31 turns at the most, 2^-52 of them twice: 2^-18 radians); then one rounding, of
     # numbers down to the type's smallest
-    reach = np.abs(position).max(initial=1)
+    reach = np.abs(position.astype(np.float64)).max(initial=1.0)
     far = size * (2.0 ** -21 + 8 * reach * 2.0 ** -52) + half * np.abs(e) * 1.01 + (2.0 ** -25 if dtype == "fp16" else 2.0 ** -134)
     same = (got == e) | (np.isnan(got) & np.isnan(e))
     with np.errstate(invalid="ignore"):
