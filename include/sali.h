@@ -554,7 +554,7 @@ int sali_pages_rotate(sali_pages* p, const sali_rotary* rotary, const int32_t* d
  * already (sali_pages_append).  A drafted token sees all tokens before the draft, and of the draft those that its mask names:
  *   d_seen        uint64[n_tokens], bit i of a row: the draft's i-th token (itself too only if its bit is set); bits of more tokens than the draft has mean nothing
  * and nothing else; what else there is, is as in sali_pages_attend.  SALI_ERR_SHAPE for a max_q above 64 too.  What was accepted of the draft is moved together by
- * sali_pages_keep. */
+ * sali_pages_keep.  Asynchronous on `stream`; uses the area of partial results as sali_pages_attend does. */
 int sali_pages_attend_tree(sali_pages* p, int32_t layer, const sali_page_batch* batch, const uint64_t* d_seen, const sali_rows* q,
                            float softmax_scale, const float* d_prior_or_null, const float* d_prior_lse_or_null, const sali_rows* out,
                            float* d_lse_or_null, void* stream);
@@ -566,8 +566,8 @@ int sali_pages_attend_tree(sali_pages* p, int32_t layer, const sali_page_batch* 
  *   d_weights     fp32[n_pages][n_kv_heads][page_tokens], of this layer: the caller keeps one for every layer
  *   add           0: the weights of all of the sequence's positions are set to w; else w is added to the weights of positions before the new tokens, and those of the
  *                 new tokens are set (their pages may have been others' before)
- * Weights of other positions, and of pages that are none, are not touched.  No two sequences of a batch may share a page.  Asynchronous on `stream`.
- * Errors as sali_pages_attend's; n_seqs * n_kv_heads * (max_kv / 128 rounded up) is below 2^24 (SALI_ERR_SHAPE). */
+ * Weights of other positions, and of pages that are none, are not touched.  No two sequences of a batch may share a page.  Asynchronous on `stream`; uses the area
+ * of partial results as sali_pages_attend does.  Errors as sali_pages_attend's; n_seqs * n_kv_heads * (max_kv / 128 rounded up) is below 2^23 (SALI_ERR_SHAPE). */
 int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, float softmax_scale, int32_t window,
                      int32_t sinks, const float* d_lse, int32_t add, float* d_weights, void* stream);
 

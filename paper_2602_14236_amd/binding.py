@@ -614,7 +614,7 @@ class SaliPages:
         if rotary.index != index:
             raise ValueError(f"the frequencies lie on {rotary.device}, the pages on {self.device}")
         shape = position.shape
-        n = shape[-1]
+        n = shape[-1] if shape else 0
         if position.dtype is not torch.int32 or (shape != (rotary.axes, n) and (rotary.axes != 1 or len(shape) != 1)) or not position.is_contiguous() or \
                 position.get_device() != index:
             raise self._wrong("position", position, torch.int32, [rotary.axes, "tokens"])

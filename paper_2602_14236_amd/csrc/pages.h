@@ -104,7 +104,7 @@ hipError_t launch_pages_attend_fp16(int store, int dim, const PagesAttend& a, hi
 hipError_t launch_pages_attend_bf16(int store, int dim, const PagesAttend& a, hipStream_t s);
 hipError_t launch_pages_attend_tree_fp16(int store, int dim, const PagesAttend& a, hipStream_t s);
 hipError_t launch_pages_attend_tree_bf16(int store, int dim, const PagesAttend& a, hipStream_t s);
-constexpr int kWeighTokens = 128;           // keys of a thread block
+constexpr int kWeighTokens = 128;           // keys of a thread block at the least
 inline int64_t weigh_blocks(const PageSeqs& q) { return ((int64_t)q.max_kv + kWeighTokens - 1) / kWeighTokens; }
 constexpr int kKeepTokens = 64;             // rows of a thread block, if they go to other pages
 inline int64_t keep_chunks(const PageSeqs& q, int32_t width, bool in_place) {

@@ -279,7 +279,7 @@ int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch,
     PagesWeigh a = {};
     a.geom = geom_of(p, layer);
     a.seqs = seqs_of(p, *batch);
-    if (weigh_blocks(a.seqs) * p->cfg.n_kv_heads > kMostBlocks / batch->n_seqs) return SALI_ERR_SHAPE;
+    if (weigh_blocks(a.seqs) * p->cfg.n_kv_heads > kMostBlocks / 2 / batch->n_seqs) return SALI_ERR_SHAPE;        // half as many of 512 threads
     a.q = rows_of<RowsIn>(*q);
     a.lse = d_lse;
     a.weights = d_weights;

@@ -168,6 +168,30 @@ def test_rows_past_the_batch_and_strides():
     assert (wide[:, :2] == 7).all() and (wide[:, 10:] == 7).all()
 
 
+@pytest.mark.parametrize("n", [3, 9, 50])
+def test_a_batch_that_begins_later(n):
+    """Rows before the batch's first keep what they hold."""
+    c = Cache(op.PagesSpec(2, 8, 64, 16, "bf16", "int8"), [300, 100], 10)
+    batch, t = [(n, 300), (n, 100)], 2 * n + 6
+    masks = trees(c.rng, batch)
+    q = rows(c.rng, t, 8, 64, "bf16").to(DEV)
+    out, lse = torch.full_like(q, 7.0), torch.full((t, 8), 7.0, device=DEV)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)
+    late = c.b.PageBatch(ints(6, 6 + n, 6 + 2 * n), ints(300, 100), torch.from_numpy(c.table).to(DEV), t, max_q=n, max_kv=300)
+    c.pages.attend_tree(0, late, torch.tensor([0] * 6 + masks, device=DEV), q, 0.125, out, lse)
+    verify(c, batch, masks, q[6:], out[6:], lse[6:], 0.125)
+    assert (out[:6] == 7).all() and (lse[:6] == 7).all() and c.pages.get_status() == 0
+
+
+def test_pools_past_32_bits():
+    c = Cache(op.PagesSpec(8, 32, 128, 256, "bf16", "16"), [700], 11, extra_pages=5000, history=False)
+    c.table[0, :3] = [c.pages.cfg.n_pages - 1, 5, c.pages.cfg.n_pages - 2]
+    c.write([(700, 700)])
+    for n in (5, 40):
+        attend(c, [(n, 700)], trees(c.rng, [(n, 700)]))
+    assert c.pages.get_status() == 0
+
+
 @pytest.mark.parametrize("n", [4, 40])
 def test_pages_that_are_none(n):
     from paper_2602_14236_amd import binding

@@ -162,6 +162,49 @@ def test_wrong_batches_have_no_weights():
         assert c.pages.get_status() == binding.FAULT_BATCH and (w == 3).all() and (keep == 7).all() and torch.equal(c.pages.pool, pool)
 
 
+@pytest.mark.parametrize("n", [1, 12, 40, 150])
+def test_weights_of_a_batch_that_begins_later(n):
+    """Rows before the batch's first are not its own."""
+    from paper_2602_14236_amd import binding
+    c = Cache(op.PagesSpec(2, 8, 64, 16, "fp16", "16"), [300, 200], 23)
+    q = rows(c.rng, 2 * n + 5, 8, 64, "fp16").to(DEV)
+    lse, w, late = torch.full((2 * n + 5, 8), 3.0, device=DEV), weights_of(c), weights_of(c)
+    lse[:5] = float("nan")
+    c.pages.weigh(0, c.batch([(n, 300), (n, 200)]), q[5:], 0.125, lse[5:].contiguous(), w, add=False)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)
+    batch = binding.PageBatch(ints(5, 5 + n, 5 + 2 * n), ints(300, 200), torch.from_numpy(c.table).to(DEV), 2 * n + 5, max_q=n, max_kv=300)
+    c.pages.weigh(0, batch, q, 0.125, lse, late, add=False)
+    assert torch.equal(w, late) and c.pages.get_status() == 0
+
+
+def test_pools_past_32_bits():
+    """Weights, choice and move in the last pages of a pool of 5 GB."""
+    c = Cache(op.PagesSpec(8, 8, 128, 256, "bf16", "16"), [700], 24, extra_pages=5000, history=False)
+    n_pages = c.pages.cfg.n_pages
+    c.table[0, :3] = [n_pages - 1, n_pages - 3, n_pages - 2]
+    c.write([(700, 700)])
+    for n in (1, 40, 700):
+        weigh(c, [(n, 700)])
+    w = weights_of(c)
+    w.copy_(torch.rand(w.shape, device=DEV))
+    keep = select(c, [(700, 700)], w, 50, sinks=1, recent=9)
+    old = of_seq(c, w, 0, 700)
+    to = torch.tensor([[n_pages - 5]], dtype=torch.int32, device=DEV)
+    kept = keep.cpu().numpy()[0]
+    k, v = (torch.empty((50, 8, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    after = c.b.PageBatch(torch.tensor([0, 50], dtype=torch.int32, device=DEV), torch.tensor([50], dtype=torch.int32, device=DEV), to, 50, max_kv=50)
+    for place in (to, None):
+        c.pages.keep(0, c.batch([(700, 700)]), keep, to=place, weights=w)
+        if place is None:
+            after = c.b.PageBatch(*after.tensors[:2], torch.from_numpy(c.table).to(DEV), 50, max_kv=50)
+        c.pages.read(0, after, k, v)
+        for h in range(8):
+            assert torch.equal(k[:, h].cpu(), c.k[0][kept[h], h]) and torch.equal(v[:, h].cpu(), c.v[0][kept[h], h])
+            page = n_pages - 5 if place is not None else n_pages - 1
+            assert np.array_equal(w[page, h, :50].cpu().numpy().astype(np.float64), old[kept[h], h])
+    assert c.pages.get_status() == 0
+
+
 # ---- the choice ------------------------------------------------------------------------------------
 def select(c, new_and_len, w, budget, sinks=0, recent=0):
     keep = torch.full((len(new_and_len), c.spec.n_kv_heads, budget), 7, dtype=torch.int32, device=DEV)
@@ -504,3 +547,34 @@ def test_refusals():
     assert move(width=0, list_=None) == 0
     torch.cuda.synchronize()
     assert p.get_status() == 0 and (w == 3).all() and (keep == 7).all() and torch.equal(before, p.pool)
+
+
+def test_calls_of_more_blocks_than_a_launch_takes():
+    """By the batch's sizes, whatever its arrays hold"""
+    from paper_2602_14236_amd import binding as b
+    c = Cache(op.PagesSpec(2, 4, 64, 16, "fp16", "16"), [40], 21, extra_pages=3)
+    q = rows(c.rng, 8, 4, 64, "fp16").to(DEV)
+    lse, w, batch = torch.zeros((8, 4), device=DEV), weights_of(c), c.batch([(8, 40)])
+    long = b.sali_page_batch(*{**{n: getattr(batch.c, n) for n, _ in b.sali_page_batch._fields_}, "max_kv": 128 * 2 ** 22}.values())
+    assert c.pages.lib.sali_pages_weigh(c.pages.handle, 0, long, b.sali_rows(q.data_ptr(), 256, 64), 0.1, 0, 0, lse.data_ptr(), 0, w.data_ptr(), None) == -2
+    torch.cuda.synchronize()
+    assert (w == 3).all() and c.pages.get_status() == 0
+
+
+@pytest.mark.parametrize("n", [1, 30, 200])
+def test_weights_at_any_address_of_a_float(n):
+    c = Cache(op.PagesSpec(2, 8, 64, 32, "bf16", "16"), [430], 25)
+    q = rows(c.rng, n, 8, 64, "bf16").to(DEV)
+    size = weights_of(c).numel()
+    lists, all_weights = [], []
+    for off in range(4):
+        base = torch.full((size + 4,), 3.0, device=DEV)
+        w = base[off:off + size].view(weights_of(c).shape)
+        batch = c.batch([(n, 430)])
+        lse = torch.zeros((n, 8), device=DEV)
+        c.pages.attend(0, batch, q, 0.125, torch.empty_like(q), lse)
+        c.pages.weigh(0, batch, q, 0.125, lse, w, add=False)
+        lists.append(select(c, [(430, 430)], w, 40, sinks=1, recent=3))
+        all_weights.append(w.clone())
+        assert (base[:off] == 3).all() and (base[off + size:] == 3).all()
+    assert all(torch.equal(all_weights[0], x) for x in all_weights) and all(torch.equal(lists[0], x) for x in lists)

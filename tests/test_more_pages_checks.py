@@ -83,6 +83,15 @@ def test_tensors_that_are_none(pages_elsewhere):
     assert state.calls == []
 
 
+def test_a_single_position_is_no_array(pages_elsewhere):
+    from paper_2602_14236_amd.binding import Rotary
+    pages, state = pages_elsewhere
+    q = torch.zeros((1, 4, 64), dtype=torch.float16)
+    with pytest.raises(ValueError, match="position"):
+        pages.rotate(Rotary(torch.ones(32, dtype=torch.float64)), torch.tensor(3, dtype=torch.int32), q, None)
+    assert state.calls == []
+
+
 def test_masks_of_drafts_by_key(tmp_path):
     """What 32 keys of a tile show of a mask, for every place that the tile can have before, at and behind the draft's beginning."""
     run_pages_program(tmp_path, """
