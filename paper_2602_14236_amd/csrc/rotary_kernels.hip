@@ -6,7 +6,10 @@
 // and sine and cosine of what is left in fp32.
 //
 // Every row is read and written once, which is what bounds long calls; a block has one token (or part of its heads, where there are few tokens), whose angles it
-// works out once for all heads, in LDS, while its first rows are on their way.
+// works out once for all heads, in LDS, while its first rows are on their way.  20002 tokens, 40 and 40 heads of 128, 820 MB: 147 us, 5.6 TB/s (a plain copy of 2 GiB:
+// 4.8 by the library, 6.5 by the best kernel); 4608 tokens, 32 and 32 heads, 151 MB, out of the caches: 23.7 us; a step of 32 tokens 3.3 us, a launch's chain of trips, of 14.5
+// that the call takes the host.  Slower: heads of long calls over several blocks, one piece a thread (157 to 165 us: the angles again in each), all pieces of a thread on
+// their way together (151 us, and 69 for 62 in rows of 40 heads).
 #include <algorithm>
 #include <type_traits>
 
@@ -18,8 +21,10 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kRotaryThreads = 256;
-// Bytes of rows, half of what the last cache holds, from which on they go past the caches: longer ones would only push each other out.
+constexpr int kRotaryThreads = 256, kMostRotaryThreads = 512;
+// Bytes of rows, half of what the last cache holds, from which on they go past the caches: longer ones would only push each other out.  With the append of the keys
+// and a reader of the queries behind it, 138 MB take 109 us past them and 115 through them, 410 MB 327 and 326; alone 410 MB take 147 and 159.  Shorter ones are still there
+// for what reads them: 92 MB 71 us, outputs past the caches 74.
 constexpr int64_t kPastCaches = 128 << 20;
 
 template <bool kBf16>
@@ -49,9 +54,10 @@ __device__ __forceinline__ void turn(typename Row16<kBf16>::T& a, typename Row16
 // kAdjacent: pairs 2 i, 2 i + 1.  kPieces: else, pairs come in whole pieces of eight values (pairs a multiple of 8), two pieces at a time; otherwise value by value.
 // kOnce: see kPastCaches
 template <bool kBf16, bool kAdjacent, bool kPieces, bool kOnce>
-__global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
+__global__ __launch_bounds__(kMostRotaryThreads) void k_rotate(Rotate r) {
     typedef typename Row16<kBf16>::T T;
     __shared__ float2 s_turn[64];
+    const int threads = (int)blockDim.x;
     const int token = blockIdx.x;
     // what a thread does for a head: two pieces that turn together, one piece (adjacent; what does not turn), or one pair, or one value that does not turn
     const int turning = kAdjacent ? r.dim / 8 : (kPieces ? r.pairs / 8 : r.pairs);
@@ -85,8 +91,8 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
     auto ask = [&](int first) {
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            if (first + kRotaryThreads * i >= end) continue;
-            p[i] = place(first + kRotaryThreads * i);
+            if (first + threads * i >= end) continue;
+            p[i] = place(first + threads * i);
             if constexpr (kAdjacent) {
                 a[i].u = get(p[i].from + 16 * p[i].at);
             } else if constexpr (kPieces) {
@@ -113,10 +119,10 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
         s_turn[i] = make_float2(cosine, r.inverse ? -sine : sine);
     }
     __syncthreads();
-    for (; item < end; item += kFlight * kRotaryThreads) {
+    for (; item < end; item += kFlight * threads) {
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            if (item + kRotaryThreads * i >= end) continue;
+            if (item + threads * i >= end) continue;
             const int at = p[i].at;
             if constexpr (kAdjacent) {
 #pragma unroll
@@ -140,7 +146,7 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotate(Rotate r) {
                 *reinterpret_cast<T*>(p[i].to + 2 * (at + turning)) = a[i].h[0];
             }
         }
-        ask(item + kFlight * kRotaryThreads);
+        ask(item + kFlight * threads);
     }
 }
 
@@ -152,10 +158,13 @@ hipError_t launch_rotate(int dtype, const Rotate& r, hipStream_t s) {
     // few tokens: their heads over several blocks, a thread's work each
     const int splits = r.n_tokens >= 1024 ? 1 : std::max(1, std::min((total + kRotaryThreads - 1) / kRotaryThreads, 1024 / r.n_tokens));
     const dim3 grid((unsigned)r.n_tokens, (unsigned)splits);
+    // else blocks whose threads have an even number of items, as they come in twos, or one (1280 items by 320 threads: 147 us, by 256: 154)
+    const int most = total / kRotaryThreads, each = most < 2 ? 1 : most & ~1;
+    const int threads = splits > 1 || r.n_tokens > kMostBlocks / 2 ? kRotaryThreads : std::min(kMostRotaryThreads, ((total + each - 1) / each + 63) & ~63);
     const bool once = 2ll * r.dim * (r.q_heads + r.k_heads) * r.n_tokens >= kPastCaches;
     auto go = [&](auto bf16, auto adjacent, auto whole) {
-        if (once) hipLaunchKernelGGL((k_rotate<decltype(bf16)::value, decltype(adjacent)::value, decltype(whole)::value, true>), grid, dim3(kRotaryThreads), 0, s, r);
-        else hipLaunchKernelGGL((k_rotate<decltype(bf16)::value, decltype(adjacent)::value, decltype(whole)::value, false>), grid, dim3(kRotaryThreads), 0, s, r);
+        if (once) hipLaunchKernelGGL((k_rotate<decltype(bf16)::value, decltype(adjacent)::value, decltype(whole)::value, true>), grid, dim3((unsigned)threads), 0, s, r);
+        else hipLaunchKernelGGL((k_rotate<decltype(bf16)::value, decltype(adjacent)::value, decltype(whole)::value, false>), grid, dim3((unsigned)threads), 0, s, r);
     };
     auto by_layout = [&](auto bf16) {
         if (r.adjacent) go(bf16, std::true_type{}, std::true_type{});

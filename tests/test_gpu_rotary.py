@@ -62,6 +62,26 @@ def test_axes_and_orders(dtype, dim, axes, adjacent):
         assert torch.equal(q_out[..., still], q[..., still])
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (2, 1), (24, 8), (32, 8), (40, 40), (33, 11), (128, 1), (200, 100)])
+@pytest.mark.parametrize("pairs,adjacent", [(64, False), (64, True), (24, False), (13, False), (13, True)])
+def test_long_calls_are_their_parts(heads, kv_heads, pairs, adjacent):
+    """Of every number of heads: blocks that have a token each, and several for a token."""
+    rng = np.random.default_rng(heads)
+    torch.manual_seed(heads)
+    p, n, t = handle("bf16", 128, heads, kv_heads), 1030, rotary(pairs, None, adjacent)
+    pos = torch.from_numpy(positions(rng, 1, n)).to(DEV)
+    q, k = (torch.randn((n, h, 128), dtype=torch.float32, device=DEV).to(torch.bfloat16) for h in (heads, kv_heads))
+    q_out, k_out, q_part, k_part = (torch.full_like(x, 7.0) for x in (q, k, q, k))
+    p.rotate(t, pos, q, k, q_out, k_out)
+    for lo in range(0, n, 103):
+        at = slice(lo, lo + 103)
+        p.rotate(t, pos[:, at].contiguous(), q[at], k[at], q_part[at], k_part[at])
+    assert torch.equal(q_out, q_part) and torch.equal(k_out, k_part)
+    few = np.r_[0:3, 700, n - 1]
+    check(q_out[few], q[few], pos.cpu().numpy()[:, few], pairs, [pairs], adjacent, False, "bf16")
+    check(k_out[few], k[few], pos.cpu().numpy()[:, few], pairs, [pairs], adjacent, False, "bf16")
+
+
 @pytest.mark.parametrize("dtype", ("fp16", "bf16"))
 @pytest.mark.parametrize("pairs,adjacent", [(64, False), (64, True), (20, False), (20, True)])
 def test_in_place_strided_and_back(dtype, pairs, adjacent):
