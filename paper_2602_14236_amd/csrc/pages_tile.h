@@ -86,7 +86,8 @@ __device__ __forceinline__ TileUnit tile_unit(const PagesAttend& a, int rows_min
     return u;
 }
 
-// The plan in shares, one block (5 to 8 us: a few trips to memory one after the other)
+// The plan in shares, one block (5 to 6 us: a few trips to memory one after the other; drafts of 64 tokens of 4 long texts, cut into 64 pieces a head: 11.3 us with a
+// thread for all pieces of a row tile)
 template <int kWaves, bool kTree = false>
 __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend a, int rows_min) {
     __shared__ int64_t s_sum[kPlanThreads / 64];
@@ -95,6 +96,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
     __shared__ int s_parts, s_merges;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     int64_t slots = tile_slots(a.seqs.n_tokens, a.group, a.seqs.n_seqs, tile_rows(kWaves));
+    // few row tiles are cut into many pieces: lanes of a wave share a slot's
+    int log2 = 0;
+    while (log2 < 6 && slots << (log2 + 1) <= kPlanThreads) ++log2;
+    const int lanes = 1 << log2, sub = lane & (lanes - 1), first_slot = (int)threadIdx.x >> log2, step = kPlanThreads >> log2;
     TileScratch& t = *reinterpret_cast<TileScratch*>(a.records);
     const StartFalls starts(a.seqs.start, a.seqs.n_seqs, threadIdx.x, kPlanThreads);
     if (threadIdx.x < kUnitBuckets) s_count[threadIdx.x] = 0;
@@ -102,10 +107,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
     int64_t sum = 0;
     int longest = 1;
     TileUnit first = {{0, 0, 0}, 0, 0, 0, 0, 0, {0, 0, 0}};
-    for (int64_t i = threadIdx.x; i < slots; i += kPlanThreads) {
+    for (int64_t i = first_slot; i < slots; i += step) {
         const TileUnit u = tile_unit<kWaves, kTree>(a, rows_min, i);
-        if (i == threadIdx.x) first = u;
-        sum += u.span.tiles;
+        if (i == first_slot) first = u;
+        sum += sub == 0 ? u.span.tiles : 0;
         longest = max(longest, u.span.tiles);
     }
 #pragma unroll
@@ -131,13 +136,19 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
     if (some_falls != 0) slots = 0;
     const int share = fair_share(sum, tile_shares(a.geom.n_kv, kWaves));
     const int most_tiles = min(share, longest);             // of the longest piece
-    auto bucket_of = [&](int tiles) { return kUnitBuckets - 1 - min(kUnitBuckets - 1, (int)((int64_t)tiles * (kUnitBuckets - 1) / most_tiles)); };
-    for (int64_t i = threadIdx.x; i < slots; i += kPlanThreads) {
-        const TileUnit u = i == threadIdx.x ? first : tile_unit<kWaves, kTree>(a, rows_min, i);
+    // (63 times the tiles of the longest sequence there can be are below 2^32)
+    auto bucket_of = [&](int tiles) { return kUnitBuckets - 1 - min(kUnitBuckets - 1, (int)((uint32_t)tiles * (uint32_t)(kUnitBuckets - 1) / (uint32_t)most_tiles)); };
+    // tiles * k / parts, k up to parts, of fewer than 2^16 parts
+    auto cut = [](int tiles, int k, int parts) {
+        const uint32_t each = (uint32_t)tiles / (uint32_t)parts, rest = (uint32_t)tiles - each * (uint32_t)parts;
+        return (int)(each * (uint32_t)k + rest * (uint32_t)k / (uint32_t)parts);
+    };
+    for (int64_t i = first_slot; i < slots; i += step) {
+        const TileUnit u = i == first_slot ? first : tile_unit<kWaves, kTree>(a, rows_min, i);
         const int tiles = u.span.tiles;
         if (tiles == 0) continue;
         const int parts = parts_of(tiles, share);
-        for (int k = 0; k < parts; ++k) atomicAdd(&s_count[bucket_of((int)((int64_t)tiles * (k + 1) / parts - (int64_t)tiles * k / parts))], 1);
+        for (int k = sub; k < parts; k += lanes) atomicAdd(&s_count[bucket_of(cut(tiles, k + 1, parts) - cut(tiles, k, parts))], 1);
     }
     __syncthreads();
     if (threadIdx.x < kUnitBuckets) {
@@ -152,18 +163,19 @@ __global__ __launch_bounds__(kPlanThreads) void k_pages_plan_shares(PagesAttend 
         if (threadIdx.x == kUnitBuckets - 1) t.plan.blocks = v;
     }
     __syncthreads();
-    for (int64_t i = threadIdx.x; i < slots; i += kPlanThreads) {
-        const TileUnit u = i == threadIdx.x ? first : tile_unit<kWaves, kTree>(a, rows_min, i);
+    for (int64_t i = first_slot; i < slots; i += step) {
+        const TileUnit u = i == first_slot ? first : tile_unit<kWaves, kTree>(a, rows_min, i);
         const int tiles = u.span.tiles;
         if (tiles == 0) continue;
         const int parts = parts_of(tiles, share);
         int part = -1;
-        if (parts > 1) {
+        if (parts > 1 && sub == 0) {
             part = atomicAdd(&s_parts, parts);
             t.merges[atomicAdd(&s_merges, 1)] = {u.seq, u.row_tile, part, parts};
         }
-        for (int k = 0; k < parts; ++k) {
-            const int lo = (int)((int64_t)tiles * k / parts), hi = (int)((int64_t)tiles * (k + 1) / parts);
+        part = __shfl(part, lane - sub);
+        for (int k = sub; k < parts; k += lanes) {
+            const int lo = cut(tiles, k, parts), hi = cut(tiles, k + 1, parts);
             t.pieces[atomicAdd(&s_next[bucket_of(hi - lo)], 1)] = {u.seq, u.row_tile, u.first, u.n, u.len, lo, hi, parts > 1 ? part + k : -1};
         }
     }
