@@ -3,8 +3,15 @@
 // Rows, scores, masks and tiles of 32 keys are those of attention (pages_attn.h); with lse at hand there is no maximum to find, no second product and
 // nothing to join: keys stay with a wave, which walks the rows that see them and adds the weights up in fp32, always in the same order.
 //
-// Few rows (single tokens, drafts): the stream, bound by K's bytes.  A wave has its rows' queries in registers and walks tiles, the next one's K on its way.
-// More: the rows' queries come through LDS, 32 at a time, and a wave has 64 keys in registers, so that a query read from LDS is multiplied twice.
+// Three kernels, by rows (new tokens times heads of a group, as far as the batch's sizes tell):
+//   up to 32   k_pages_weigh_stream  bound by K's bytes: a wave has the rows' queries in registers and walks tiles, the next one's K on its way.  16 texts of up to 8192
+//                                    keys, 8 heads of 128 in 8 bits, one token each: 88 MB in 24 us, 3.6 TB/s
+//   up to 256  k_pages_weigh_few     the same with 32x32 products, the rows in LDS.  32 tokens, 4 heads each over 20001 and 10700 keys in 4 bits, 8 heads: 21.6 us, half of it
+//                                    the chain of a launch, lengths, page table, K and the first results
+//   more       k_pages_weigh_tile    keys in registers, rows through LDS, three steps of 64 on their way past the registers; in chunks where there are fewer keys than the chip
+//                                    holds, whose sums a launch of its own joins.  8192 causal tokens, 32 heads over 8 of 128: 343 us, 800 TFLOP/s (a large library product: 1369).
+//                                    What it waits for there: products alone 181 us, weights alone 229, LDS reads 122 of both; products of one half step and weights of
+//                                    the one before are side by side, and two blocks of eight waves a compute unit.  64 keys a wave, half the reads of LDS: 351 to 364
 #pragma once
 
 #include "pages_stream.h"
@@ -155,7 +162,7 @@ __global__ __launch_bounds__(64 * kWeighStreamWaves) void k_pages_weigh_stream(P
 
 // ---- more rows
 constexpr int kWeighWaves = 8, kWeighKeys = 32 * kWeighWaves;
-constexpr int kWeighRows = 64;              // of a step: two products'
+constexpr int kWeighRows = 64;              // of a step: two halves of 32
 constexpr int kWeighBuffers = 4;            // steps' rows in LDS: one worked on, three on their way
 
 // a wave's 32 keys, two blocks, as the A operand of 32x32x16 products: lane (place col % 16 of block col / 16, hh) has values 16 step + 8 hh .. + 7
