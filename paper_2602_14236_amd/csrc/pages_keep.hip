@@ -183,13 +183,14 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
 
 // ---- moving rows
 // A block of 16 tokens falls apart into strips that move by themselves: a group of 32 values of K or of V, with its scales; and the weights.  A thread block takes one strip of a
-// sequence and K/V head, kTokens tokens at a time, as they are stored: K's pieces of 16 bytes from place to place, V's values eight tokens at a time.
+// sequence and K/V head (into other pages a strip of K with that of V), kTokens tokens at a time, as they are stored: K's pieces of 16 bytes from place to place, V's values eight tokens at a time.
 //
 // In place, a row never moves to a higher position, so rows that are still to be read lie behind all that have been written if the chunks are taken in their
 // order, each read whole before it is written: one thread block walks a strip.  Into other pages chunks are blocks of their own.
 //
 // Bound by the lines that rows lie in: those that stay are spread, so that nearly all of the source is touched.  4096 of up to 24001 tokens, three texts, 8 heads of 128 in 16
-// bits: 171 MB read and 51 written in 57 us, 3.9 TB/s, 75 % of the waves' time waiting.  In place, 32 drafts of 16 tokens: 8.7 us, a launch and its chain of list, tables, rows.
+// bits: 171 MB read and 51 written in 43 us, 5.2 TB/s (57 where a block takes a strip of K or of V alone: half as much for the same chain of lengths, list, tables
+// and rows).  In place, 32 drafts of 16 tokens: 8.7 us, a launch and its chain of list, tables, rows.
 constexpr int kKeepThreads = 256;
 
 template <int kStore, int kDim>
@@ -211,7 +212,9 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
     __shared__ uint64_t s_from[kTokens];                    // where the token's block lies, bits 0 to 3 its place there; kNone: nothing moves, kZeros: of no page
     __shared__ uint64_t s_to[kTokens / 16];
     const int tid = threadIdx.x;
-    const uint32_t n_strips = 2 * S::kGroups + (a.weights != nullptr ? 1 : 0), in_heads = blockIdx.x / (uint32_t)a.geom.n_kv, in_strips = in_heads / n_strips;
+    constexpr bool kBoth = !kInPlace;                       // a strip is a group of K and that of V
+    constexpr int kStrips = kBoth ? S::kGroups : 2 * S::kGroups;
+    const uint32_t n_strips = kStrips + (a.weights != nullptr ? 1 : 0), in_heads = blockIdx.x / (uint32_t)a.geom.n_kv, in_strips = in_heads / n_strips;
     const int head = (int)(blockIdx.x - in_heads * (uint32_t)a.geom.n_kv), strip = (int)(in_heads - in_strips * n_strips);
     const int s = (int)(in_strips / (uint32_t)chunks), nth = (int)(in_strips - (uint32_t)s * (uint32_t)chunks);
     const bool notes = strip == 0;
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
     const int32_t* const table = a.seqs.table + (int64_t)s * a.seqs.width;
     const int32_t* const to_table = a.to + (int64_t)s * a.to_width;
     const uint32_t block_bytes = a.geom.head_bytes >> a.geom.blocks_log2;
-    const bool weights = strip == 2 * S::kGroups, values = strip >= S::kGroups;     // the strip's: the weights, V
+    const bool weights = strip == kStrips, keys = kBoth || strip < S::kGroups, values = kBoth || strip >= S::kGroups;    // what moves: the weights, else K, V
     const int group = strip % S::kGroups;
     // byte of a token's block of the strip's head, or the number of its first weight
     auto block_at = [&](int page, int pos) -> uint64_t {
@@ -270,9 +273,10 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
         }
         // ---- read
         const char* const pool = a.geom.pool;
-        u32x4 x[kKOwn > kVOwn ? kKOwn : kVOwn];
-        uint32_t scale[kTokens / kKeepThreads + 1];
-        uint16_t low[kTokens / kKeepThreads + 1];
+        constexpr int kX = kBoth ? kKOwn + kVOwn : (kKOwn > kVOwn ? kKOwn : kVOwn), kFirstV = kBoth ? kKOwn : 0, kSides = kBoth ? 2 : 1, kOwn = kTokens / kKeepThreads + 1;
+        u32x4 x[kX];
+        uint32_t scale[kSides * kOwn];
+        uint16_t low[kSides * kOwn];
         auto from_of = [&](int t, int& place) -> uint64_t {
             const uint64_t f = s_from[t];
             place = (int)(f & 15u);
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
                 scale[i] = f < kZeros ? reinterpret_cast<const uint32_t*>(a.weights)[f] : 0u;
             }
         } else {
-            if (!values) {
+            if (keys) {
 #pragma unroll
                 for (int i = 0; i < kKOwn; ++i) {
                     const int p = tid + kKeepThreads * i;
@@ -294,11 +298,13 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
                     const uint64_t f = from_of(p % kTokens, place);
                     if (f < kZeros) x[i] = *reinterpret_cast<const u32x4*>(pool + f + ((group * S::kPieces + p / kTokens) * 16 + place_of_token(place)) * 16);
                 }
-            } else {
+            }
+            if (values) {
 #pragma unroll
                 for (int i = 0; i < kVOwn; ++i) {
                     const int p = tid + kKeepThreads * i, e = p % S::kElems, octet = p / S::kElems;
-                    x[i] = (u32x4){0u, 0u, 0u, 0u};
+                    u32x4& v = x[kFirstV + i];
+                    v = (u32x4){0u, 0u, 0u, 0u};
                     if (p >= kVItems) continue;
 #pragma unroll
                     for (int t = 0; t < 8; ++t) {
@@ -306,22 +312,25 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
                         const uint64_t f = from_of(8 * octet + t, place);
                         if (f >= kZeros) continue;
                         const char* const at = pool + f + kAt.v + (((place >> 3) * (S::kGroups * S::kElems) + group * S::kElems + e) * 8 + (place & 7)) * S::kElem;
-                        if constexpr (S::kElem == 2) x[i][t / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(at) << (16 * (t & 1));
-                        else x[i][t / 4] |= (uint32_t)*reinterpret_cast<const uint8_t*>(at) << (8 * (t & 3));
+                        if constexpr (S::kElem == 2) v[t / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(at) << (16 * (t & 1));
+                        else v[t / 4] |= (uint32_t)*reinterpret_cast<const uint8_t*>(at) << (8 * (t & 3));
                     }
                 }
             }
             if constexpr (kStore != SALI_STORE_16)
-                for (int t = tid, i = 0; t < kTokens; t += kKeepThreads, ++i) {
-                    int place;
-                    const uint64_t f = from_of(t, place);
-                    scale[i] = 0u;
-                    low[i] = 0;
-                    if (f >= kZeros) continue;
-                    const uint32_t at = (uint32_t)(group * 16 + (values ? place : place_of_token(place)));
-                    scale[i] = *reinterpret_cast<const uint32_t*>(pool + f + (values ? kAt.vs : kAt.ks) + at * 4);
-                    if constexpr (kStore == SALI_STORE_INT4) low[i] = *reinterpret_cast<const uint16_t*>(pool + f + (values ? kAt.vz : kAt.kz) + at * 2);
-                }
+#pragma unroll
+                for (int side = 0; side < kSides; ++side)
+                    for (int t = tid, i = side * kOwn; t < kTokens; t += kKeepThreads, ++i) {
+                        int place;
+                        const uint64_t f = from_of(t, place);
+                        const bool v = kBoth ? side == 1 : values;
+                        scale[i] = 0u;
+                        low[i] = 0;
+                        if (f >= kZeros) continue;
+                        const uint32_t at = (uint32_t)(group * 16 + (v ? place : place_of_token(place)));
+                        scale[i] = *reinterpret_cast<const uint32_t*>(pool + f + (v ? kAt.vs : kAt.ks) + at * 4);
+                        if constexpr (kStore == SALI_STORE_INT4) low[i] = *reinterpret_cast<const uint16_t*>(pool + f + (v ? kAt.vz : kAt.kz) + at * 2);
+                    }
         }
         if constexpr (kInPlace) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                          // all of the chunk is here before any of it is written
@@ -333,17 +342,19 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
             for (int t = tid, i = 0; t < kTokens; t += kKeepThreads, ++i)
                 if (s_from[t] != kNone) reinterpret_cast<uint32_t*>(a.weights)[s_to[t / 16] + (uint64_t)(t & 15)] = scale[i];
         } else {
-            if (!values) {
+            if (keys) {
 #pragma unroll
                 for (int i = 0; i < kKOwn; ++i) {
                     const int p = tid + kKeepThreads * i, t = p % kTokens;
                     if (p >= kKItems || s_from[t] == kNone) continue;
                     *reinterpret_cast<u32x4*>(pool_to + s_to[t / 16] + ((group * S::kPieces + p / kTokens) * 16 + place_of_token(t & 15)) * 16) = x[i];
                 }
-            } else {
+            }
+            if (values) {
 #pragma unroll
                 for (int i = 0; i < kVOwn; ++i) {
                     const int p = tid + kKeepThreads * i, e = p % S::kElems, octet = p / S::kElems;
+                    const u32x4 v = x[kFirstV + i];
                     if (p >= kVItems) continue;
                     uint32_t moves = 0;
 #pragma unroll
@@ -351,26 +362,29 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
                     if (moves == 0u) continue;
                     char* const at = pool_to + s_to[octet / 2] + kAt.v + ((octet & 1) * (S::kGroups * S::kElems) + group * S::kElems + e) * (8 * S::kElem);
                     if (moves == 0xFFu) {
-                        if constexpr (S::kElem == 2) *reinterpret_cast<u32x4*>(at) = x[i];
-                        else *reinterpret_cast<u32x2*>(at) = (u32x2){x[i].x, x[i].y};
+                        if constexpr (S::kElem == 2) *reinterpret_cast<u32x4*>(at) = v;
+                        else *reinterpret_cast<u32x2*>(at) = (u32x2){v.x, v.y};
                         continue;
                     }
 #pragma unroll
                     for (int t = 0; t < 8; ++t) {
                         if ((moves >> t & 1u) == 0u) continue;
-                        if constexpr (S::kElem == 2) reinterpret_cast<uint16_t*>(at)[t] = (uint16_t)(x[i][t / 2] >> (16 * (t & 1)));
-                        else reinterpret_cast<uint8_t*>(at)[t] = (uint8_t)(x[i][t / 4] >> (8 * (t & 3)));
+                        if constexpr (S::kElem == 2) reinterpret_cast<uint16_t*>(at)[t] = (uint16_t)(v[t / 2] >> (16 * (t & 1)));
+                        else reinterpret_cast<uint8_t*>(at)[t] = (uint8_t)(v[t / 4] >> (8 * (t & 3)));
                     }
                 }
             }
             if constexpr (kStore != SALI_STORE_16)
-                for (int t = tid, i = 0; t < kTokens; t += kKeepThreads, ++i) {
-                    if (s_from[t] == kNone) continue;
-                    char* const block = pool_to + s_to[t / 16];
-                    const uint32_t at = (uint32_t)(group * 16 + (values ? t & 15 : place_of_token(t & 15)));
-                    *reinterpret_cast<uint32_t*>(block + (values ? kAt.vs : kAt.ks) + at * 4) = scale[i];
-                    if constexpr (kStore == SALI_STORE_INT4) *reinterpret_cast<uint16_t*>(block + (values ? kAt.vz : kAt.kz) + at * 2) = low[i];
-                }
+#pragma unroll
+                for (int side = 0; side < kSides; ++side)
+                    for (int t = tid, i = side * kOwn; t < kTokens; t += kKeepThreads, ++i) {
+                        if (s_from[t] == kNone) continue;
+                        char* const block = pool_to + s_to[t / 16];
+                        const bool v = kBoth ? side == 1 : values;
+                        const uint32_t at = (uint32_t)(group * 16 + (v ? t & 15 : place_of_token(t & 15)));
+                        *reinterpret_cast<uint32_t*>(block + (v ? kAt.vs : kAt.ks) + at * 4) = scale[i];
+                        if constexpr (kStore == SALI_STORE_INT4) *reinterpret_cast<uint16_t*>(block + (v ? kAt.vz : kAt.kz) + at * 2) = low[i];
+                    }
         }
         if constexpr (!kInPlace) return;
         __syncthreads();                                    // s_from and s_to have been read
@@ -386,7 +400,8 @@ hipError_t launch_pages_select(const PagesSelect& a, hipStream_t s) {
 
 hipError_t launch_pages_keep(int store, int dim, const PagesKeep& a, hipStream_t s) {
     const int chunks = (int)keep_chunks(a.seqs, a.width, a.in_place != 0);
-    const dim3 grid((unsigned)(a.seqs.n_seqs * (int64_t)chunks * a.geom.n_kv * keep_strips(dim, a.weights != nullptr)));
+    const int strips = a.in_place ? keep_strips(dim, a.weights != nullptr) : dim / 32 + (a.weights != nullptr ? 1 : 0);
+    const dim3 grid((unsigned)(a.seqs.n_seqs * (int64_t)chunks * a.geom.n_kv * strips));
     auto go = [&](auto st, auto d) {
         auto launch = [&](auto in_place, auto tokens) {
             hipLaunchKernelGGL((k_pages_keep<decltype(st)::value, decltype(d)::value, decltype(in_place)::value, decltype(tokens)::value>), grid, dim3(kKeepThreads), 0, s, a, chunks);
