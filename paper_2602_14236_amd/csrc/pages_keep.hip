@@ -189,8 +189,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
 // order, each read whole before it is written: one thread block walks a strip.  Into other pages chunks are blocks of their own.
 //
 // Bound by the lines that rows lie in: those that stay are spread, so that nearly all of the source is touched.  4096 of up to 24001 tokens, three texts, 8 heads of 128 in 16
-// bits: 171 MB read and 51 written in 43 us, 5.2 TB/s (57 where a block takes a strip of K or of V alone: half as much for the same chain of lengths, list, tables
-// and rows).  In place, 32 drafts of 16 tokens: 8.7 us, a launch and its chain of list, tables, rows.
+// bits: 171 MB read and 51 written in 41 us, 5.4 TB/s (57 where a block takes a strip of K or of V alone: half as much for the same chain of lengths, list, tables
+// and rows; 43 with V's values asked for behind branches; chunks of 128 or blocks of 128 threads 40).  In place, 32 drafts of 16 tokens: 9 us, a launch and its chain of list, tables, rows.
 constexpr int kKeepThreads = 256;
 
 template <int kStore, int kDim>
@@ -306,15 +306,22 @@ __global__ __launch_bounds__(kKeepThreads) void k_pages_keep(PagesKeep a, int ch
                     u32x4& v = x[kFirstV + i];
                     v = (u32x4){0u, 0u, 0u, 0u};
                     if (p >= kVItems) continue;
+                    // (Into other pages all are asked for, of nothing the pool's first, so that they are on their way together; of a draft most stay where they are.)
+                    uint32_t of[8];
+                    bool is[8];
 #pragma unroll
                     for (int t = 0; t < 8; ++t) {
                         int place;
                         const uint64_t f = from_of(8 * octet + t, place);
-                        if (f >= kZeros) continue;
-                        const char* const at = pool + f + kAt.v + (((place >> 3) * (S::kGroups * S::kElems) + group * S::kElems + e) * 8 + (place & 7)) * S::kElem;
-                        if constexpr (S::kElem == 2) v[t / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(at) << (16 * (t & 1));
-                        else v[t / 4] |= (uint32_t)*reinterpret_cast<const uint8_t*>(at) << (8 * (t & 3));
+                        is[t] = f < kZeros;
+                        const char* const at = pool + (is[t] ? f : 0) + kAt.v + (((place >> 3) * (S::kGroups * S::kElems) + group * S::kElems + e) * 8 + (place & 7)) * S::kElem;
+                        of[t] = 0u;
+                        if (kInPlace && !is[t]) continue;
+                        if constexpr (S::kElem == 2) of[t] = *reinterpret_cast<const uint16_t*>(at);
+                        else of[t] = *reinterpret_cast<const uint8_t*>(at);
                     }
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) v[S::kElem == 2 ? t / 2 : t / 4] |= (is[t] ? of[t] : 0u) << (8 * S::kElem * (t % (4 / S::kElem)));
                 }
             }
             if constexpr (kStore != SALI_STORE_16)
