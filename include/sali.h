@@ -553,7 +553,7 @@ int sali_pages_rotate(sali_pages* p, const sali_rotary* rotary, const int32_t* d
 /* Attention of drafted tokens, several guesses of what follows at once: the batch's new tokens are a draft of up to 64 tokens a sequence, which the pages hold
  * already (sali_pages_append).  A drafted token sees all tokens before the draft, and of the draft those that its mask names:
  *   d_seen        uint64[n_tokens], bit i of a row: the draft's i-th token (itself too only if its bit is set); bits of more tokens than the draft has mean nothing
- * and nothing else; what else there is, is as in sali_pages_attend.  SALI_ERR_SHAPE for a max_q above 64 too.  What was accepted of the draft is moved together by
+ * and nothing else; what else there is, is as in sali_pages_attend (of the weights the second number is always kept).  SALI_ERR_SHAPE for a max_q above 64 too.  What was accepted of the draft is moved together by
  * sali_pages_keep.  Asynchronous on `stream`; uses the area of partial results as sali_pages_attend does. */
 int sali_pages_attend_tree(sali_pages* p, int32_t layer, const sali_page_batch* batch, const uint64_t* d_seen, const sali_rows* q,
                            float softmax_scale, const float* d_prior_or_null, const float* d_prior_lse_or_null, const sali_rows* out,

@@ -592,6 +592,35 @@ __global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
             for (int x = 0; x < 4; ++x) tops[x] = (st[4 * x] + st[4 * x + 1]) + (st[4 * x + 2] + st[4 * x + 3]);
             l += (tops[0] + tops[1]) + (tops[2] + tops[3]);
+            if constexpr (kTree) {
+                // The weights in two 16-bit numbers each, what the first one's rounding leaves in the second, as the stream has them: only the output is rounded, whatever
+                // other drafts a batch has.  With one number a draft's results are off by 2.3e-3 in bfloat16 (norms, 24 drafts of 16 tokens over up to 6000 keys) where
+                // rounding them takes 1.7e-3; two cost 9 us of 87 there, the matrix cores' part of a tile's chain.  A block of 16 keys at a time: both at once spill.
+                u32x4 values[2] = {load16(v), load16(v + 512)};
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    u32x4 p, rest;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const float w0 = st[8 * b + 2 * x], w1 = st[8 * b + 2 * x + 1];
+                        p[x] = pack2<kBf16>(w0, w1);
+                        asm("" : "+v"(p[x]));           // taken apart as it is: else the compiler rounds each half once more
+                        rest[x] = pack2<kBf16>(w0 - low_half<kBf16>(p[x]), w1 - high_half<kBf16>(p[x]));
+                    }
+#pragma unroll
+                    for (int d = 0; d < kDt; d += 2) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) acc[d + i] = Num<kBf16>::mma32(values[i], p, acc[d + i]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) acc[d + i] = Num<kBf16>::mma32(values[i], rest, acc[d + i]);
+                        const int next = b * kDt + d + 2;
+                        if (next < 2 * kDt)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) values[i] = load16(v + (next + i) / kDt * kBlock + (next + i) % kDt * 512);
+                    }
+                }
+                return;
+            }
             // the weights once rounded to 16 bits, half a step each, against the sum's fp32: a second number each, as the stream has it, is half as many
             // products again where the matrix cores are what a prompt waits for, and registers that three waves a SIMD do not leave (they spill)
             u32x4 p[2];

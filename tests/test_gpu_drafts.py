@@ -255,3 +255,25 @@ def test_replayed():
             graph.replay()
             torch.cuda.synchronize()
             verify(c, lens, masks, q, out, lse, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("store,dtype,dim", FORMATS)
+@pytest.mark.parametrize("n,total,group", [(5, 5, 4), (40, 40, 4), (64, 64, 2), (30, 41, 8), (40, 500, 4)])
+def test_only_the_output_is_rounded(store, dtype, dim, n, total, group):
+    """Weights are two 16-bit numbers each, whichever kernel a draft takes: in op.bounds the weights' own term is then half a step of half a step (what the first number
+    leaves is at most half a step of the weight, and the second one rounds that; fp16's smallest step counts as there).  Rows that see three drafted tokens, whose values
+    cancel: a weight rounded once would be off by some hundred times the rest of the bound."""
+    c = Cache(op.PagesSpec(2, 2 * group, dim, 16, dtype, store), [total], 31)
+    spec, scale = c.spec, dim ** -0.5
+    masks = [signed(sum(1 << int(i) for i in c.rng.choice(n, 3, replace=False))) for _ in range(n)]
+    q, out, lse = attend(c, [(n, total)], masks)
+    k, v = c.stored(c.k[0][:total]), c.stored(c.v[0][:total])
+    qs = op.to_f32(bits_of(q), dtype).astype(np.float64)
+    e_out, e_lse, mass, reach = op.attend(qs, k, v, total, scale, seen=op.drafted(masks, total))
+    u = spec.half_step
+    step = reach * (dim * 2.0 ** -24 + 4 * 2.0 ** -23) + 2.0 ** -21 + (total + 64) * 2.0 ** -24
+    far = 1.01 * ((2 * step[..., None] + u * u) * mass + u * np.abs(e_out)) + 2.0 ** -24
+    if dtype == "fp16":
+        far = far + total * 2.0 ** -35 * np.abs(v).max()
+    bad = np.abs(op.to_f32(bits_of(out), dtype) - e_out) > far
+    assert not bad.any(), f"{bad.sum()} of {bad.size} off, first {np.argwhere(bad)[0]}"
