@@ -28,6 +28,12 @@ SALI_BOTH T least(T a, T b) { return a < b ? a : b; }
 template <typename T>
 SALI_BOTH T most(T a, T b) { return a < b ? b : a; }
 
+// first, first + step, .. below count, all of them up to 2^31 - 1: counted without a sign, since the last step may end behind that
+template <typename F>
+SALI_BOTH void each_from(int first, int count, int step, F f) {
+    for (uint32_t i = (uint32_t)first; i < (uint32_t)count; i += (uint32_t)step) f(i);
+}
+
 // One sequence of a batch: rows first .. first + n - 1 are its tokens len - n .. len - 1.  n = 0 where its numbers contradict each other, the
 // rows or its table.
 struct PageSeq {

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
     int32_t* const out = a.keep + ((int64_t)s * a.geom.n_kv + head) * a.budget;
     const int n = seq.n, base = seq.len - seq.n;
     if (n <= a.budget) {
-        for (int i = tid; i < a.budget; i += kSelectThreads) out[i] = i < n ? i : -1;
+        each_from(tid, a.budget, kSelectThreads, [&](uint32_t i) { out[i] = i < (uint32_t)n ? (int)i : -1; });
         return;
     }
     const int shift = a.geom.blocks_log2 + 4, page_tokens = 1 << shift;
@@ -106,14 +106,15 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
                 __syncthreads();
                 // several keys on their way together: the loop is a chain of trips to LDS
                 constexpr int kKeys = 4;
-                for (int j0 = tid; j0 < m; j0 += kKeys * kSelectThreads) {
+                each_from(tid, m, kKeys * kSelectThreads, [&](uint32_t j0) {
                     uint32_t k[kKeys];
 #pragma unroll
-                    for (int i = 0; i < kKeys; ++i) k[i] = key(min(j0 + kSelectThreads * i, m - 1));
+                    for (int i = 0; i < kKeys; ++i) k[i] = key((int)min(j0 + (uint32_t)(kSelectThreads * i), (uint32_t)m - 1u));
 #pragma unroll
                     for (int i = 0; i < kKeys; ++i)
-                        if (j0 + kSelectThreads * i < m && (d == 0 || k[i] >> high == prefix)) atomicAdd(&s_bins[k[i] >> low & (kBins - 1) & ((1u << (high - low)) - 1u)], 1u);
-                }
+                        if (j0 + (uint32_t)(kSelectThreads * i) < (uint32_t)m && (d == 0 || k[i] >> high == prefix))
+                            atomicAdd(&s_bins[k[i] >> low & (kBins - 1) & ((1u << (high - low)) - 1u)], 1u);
+                });
                 __syncthreads();
                 // tokens from the highest bin down: thread t has bins kBins - 1 - 2 t and the one below
                 const uint32_t upper = s_bins[kBins - 1 - 2 * tid], lower = s_bins[kBins - 2 - 2 * tid];

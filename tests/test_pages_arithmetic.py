@@ -225,3 +225,26 @@ int main() {
     return 0;
 }
 """ % seed)
+
+
+def test_counts_up_to_31_bits(tmp_path):
+    """Threads that share out up to 2^31 - 1 tokens or list entries take each of theirs once and end, where a signed counter would step past the largest number and begin
+    again below zero."""
+    run_pages_program(tmp_path, """
+int main() {
+    for (int count : {0, 1, 1023, 1024, 1025, 2147483647, 2147483646, 2147483647 - 1023, 2147483647 - 1024, 2147483647 - 1025, 2147483647 - 4096})
+        for (int step : {1024, 4096})
+            for (int first : {0, 1, 500, 1022, 1023}) {
+                const int64_t all = first < count ? ((int64_t)count - first + step - 1) / step : 0;
+                int64_t seen = 0, next = first;
+                bool right = true;
+                each_from(first, count, step, [&](uint32_t i) {
+                    right &= (int64_t)i == next && next < count;
+                    next += step;
+                    if (++seen > all) { printf("%d from %d by %d does not end\\n", count, first, step); exit(1); }
+                });
+                if (!right || seen != all) { printf("%d from %d by %d: %ld of %ld\\n", count, first, step, (long)seen, (long)all); return 2; }
+            }
+    return 0;
+}
+""")
