@@ -686,7 +686,8 @@ class SaliPages:
         if to is not None:
             if to.dtype is not torch.int32 or to.dim() != 2 or to.shape[0] != n or not to.is_contiguous() or to.get_device() != self.index:
                 raise self._wrong("to", to, torch.int32, [n, "width"])
-            to_at, to_width = to.data_ptr(), to.shape[1]
+            # (a table of no width has no address, and without one rows would move in their own pages)
+            to_at, to_width = to.data_ptr() or batch.c.d_start, to.shape[1]
         _check(self.lib.sali_pages_keep(self.handle, layer, batch.c, keep.data_ptr(), shape[1], shape[2], to_at, to_width,
                                         self._dense(weights, self._weights_shape, "weights"), self._call(batch, stream)), "sali_pages_keep")
 

@@ -386,6 +386,19 @@ def test_entries_that_move_nothing(store):
     assert c.pages.get_status() == binding.FAULT_BATCH
 
 
+@pytest.mark.parametrize("width", [0, 1])
+def test_tables_too_narrow_for_all_of_a_list(width):
+    """Nothing moves, in the batch's pages either."""
+    from paper_2602_14236_amd import binding
+    batch = [(30, 60), (20, 50)]
+    c = Cache(op.PagesSpec(2, 2, 64, 16, "fp16", "16"), [60, 50], 26, extra_pages=20)
+    w = weights_of(c)
+    keep = lists(c.rng, batch, 2, 20, 0.5)
+    before = c.pages.pool.clone()
+    c.pages.keep(0, c.batch(batch), torch.from_numpy(keep).to(DEV), to=torch.zeros((2, width), dtype=torch.int32, device=DEV), weights=w)
+    assert torch.equal(before, c.pages.pool) and (w == 3).all() and c.pages.get_status() == binding.FAULT_BATCH
+
+
 def test_any_order_elsewhere():
     """Elsewhere a list may be in any order, a row twice."""
     batch = [(100, 100), (40, 50)]

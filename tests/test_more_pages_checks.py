@@ -92,6 +92,20 @@ def test_a_single_position_is_no_array(pages_elsewhere):
     assert state.calls == []
 
 
+def test_a_table_of_no_width_is_still_a_table(pages_elsewhere):
+    """It has no address of its own; without one rows would move in the pages that they lie in."""
+    from paper_2602_14236_amd.binding import PageBatch
+    pages, state = pages_elsewhere
+    pages._weights_shape = (5, 2, 16)
+    pages.lib.sali_pages_keep = lambda *a: state.calls.append(a) or 0
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    batch = PageBatch(i(2), i(1), i(1, 5), 3, max_kv=80)
+    pages.keep(0, batch, i(1, 2, 7), to=i(1, 0))
+    pages.keep(0, batch, i(1, 2, 7))
+    (table, width), (none, _) = ((a[6], a[7]) for a in state.calls)
+    assert table and width == 0 and not none
+
+
 def test_masks_of_drafts_by_key(tmp_path):
     """What 32 keys of a tile show of a mask, for every place that the tile can have before, at and behind the draft's beginning."""
     run_pages_program(tmp_path, """
