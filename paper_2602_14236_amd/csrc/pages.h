@@ -91,8 +91,8 @@ struct PagesKeep {
     int32_t width, keep_heads, to_width, in_place;
 };
 
-// scratch of the pages object: the status word, then the partial results of attention
-constexpr size_t kPagesStatusBytes = 256;
+// scratch of the pages object: the status word, a row of zeros, then the partial results of attention
+constexpr size_t kPagesZeros = 256, kPagesStatusBytes = kPagesZeros + 256;
 struct PagesScratch {
     size_t partial, records, bytes;         // where the two areas start
 };

@@ -280,7 +280,8 @@ int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch,
     a.geom = geom_of(p, layer);
     a.seqs = seqs_of(p, *batch);
     if (weigh_blocks(a.seqs) * p->cfg.n_kv_heads > kMostBlocks / 2 / batch->n_seqs) return SALI_ERR_SHAPE;        // half as many of 512 threads
-    a.q = rows_of<RowsIn>(*q);
+    // (a scale of zero makes queries zero, as in attention: 0 times a product that is no fp32 number would be a NaN)
+    a.q = softmax_scale == 0.0f ? RowsIn{reinterpret_cast<const char*>(p->scratch + kPagesZeros), 0, 0} : rows_of<RowsIn>(*q);
     a.lse = d_lse;
     a.weights = d_weights;
     a.scale2 = softmax_scale * 1.44269504088896340736f;

@@ -134,6 +134,24 @@ def test_weights_by_scale(scale):
     weigh(c, [(6, 150), (30, 30)], scale=scale, room=3, lse=torch.full((39, 4), 20.0, device=DEV))
 
 
+@pytest.mark.parametrize("n", [1, 6, 20, 150])
+def test_a_scale_of_zero_whatever_the_products(n):
+    """All keys that a row sees have exp(-lse) of it, as the attention whose log-sum that is has it, though products of the queries and keys pass fp32."""
+    c = Cache(op.PagesSpec(1, 4, 128, 16, "bf16", "16"), [200], 27, history=False)
+    c.k[0][:] = c.k[0] * 2.0 ** 70
+    c.write([(200, 200)])
+    q = rows(c.rng, n, 4, 128, "bf16").to(DEV) * 2.0 ** 70
+    q[n // 2, 1, 5] = float("nan")
+    out, lse, w = torch.empty_like(q), torch.empty((n, 4), device=DEV), weights_of(c)
+    c.pages.attend(0, c.batch([(n, 200)]), q, 0.0, out, lse)
+    seen = np.arange(201 - n, 201)
+    assert np.abs(lse.cpu().numpy() - np.log(seen)[:, None]).max() < 2.0 ** -18       # sums of ones and a logarithm below 8 in fp32
+    c.pages.weigh(0, c.batch([(n, 200)]), q, 0.0, lse, w, add=False)
+    e = np.array([4 * (1.0 / seen[seen > j]).sum() for j in range(200)])
+    # lse and its product with log2 e a rounding each of numbers below 8, exp2, and sums of up to 4 n numbers
+    assert np.abs(of_seq(c, w, 0, 200)[:, 0] / e - 1).max() < 2.0 ** -17 + (4 * n + 64) * 2.0 ** -24
+
+
 def test_weights_of_pages_that_are_none():
     from paper_2602_14236_amd import binding
     c = Cache(op.PagesSpec(1, 2, 64, 16, "bf16", "int4"), [200], 7)
