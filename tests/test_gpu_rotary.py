@@ -83,6 +83,35 @@ def test_long_calls_are_their_parts(heads, kv_heads, pairs, adjacent):
 
 
 @pytest.mark.parametrize("dtype", ("fp16", "bf16"))
+@pytest.mark.parametrize("pairs,adjacent", [(64, False), (24, False), (64, True), (12, False), (12, True)])
+def test_rows_past_the_caches(dtype, pairs, adjacent):
+    """Calls of 128 MB of rows and more, and one just below, in every layout, in place and not: the same bits as in short calls."""
+    rng, heads, kv_heads = np.random.default_rng(7), 200, 100
+    torch.manual_seed(7)
+    p, t = handle(dtype, 128, heads, kv_heads), rotary(pairs, None, adjacent)
+    limit = (128 << 20) // (2 * 128 * (heads + kv_heads))
+    for n in (limit, limit + 1, 2100):
+        pos = torch.from_numpy(positions(rng, 1, n)).to(DEV)
+        qkv = torch.randn((n, heads + 2 * kv_heads, 128), dtype=torch.float32, device=DEV).to(TORCH[dtype])
+        q, k, v = qkv[:, :heads], qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:]
+        q_out, k_out, q_part, k_part = (torch.full_like(x, 7.0, memory_format=torch.contiguous_format) for x in (q, k, q, k))
+        p.rotate(t, pos, q, k, q_out, k_out)
+        for lo in range(0, n, 300):
+            at = slice(lo, lo + 300)
+            p.rotate(t, pos[:, at].contiguous(), q[at], k[at], q_part[at], k_part[at])
+        assert torch.equal(q_out, q_part) and torch.equal(k_out, k_part)
+        few = np.r_[0:2, n - 1]
+        check(q_out[few], q[few], pos.cpu().numpy()[:, few], pairs, [pairs], adjacent, False, dtype)
+        check(k_out[few], k[few], pos.cpu().numpy()[:, few], pairs, [pairs], adjacent, False, dtype)
+        still = v.clone()
+        p.rotate(t, pos, q, k)
+        assert torch.equal(q, q_out) and torch.equal(k, k_out) and torch.equal(v, still)
+        p.rotate(t, pos, q, k, inverse=True)
+        p.rotate(t, pos, q_out, k_out, q_part, k_part, inverse=True)
+        assert torch.equal(q, q_part) and torch.equal(k, k_part)
+
+
+@pytest.mark.parametrize("dtype", ("fp16", "bf16"))
 @pytest.mark.parametrize("pairs,adjacent", [(64, False), (64, True), (20, False), (20, True)])
 def test_in_place_strided_and_back(dtype, pairs, adjacent):
     """Queries and keys as slices of one product's output, in place; inverse is the oracle's too; the rest of the array keeps its bits."""
