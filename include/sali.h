@@ -566,7 +566,7 @@ int sali_pages_attend_tree(sali_pages* p, int32_t layer, const sali_page_batch* 
  *   d_weights     fp32[n_pages][n_kv_heads][page_tokens], of this layer: the caller keeps one for every layer
  *   add           0: the weights of all of the sequence's positions are set to w; else w is added to the weights of positions before the new tokens, and those of the
  *                 new tokens are set (their pages may have been others' before)
- * Weights of other positions, and of pages that are none, are not touched.  No two sequences of a batch may share a page.  Asynchronous on `stream`; uses the area
+ * Weights of other positions, of pages that are none, and of sequences without new tokens (whatever `add` is) are not touched.  No two sequences of a batch may share a page.  Asynchronous on `stream`; uses the area
  * of partial results as sali_pages_attend does.  Errors as sali_pages_attend's; n_seqs * n_kv_heads * (max_kv / 128 rounded up) is below 2^23 (SALI_ERR_SHAPE). */
 int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch, const sali_rows* q, float softmax_scale, int32_t window,
                      int32_t sinks, const float* d_lse, int32_t add, float* d_weights, void* stream);
@@ -575,7 +575,8 @@ int sali_pages_weigh(sali_pages* p, int32_t layer, const sali_page_batch* batch,
  * them, and of the others those of most weight, the first ones of equal weight, `budget` in all; all n if there are no more.  A NaN counts as more than
  * all numbers; tokens of a page that is none as less.
  *   d_weights     as above
- *   d_keep        int32[n_seqs][n_kv_heads][budget]: their places among the n, rising; -1 behind the last
+ *   d_keep        int32[n_seqs][n_kv_heads][budget]: their places among the n, rising; -1 behind the last (of a sequence without new tokens from the first on).  Lists of
+ *                 sequences that are left out, and all lists of a call that has nothing to do (see above), are not written
  * Asynchronous on `stream`.  SALI_ERR_SHAPE for a budget below 1 or below sinks + recent, and for 2^22 sequences times K/V heads. */
 int sali_pages_select(sali_pages* p, const sali_page_batch* batch, const float* d_weights, int32_t budget, int32_t sinks, int32_t recent,
                       int32_t* d_keep, void* stream);

@@ -239,7 +239,8 @@ def rotate(x, position, frequency, sections, adjacent=False, inverse=False):
 def weigh(q, k, length, scale, lse, window=0, sinks=0, hidden=None):
     """w [length, n_kv]: exp(s - lse) summed over the rows that see a position and the heads of a group, and how far a right result may be from it: the D products of
     a score in fp32, D 2^-24 of the sum of their sizes, the scale's two roundings and the products' 2^-22 of it; lse times log2 e 2^-23 of it, their difference 2^-23 of it; exp2
-    2^-22; the sum over the rows and lanes, a rounding each.  Weights below fp32's normal numbers may be zero."""
+    2^-22; the sum over the rows and lanes, a rounding each.  Weights below fp32's normal numbers may be zero.  (Of a sequence without new tokens, n = 0, nothing is
+    asked, so its weights stay what they are, set or added.)"""
     n, hq, d = q.shape
     group = hq // k.shape[1]
     seen = visible(n, length, window, sinks)

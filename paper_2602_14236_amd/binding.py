@@ -637,8 +637,9 @@ class SaliPages:
     def attend_tree(self, layer: int, batch: PageBatch, seen: torch.Tensor, q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
                     lse: Optional[torch.Tensor] = None, *, prior: Optional[torch.Tensor] = None, prior_lse: Optional[torch.Tensor] = None,
                     stream: Optional[torch.cuda.Stream] = None):
-        """Attention of drafted tokens, the batch's new ones (64 a sequence at most): each sees what came before the draft, and of the draft the tokens whose bits are
-        set in its mask (`seen`, int64 [tokens]; draft_masks makes them from a tree).  The others as in attend."""
+        """Attention of drafted tokens, the batch's new ones (64 a sequence at most; the batch's max_q, which is all its tokens if not given, says so, and a larger one is
+        refused): each sees what came before the draft, and of the draft the tokens whose bits are set in its mask (`seen`, int64 [tokens]; draft_masks makes them from a
+        tree).  The others as in attend."""
         if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.attend_tree(layer, batch, seen, q, softmax_scale, out, lse, prior=prior, prior_lse=prior_lse, stream=stream)
@@ -652,7 +653,8 @@ class SaliPages:
     def weigh(self, layer: int, batch: PageBatch, q: torch.Tensor, softmax_scale: float, lse: torch.Tensor, weights: torch.Tensor, *, add: bool = True,
               window: int = 0, sinks: int = 0, stream: Optional[torch.cuda.Stream] = None):
         """What attention weight each key had from the batch's new tokens, summed over them and the query heads of its K/V head, into `weights`, fp32 [n_pages,
-        n_kv_heads, page_tokens] of this layer: added to those of earlier tokens (add), or set.  q, lse, window and sinks: of the attention."""
+        n_kv_heads, page_tokens] of this layer: added to those of earlier tokens (add), or set.  q, lse, window and sinks: of the attention.  No two sequences of the batch
+        may share a page (sequences with a common beginning are weighed one call after the other, and added); those without new tokens keep the weights they have."""
         if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.weigh(layer, batch, q, softmax_scale, lse, weights, add=add, window=window, sinks=sinks, stream=stream)
@@ -663,7 +665,7 @@ class SaliPages:
     def select(self, batch: PageBatch, weights: torch.Tensor, budget: int, keep: torch.Tensor, *, sinks: int = 0, recent: int = 0,
                stream: Optional[torch.cuda.Stream] = None):
         """Which of each sequence's new tokens (all, if it has no others) stay: the first `sinks`, the last `recent`, and those of most weight, `budget` in all.  Their places go
-        to `keep`, int32 [sequences, n_kv_heads, budget], rising, -1 behind the last."""
+        to `keep`, int32 [sequences, n_kv_heads, budget], rising, -1 behind the last; lists of sequences that are left out, and of a batch without any token, are not written."""
         if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.select(batch, weights, budget, keep, sinks=sinks, recent=recent, stream=stream)

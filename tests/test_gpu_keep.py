@@ -180,6 +180,25 @@ def test_wrong_batches_have_no_weights():
         assert c.pages.get_status() == binding.FAULT_BATCH and (w == 3).all() and (keep == 7).all() and torch.equal(c.pages.pool, pool)
 
 
+@pytest.mark.parametrize("n", [1, 9, 40, 150])
+def test_sequences_without_new_tokens(n):
+    """Their weights stay what they are, set or added, and their lists are empty; of a batch of such sequences alone nothing is written, lists neither."""
+    c = Cache(op.PagesSpec(2, 8, 64, 16, "fp16", "16"), [60, 200, 17], 28)
+    for add in (False, True):
+        _, _, w = weigh(c, [(0, 60), (n, 200), (0, 17)], add)
+        assert (of_seq(c, w, 0, 60) == 3).all() and (of_seq(c, w, 2, 17) == 3).all()
+    before = c.pages.pool.clone()
+    keep = select(c, [(0, 60), (n, 200), (0, 17)], w, 5)
+    assert (keep[[0, 2]] == -1).all() and (keep[1] >= 0).any()
+    keep.fill_(7)
+    old = w.clone()
+    empty = c.batch([(0, 60), (0, 200), (0, 17)])
+    c.pages.weigh(0, empty, torch.empty((0, 8, 64), dtype=torch.float16, device=DEV), 0.125, torch.empty((0, 8), device=DEV), w, add=False)
+    c.pages.select(empty, w, 5, keep)
+    c.pages.keep(0, empty, keep)
+    assert (keep == 7).all() and torch.equal(w, old) and torch.equal(before, c.pages.pool) and c.pages.get_status() == 0
+
+
 @pytest.mark.parametrize("n", [1, 12, 40, 150])
 def test_weights_of_a_batch_that_begins_later(n):
     """Rows before the batch's first are not its own."""
