@@ -529,14 +529,7 @@ class SaliPages:
         except Exception:
             pass
 
-    def _rows(self, t: torch.Tensor, batch: PageBatch, heads: int, name: str) -> sali_rows:
-        token, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
-        if t.dtype is not self.dtype or t.shape != (batch.tokens, heads, self.head_dim) or one != 1 or t.get_device() != self.index:
-            raise ValueError(f"{name}: {self.dtype} [{batch.tokens}, {heads}, {self.head_dim}] on {self.device} with its last dimension side by "
-                             f"side expected, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
-        return sali_rows(t.data_ptr(), token, head)
-
-    def _token_rows(self, t: torch.Tensor, tokens: int, heads: int, name: str) -> sali_rows:
+    def _rows(self, t: torch.Tensor, tokens: int, heads: int, name: str) -> sali_rows:
         token, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
         if t.dtype is not self.dtype or t.shape != (tokens, heads, self.head_dim) or one != 1 or t.get_device() != self.index:
             raise ValueError(f"{name}: {self.dtype} [{tokens}, {heads}, {self.head_dim}] on {self.device} with its last dimension side by "
@@ -574,7 +567,7 @@ class SaliPages:
             with torch.cuda.device(self.index):
                 return self.append(layer, batch, k, v, stream)
         n = self.n_kv_heads
-        _check(self.lib.sali_pages_append(self.handle, layer, batch.c, self._rows(k, batch, n, "k"), self._rows(v, batch, n, "v"),
+        _check(self.lib.sali_pages_append(self.handle, layer, batch.c, self._rows(k, batch.tokens, n, "k"), self._rows(v, batch.tokens, n, "v"),
                                           self._call(batch, stream)), "sali_pages_append")
 
     def read(self, layer: int, batch: PageBatch, k_out: torch.Tensor, v_out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
@@ -583,7 +576,7 @@ class SaliPages:
             with torch.cuda.device(self.index):
                 return self.read(layer, batch, k_out, v_out, stream)
         n = self.n_kv_heads
-        _check(self.lib.sali_pages_read(self.handle, layer, batch.c, self._rows(k_out, batch, n, "k_out"), self._rows(v_out, batch, n, "v_out"),
+        _check(self.lib.sali_pages_read(self.handle, layer, batch.c, self._rows(k_out, batch.tokens, n, "k_out"), self._rows(v_out, batch.tokens, n, "v_out"),
                                         self._call(batch, stream)), "sali_pages_read")
 
     def attend(self, layer: int, batch: PageBatch, q: torch.Tensor, softmax_scale: float, out: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
@@ -595,9 +588,9 @@ class SaliPages:
             with torch.cuda.device(self.index):
                 return self.attend(layer, batch, q, softmax_scale, out, lse, window=window, sinks=sinks, prior=prior, prior_lse=prior_lse, stream=stream)
         n, d = self.n_heads, self.head_dim
-        _check(self.lib.sali_pages_attend(self.handle, layer, batch.c, self._rows(q, batch, n, "q"), softmax_scale, window, sinks,
+        _check(self.lib.sali_pages_attend(self.handle, layer, batch.c, self._rows(q, batch.tokens, n, "q"), softmax_scale, window, sinks,
                                           self._dense(prior, (batch.tokens, n, d), "prior"), self._dense(prior_lse, (batch.tokens, n), "prior_lse"),
-                                          self._rows(out, batch, n, "out"), self._dense(lse, (batch.tokens, n), "lse"),
+                                          self._rows(out, batch.tokens, n, "out"), self._dense(lse, (batch.tokens, n), "lse"),
                                           self._call(batch, stream)), "sali_pages_attend")
 
     def _wrong(self, name: str, t: torch.Tensor, dtype, dims):
@@ -622,13 +615,13 @@ class SaliPages:
             raise ValueError("an output is given without its input")
         q_rows = k_rows = q_to = k_to = None
         if q is not None:
-            q_rows = q_to = self._token_rows(q, n, self.n_heads, "q")
+            q_rows = q_to = self._rows(q, n, self.n_heads, "q")
             if q_out is not None:
-                q_to = self._token_rows(q_out, n, self.n_heads, "q_out")
+                q_to = self._rows(q_out, n, self.n_heads, "q_out")
         if k is not None:
-            k_rows = k_to = self._token_rows(k, n, self.n_kv_heads, "k")
+            k_rows = k_to = self._rows(k, n, self.n_kv_heads, "k")
             if k_out is not None:
-                k_to = self._token_rows(k_out, n, self.n_kv_heads, "k_out")
+                k_to = self._rows(k_out, n, self.n_kv_heads, "k_out")
         code = self.lib.sali_pages_rotate(self.handle, rotary.c, position.data_ptr(), n, inverse, q_rows, k_rows, q_to, k_to,
                                           torch._C._cuda_getCurrentRawStream(index) if stream is None else self._stream_of(stream))
         if code != 0:
@@ -646,8 +639,8 @@ class SaliPages:
         n, d = self.n_heads, self.head_dim
         if seen.dtype is not torch.int64 or seen.shape != (batch.tokens,) or not seen.is_contiguous() or seen.get_device() != self.index:
             raise self._wrong("seen", seen, torch.int64, [batch.tokens])
-        _check(self.lib.sali_pages_attend_tree(self.handle, layer, batch.c, seen.data_ptr(), self._rows(q, batch, n, "q"), softmax_scale, self._dense(prior, (batch.tokens, n, d), "prior"),
-                                               self._dense(prior_lse, (batch.tokens, n), "prior_lse"), self._rows(out, batch, n, "out"),
+        _check(self.lib.sali_pages_attend_tree(self.handle, layer, batch.c, seen.data_ptr(), self._rows(q, batch.tokens, n, "q"), softmax_scale, self._dense(prior, (batch.tokens, n, d), "prior"),
+                                               self._dense(prior_lse, (batch.tokens, n), "prior_lse"), self._rows(out, batch.tokens, n, "out"),
                                                self._dense(lse, (batch.tokens, n), "lse"), self._call(batch, stream)), "sali_pages_attend_tree")
 
     def weigh(self, layer: int, batch: PageBatch, q: torch.Tensor, softmax_scale: float, lse: torch.Tensor, weights: torch.Tensor, *, add: bool = True,
@@ -658,7 +651,7 @@ class SaliPages:
         if torch._C._cuda_getDevice() != self.index:
             with torch.cuda.device(self.index):
                 return self.weigh(layer, batch, q, softmax_scale, lse, weights, add=add, window=window, sinks=sinks, stream=stream)
-        _check(self.lib.sali_pages_weigh(self.handle, layer, batch.c, self._rows(q, batch, self.n_heads, "q"), softmax_scale, window, sinks,
+        _check(self.lib.sali_pages_weigh(self.handle, layer, batch.c, self._rows(q, batch.tokens, self.n_heads, "q"), softmax_scale, window, sinks,
                                          self._dense(lse, (batch.tokens, self.n_heads), "lse"), add,
                                          self._dense(weights, self._weights_shape, "weights"), self._call(batch, stream)), "sali_pages_weigh")
 
