@@ -24,7 +24,8 @@ __device__ __forceinline__ uint32_t key_of(float w) {
 // A block a sequence and K/V head.  The weight that the last of the tokens that stay has is found digit by digit, highest first, in a histogram of the tokens that are alike so
 // far; then every wave takes a stretch of tokens, counts those above and at that weight, and writes the places of those that stay behind what the waves before it have.
 // Bound by its chain of passes over LDS: three texts of up to 24001 tokens, 8 heads, in 27 us, where their weights are 1.7 MB.  Keys are kept there once read (48 us
-// with loads of one weight), several on their way together and without branches (33 us with them).
+// with loads of one weight), several on their way together and without branches (33 us with them).  Keys behind those that LDS has room for are fetched again in every pass, page and
+// weight one after the other: 32768 tokens of 8 heads 34 us, 131072 255.
 __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) {
     __shared__ uint32_t s_keys[kInLds];
     __shared__ uint32_t s_bins[kBins];
@@ -191,7 +192,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_pages_select(PagesSelect a) 
 //
 // Bound by the lines that rows lie in: those that stay are spread, so that nearly all of the source is touched.  4096 of up to 24001 tokens, three texts, 8 heads of 128 in 16
 // bits: 171 MB read and 51 written in 41 us, 5.4 TB/s (57 where a block takes a strip of K or of V alone: half as much for the same chain of lengths, list, tables
-// and rows; 43 with V's values asked for behind branches; chunks of 128 or blocks of 128 threads 40).  In place, 32 drafts of 16 tokens: 9 us, a launch and its chain of list, tables, rows.
+// and rows; 43 with V's values asked for behind branches; chunks of 128 or blocks of 128 threads 40).  In place, 32 drafts of 16 tokens: 9 us, a launch and its chain of list, tables, rows;
+// the three texts 91 us (37 elsewhere, the call alone): a chunk waits for the one before.
 constexpr int kKeepThreads = 256;
 
 template <int kStore, int kDim>

@@ -4,9 +4,10 @@
 // causal attention with another look at the keys from the history's end on (at most four tiles of 32), and without what only windows need.
 //
 // Up to 32 rows (new tokens times heads of a group) go through the stream, a launch's chain of trips where there is little history: 7 tokens of 4 heads over 777 keys, 14.4 us.
-// More are row tiles of 128, four waves of 32 rows: 24 drafts of 16 tokens over up to 6000 keys in 8 bits, 8 heads, plan 6, tiles 64, merge 7 us, 190 MB at 3.0 TB/s; 4 of 64
-// tokens over up to 9000 in 16 bits 6 + 49 + 13.  What bounds them is a tile's chain of load, first product, softmax and second product with three blocks a compute unit to hide it
-// (64 and 128 rows give the matrix cores little: 12 and 20 % busy).  Slower: 64 rows in the stream, 136 us for the first; kernels of eight waves that take keys
+// More are row tiles of 128, four waves of 32 rows: 24 drafts of 16 tokens over up to 6000 keys in 8 bits, 8 heads, plan 6, tiles 77, merge 7 us, 190 MB at 2.5 TB/s; 4 of 64
+// tokens over up to 9000 in 16 bits 6 + 58 + 13.  What bounds them is a tile's chain of load, first product, softmax and second product with three blocks a compute unit to hide it
+// (64 and 128 rows give the matrix cores little: 16 and 26 % busy).  Weights are two 16-bit numbers each; with one the tiles take 64 and 49 us, and results
+// are off by 2.3e-3 instead of 1.7e-3 in bfloat16.  Slower, the whole call with one number a weight, 75 us for the first as it is: 64 rows in the stream, 136; kernels of eight waves that take keys
 // straight into registers, 122, or through a ring of four tiles in LDS, 115; tiles of two waves, 82, or twelve, 118; 384 or 768 shares instead of 512, 83.
 #pragma once
 

@@ -12,6 +12,9 @@
 //                                    holds, whose sums a launch of its own joins.  8192 causal tokens, 32 heads over 8 of 128: 343 us, 800 TFLOP/s (a large library product: 1369).
 //                                    What it waits for there: products alone 181 us, weights alone 229, LDS reads 122 of both; products of one half step and weights of
 //                                    the one before are side by side, and two blocks of eight waves a compute unit.  64 keys a wave, half the reads of LDS: 351 to 364
+//
+// Under a window the first two walk all of a text's keys and leave out what is out of sight only then: 16 texts of 20000 keys in 16 bits, 8 heads, one token each, take 125 us
+// with a window of 1024 as without one, 20 times the bytes that are in sight.
 #pragma once
 
 #include "pages_stream.h"
